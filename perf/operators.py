@@ -269,7 +269,7 @@ def own_write(st):
     if c["new_hi"] == 1:
         st["cache"].write(st["k"], st["v"], st["seqs"])
     else:
-        st["cache"].write(st["k"], st["v"], st["seqs"], st["starts"], max_new=c["new_hi"])
+        st["cache"].write(st["k"], st["v"], st["seqs"], st["starts"])
 
 
 def own_beam(st):
