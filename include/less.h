@@ -325,6 +325,101 @@ int less_selftest_wait_timeout(less_ctx* ctx, uint32_t polls, void* cuda_stream)
 int less_prompt_scores_noalloc(const void* Q, const void* K, int32_t n_inst, int32_t prompt_len,
                                float* acc_out, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged 8-bit cache: the ordinary key / value cache beside LESS's own (the full cache that the paper compares with,
+ * Section 4, or first tokens plus a sliding window), for batches whose sequences have lengths of their own, grow, end
+ * and fork.  Keys and values are kept in 8 bits, LESS_PAGE_BLOCK tokens of a (layer, head) sharing one magnitude for
+ * their keys and one for their values:
+ *     value = code * amax / 127   (int8)         value = code * amax / 448   (e4m3, LESS_PAGES_E4M3)
+ * All calls are asynchronous on the given stream, allocate nothing, read lengths and tables on the device, and can be
+ * captured in a CUDA graph.  Lists (`seqs`, `lens`, `src`, `dst`, `starts`) are device int32 arrays.  Errors that only
+ * the device can see (an index out of range, no free page) go to the status word that less_pages_poll_status reads;
+ * until it has been read, calls that change the cache do nothing.  One call at a time per cache (its workspace is
+ * shared by all of them, replays of captured ones included); different caches are independent.
+ * Every function runs on the current device, which is the one the buffers are on. */
+enum {
+  LESS_PAGES_E4M3 = 1u,   /* codes are e4m3 instead of int8 */
+  LESS_PAGES_BF16 = 2u    /* q, k, v and out are bf16 instead of fp16 */
+};
+#define LESS_PAGE_BLOCK 16
+#define LESS_ERR_PAGES_EXHAUSTED (-13)
+
+/* Buffers are the caller's, 16-byte aligned (workspace: 256).  less_pages_reset makes them an empty cache; a caller
+ * that fills the maps itself clears the workspace once. */
+typedef struct less_pages {
+  int32_t layers, heads;      /* heads = KV heads */
+  int32_t group;              /* query heads per KV head, 1 .. 128 */
+  int32_t head_dim;           /* D: 64 or 128 */
+  int32_t page_tokens;        /* tokens per page: 16, 32, 64, 128 or 256 */
+  int32_t pages;              /* pages of the pool */
+  int32_t seqs, seq_pages;    /* sequences, and pages a sequence can have */
+  uint32_t flags;
+  void* codes;                /* [layers, pages, heads, 2 (keys, values), page_tokens * D] bytes: tiles of 16 tokens, 16 * D
+                               * bytes, each 16-byte pieces 32 c + 4 g + t (t < 4, g < 8):
+                               *   keys:    c = j * (D / 64) + half: token 4 (g / 2) + 2 j + g % 2, dimensions
+                               *            t * D / 4 + 16 half ..  + 15
+                               *   values:  c: dimensions g * D / 8 + 4 c .. + 3, of each the tokens 4 t .. 4 t + 3 */
+  float* amax;                /* [layers, pages, heads, 2, page_tokens / 16] */
+  int32_t* table;             /* [seqs, seq_pages]: page of a sequence's tokens [i * page_tokens, + page_tokens), -1 = none */
+  int32_t* lens;              /* [seqs]: tokens of a sequence */
+  int32_t* refs;              /* [pages]: sequences that hold a page, 0 = free */
+  void* workspace;
+  size_t workspace_bytes;     /* at least less_pages_workspace_bytes */
+} less_pages;
+
+#define LESS_PAGES_PARTIAL_BYTES ((size_t)48 << 20)   /* part of the workspace: partial attention results */
+size_t less_pages_workspace_bytes(const less_pages* cache);   /* 0 if the description is invalid; pointers are not read */
+int less_pages_reset(const less_pages* cache, void* cuda_stream);
+
+/* The n listed sequences get the listed lengths.  Pages behind an end that moved back are released; missing pages are
+ * taken from the lowest free ones, in the order of the list (releases come first).  A sequence that grows inside a
+ * page that other sequences hold too gets a copy of it.  With too few free pages no sequence grows (those that shrink
+ * still do) and the status is LESS_ERR_PAGES_EXHAUSTED; growth inside a page that less_pages_trim has released is
+ * LESS_ERR_BAD_STATE.  Length 0 frees a sequence.  Of a sequence listed twice the first entry counts.  n <= seqs. */
+int less_pages_resize(const less_pages* cache, int32_t n, const int32_t* seqs, const int32_t* lens, void* cuda_stream);
+
+/* Sequence dst[i], which must be empty, becomes a copy of src[i]: whole pages are shared, the page that is still being
+ * filled is copied to the lowest free page (in the order of the list).  A source may be listed often, a destination
+ * once and not as a source.  All or nothing: LESS_ERR_PAGES_EXHAUSTED, LESS_ERR_BAD_STATE. */
+int less_pages_fork(const less_pages* cache, int32_t n, const int32_t* src, const int32_t* dst, void* cuda_stream);
+
+/* Releases the pages of the listed sequences that hold neither one of the first `sinks` tokens nor one of the last
+ * `window` (>= 1): what less_pages_attention with these arguments never reads again. */
+int less_pages_trim(const less_pages* cache, int32_t n, const int32_t* seqs, int32_t sinks, int32_t window,
+                    void* cuda_stream);
+
+/* Moves pages so that those in use are the first ones of the pool: with m in use, the i-th one in use at index >= m
+ * goes to the i-th free index below m; tables follow. */
+int less_pages_compact(const less_pages* cache, void* cuda_stream);
+
+/* Writes the last tokens of n sequences (less_pages_resize has made room): entry i's tokens are the rows [starts[i],
+ * starts[i + 1]) of k and v (starts NULL: one row each), and go to positions [lens - count, lens) of sequence seqs[i].
+ * k, v: device fp16 / bf16 [rows, layer_count, heads, D], `stride` elements from row to row (a multiple of 8), for
+ * layers [layer_begin, + layer_count).  code = round(x * top / amax), ties to even, with amax = the largest |x| of the
+ * block (16 tokens x D of a layer and head); where a block holds older tokens, its amax only grows and their codes
+ * are rounded again.  Infinities count as the largest finite value (bf16: 2^100), NaN as 0.  Rows behind starts[n] are
+ * not read; of a sequence listed twice the first entry counts; a page that other sequences hold too is not
+ * written (LESS_ERR_BAD_STATE). */
+int less_pages_write(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n, const int32_t* seqs,
+                     const int32_t* starts, int32_t rows, const void* k, int64_t k_stride, const void* v,
+                     int64_t v_stride, void* cuda_stream);
+
+/* Attention of the last tokens of n sequences over their cached keys and values (entries as in less_pages_write; the
+ * tokens' own keys are in the cache).  The token at position i sees the keys j <= i and, with window > 0, of those
+ * only j > i - window and j < sinks (first tokens that stay visible); tokens of released pages are not seen.
+ *     out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale * q . k_j);  a token that sees nothing gets zeros
+ * q: device [rows, layer_count, heads * group, D], q_stride elements from row to row (a multiple of 8); out: device
+ * [rows, layer_count, heads * group, D], contiguous, q's type; rows behind starts[n] are left as they are.
+ * max_new: the most new tokens any entry has, as far as the host knows; it chooses among kernels, results do not
+ * depend on it.  scale: > 0, 1 / sqrt(D) as a rule. */
+int less_pages_attention(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n,
+                         const int32_t* seqs, const int32_t* starts, int32_t rows, int32_t max_new, const void* q,
+                         int64_t q_stride, int32_t window, int32_t sinks, float scale, void* out, void* cuda_stream);
+
+/* Reads and clears the status word (synchronises the stream): 0, LESS_ERR_DEVICE_BOUNDS, LESS_ERR_PAGES_EXHAUSTED,
+ * LESS_ERR_BAD_STATE or LESS_ERR_DEVICE_TIMEOUT. */
+int less_pages_poll_status(const less_pages* cache, void* cuda_stream);
+
 const char* less_strerror(int code);
 
 /* Releases the context; frees nothing the caller owns. */

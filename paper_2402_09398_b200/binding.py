@@ -31,9 +31,16 @@ EXPORTED = [
     "less_destroy", "less_decode_step_host", "less_profile", "less_profile_read",
     "less_prompt_scores_noalloc", "less_masked_attention", "less_kernel_variant",
     "less_last_status_where", "less_selftest_wait_timeout",
+    "less_pages_workspace_bytes", "less_pages_reset", "less_pages_resize", "less_pages_fork",
+    "less_pages_trim", "less_pages_compact", "less_pages_write", "less_pages_attention",
+    "less_pages_poll_status",
 ]
 LESS_NOALLOC_MAX_ROWS = 65536
 LESS_ERR_NOALLOC_TOO_LARGE = -12
+LESS_ERR_PAGES_EXHAUSTED = -13
+LESS_PAGES_E4M3 = 1
+LESS_PAGES_BF16 = 2
+LESS_PAGE_BLOCK = 16
 
 KERNEL_NAMES = ["feature_map", "decode", "rowstat", "colsum", "attn_out", "select", "build", "finalize",
                 "psi", "gather", "masked_pack", "masked_out"]
@@ -49,6 +56,14 @@ class less_config(C.Structure):
 class less_weights(C.Structure):
     _fields_ = [("w_phi1", C.c_void_p), ("w_phi2", C.c_void_p), ("w_psi1", C.c_void_p),
                 ("w_psi2", C.c_void_p), ("w_psi3", C.c_void_p), ("psi_scale", C.c_void_p)]
+
+
+class less_pages(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("heads", C.c_int32), ("group", C.c_int32), ("head_dim", C.c_int32),
+                ("page_tokens", C.c_int32), ("pages", C.c_int32), ("seqs", C.c_int32), ("seq_pages", C.c_int32),
+                ("flags", C.c_uint32), ("codes", C.c_void_p), ("amax", C.c_void_p), ("table", C.c_void_p),
+                ("lens", C.c_void_p), ("refs", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
 
 
 class LessError(RuntimeError):
@@ -114,6 +129,17 @@ def lib() -> C.CDLL:
     L.less_last_status_where.argtypes = [vp]
     L.less_selftest_wait_timeout.restype = C.c_int
     L.less_selftest_wait_timeout.argtypes = [vp, C.c_uint32, vp]
+    pg = C.POINTER(less_pages)
+    L.less_pages_workspace_bytes.restype = sz
+    L.less_pages_workspace_bytes.argtypes = [pg]
+    for name, args in (("reset", [vp]), ("resize", [i32, vp, vp, vp]), ("fork", [i32, vp, vp, vp]),
+                       ("trim", [i32, vp, i32, i32, vp]), ("compact", [vp]),
+                       ("write", [i32, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp]),
+                       ("attention", [i32, i32, i32, vp, vp, i32, i32, vp, i64, i32, i32, C.c_float, vp, vp]),
+                       ("poll_status", [vp])):
+        fn = getattr(L, "less_pages_" + name)
+        fn.restype = C.c_int
+        fn.argtypes = [pg] + args
     _lib = L
     return L
 
@@ -210,6 +236,46 @@ def less_last_status_where(ctx) -> int:
 
 def less_selftest_wait_timeout(ctx, polls: int, stream) -> int:
     return lib().less_selftest_wait_timeout(ctx, int(polls), stream)
+
+
+def less_pages_workspace_bytes(cache: less_pages) -> int:
+    return int(lib().less_pages_workspace_bytes(C.byref(cache)))
+
+
+def less_pages_reset(cache: less_pages, stream) -> int:
+    return lib().less_pages_reset(cache, stream)
+
+
+def less_pages_resize(cache: less_pages, n, seqs, lens, stream) -> int:
+    return lib().less_pages_resize(cache, n, seqs, lens, stream)
+
+
+def less_pages_fork(cache: less_pages, n, src, dst, stream) -> int:
+    return lib().less_pages_fork(cache, n, src, dst, stream)
+
+
+def less_pages_trim(cache: less_pages, n, seqs, sinks, window, stream) -> int:
+    return lib().less_pages_trim(cache, n, seqs, sinks, window, stream)
+
+
+def less_pages_compact(cache: less_pages, stream) -> int:
+    return lib().less_pages_compact(cache, stream)
+
+
+def less_pages_write(cache: less_pages, layer_begin, layer_count, n, seqs, starts, rows, k, k_stride, v, v_stride,
+                     stream) -> int:
+    return lib().less_pages_write(cache, layer_begin, layer_count, n, seqs, starts, rows, k, k_stride, v, v_stride,
+                                  stream)
+
+
+def less_pages_attention(cache: less_pages, layer_begin, layer_count, n, seqs, starts, rows, max_new, q, q_stride,
+                         window, sinks, scale, out, stream) -> int:
+    return lib().less_pages_attention(cache, layer_begin, layer_count, n, seqs, starts, rows, max_new, q, q_stride,
+                                      window, sinks, scale, out, stream)
+
+
+def less_pages_poll_status(cache: less_pages, stream) -> int:
+    return lib().less_pages_poll_status(cache, stream)
 
 
 # --------------------------------------------------------------------------- #
@@ -405,3 +471,146 @@ def from_workload(w, weights=None, device="cuda", max_prefill_layers=1, flags=0,
                        w.prompt if max_prompt is None else max_prompt, weights,
                        max_prefill_layers=max_prefill_layers, flags=flags, psi_scale=psi_scale,
                        device=device, group=getattr(w, "group", 1))
+
+
+class PagedCache:
+    """The paged 8-bit cache (less_pages): holds its torch buffers and forwards calls.
+
+    Sequences are rows of `table`; lists of them and of lengths are int32 tensors on the cache's device.  `buffers`
+    gives the cache tensors that exist already (codes, amax, table, lens, refs), contiguous, in the shapes below;
+    without it the cache starts empty.  Calls are asynchronous on the current stream (or `stream`); `poll_status`
+    tells what the device found wrong."""
+
+    def __init__(self, layers, heads, head_dim, pages, seqs, seq_pages, group=1, page_tokens=64, fmt="int8",
+                 dtype=torch.float16, device="cuda", buffers: Optional[Dict[str, torch.Tensor]] = None):
+        if fmt not in ("int8", "e4m3"):
+            raise ValueError(f"fmt is 'int8' or 'e4m3', not {fmt!r}")
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError(f"dtype is torch.float16 or torch.bfloat16, not {dtype}")
+        self.fmt, self.dtype = fmt, dtype
+        flags = (LESS_PAGES_E4M3 if fmt == "e4m3" else 0) | (LESS_PAGES_BF16 if dtype == torch.bfloat16 else 0)
+        desc = less_pages(layers, heads, group, head_dim, page_tokens, pages, seqs, seq_pages, flags)
+        nbytes = less_pages_workspace_bytes(desc)
+        if nbytes == 0:
+            raise LessError(-1, "less_pages_workspace_bytes")
+        if not torch.cuda.is_available():
+            raise RuntimeError("the LESS library needs a CUDA device (there is no CPU path)")
+        shapes = {"codes": ((layers, pages, heads, 2, page_tokens * head_dim), torch.uint8),
+                  "amax": ((layers, pages, heads, 2, page_tokens // LESS_PAGE_BLOCK), torch.float32),
+                  "table": ((seqs, seq_pages), torch.int32), "lens": ((seqs,), torch.int32),
+                  "refs": ((pages,), torch.int32)}
+        if buffers is None:
+            buffers = {n: torch.empty(s, dtype=t, device=device) for n, (s, t) in shapes.items()}
+            empty = True
+        else:
+            empty = False
+            for n, (s, t) in shapes.items():
+                b = buffers[n]
+                if tuple(b.shape) != s or b.dtype != t or not b.is_contiguous() or not b.is_cuda:
+                    raise ValueError(f"{n}: a contiguous CUDA tensor {s} of {t} is wanted, "
+                                     f"got {tuple(b.shape)} of {b.dtype} on {b.device}")
+        self.codes, self.amax, self.table, self.lens, self.refs = (buffers[n] for n in shapes)
+        self.device = self.codes.device
+        if any(b.device != self.device for b in (self.amax, self.table, self.lens, self.refs)):
+            raise ValueError("the buffers of a cache are on one device")
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        for n in shapes:
+            setattr(desc, n, buffers[n].data_ptr())
+        desc.workspace, desc.workspace_bytes = self.workspace.data_ptr(), nbytes
+        self.desc = desc
+        self.scale = head_dim ** -0.5
+        self._index = self.device.index
+        if empty:
+            self.reset()
+
+    # -- helpers ----------------------------------------------------------- #
+    def _call(self, fn, where, *args, stream=None):
+        if torch.cuda.current_device() == self._index:
+            s = torch.cuda.current_stream(self._index) if stream is None else stream
+            rc = fn(self.desc, *args, s.cuda_stream)
+        else:
+            with torch.cuda.device(self._index):
+                s = torch.cuda.current_stream(self._index) if stream is None else stream
+                rc = fn(self.desc, *args, s.cuda_stream)
+        if rc != LESS_OK:
+            raise LessError(rc, where)
+
+    def _list(self, t: torch.Tensor, name: str, n: Optional[int] = None) -> int:
+        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous 1-d int32 tensor on {self.device} is wanted")
+        if n is not None and t.shape[0] != n:
+            raise ValueError(f"{name}: {n} values are wanted, got {t.shape[0]}")
+        return t.data_ptr()
+
+    def _rows(self, t: torch.Tensor, name: str, heads: int):
+        d = self.desc
+        if t.dtype != self.dtype or t.device != self.device or t.dim() != 4:
+            raise ValueError(f"{name}: a [rows, layers, heads, D] tensor of {self.dtype} on {self.device} is wanted")
+        rows, layers, h, dim = t.shape
+        if h != heads or dim != d.head_dim or layers > d.layers:
+            raise ValueError(f"{name}: [rows, layers, {heads}, {d.head_dim}] is wanted, got {tuple(t.shape)}")
+        if rows and (t.stride(3) != 1 or (h > 1 and t.stride(2) != dim) or (layers > 1 and t.stride(1) != h * dim)):
+            raise ValueError(f"{name}: everything but the rows has to be contiguous")
+        stride = t.stride(0) if rows > 1 else layers * h * dim
+        return rows, layers, stride
+
+    # -- the maps ---------------------------------------------------------- #
+    def reset(self, stream=None):
+        """Empties the cache."""
+        self._call(lib().less_pages_reset, "less_pages_reset", stream=stream)
+
+    def resize(self, seqs, lens, stream=None):
+        """Sequences get new lengths: pages are taken or released (0 frees a sequence)."""
+        n = seqs.shape[0]
+        self._call(lib().less_pages_resize, "less_pages_resize", n, self._list(seqs, "seqs"),
+                   self._list(lens, "lens", n), stream=stream)
+
+    def fork(self, src, dst, stream=None):
+        """The empty sequences dst become copies of src (whole pages shared)."""
+        n = src.shape[0]
+        self._call(lib().less_pages_fork, "less_pages_fork", n, self._list(src, "src"), self._list(dst, "dst", n),
+                   stream=stream)
+
+    def trim(self, seqs, sinks, window, stream=None):
+        """Releases the pages between the first `sinks` tokens and the last `window`."""
+        self._call(lib().less_pages_trim, "less_pages_trim", seqs.shape[0], self._list(seqs, "seqs"), sinks, window,
+                   stream=stream)
+
+    def compact(self, stream=None):
+        """Moves the pages in use to the front of the pool."""
+        self._call(lib().less_pages_compact, "less_pages_compact", stream=stream)
+
+    # -- contents ---------------------------------------------------------- #
+    def write(self, k, v, seqs, starts=None, layer_begin=0, stream=None):
+        """k, v [rows, layers, heads, D]: the last tokens of the listed sequences (rows starts[i] .. starts[i + 1]
+        belong to seqs[i]; without starts one row each)."""
+        n = seqs.shape[0]
+        rows, layers, ks = self._rows(k, "k", self.desc.heads)
+        vrows, vlayers, vs = self._rows(v, "v", self.desc.heads)
+        if (vrows, vlayers) != (rows, layers):
+            raise ValueError("k and v have the same shape")
+        self._call(lib().less_pages_write, "less_pages_write", layer_begin, layers, n, self._list(seqs, "seqs"),
+                   None if starts is None else self._list(starts, "starts", n + 1), rows, k.data_ptr(), ks,
+                   v.data_ptr(), vs, stream=stream)
+
+    def attention(self, q, seqs, starts=None, max_new=None, layer_begin=0, window=0, sinks=0, scale=None, out=None,
+                  stream=None):
+        """q [rows, layers, heads * group, D]: attention of the last tokens of the listed sequences over the cache.
+        max_new: the most new tokens of a sequence, as far as the host knows (default: all rows)."""
+        d = self.desc
+        n = seqs.shape[0]
+        rows, layers, qs = self._rows(q, "q", d.heads * d.group)
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        elif out.shape != q.shape or out.dtype != self.dtype or out.device != self.device or not out.is_contiguous():
+            raise ValueError("out: a contiguous tensor of q's shape and type is wanted")
+        self._call(lib().less_pages_attention, "less_pages_attention", layer_begin, layers, n,
+                   self._list(seqs, "seqs"), None if starts is None else self._list(starts, "starts", n + 1), rows,
+                   max(1, rows if max_new is None else max_new), q.data_ptr(), qs, window, sinks,
+                   self.scale if scale is None else scale, out.data_ptr(), stream=stream)
+        return out
+
+    def poll_status(self, stream=None) -> int:
+        """What the device found wrong since the last poll (0 = nothing); clears it."""
+        with torch.cuda.device(self._index):
+            return less_pages_poll_status(self.desc, _stream_ptr(stream))

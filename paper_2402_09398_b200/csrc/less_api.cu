@@ -594,6 +594,7 @@ const char* less_strerror(int code) {
     case LESS_ERR_BAD_STATE: return "state record or context state not usable";
     case LESS_ERR_BUFFER_TOO_SMALL: return "host buffer too small";
     case LESS_ERR_NOALLOC_TOO_LARGE: return "more rows than the built-in scratch array holds";
+    case LESS_ERR_PAGES_EXHAUSTED: return "not enough free pages";
     default: return "unknown error";
   }
 }

@@ -1,0 +1,199 @@
+// The write of the paged 8-bit cache: the new tokens of every sequence, rounded to 8 bits.
+//
+//   a = max |x| over the 16 tokens x D dimensions of a block (with the magnitude it had, if it holds older tokens)
+//   code = rn(x * top / a)            top = 127 (int8) or 448 (e4m3), ties to even
+//   older tokens of the block, where a has grown:  code = rn(code * a_old / a)
+//
+// x * top and code * a_old are exact in fp32 (16-bit inputs), the quotient is correctly rounded, and a quotient that
+// is not a tie is further than 2^-19 (relative) from one: the codes are those of exact arithmetic.
+// Infinities are written as the largest finite fp16 number (bf16: 2^100, so that x * top stays finite), NaN as 0:
+// one bad token must not take the other fifteen of its block with it.  Tokens of the last block behind the
+// sequence's end get code 0.
+//
+// Bound by memory: 2 bytes read and 1 written per value.  A block of threads takes one 16-token block of one layer
+// for a few heads; a thread owns one 16-byte piece of the stored tile (pages.cuh), so the stores are contiguous.
+#include <type_traits>
+
+#include "less_internal.cuh"
+#include "pages.cuh"
+
+namespace less {
+
+constexpr int PW_THREADS = 256;
+
+struct PwArgs {
+  const void* k;
+  const void* v;
+  int64_t k_stride, v_stride;        // elements from token to token
+  const int32_t* seqs;
+  const int32_t* starts;
+  int n, rows, layer0;
+};
+
+// block slots of a call: entry i owns slots [starts[i] / 16 + 2 i, starts[i + 1] / 16 + 2 (i + 1)) - at least as many
+// as its `count` tokens can touch, (count + 14) / 16 + 1, whatever their first position is
+__device__ __forceinline__ int pw_slot(const PwArgs& a, int i) {
+  const int row = a.starts ? min(max(__ldg(a.starts + i), 0), a.rows) : i;
+  return row / kPageBlock + 2 * i;
+}
+
+template <typename T>
+__device__ __forceinline__ float pw_load(T x) {
+  constexpr float most = std::is_same<T, __half>::value ? 65504.f : 0x1p100f;
+  const float f = static_cast<float>(x);
+  return f == f ? fminf(fmaxf(f, -most), most) : 0.f;
+}
+
+template <bool E4M3>
+__device__ __forceinline__ float pw_value(uint32_t code) {   // in units of amax / top
+  if (E4M3) {
+    const __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3);
+    return __half2float(__half(h));
+  }
+  return (float)(int8_t)code;
+}
+
+template <bool E4M3>
+__device__ __forceinline__ uint32_t pw_code(float x) {
+  if (E4M3) return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+  return (uint32_t)__float2int_rn(x) & 0xffu;
+}
+
+template <typename T, int D, bool E4M3>
+__global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwArgs a) {
+  constexpr int PER = D;                        // threads per (head, keys or values): one 16-byte piece each
+  constexpr int HEADS = PW_THREADS / (2 * PER); // heads per turn
+  __shared__ float red[PW_THREADS / 32];
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int slot = blockIdx.x;
+  int lo = 0, hi = a.n - 1;                     // the last entry whose slots start at or before this one
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (pw_slot(a, mid) <= slot) lo = mid; else hi = mid - 1;
+  }
+  const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, lo);
+  const int begin = e.len - e.count;            // first new position
+  if (e.count == 0) return;
+  if (begin < 0) {
+    if (tid == 0) pg_status(p.status, kPagesBounds, 40);
+    return;
+  }
+  const int pos0 = (begin / kPageBlock + slot - pw_slot(a, lo)) * kPageBlock;
+  if (pos0 >= e.len) return;
+  // nothing after an error; a sequence listed twice: the first entry counts
+  bool again = __ldcg(p.status) != 0;
+  for (int j = tid; j < lo; j += PW_THREADS) again |= __ldg(a.seqs + j) == e.seq;
+  if (__syncthreads_or(again)) return;
+  const int page = pg_page(p, e.seq, pos0 >> p.pt_shift);
+  if (page < 0 || __ldcg(p.refs + page) != 1) {          // trimmed, or held by other sequences too
+    if (tid == 0) pg_status(p.status, page < 0 ? kPagesBounds : kPagesState, 41);
+    return;
+  }
+  const int inner = (pos0 & (p.pt - 1)) / kPageBlock;
+  const int keep = begin - pos0;                         // tokens of the block older than the call (<= 0: none)
+  const int live = min(kPageBlock, e.len - pos0);
+  const int lj = blockIdx.z, layer = a.layer0 + lj;
+
+  const int piece = tid % PER, which = (tid / PER) & 1, c = piece >> 5, g = (piece >> 2) & 7, t = piece & 3;
+  for (int h0 = (int)blockIdx.y * HEADS; h0 < p.heads; h0 += (int)gridDim.y * HEADS) {
+    const int h = h0 + tid / (2 * PER);
+    const bool in = h < p.heads;
+    uint8_t* tile = nullptr;
+    float* mag = nullptr;
+    float x[16];
+    uint4 was = make_uint4(0, 0, 0, 0);
+    float old = 0.f, m = 0.f;
+    if (in) {
+      tile = p.codes + pg_slab(p, D, layer, page, h) + ((size_t)which * p.pt + inner * kPageBlock) * D + piece * 16;
+      mag = p.amax + pg_mag(p, layer, page, h) + which * (p.pt / kPageBlock) + inner;
+      if (keep > 0) {
+        was = *reinterpret_cast<const uint4*>(tile);
+        old = *mag;
+      }
+      const int64_t stride = which ? a.v_stride : a.k_stride;
+      const T* src = reinterpret_cast<const T*>(which ? a.v : a.k) + (int64_t)(e.row0 - keep) * stride +
+                     (int64_t)(lj * p.heads + h) * D;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      if (which == 0) {
+        const int token = 4 * (g >> 1) + 2 * (c / (D / 64)) + (g & 1);
+        if (token >= keep && token < live) {
+          const uint4* s4 = reinterpret_cast<const uint4*>(src + (int64_t)token * stride + t * (D / 4) + (c % (D / 64)) * 16);
+          uint4 u[2] = {__ldg(s4), __ldg(s4 + 1)};
+          const T* y = reinterpret_cast<const T*>(u);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = pw_load(y[i]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int token = 4 * t + k;
+          if (token >= keep && token < live) {
+            uint2 u = __ldg(reinterpret_cast<const uint2*>(src + (int64_t)token * stride + g * (D / 8) + c * 4));
+            const T* y = reinterpret_cast<const T*>(&u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i * 4 + k] = pw_load(y[i]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    __syncthreads();
+    if (lane == 0) red[tid >> 5] = m;
+    __syncthreads();
+    m = old;
+#pragma unroll
+    for (int w = 0; w < PER / 32; ++w) m = fmaxf(m, red[tid / PER * (PER / 32) + w]);
+    if (in) {
+      const float unit = m > 0.f ? m : 1.f, top = pg_top<E4M3>();
+      uint32_t out[4];
+      const uint32_t* wasw = reinterpret_cast<const uint32_t*>(&was);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int token = which ? 4 * t + (i & 3) : 4 * (g >> 1) + 2 * (c / (D / 64)) + (g & 1);
+        const float num = token < keep ? pw_value<E4M3>((wasw[i / 4] >> (8 * (i & 3))) & 0xffu) * old : x[i] * top;
+        const uint32_t code = pw_code<E4M3>(__fdiv_rn(num, unit));
+        out[i / 4] = (i & 3) ? out[i / 4] | code << (8 * (i & 3)) : code;
+      }
+      *reinterpret_cast<uint4*>(tile) = make_uint4(out[0], out[1], out[2], out[3]);
+      if (piece == 0) *mag = m;
+    }
+  }
+}
+
+}  // namespace less
+
+using namespace less;
+
+extern "C" int less_pages_write(const less_pages* d, int32_t layer_begin, int32_t layer_count, int32_t n,
+                                const int32_t* seqs, const int32_t* starts, int32_t rows, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
+  PgParams p;
+  const int rc = pg_view(d, &p);
+  if (rc != LESS_OK) return rc;
+  if (layer_begin < 0 || layer_count < 1 || layer_begin > d->layers - layer_count) return LESS_ERR_BAD_LAYER_RANGE;
+  if (n < 0 || n > (1 << 24) || rows < 0 || (!starts && rows != n)) return LESS_ERR_INVALID_CONFIG;
+  if (n == 0 || rows == 0) return LESS_OK;
+  if (!seqs || !k || !v) return LESS_ERR_NULL_POINTER;
+  if (((uintptr_t)seqs | (uintptr_t)starts) & 3) return LESS_ERR_MISALIGNED;
+  const int64_t row = (int64_t)layer_count * d->heads * d->head_dim;
+  if (k_stride < row || v_stride < row) return LESS_ERR_INVALID_CONFIG;
+  if ((((uintptr_t)k | (uintptr_t)v) & 15) || ((k_stride | v_stride) & 7)) return LESS_ERR_MISALIGNED;
+  PwArgs a = {k, v, k_stride, v_stride, seqs, starts, n, rows, layer_begin};
+  const bool bf16 = d->flags & LESS_PAGES_BF16, e4m3 = d->flags & LESS_PAGES_E4M3;
+  const int turn = PW_THREADS / (2 * d->head_dim);
+  const dim3 grid(rows / kPageBlock + 2 * n, pg_ceil(d->heads, turn), layer_count);
+  if (grid.y > 65535) return LESS_ERR_INVALID_CONFIG;
+  cudaStream_t s = (cudaStream_t)stream;
+#define PW_LAUNCH(T, D, E) pages_write_kernel<T, D, E><<<grid, PW_THREADS, 0, s>>>(p, a)
+#define PW_TYPES(D)                                                                         \
+  if (bf16) { if (e4m3) PW_LAUNCH(__nv_bfloat16, D, true); else PW_LAUNCH(__nv_bfloat16, D, false); } \
+  else { if (e4m3) PW_LAUNCH(__half, D, true); else PW_LAUNCH(__half, D, false); }
+  if (d->head_dim == 128) { PW_TYPES(128) } else { PW_TYPES(64) }
+#undef PW_TYPES
+#undef PW_LAUNCH
+  return check_launch("pages_write_kernel");
+}
