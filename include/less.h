@@ -397,7 +397,7 @@ int less_pages_compact(const less_pages* cache, void* cuda_stream);
  * k, v: device fp16 / bf16 [rows, layer_count, heads, D], `stride` elements from row to row (a multiple of 8), for
  * layers [layer_begin, + layer_count).  code = round(x * top / amax), ties to even, with amax = the largest |x| of the
  * block (16 tokens x D of a layer and head); where a block holds older tokens, its amax only grows and their codes
- * are rounded again.  Infinities count as the largest finite value (bf16: 2^100), NaN as 0.  Rows behind starts[n] are
+ * are rounded again.  Infinities count as the largest finite value (bf16: 2^100), NaN and an amax below 2^-100 as 0.  Rows behind starts[n] are
  * not read; of a sequence listed twice the first entry counts; a page that other sequences hold too is not
  * written (LESS_ERR_BAD_STATE). */
 int less_pages_write(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n, const int32_t* seqs,

@@ -126,8 +126,5 @@ __device__ __forceinline__ int pg_page(const PgParams& p, int seq, int ordinal) 
 // host: checks a description; on success fills the device view
 int pg_view(const less_pages* d, PgParams* p);
 int pg_sms();
-int launch_pages_step(const less_pages* d, const PgParams& p, int layer0, int nl, int n, const int32_t* seqs,
-                      const int32_t* starts, int rows, int max_rows, const void* q, int64_t q_stride, int window,
-                      int sinks, float scale, void* out, cudaStream_t s);
 
 }  // namespace less

@@ -25,7 +25,7 @@
 #include <type_traits>
 
 #include "less_internal.cuh"
-#include "pages.cuh"
+#include "pages_attn.cuh"
 
 namespace less {
 
@@ -37,47 +37,12 @@ constexpr int PS_SLOT_FLOATS = 2112;           // rows x (D + 2) floats: 16 x 13
 // 128 registers a thread hold the sums and queries of eight rows; more rows take what one block per SM leaves
 __host__ __device__ constexpr int ps_blocks_per_sm(int NT) { return NT == 1 ? 2 : 1; }
 
-struct PaArgs {
-  const void* q;
-  void* out;
-  int64_t q_stride;              // elements from token to token
-  const int32_t* seqs;
-  const int32_t* starts;
-  int n, rows, layer0, nl;
-  int max_rows;                  // entries with more rows (tokens x query heads of a group) are not this kernel's
-  int window, sinks;             // window 0 = all
-  float scale;
-};
-
-// the 16-token blocks that the tokens of an entry see: [0, sb) and [wb, eb)
-struct Blocks {
-  int sb, wb, eb;
-  __device__ __forceinline__ int count() const { return sb + eb - wb; }
-  __device__ __forceinline__ int at(int u) const { return u < sb ? u : wb + (u - sb); }
-};
-__device__ __forceinline__ Blocks visible_blocks(const PaArgs& a, int len, int count) {
-  Blocks b;
-  b.eb = pg_ceil(len, kPageBlock);
-  b.sb = b.wb = 0;
-  if (a.window) {
-    b.wb = max(0, len - count - a.window + 1) / kPageBlock;
-    b.sb = min(b.wb, pg_ceil(a.sinks, kPageBlock));
-  }
-  return b;
-}
-
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-__device__ __forceinline__ float pa_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -92,29 +57,6 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
   return y;
 }
 
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T* dst, const float* f);       // 8 values, 16 bytes
-template <>
-__device__ __forceinline__ void store8<__half>(__half* dst, const float* f) {
-  uint4 u;
-  __half2* h = reinterpret_cast<__half2*>(&u);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
-  *reinterpret_cast<uint4*>(dst) = u;
-}
-template <>
-__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* dst, const float* f) {
-  uint4 u;
-  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-  *reinterpret_cast<uint4*>(dst) = u;
-}
 __device__ __forceinline__ void store4(__half* dst, float4 f) {
   __half2 h[2] = {__floats2half2_rn(f.x, f.y), __floats2half2_rn(f.z, f.w)};
   *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(h);
@@ -651,7 +593,7 @@ extern "C" int less_pages_attention(const less_pages* d, int32_t layer_begin, in
                                     const void* q, int64_t q_stride, int32_t window, int32_t sinks, float scale,
                                     void* out, void* stream) {
   PgParams p;
-  const int rc = pg_view(d, &p);
+  int rc = pg_view(d, &p);
   if (rc != LESS_OK) return rc;
   if (layer_begin < 0 || layer_count < 1 || layer_begin > d->layers - layer_count) return LESS_ERR_BAD_LAYER_RANGE;
   if (n < 0 || n > (1 << 24) || rows < 0 || (!starts && rows != n) || max_new < 1) return LESS_ERR_INVALID_CONFIG;
@@ -667,8 +609,14 @@ extern "C" int less_pages_attention(const less_pages* d, int32_t layer_begin, in
               window > (1 << 30) ? 0 : window, sinks > (1 << 30) ? 1 << 30 : sinks, scale};
   if (!starts) max_new = 1;
   const int64_t most = (int64_t)max_new * d->group;
-  const int r = most > 0x7fffffff ? 0x7fffffff : (int)most;
+  int r = most > 0x7fffffff ? 0x7fffffff : (int)most;
   cudaStream_t s = (cudaStream_t)stream;
+  if (r > kStepRows) {
+    a.max_rows = kStepRows;
+    rc = launch_pages_chunk(p, a, d->head_dim, d->flags, s);
+    if (rc != LESS_OK || !starts || d->group > kStepRows) return rc;   // without starts all entries are alike
+    r = kStepRows;
+  }
   if (d->flags & LESS_PAGES_BF16)
     return (d->flags & LESS_PAGES_E4M3) ? launch_step_dim<__nv_bfloat16, true>(p, a, d->head_dim, r, s)
                                         : launch_step_dim<__nv_bfloat16, false>(p, a, d->head_dim, r, s);

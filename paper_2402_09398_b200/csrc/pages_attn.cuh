@@ -1,0 +1,71 @@
+// What the two attention kernels over the paged 8-bit cache share (pages_attn.cu, pages_chunk.cu).
+#pragma once
+
+#include "pages.cuh"
+
+namespace less {
+
+struct PaArgs {
+  const void* q;
+  void* out;
+  int64_t q_stride;              // elements from token to token
+  const int32_t* seqs;
+  const int32_t* starts;
+  int n, rows, layer0, nl;
+  int max_rows;                  // entries with more rows (tokens x query heads of a group) are not this kernel's
+  int window, sinks;             // window 0 = all
+  float scale;
+};
+
+// the 16-token blocks that the tokens of an entry see: [0, sb) and [wb, eb)
+struct Blocks {
+  int sb, wb, eb;
+  __device__ __forceinline__ int count() const { return sb + eb - wb; }
+  __device__ __forceinline__ int at(int u) const { return u < sb ? u : wb + (u - sb); }
+};
+__device__ __forceinline__ Blocks visible_blocks(const PaArgs& a, int len, int count) {
+  Blocks b;
+  b.eb = pg_ceil(len, kPageBlock);
+  b.sb = b.wb = 0;
+  if (a.window) {
+    b.wb = max(0, len - count - a.window + 1) / kPageBlock;
+    b.sb = min(b.wb, pg_ceil(a.sinks, kPageBlock));
+  }
+  return b;
+}
+
+__device__ __forceinline__ float pa_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* dst, const float* f);       // 8 values, 16 bytes
+template <>
+__device__ __forceinline__ void store8<__half>(__half* dst, const float* f) {
+  uint4 u;
+  __half2* h = reinterpret_cast<__half2*>(&u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+  *reinterpret_cast<uint4*>(dst) = u;
+}
+template <>
+__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* dst, const float* f) {
+  uint4 u;
+  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+  *reinterpret_cast<uint4*>(dst) = u;
+}
+// rows of an entry (tokens x query heads of a group) up to which it is the step kernel's
+constexpr int kStepRows = 32;
+
+int launch_pages_chunk(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);
+
+}  // namespace less

@@ -1,0 +1,539 @@
+// Attention of many new tokens over the paged 8-bit cache (the chunk kernel): the same result as the step kernel
+// (pages_attn.cu) where a sequence brings enough rows - tokens x query heads of a KV head - to fill tensor-core tiles.
+//
+// Bound by arithmetic: 4 D flops per visible (query, key) pair and one exponential.  One CTA = 256 rows of one
+// (sequence, layer, KV head) as two tiles of 128 (a tensor-memory lane per row), key tiles of 128 tokens:
+//   warps 8 - 11   codes -> fp16 operand tiles in shared memory.  A stored tile is read with coalesced 16-byte loads
+//                  straight into registers (the next tile's while this one is converted), so there is no staging;
+//                  both operands are written K-major with the 128-byte swizzle, free of bank conflicts: the keys of
+//                  a tile are ordered (8 token groups of 4, alternating between two stored tiles) such that the four
+//                  tokens that a stored value word holds, of two tiles, are one 16-byte piece of V^T.
+//   warp 12        S = Q K^T                tcgen05, 128 x 128, fp32 in tensor memory, one buffer per row tile
+//   warps 0 - 7    softmax, a thread per row: P back over S as the A operand of
+//   warp 13        O += P V                 tcgen05, A from tensor memory, fp32 accumulator in tensor memory
+// The two row tiles alternate: while one is in softmax, the tensor cores work on the other.
+// Codes are exact in fp16 and are never scaled.  The magnitude a_k of a key block is part of the factor that turns a
+// score into the exponent, and that of a value block, as log2 a_v, part of the exponent's offset:
+//   P = 2^(s a_k c + log2 a_v - M)            sum of the probabilities: sum over blocks of (sum P) / a_v
+// M is a running reference of a row: scores are exponentiated against the M at hand in one pass, and only if one
+// exceeds it by 2^8 - as a rule in the first tile alone - are O and the sums rescaled and the pass repeated.
+// Roundings: P (at most 2^8, the largest of a row at least near 1) is rounded once to fp16, 2^-11 of each with
+// independent signs, queries as in the step kernel, the output once.
+#include <atomic>
+#include <type_traits>
+
+#include "less_internal.cuh"
+#include "pages_attn.cuh"
+#include "tc_common.cuh"
+
+namespace less {
+
+constexpr int PC_ROWS = 128, PC_KEYS = 128;
+constexpr int PC_TILES = PC_KEYS / kPageBlock;            // stored tiles of a key tile
+constexpr int PC_SOFT_WARPS = 8, PC_DEQ_WARPS = 4;
+constexpr int PC_THREADS = (PC_SOFT_WARPS + PC_DEQ_WARPS + 2) * 32;
+constexpr int PC_STAGES = 2, PC_META = 4;
+
+struct PcMeta {                                           // of the eight stored tiles of a key tile
+  float k1[PC_TILES];                                     // a_k / top
+  float lav[PC_TILES], iav[PC_TILES];                     // log2 a_v, 1 / a_v
+  int j0[PC_TILES];                                       // position of the first token, 2^30 = no tile
+  uint32_t part[PC_TILES];                                // bit x: row tile x does not see all of it
+};
+
+struct PcShared {
+  uint64_t q_full, k_full[PC_STAGES], k_empty[PC_STAGES], v_full[PC_STAGES], v_empty[PC_STAGES];
+  uint64_t s_full[2], p_full[2], pv_done[2];
+  PcMeta meta[PC_META];
+  uint32_t tmem_base;
+  int abort;
+};
+
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      :
+      : "r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+// Slots of the grid: entry i owns slots [starts[i] G / 256 + i, starts[i + 1] G / 256 + i + 1) - at least as many as it
+// has pairs of row tiles
+__device__ __forceinline__ int64_t pc_slot(const PgParams& p, const PaArgs& a, int i) {
+  const int row = a.starts ? min(max(__ldg(a.starts + i), 0), a.rows) : i;
+  return (int64_t)row * p.group / (2 * PC_ROWS) + i;
+}
+
+// visibility of the 32 columns of a stored-tile pair, bit 16 e + r = token r of tile e
+__device__ __forceinline__ uint32_t pc_mask16(int j0, int pos, int window, int sinks) {
+  const int hi = min(max(pos + 1 - j0, 0), 16);
+  uint32_t m = (1u << hi) - 1;                            // j <= pos
+  if (window) {
+    const int lo = min(max(pos - window + 1 - j0, 0), 16), sk = min(max(sinks - j0, 0), 16);
+    m &= ~((1u << lo) - 1) | ((1u << sk) - 1);
+  }
+  return m & 0xffffu;
+}
+
+template <typename T, int D, bool E4M3>
+__global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, PaArgs a) {
+  constexpr int QT = PC_ROWS * D * 2;                     // bytes of a Q tile; K and V tiles alike
+  constexpr int KT = PC_KEYS * D * 2;
+  extern __shared__ __align__(1024) unsigned char pc_smem[];
+  unsigned char* qres = pc_smem;                          // [2 row tiles][D / 64][128 rows][128 B]
+  unsigned char* kring = qres + 2 * QT;                   // [stages][D / 64][128 keys][128 B]
+  unsigned char* vring = kring + PC_STAGES * KT;          // [stages][2 key halves][D dims][128 B]
+  PcShared* sh = reinterpret_cast<PcShared*>(vring + PC_STAGES * KT);
+  if (smem_misaligned(pc_smem, p.status, 120)) return;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // ---- the item: late rows, which see most, first ----
+  const int64_t slot = gridDim.y - 1 - blockIdx.y;
+  int lo = 0, hi = a.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (pc_slot(p, a, mid) <= slot) lo = mid; else hi = mid - 1;
+  }
+  const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, lo);
+  const int64_t rows = (int64_t)e.count * p.group;
+  const int64_t row0 = (slot - pc_slot(p, a, lo)) * (2 * PC_ROWS);
+  if (rows <= a.max_rows || row0 >= rows) return;         // the step kernel's, or no rows left
+  const int valid = (int)min(rows - row0, (int64_t)2 * PC_ROWS), nx = valid > PC_ROWS ? 2 : 1;
+  const int lj = blockIdx.x / p.heads, h = blockIdx.x - lj * p.heads, layer = a.layer0 + lj;
+  const int base = e.len - e.count;                       // position of the entry's first token
+  const int tok0 = (int)(row0 / p.group), tok1 = (int)((row0 + valid - 1) / p.group);
+  const Blocks vb = visible_blocks(a, base + tok1 + 1, tok1 - tok0 + 1);
+  const int units = base + tok1 < 0 ? 0 : vb.count();
+  const int nk = pg_ceil(units, PC_TILES);
+  const int64_t head_row = ((int64_t)lj * p.heads + h) * p.group * D;
+  T* out = reinterpret_cast<T*>(a.out);
+
+  if (nk == 0) {                                          // nothing to see
+    for (int i = tid; i < valid * (D / 8); i += PC_THREADS) {
+      const int64_t rr = row0 + i / (D / 8);
+      const int tok = (int)(rr / p.group), hd = (int)(rr - (int64_t)tok * p.group);
+      *reinterpret_cast<uint4*>(out + (int64_t)(e.row0 + tok) * a.nl * p.heads * p.group * D + head_row + hd * D +
+                                i % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+    }
+    return;
+  }
+
+  if (tid == 0) {
+    mbar_init(&sh->q_full, 4 * nx);
+    for (int s = 0; s < PC_STAGES; ++s) {
+      mbar_init(&sh->k_full[s], PC_DEQ_WARPS);
+      mbar_init(&sh->k_empty[s], 1);
+      mbar_init(&sh->v_full[s], PC_DEQ_WARPS);
+      mbar_init(&sh->v_empty[s], 1);
+    }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(&sh->s_full[x], 2);
+      mbar_init(&sh->p_full[x], 4);
+      mbar_init(&sh->pv_done[x], 1);
+    }
+    sh->abort = 0;
+    mbar_fence_init();
+  }
+  if (warp == 12) tmem_alloc(&sh->tmem_base, 512);
+  fence_proxy_async_smem();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = sh->tmem_base;
+  constexpr uint32_t OCOL = 2 * PC_KEYS;                  // S / P of the two row tiles, then their accumulators
+  volatile int* abortp = &sh->abort;
+  int32_t* status = p.status;
+
+  if (warp < PC_SOFT_WARPS) {
+    // ---------------- softmax: thread = row ----------------
+    const int x = warp >> 2, quad = warp & 3;
+    if (x < nx) {
+      const int r = x * PC_ROWS + quad * 32 + lane;
+      const int64_t rr = row0 + min(r, valid - 1);
+      const int tok = (int)(rr / p.group), hd = (int)(rr - (int64_t)tok * p.group);
+      const int pos = base + tok;
+      // the row's query, as fp16, into the operand tile
+      float crow = a.scale * 1.4426950408889634f;
+      {
+        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + (int64_t)(e.row0 + tok) * a.q_stride +
+                                                          head_row + hd * D);
+        unsigned char* dst = qres + x * QT + (r & (PC_ROWS - 1)) * 128;
+        float down = 1.f;
+        if (!std::is_same<T, __half>::value) {
+          float most = 0.f;
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 w = __ldg(src + c);
+            const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 f = __bfloat1622float2(y[i]);
+              most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
+            }
+          }
+          const int ex = min(max((int)(__float_as_uint(most) >> 23), 1), 253);
+          crow *= __uint_as_float((uint32_t)ex << 23);
+          down = __uint_as_float((uint32_t)(254 - ex) << 23);
+        }
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          uint4 w = r < valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+          if (!std::is_same<T, __half>::value) {
+            const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&w);
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 f = __bfloat1622float2(y[i]);
+              u[i] = pack2(f.x * down, f.y * down);
+            }
+            w = make_uint4(u[0], u[1], u[2], u[3]);
+          }
+          *reinterpret_cast<uint4*>(dst + (c >> 3) * (QT / (D / 64)) + (((c & 7) ^ (r & 7)) << 4)) = w;
+        }
+        fence_proxy_async_smem();
+        mbar_arrive_warp(&sh->q_full);
+      }
+
+      const uint32_t lane_addr = tmem + ((uint32_t)(quad * 32) << 16);
+      const uint32_t scol = lane_addr + x * PC_KEYS, ocol = lane_addr + OCOL + x * D;
+      float M = -INFINITY, l = 0.f;
+      for (int kt = 0; kt < nk; ++kt) {
+        wait_or_give_up(&sh->s_full[x], kt & 1, abortp, status, 122);
+        if (__any_sync(0xffffffffu, *abortp)) break;
+        tc_fence_after_sync();
+        const PcMeta& meta = sh->meta[kt % PC_META];
+        uint32_t part = 0;
+#pragma unroll
+        for (int i = 0; i < PC_TILES; ++i) part |= meta.part[i];
+        const bool masked = part >> x & 1;
+
+        uint32_t pk[PC_KEYS / 2];
+        float most, add;
+        auto pass = [&](auto with_mask, float ref) {
+          most = -INFINITY;
+          add = 0.f;
+#pragma unroll
+          for (int c = 0; c < PC_KEYS / 32; ++c) {        // a pair of stored tiles: 4 columns of one, 4 of the other, ...
+            uint32_t s[32];
+            tmem_ld32(scol + 32 * c, s);
+            const float ke = meta.k1[2 * c] * crow, ko = meta.k1[2 * c + 1] * crow;
+            const float be = meta.lav[2 * c] - ref, bo = meta.lav[2 * c + 1] - ref;
+            uint32_t m = 0xffffffffu;
+            if (decltype(with_mask)::value)
+              m = pc_mask16(meta.j0[2 * c], pos, a.window, a.sinks) |
+                  pc_mask16(meta.j0[2 * c + 1], pos, a.window, a.sinks) << 16;
+            const uint64_t k2[2] = {f32x2_pack(ke, ke), f32x2_pack(ko, ko)}, b2[2] = {f32x2_pack(be, be), f32x2_pack(bo, bo)};
+            uint64_t sum[2] = {0, 0};
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {                // columns 2 i, 2 i + 1
+              const int ev = (i >> 1) & 1, tokbit = 16 * ev + 4 * (i >> 2) + 2 * (i & 1);
+              float y0, y1;
+              f32x2_unpack(f32x2_fma((uint64_t)s[2 * i] | (uint64_t)s[2 * i + 1] << 32, k2[ev], b2[ev]), y0, y1);
+              if (decltype(with_mask)::value) {
+                y0 = m >> tokbit & 1 ? y0 : -INFINITY;
+                y1 = m >> (tokbit + 1) & 1 ? y1 : -INFINITY;
+              }
+              most = fmaxf(most, fmaxf(y0, y1));
+              const float p0 = pa_ex2(y0), p1 = pa_ex2(y1);
+              sum[ev] = f32x2_add(sum[ev], f32x2_pack(p0, p1));
+              pk[16 * c + i] = pack2(p0, p1);
+            }
+            float e0, e1, o0, o1;
+            f32x2_unpack(sum[0], e0, e1);
+            f32x2_unpack(sum[1], o0, o1);
+            add = fmaf(e0 + e1, meta.iav[2 * c], fmaf(o0 + o1, meta.iav[2 * c + 1], add));
+          }
+        };
+        for (bool again = false;; again = true) {
+          const float ref = M == -INFINITY ? 0.f : M;
+          if (masked) pass(std::true_type{}, ref); else pass(std::false_type{}, ref);
+          const bool up = M == -INFINITY ? most > -INFINITY : most > 8.f;
+          if (again || !__any_sync(0xffffffffu, up)) break;
+          const float f = M == -INFINITY || !up ? 1.f : pa_ex2(-most);
+          if (up) M = ref + most;
+          l *= f;
+          if (kt) {
+            wait_or_give_up(&sh->pv_done[x], (kt - 1) & 1, abortp, status, 123);
+            tc_fence_after_sync();
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[32];
+              tmem_ld32(ocol + 32 * c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st32(ocol + 32 * c, o);
+            }
+            tmem_st_wait();
+          }
+        }
+        l += add;
+        tmem_st32(scol, pk);
+        tmem_st32(scol + 32, pk + 32);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        mbar_arrive_warp(&sh->p_full[x]);
+      }
+      wait_or_give_up(&sh->pv_done[x], (nk - 1) & 1, abortp, status, 124);
+      tc_fence_after_sync();
+      if (!*abortp) {
+        const float inv = l == 0.f ? 0.f : 1.f / l, unit = 1.f / pg_top<E4M3>();
+        T* dst = out + (int64_t)(e.row0 + tok) * a.nl * p.heads * p.group * D + head_row + hd * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(ocol + 32 * c, o);
+          tmem_ld_wait();
+          float f[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(o[i]) * inv * unit;
+          if (r < valid) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) store8<T>(dst + 32 * c + i, f + i);
+          }
+        }
+      }
+    }
+  } else if (warp < PC_SOFT_WARPS + PC_DEQ_WARPS) {
+    // ---------------- codes -> operand tiles: a warp per pair of stored tiles ----------------
+    constexpr int KP = D / 32;                            // 16-byte pieces of a lane in a stored tile
+    const int dw = warp - PC_SOFT_WARPS, g = lane >> 2, t = lane & 3;
+    // positions of the rows of the two row tiles
+    int first_pos[2], last_pos[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      first_pos[x] = base + (int)((row0 + min(x * PC_ROWS, valid - 1)) / p.group);
+      last_pos[x] = base + (int)((row0 + min((x + 1) * PC_ROWS, valid) - 1) / p.group);
+    }
+    // lane 2 i + b knows tile b of this warp's pair in key tile `batch + i`
+    int page_l = -1, j_l = 0;
+    float ak_l = 0.f, av_l = 0.f, vlast = 1.f;
+    auto lookup = [&](int batch) {
+      const int u = (batch + (lane >> 1)) * PC_TILES + 2 * dw + (lane & 1);
+      page_l = -1;
+      j_l = 0;
+      if (u < units) {
+        j_l = vb.at(u) * kPageBlock;
+        page_l = pg_page(p, e.seq, j_l >> p.pt_shift);
+        if (page_l >= 0) {
+          const float* mg = p.amax + pg_mag(p, layer, page_l, h) + (j_l & (p.pt - 1)) / kPageBlock;
+          ak_l = __ldg(mg);
+          av_l = __ldg(mg + p.pt / kPageBlock);
+        }
+      }
+    };
+    uint4 kreg[2][KP], vreg[2][KP];
+    int kpage[2], kj[2];
+    float kak[2], kav[2];
+    // K of key tile kt on its way to registers; which piece a slot holds depends on the lane (see the stores)
+    auto load = [&](int kt, bool values) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int src = 2 * (kt & 15) + b;
+        const int page = __shfl_sync(0xffffffffu, page_l, src), j = __shfl_sync(0xffffffffu, j_l, src);
+        const float av = __shfl_sync(0xffffffffu, av_l, src);
+        if (!values) {
+          kpage[b] = page;
+          kj[b] = j;
+          kak[b] = __shfl_sync(0xffffffffu, ak_l, src);
+          kav[b] = av;
+        }
+        uint4(&reg)[KP] = values ? vreg[b] : kreg[b];
+        // values of magnitude 0 are zeros whatever their codes are: the exponent then carries another magnitude
+        if (page >= 0 && (!values || av > 0.f)) {
+          const uint8_t* s = p.codes + pg_slab(p, D, layer, page, h) + (size_t)(j & (p.pt - 1)) * D + lane * 16;
+          if (values) s += (size_t)p.pt * D;
+#pragma unroll
+          for (int i = 0; i < KP; ++i) {
+            const int piece = values ? i ^ (g & 1) : (D == 128 ? i ^ (t >> 1) : i);
+            reg[i] = __ldg(reinterpret_cast<const uint4*>(s + piece * 512));
+          }
+          // tokens behind the end may hold any byte; a NaN code would survive its zero probability
+          if (E4M3 && values && j + kPageBlock > e.len) {
+            const int left = e.len - (j + 4 * t);
+            const uint32_t keep = left <= 0 ? 0u : (left >= 4 ? 0xffffffffu : 0xffffffffu >> (8 * (4 - left)));
+#pragma unroll
+            for (int i = 0; i < KP; ++i) {
+              reg[i].x &= keep;
+              reg[i].y &= keep;
+              reg[i].z &= keep;
+              reg[i].w &= keep;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < KP; ++i) reg[i] = make_uint4(0, 0, 0, 0);
+        }
+      }
+    };
+    lookup(0);
+    load(0, false);
+    load(0, true);
+    for (int kt = 0; kt < nk; ++kt) {
+      const int st = kt % PC_STAGES, ph = (kt / PC_STAGES) & 1;
+      wait_or_give_up(&sh->k_empty[st], ph ^ 1, abortp, status, 125);
+      if (__any_sync(0xffffffffu, *abortp)) break;
+      unsigned char* kd = kring + st * KT;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < KP; ++i) {
+          // piece j * (D / 64) + half: token 4 (g / 2) + 2 j + g % 2, dimensions t D / 4 + 16 half ..  Lanes with t >= 2
+          // take the halves in the other order: then the eight lanes of a store phase hit eight different banks.
+          const int j = i / (D / 64), half = D == 128 ? (i & 1) ^ (t >> 1) : 0;
+          const int key = dw * 32 + (g >> 1) * 8 + b * 4 + 2 * j + (g & 1);
+          const int d0 = t * (D / 4) + 16 * half;
+          unsigned char* row = kd + (d0 >> 6) * (PC_KEYS * 128) + key * 128;
+          const int c = (d0 & 63) >> 3;
+          const uint32_t w[4] = {kreg[b][i].x, kreg[b][i].y, kreg[b][i].z, kreg[b][i].w};
+          uint32_t u[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) pg_unpack4<E4M3>(w[k], u[2 * k], u[2 * k + 1]);
+          *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
+          *reinterpret_cast<uint4*>(row + (((c + 1) ^ (key & 7)) << 4)) = make_uint4(u[4], u[5], u[6], u[7]);
+        }
+      if (lane < 2) {
+        const int b = lane, i = 2 * dw + b;
+        const int page = b ? kpage[1] : kpage[0], j = b ? kj[1] : kj[0];
+        const float ak = b ? kak[1] : kak[0], av = b ? kav[1] : kav[0];
+        PcMeta& m = sh->meta[kt % PC_META];
+        // values that are all zero may have any magnitude: the last one seen
+        if (page >= 0 && av > 0.f) vlast = fmaxf(av, 0x1p-100f);
+        m.k1[i] = page >= 0 ? ak * (1.f / pg_top<E4M3>()) : 0.f;
+        m.lav[i] = log2f(vlast);
+        m.iav[i] = 1.f / vlast;
+        m.j0[i] = page >= 0 ? j : 1 << 30;
+        uint32_t part = 0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (page < 0 || j + kPageBlock - 1 > first_pos[x] ||
+              (a.window && j <= last_pos[x] - a.window && j + kPageBlock > a.sinks))
+            part |= 1u << x;
+        m.part[i] = part;
+      }
+      fence_proxy_async_smem();
+      mbar_arrive_warp(&sh->k_full[st]);
+      // V of this key tile is in its registers; pages of the next batch before the next K is asked for
+      if (kt + 1 < nk) {
+        if (((kt + 1) & 15) == 0) lookup(kt + 1);
+        load(kt + 1, false);
+      }
+      wait_or_give_up(&sh->v_empty[st], ph ^ 1, abortp, status, 126);
+      if (__any_sync(0xffffffffu, *abortp)) break;
+      unsigned char* vd = vring + st * KT + (dw >> 1) * (D * 128);
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        // lanes with odd g take the pieces in the other order: the banks again
+        const uint32_t w0[4] = {vreg[0][i].x, vreg[0][i].y, vreg[0][i].z, vreg[0][i].w};
+        const uint32_t w1[4] = {vreg[1][i].x, vreg[1][i].y, vreg[1][i].z, vreg[1][i].w};
+#pragma unroll
+        for (int dd = 0; dd < 4; ++dd) {
+          const int dim = g * (D / 8) + 4 * (i ^ (g & 1)) + dd;
+          uint32_t u[4];
+          pg_unpack4<E4M3>(w0[dd], u[0], u[1]);
+          pg_unpack4<E4M3>(w1[dd], u[2], u[3]);
+          *reinterpret_cast<uint4*>(vd + dim * 128 + ((((dw & 1) * 4 + t) ^ (dim & 7)) << 4)) =
+              make_uint4(u[0], u[1], u[2], u[3]);
+        }
+      }
+      fence_proxy_async_smem();
+      mbar_arrive_warp(&sh->v_full[st]);
+      if (kt + 1 < nk) load(kt + 1, true);
+    }
+  } else if (warp == 12) {
+    // ---------------- S = Q K^T ----------------
+    if (lane == 0) {
+      constexpr uint32_t idesc = idesc_f16(PC_ROWS, PC_KEYS, 0, 0);
+      const uint64_t ad = smem_desc(smem_u32(qres), 16, 1024, kLayoutSw128);
+      const uint64_t bd = smem_desc(smem_u32(kring), 16, 1024, kLayoutSw128);
+      wait_or_give_up(&sh->q_full, 0, abortp, status, 127);
+      for (int kt = 0; kt < nk; ++kt) {
+        const int st = kt % PC_STAGES;
+        wait_or_give_up(&sh->k_full[st], (kt / PC_STAGES) & 1, abortp, status, 128);
+        for (int x = 0; x < nx; ++x) {
+          // the buffer held S and then P of the key tile before
+          if (kt) wait_or_give_up(&sh->pv_done[x], (kt - 1) & 1, abortp, status, 129);
+          if (*abortp) break;
+          tc_fence_after_sync();
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks)
+            mma_f16_ss(tmem + x * PC_KEYS,
+                       ad + (uint64_t)((x * QT + (ks >> 2) * (PC_ROWS * 128)) >> 4) + (uint64_t)((ks & 3) * 2),
+                       bd + (uint64_t)((st * KT + (ks >> 2) * (PC_KEYS * 128)) >> 4) + (uint64_t)((ks & 3) * 2), idesc,
+                       ks ? 1u : 0u);
+          mma_commit(&sh->s_full[x]);
+          mbar_arrive(&sh->s_full[x]);                    // passes on what came with k_full (the magnitudes)
+        }
+        if (*abortp) break;
+        mma_commit(&sh->k_empty[st]);
+      }
+    }
+  } else {
+    // ---------------- O += P V ----------------
+    if (lane == 0) {
+      constexpr uint32_t idesc = idesc_f16(PC_ROWS, D, 0, 0);
+      const uint64_t bd = smem_desc(smem_u32(vring), 16, 1024, kLayoutSw128);
+      for (int kt = 0; kt < nk; ++kt) {
+        const int st = kt % PC_STAGES;
+        wait_or_give_up(&sh->v_full[st], (kt / PC_STAGES) & 1, abortp, status, 130);
+        for (int x = 0; x < nx; ++x) {
+          wait_or_give_up(&sh->p_full[x], kt & 1, abortp, status, 131);
+          if (*abortp) break;
+          tc_fence_after_sync();
+#pragma unroll
+          for (int ks = 0; ks < PC_KEYS / 16; ++ks)
+            mma_f16_ts(tmem + OCOL + x * D, tmem + x * PC_KEYS + 8 * ks,
+                       bd + (uint64_t)((st * KT + (ks >> 2) * (D * 128)) >> 4) + (uint64_t)((ks & 3) * 2), idesc,
+                       (kt | ks) ? 1u : 0u);
+          mma_commit(&sh->pv_done[x]);
+        }
+        if (*abortp) break;
+        mma_commit(&sh->v_empty[st]);
+      }
+    }
+  }
+  drain_after_abort(abortp);
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 12) tmem_dealloc(tmem, 512);
+}
+
+template <typename T, int D, bool E4M3>
+static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
+  constexpr size_t smem = (size_t)(2 * PC_ROWS + 2 * PC_STAGES * PC_KEYS) * D * 2 + sizeof(PcShared);
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return fail_cuda("cudaGetDevice");
+  if (dev >= 64 || !(done.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (cudaFuncSetAttribute(pages_chunk_kernel<T, D, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
+        cudaSuccess)
+      return fail_cuda("shared memory opt-in of pages_chunk_kernel");
+    if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n;
+  if (slots > 65535) return LESS_ERR_INVALID_CONFIG;
+  pages_chunk_kernel<T, D, E4M3><<<dim3(p.heads * a.nl, (unsigned)slots), PC_THREADS, smem, s>>>(p, a);
+  return check_launch("pages_chunk_kernel");
+}
+
+int launch_pages_chunk(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s) {
+  const bool e4m3 = flags & LESS_PAGES_E4M3;
+  if (flags & LESS_PAGES_BF16) {
+    if (dim == 128) return e4m3 ? launch_chunk<__nv_bfloat16, 128, true>(p, a, s) : launch_chunk<__nv_bfloat16, 128, false>(p, a, s);
+    return e4m3 ? launch_chunk<__nv_bfloat16, 64, true>(p, a, s) : launch_chunk<__nv_bfloat16, 64, false>(p, a, s);
+  }
+  if (dim == 128) return e4m3 ? launch_chunk<__half, 128, true>(p, a, s) : launch_chunk<__half, 128, false>(p, a, s);
+  return e4m3 ? launch_chunk<__half, 64, true>(p, a, s) : launch_chunk<__half, 64, false>(p, a, s);
+}
+
+}  // namespace less

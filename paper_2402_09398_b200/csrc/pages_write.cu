@@ -7,7 +7,8 @@
 // x * top and code * a_old are exact in fp32 (16-bit inputs), the quotient is correctly rounded, and a quotient that
 // is not a tie is further than 2^-19 (relative) from one: the codes are those of exact arithmetic.
 // Infinities are written as the largest finite fp16 number (bf16: 2^100, so that x * top stays finite), NaN as 0:
-// one bad token must not take the other fifteen of its block with it.  Tokens of the last block behind the
+// one bad token must not take the other fifteen of its block with it.  Magnitudes below 2^-100 (bf16) become 0: the
+// attention divides by magnitudes.  Tokens of the last block behind the
 // sequence's end get code 0.
 //
 // Bound by memory: 2 bytes read and 1 written per value.  A block of threads takes one 16-token block of one layer
@@ -147,6 +148,7 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwA
     m = old;
 #pragma unroll
     for (int w = 0; w < PER / 32; ++w) m = fmaxf(m, red[tid / PER * (PER / 32) + w]);
+    if (m < 0x1p-100f) m = 0.f;                          // its codes come out as 0 too
     if (in) {
       const float unit = m > 0.f ? m : 1.f, top = pg_top<E4M3>();
       uint32_t out[4];

@@ -157,6 +157,7 @@ class Model:
                             cell = (layer_begin + lj, page, h, which)
                             old = self.amax[cell + (inner,)] if keep else 0.0
                             a = max(old, np.abs(x[:, lj, h]).max())
+                            a = 0.0 if a < 2.0 ** -100 else a
                             unit, top = a if a > 0 else 1.0, TOP[self.fmt]
                             tile = np.zeros((BLOCK, self.D), np.uint8)
                             if keep:
@@ -179,7 +180,9 @@ class Model:
 
         The bound: 8 (D / 16) accumulations of a score round to 2^-22 of at most scale * sum |q| |k| each (the tensor
         cores' fp32 sums may truncate), so a probability is off by that much relative, an output by twice that of the
-        largest |v|; exponentials and the two sums add less than 2^-19 of it."""
+        largest |v|; exponentials and the two sums add less than 2^-19 of it.  An entry of more than 32 rows (tokens x
+        query heads of a KV head) may have its probabilities rounded to fp16 once, half a step being 2^-11 of each or,
+        below 2^-14 of the row's largest, 2^-25: 2^-11 + n 2^-25 of the largest |v| more."""
         scale = self.D ** -0.5 if scale is None else scale
         out, bound = np.zeros(q.shape), np.zeros(q.shape)
         for i, s in enumerate(seqs):
@@ -208,5 +211,7 @@ class Model:
                         reach = np.where(ok, np.abs(qq) @ np.abs(k).T * scale, 0.0).max(1)
                         most = np.abs(v).max() if v.size else 0.0
                         rel = 2 * (self.D // 16) * reach * 2.0 ** -22 + 2.0 ** -19
+                        if m * self.G > 32:
+                            rel = rel + 2.0 ** -11 + n * 2.0 ** -25
                         bound[starts[i]:starts[i + 1], lj, h * self.G + g] = (rel * most)[:, None]
         return out, bound

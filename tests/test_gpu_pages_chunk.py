@@ -1,0 +1,108 @@
+"""Attention of many new tokens over the paged cache (tensor-core kernel), against the model of pages_ref.py."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_pages import DEV, attend, fill, ints, make
+
+pytestmark = pytest.mark.gpu
+
+
+def starts_of(new):
+    return np.concatenate([[0], np.cumsum(new)]).astype(int).tolist()
+
+
+@pytest.mark.parametrize("dim,heads,group,pt,fmt,dtype", [
+    (128, 1, 1, 64, "int8", torch.float16), (128, 1, 1, 16, "e4m3", torch.bfloat16),
+    (64, 1, 1, 128, "int8", torch.bfloat16), (64, 2, 1, 32, "e4m3", torch.float16)])
+@pytest.mark.parametrize("length,new", [(128, 128), (33, 33), (300, 40), (700, 700), (129, 129), (513, 257)])
+def test_one_prompt(dim, heads, group, pt, fmt, dtype, length, new):
+    c, m = make(layers=1, heads=heads, dim=dim, group=group, pt=pt, fmt=fmt, dtype=dtype, pages=-(-720 // pt) + 2,
+                seq_pages=-(-720 // pt), seqs=1)
+    fill(c, m, [length])
+    attend(c, m, [0], [0, new], max_new=new)
+
+
+@pytest.mark.parametrize("dim,heads,group,pt,fmt,dtype", [
+    (128, 2, 4, 64, "int8", torch.bfloat16), (64, 1, 71, 64, "int8", torch.float16),
+    (128, 1, 5, 32, "e4m3", torch.float16), (64, 3, 8, 16, "e4m3", torch.bfloat16)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (37, 5), (150, 20), (100000, 3)])
+def test_ragged_chunks(dim, heads, group, pt, fmt, dtype, window, sinks):
+    """Long and short chunks, single tokens and an empty entry in one call: both kernels, each its own rows."""
+    lens, new = [400, 90, 300, 20, 260], [130, 90, 1, 0, 70]
+    c, m = make(layers=2, heads=heads, dim=dim, group=group, pt=pt, fmt=fmt, dtype=dtype, pages=100,
+                seq_pages=-(-400 // pt))
+    fill(c, m, lens)
+    order = [2, 0, 3, 4, 1]
+    attend(c, m, order, starts_of([new[i] for i in order]), max_new=max(new), layers=1, layer_begin=1, window=window,
+           sinks=sinks)
+
+
+def test_result_does_not_depend_on_the_hint():
+    c, m = make(heads=1, group=2, pages=30)
+    fill(c, m, [300, 200])
+    for hint in (1, 16, 17, 100, 1 << 30, None):
+        attend(c, m, [0, 1], [0, 60, 70], max_new=hint)
+
+
+def test_more_tokens_than_the_sequence_has():
+    c, m = make(heads=2, group=1, pages=30)
+    fill(c, m, [0, 50, 20])
+    attend(c, m, [0, 1, 2], [0, 40, 140, 540], max_new=400)
+
+
+def test_trimmed_pages_are_not_seen():
+    c, m = make(heads=1, group=2, pt=16, pages=60, seq_pages=30, fmt="e4m3")
+    fill(c, m, [400, 130])
+    c.trim(ints([0]), 20, 130)
+    m.trim([0], 20, 130)
+    attend(c, m, [0, 1], [0, 50, 100], max_new=50)
+    attend(c, m, [0, 1], [0, 50, 100], max_new=50, window=60, sinks=20)
+
+
+def test_scores_that_grow_and_value_magnitudes_far_apart():
+    """Keys that get larger along the sequence (the reference moves many times), zero value blocks among others."""
+    for dtype in (torch.float16, torch.bfloat16):
+        c, m = make(heads=1, dim=128, group=4, pt=16, pages=60, seqs=2, seq_pages=40, dtype=dtype)
+        fill(c, m, [600, 300])
+        rng = np.random.default_rng(4)
+        for s, n in ((0, 600), (1, 300)):
+            for b in range(-(-n // 16)):
+                m.amax[:, m.table[s, b], :, 0] = np.float32(0.5 * (1 + b))
+                m.amax[:, m.table[s, b], :, 1] = np.float32(0.0 if b % 7 == 3 else 2.0 ** rng.integers(-9, 6))
+        c.amax.copy_(torch.from_numpy(m.amax))
+        attend(c, m, [0, 1], [0, 64, 364], max_new=300)
+        m.amax[..., 1, :] = 0                               # all values are zero
+        c.amax.copy_(torch.from_numpy(m.amax))
+        got = attend(c, m, [0, 1], [0, 64, 364], max_new=300)
+        assert (got[:364] == 0).all()
+
+
+def test_same_bits_again_and_after_a_replay():
+    c, m = make(heads=2, group=4, pages=40, dtype=torch.bfloat16)
+    fill(c, m, [500, 700, 64])
+    q = torch.randn(400, 1, 8, 128, device=DEV).bfloat16()
+    seqs, starts = ints([0, 1, 2]), ints([0, 100, 399, 400])
+    want = c.attention(q, seqs, starts, max_new=299).clone()
+    assert torch.equal(want, c.attention(q, seqs, starts, max_new=299))
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.attention(q, seqs, starts, max_new=299, out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_a_bad_query_stays_in_its_row_of_a_tile():
+    c, m = make(heads=1, group=1, dtype=torch.bfloat16)
+    fill(c, m, [200])
+    q = torch.randn(200, 1, 1, 128, device=DEV).bfloat16()
+    good = c.attention(q, ints([0]), ints([0, 200])).clone()
+    q[77, 0, 0, 3] = float("inf")
+    bad = c.attention(q, ints([0]), ints([0, 200]))
+    keep = torch.arange(200, device=DEV) != 77
+    assert torch.equal(bad[keep], good[keep]) and not torch.isfinite(bad[77]).all()
