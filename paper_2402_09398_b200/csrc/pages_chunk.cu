@@ -28,13 +28,13 @@
 
 namespace less {
 
-constexpr int PC_ROWS = 128, PC_KEYS = 128;
+constexpr int PC_ROWS = 128, PC_KEYS = 64;
 constexpr int PC_TILES = PC_KEYS / kPageBlock;            // stored tiles of a key tile
 constexpr int PC_SOFT_WARPS = 8, PC_DEQ_WARPS = 4;
 constexpr int PC_THREADS = (PC_SOFT_WARPS + PC_DEQ_WARPS + 2) * 32;
-constexpr int PC_STAGES = 2, PC_META = 4;
+constexpr int PC_STAGES = 4, PC_META = 8;
 
-struct PcMeta {                                           // of the eight stored tiles of a key tile
+struct PcMeta {                                           // of the stored tiles of a key tile
   float k1[PC_TILES];                                     // a_k / top
   float lav[PC_TILES], iav[PC_TILES];                     // log2 a_v, 1 / a_v
   int j0[PC_TILES];                                       // position of the first token, 2^30 = no tile
@@ -43,7 +43,7 @@ struct PcMeta {                                           // of the eight stored
 
 struct PcShared {
   uint64_t q_full, k_full[PC_STAGES], k_empty[PC_STAGES], v_full[PC_STAGES], v_empty[PC_STAGES];
-  uint64_t s_full[2], p_full[2], pv_done[2];
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];     // [row tile][buffer]: key tiles alternate
   PcMeta meta[PC_META];
   uint32_t tmem_base;
   int abort;
@@ -63,6 +63,42 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
         "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
         "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+// The issuing warps stay converged and only the instruction itself is predicated on one elected lane: operands then
+// live in uniform registers.  Issued from a divergent branch, each MMA first moves its operands there one by one - 108
+// against 77 cycles per MMA measured here (no softmax, no conversion), 1.4 x on the whole.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t on;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(on));
+  return on;
+}
+// a descriptor moved by `off` 16-byte units (addresses stay below 2^18: the low word does not carry over)
+__device__ __forceinline__ uint64_t desc_at(uint64_t d, uint32_t off) {
+  return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + off);
+}
+__device__ __forceinline__ void mma_ss_if(uint32_t on, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts_if(uint32_t on, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit_if(uint32_t on, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)),
+      "r"(on)
       : "memory");
 }
 
@@ -86,12 +122,12 @@ __device__ __forceinline__ uint32_t pc_mask16(int j0, int pos, int window, int s
 
 template <typename T, int D, bool E4M3>
 __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, PaArgs a) {
-  constexpr int QT = PC_ROWS * D * 2;                     // bytes of a Q tile; K and V tiles alike
-  constexpr int KT = PC_KEYS * D * 2;
+  constexpr int QT = PC_ROWS * D * 2;                     // bytes of a Q tile
+  constexpr int KT = PC_KEYS * D * 2;                     // of a K or V tile
   extern __shared__ __align__(1024) unsigned char pc_smem[];
   unsigned char* qres = pc_smem;                          // [2 row tiles][D / 64][128 rows][128 B]
-  unsigned char* kring = qres + 2 * QT;                   // [stages][D / 64][128 keys][128 B]
-  unsigned char* vring = kring + PC_STAGES * KT;          // [stages][2 key halves][D dims][128 B]
+  unsigned char* kring = qres + 2 * QT;                   // [stages][D / 64][64 keys][128 B]
+  unsigned char* vring = kring + PC_STAGES * KT;          // [stages][D dims][128 B]
   PcShared* sh = reinterpret_cast<PcShared*>(vring + PC_STAGES * KT);
   if (smem_misaligned(pc_smem, p.status, 120)) return;
 
@@ -130,15 +166,15 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   if (tid == 0) {
     mbar_init(&sh->q_full, 4 * nx);
     for (int s = 0; s < PC_STAGES; ++s) {
-      mbar_init(&sh->k_full[s], PC_DEQ_WARPS);
+      mbar_init(&sh->k_full[s], PC_DEQ_WARPS / 2);
       mbar_init(&sh->k_empty[s], 1);
-      mbar_init(&sh->v_full[s], PC_DEQ_WARPS);
+      mbar_init(&sh->v_full[s], PC_DEQ_WARPS / 2);
       mbar_init(&sh->v_empty[s], 1);
     }
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(&sh->s_full[x], 2);
-      mbar_init(&sh->p_full[x], 4);
-      mbar_init(&sh->pv_done[x], 1);
+    for (int x = 0; x < 4; ++x) {
+      mbar_init(&sh->s_full[x >> 1][x & 1], 2);
+      mbar_init(&sh->p_full[x >> 1][x & 1], 4);
+      mbar_init(&sh->pv_done[x >> 1][x & 1], 1);
     }
     sh->abort = 0;
     mbar_fence_init();
@@ -149,7 +185,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = sh->tmem_base;
-  constexpr uint32_t OCOL = 2 * PC_KEYS;                  // S / P of the two row tiles, then their accumulators
+  constexpr uint32_t OCOL = 4 * PC_KEYS;                  // S / P of the two row tiles, two buffers each; accumulators
   volatile int* abortp = &sh->abort;
   int32_t* status = p.status;
 
@@ -204,10 +240,12 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       }
 
       const uint32_t lane_addr = tmem + ((uint32_t)(quad * 32) << 16);
-      const uint32_t scol = lane_addr + x * PC_KEYS, ocol = lane_addr + OCOL + x * D;
+      const uint32_t ocol = lane_addr + OCOL + x * D;
       float M = -INFINITY, l = 0.f;
       for (int kt = 0; kt < nk; ++kt) {
-        wait_or_give_up(&sh->s_full[x], kt & 1, abortp, status, 122);
+        const int buf = kt & 1;
+        const uint32_t scol = lane_addr + (2 * x + buf) * PC_KEYS;
+        wait_or_give_up(&sh->s_full[x][buf], (kt >> 1) & 1, abortp, status, 122);
         if (__any_sync(0xffffffffu, *abortp)) break;
         tc_fence_after_sync();
         const PcMeta& meta = sh->meta[kt % PC_META];
@@ -263,7 +301,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           if (up) M = ref + most;
           l *= f;
           if (kt) {
-            wait_or_give_up(&sh->pv_done[x], (kt - 1) & 1, abortp, status, 123);
+            wait_or_give_up(&sh->pv_done[x][(kt - 1) & 1], ((kt - 1) >> 1) & 1, abortp, status, 123);
             tc_fence_after_sync();
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -279,12 +317,11 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         }
         l += add;
         tmem_st32(scol, pk);
-        tmem_st32(scol + 32, pk + 32);
         tmem_st_wait();
         tc_fence_before_sync();
-        mbar_arrive_warp(&sh->p_full[x]);
+        mbar_arrive_warp(&sh->p_full[x][buf]);
       }
-      wait_or_give_up(&sh->pv_done[x], (nk - 1) & 1, abortp, status, 124);
+      wait_or_give_up(&sh->pv_done[x][(nk - 1) & 1], ((nk - 1) >> 1) & 1, abortp, status, 124);
       tc_fence_after_sync();
       if (!*abortp) {
         const float inv = l == 0.f ? 0.f : 1.f / l, unit = 1.f / pg_top<E4M3>();
@@ -305,9 +342,9 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       }
     }
   } else if (warp < PC_SOFT_WARPS + PC_DEQ_WARPS) {
-    // ---------------- codes -> operand tiles: a warp per pair of stored tiles ----------------
+    // ---------------- codes -> operand tiles: two warps per key tile, a pair of stored tiles each ----------------
     constexpr int KP = D / 32;                            // 16-byte pieces of a lane in a stored tile
-    const int dw = warp - PC_SOFT_WARPS, g = lane >> 2, t = lane & 3;
+    const int dw = warp & 1, odd = (warp - PC_SOFT_WARPS) >> 1, g = lane >> 2, t = lane & 3;
     // positions of the rows of the two row tiles
     int first_pos[2], last_pos[2];
 #pragma unroll
@@ -315,11 +352,11 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       first_pos[x] = base + (int)((row0 + min(x * PC_ROWS, valid - 1)) / p.group);
       last_pos[x] = base + (int)((row0 + min((x + 1) * PC_ROWS, valid) - 1) / p.group);
     }
-    // lane 2 i + b knows tile b of this warp's pair in key tile `batch + i`
+    // lane 2 i + b knows tile b of this warp's pair in its i-th key tile of the batch, key tile batch + 2 i
     int page_l = -1, j_l = 0;
     float ak_l = 0.f, av_l = 0.f, vlast = 1.f;
     auto lookup = [&](int batch) {
-      const int u = (batch + (lane >> 1)) * PC_TILES + 2 * dw + (lane & 1);
+      const int u = (batch + (lane & ~1)) * PC_TILES + 2 * dw + (lane & 1);
       page_l = -1;
       j_l = 0;
       if (u < units) {
@@ -339,7 +376,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     auto load = [&](int kt, bool values) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int src = 2 * (kt & 15) + b;
+        const int src = (kt & 30) + b;
         const int page = __shfl_sync(0xffffffffu, page_l, src), j = __shfl_sync(0xffffffffu, j_l, src);
         const float av = __shfl_sync(0xffffffffu, av_l, src);
         if (!values) {
@@ -376,10 +413,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         }
       }
     };
-    lookup(0);
-    load(0, false);
-    load(0, true);
-    for (int kt = 0; kt < nk; ++kt) {
+    lookup(odd);
+    load(odd, false);
+    load(odd, true);
+    for (int kt = odd; kt < nk; kt += 2) {
       const int st = kt % PC_STAGES, ph = (kt / PC_STAGES) & 1;
       wait_or_give_up(&sh->k_empty[st], ph ^ 1, abortp, status, 125);
       if (__any_sync(0xffffffffu, *abortp)) break;
@@ -424,13 +461,13 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       fence_proxy_async_smem();
       mbar_arrive_warp(&sh->k_full[st]);
       // V of this key tile is in its registers; pages of the next batch before the next K is asked for
-      if (kt + 1 < nk) {
-        if (((kt + 1) & 15) == 0) lookup(kt + 1);
-        load(kt + 1, false);
+      if (kt + 2 < nk) {
+        if (((kt + 2) & 30) == 0) lookup(kt + 2);
+        load(kt + 2, false);
       }
       wait_or_give_up(&sh->v_empty[st], ph ^ 1, abortp, status, 126);
       if (__any_sync(0xffffffffu, *abortp)) break;
-      unsigned char* vd = vring + st * KT + (dw >> 1) * (D * 128);
+      unsigned char* vd = vring + st * KT;
 #pragma unroll
       for (int i = 0; i < KP; ++i) {
         // lanes with odd g take the pieces in the other order: the banks again
@@ -442,64 +479,61 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           uint32_t u[4];
           pg_unpack4<E4M3>(w0[dd], u[0], u[1]);
           pg_unpack4<E4M3>(w1[dd], u[2], u[3]);
-          *reinterpret_cast<uint4*>(vd + dim * 128 + ((((dw & 1) * 4 + t) ^ (dim & 7)) << 4)) =
+          *reinterpret_cast<uint4*>(vd + dim * 128 + (((dw * 4 + t) ^ (dim & 7)) << 4)) =
               make_uint4(u[0], u[1], u[2], u[3]);
         }
       }
       fence_proxy_async_smem();
       mbar_arrive_warp(&sh->v_full[st]);
-      if (kt + 1 < nk) load(kt + 1, true);
+      if (kt + 2 < nk) load(kt + 2, true);
     }
   } else if (warp == 12) {
     // ---------------- S = Q K^T ----------------
-    if (lane == 0) {
-      constexpr uint32_t idesc = idesc_f16(PC_ROWS, PC_KEYS, 0, 0);
-      const uint64_t ad = smem_desc(smem_u32(qres), 16, 1024, kLayoutSw128);
-      const uint64_t bd = smem_desc(smem_u32(kring), 16, 1024, kLayoutSw128);
-      wait_or_give_up(&sh->q_full, 0, abortp, status, 127);
-      for (int kt = 0; kt < nk; ++kt) {
-        const int st = kt % PC_STAGES;
-        wait_or_give_up(&sh->k_full[st], (kt / PC_STAGES) & 1, abortp, status, 128);
-        for (int x = 0; x < nx; ++x) {
-          // the buffer held S and then P of the key tile before
-          if (kt) wait_or_give_up(&sh->pv_done[x], (kt - 1) & 1, abortp, status, 129);
-          if (*abortp) break;
-          tc_fence_after_sync();
+    constexpr uint32_t idesc = idesc_f16(PC_ROWS, PC_KEYS, 0, 0);
+    const uint32_t on = elect_one();
+    const uint64_t ad = smem_desc(smem_u32(qres), 16, 1024, kLayoutSw128);
+    const uint64_t bd = smem_desc(smem_u32(kring), 16, 1024, kLayoutSw128);
+    wait_or_give_up(&sh->q_full, 0, abortp, status, 127);
+    for (int kt = 0; kt < nk; ++kt) {
+      const int st = kt % PC_STAGES;
+      wait_or_give_up(&sh->k_full[st], (kt / PC_STAGES) & 1, abortp, status, 128);
+      for (int x = 0; x < nx; ++x) {
+        // the buffer held S and then P of key tile kt - 2
+        if (kt >= 2) wait_or_give_up(&sh->pv_done[x][kt & 1], ((kt >> 1) - 1) & 1, abortp, status, 129);
+        tc_fence_after_sync();
+        const uint64_t a0 = desc_at(ad, x * (QT >> 4)), b0 = desc_at(bd, st * (KT >> 4));
+        const uint32_t s0 = tmem + (2 * x + (kt & 1)) * PC_KEYS;
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-            mma_f16_ss(tmem + x * PC_KEYS,
-                       ad + (uint64_t)((x * QT + (ks >> 2) * (PC_ROWS * 128)) >> 4) + (uint64_t)((ks & 3) * 2),
-                       bd + (uint64_t)((st * KT + (ks >> 2) * (PC_KEYS * 128)) >> 4) + (uint64_t)((ks & 3) * 2), idesc,
-                       ks ? 1u : 0u);
-          mma_commit(&sh->s_full[x]);
-          mbar_arrive(&sh->s_full[x]);                    // passes on what came with k_full (the magnitudes)
-        }
-        if (*abortp) break;
-        mma_commit(&sh->k_empty[st]);
+        for (int ks = 0; ks < D / 16; ++ks)
+          mma_ss_if(on, s0, desc_at(a0, (ks >> 2) * (PC_ROWS * 128 >> 4) + (ks & 3) * 2),
+                    desc_at(b0, (ks >> 2) * (PC_KEYS * 128 >> 4) + (ks & 3) * 2), idesc, ks ? 1u : 0u);
+        mma_commit_if(on, &sh->s_full[x][kt & 1]);
+        if (on) mbar_arrive(&sh->s_full[x][kt & 1]);      // passes on what came with k_full (the magnitudes)
+        __syncwarp();
       }
+      if (__any_sync(0xffffffffu, *abortp)) break;
+      mma_commit_if(on, &sh->k_empty[st]);
     }
   } else {
     // ---------------- O += P V ----------------
-    if (lane == 0) {
-      constexpr uint32_t idesc = idesc_f16(PC_ROWS, D, 0, 0);
-      const uint64_t bd = smem_desc(smem_u32(vring), 16, 1024, kLayoutSw128);
-      for (int kt = 0; kt < nk; ++kt) {
-        const int st = kt % PC_STAGES;
-        wait_or_give_up(&sh->v_full[st], (kt / PC_STAGES) & 1, abortp, status, 130);
-        for (int x = 0; x < nx; ++x) {
-          wait_or_give_up(&sh->p_full[x], kt & 1, abortp, status, 131);
-          if (*abortp) break;
-          tc_fence_after_sync();
+    constexpr uint32_t idesc = idesc_f16(PC_ROWS, D, 0, 0);
+    const uint32_t on = elect_one();
+    const uint64_t bd = smem_desc(smem_u32(vring), 16, 1024, kLayoutSw128);
+    for (int kt = 0; kt < nk; ++kt) {
+      const int st = kt % PC_STAGES;
+      wait_or_give_up(&sh->v_full[st], (kt / PC_STAGES) & 1, abortp, status, 130);
+      for (int x = 0; x < nx; ++x) {
+        wait_or_give_up(&sh->p_full[x][kt & 1], (kt >> 1) & 1, abortp, status, 131);
+        tc_fence_after_sync();
+        const uint64_t b0 = desc_at(bd, st * (KT >> 4));
+        const uint32_t p0 = tmem + (2 * x + (kt & 1)) * PC_KEYS;
 #pragma unroll
-          for (int ks = 0; ks < PC_KEYS / 16; ++ks)
-            mma_f16_ts(tmem + OCOL + x * D, tmem + x * PC_KEYS + 8 * ks,
-                       bd + (uint64_t)((st * KT + (ks >> 2) * (D * 128)) >> 4) + (uint64_t)((ks & 3) * 2), idesc,
-                       (kt | ks) ? 1u : 0u);
-          mma_commit(&sh->pv_done[x]);
-        }
-        if (*abortp) break;
-        mma_commit(&sh->v_empty[st]);
+        for (int ks = 0; ks < PC_KEYS / 16; ++ks)
+          mma_ts_if(on, tmem + OCOL + x * D, p0 + 8 * ks, desc_at(b0, ks * 2), idesc, (kt | ks) ? 1u : 0u);
+        mma_commit_if(on, &sh->pv_done[x][kt & 1]);
       }
+      if (__any_sync(0xffffffffu, *abortp)) break;
+      mma_commit_if(on, &sh->v_empty[st]);
     }
   }
   drain_after_abort(abortp);
