@@ -29,13 +29,15 @@
 
 namespace less {
 
-constexpr int PS_WARPS = 8, PS_THREADS = PS_WARPS * 32;
-constexpr int PS_STAGES = 3;
-constexpr int PS_MIN_BLOCKS = 2;               // blocks a warp takes at least: below that, merging costs more
+constexpr int PS_WARPS = 6, PS_THREADS = PS_WARPS * 32;
+// CTAs per SM: two (168 registers a thread, 96 KB of tiles per CTA) unless the rows' sums need more registers
+__host__ __device__ constexpr int ps_ctas(int NT, int D) { return NT * D <= 128 ? 2 : 1; }
+constexpr int PS_RING = 4;                     // tiles of a warp: two being worked on, two on their way
+constexpr int PS_MIN_BLOCKS = 4;               // blocks a warp takes at least: below that, merging costs more
+// With no more items than CTAs, none longer than this many blocks per warp, an item is one CTA's: no merging over CTAs
+constexpr int PS_ITEM_BLOCKS = 12;
 constexpr int PS_SLOT_FLOATS = 2112;           // rows x (D + 2) floats: 16 x 130 or 32 x 66
-
-// 128 registers a thread hold the sums and queries of eight rows; more rows take what one block per SM leaves
-__host__ __device__ constexpr int ps_blocks_per_sm(int NT) { return NT == 1 ? 2 : 1; }
+constexpr int PS_SLOTS = 2 * PS_WARPS + 2;     // partial results of a CTA: two per warp, two of the CTA's own
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -75,11 +77,15 @@ struct Item {
 };
 
 struct PsShared {
-  int64_t pre[PS_THREADS + 1];  // blocks of the entries before a thread's
-  Item part[PS_WARPS][2];       // the item that a warp's slot 0 / 1 holds a part of
+  int64_t units[PS_THREADS + 1];  // blocks of the entries before a thread's
+  int items[PS_THREADS + 1];      // items of the entries before a thread's
+  int most[PS_WARPS];             // blocks of the longest item
+  int64_t sum_u[PS_WARPS];
+  int sum_i[PS_WARPS];
+  PgEntry entry[PS_THREADS];      // with no more entries than threads: the entries
+  Item part[PS_WARPS][2];         // the item that a warp's slot 0 / 1 holds a part of
   int has[PS_WARPS][2];
-  Item fin[2];                  // items that this block merges over all blocks
-  int fin_on[2];
+  int last[2];                    // whether this CTA merges its slot 0 / 1 item over all CTAs
 };
 
 // address of an item's row: rows are (token, query head of the group)
@@ -90,10 +96,12 @@ __device__ __forceinline__ int64_t row_offset(const PgParams& p, const PaArgs& a
 }
 
 template <typename T, int D, int NT, bool E4M3>
-__global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_kernel(PgParams p, PaArgs a) {
-  constexpr int R = 8 * NT, MT = D / 16, KS = D / 16;
+__global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(PgParams p, PaArgs a) {
+  constexpr int R = 8 * NT, MT = D / 16;
   constexpr int TILE = 16 * D, CH = TILE / 512;           // bytes of a tile; 16-byte pieces per lane
   constexpr int SLOT = R * (D + 2);
+  // the rest of the probabilities matters next to an fp16 output (2^-12), not next to a bf16 one (2^-9)
+  constexpr bool LO = std::is_same<T, __half>::value;
   static_assert(SLOT <= PS_SLOT_FLOATS, "slot");
   extern __shared__ __align__(16) unsigned char ps_ring[];
   __shared__ PsShared sh;
@@ -101,79 +109,118 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
 
   // ---- the list of blocks: a thread counts the entries of a stretch of its own, one scan orders them ----
   const int per_thread = pg_ceil(a.n, PS_THREADS);
-  auto entry_units = [&](const PgEntry& e, Blocks& b, int& tiles) -> int64_t {
+  auto entry_items = [&](const PgEntry& e, Blocks& b, int& tiles) -> int {
     const int64_t nr = (int64_t)e.count * p.group;
     if (nr == 0 || nr > a.max_rows) return 0;
     b = visible_blocks(a, e.len, e.count);
     tiles = (int)((nr + R - 1) / R);
-    return (int64_t)max(1, b.count()) * tiles * a.nl * p.heads;
+    return tiles * a.nl * p.heads;
   };
+  int64_t pad = 0;
   {
-    int64_t mine = 0;
+    int64_t mu = 0;
+    int mi = 0, most = 0;
     for (int i = tid * per_thread; i < min(a.n, (tid + 1) * per_thread); ++i) {
       Blocks b;
       int tiles;
-      mine += entry_units(pg_entry(p, a.seqs, a.starts, a.rows, i), b, tiles);
+      const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, i);
+      if (per_thread == 1) sh.entry[tid] = e;
+      const int items = entry_items(e, b, tiles);
+      if (items) {
+        const int blocks = max(1, b.count());
+        mu += (int64_t)items * blocks;
+        mi += items;
+        most = max(most, blocks);
+      }
     }
-    int64_t x = mine;
+    int64_t xu = mu;
+    int xi = mi;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
-      if (lane >= d) x += y;
+      const int64_t yu = __shfl_up_sync(0xffffffffu, xu, d);
+      const int yi = __shfl_up_sync(0xffffffffu, xi, d);
+      if (lane >= d) {
+        xu += yu;
+        xi += yi;
+      }
     }
-    __shared__ int64_t sums[PS_WARPS];
-    if (lane == 31) sums[warp] = x;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 31) {
+      sh.sum_u[warp] = xu;
+      sh.sum_i[warp] = xi;
+      sh.most[warp] = most;
+    }
     if (tid < 2 * PS_WARPS) sh.has[tid >> 1][tid & 1] = 0;
-    if (tid < 2) sh.fin_on[tid] = 0;
+    if (tid < 2) sh.last[tid] = 0;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) x += sums[w];
-    sh.pre[tid + 1] = x;
-    if (tid == 0) sh.pre[0] = 0;
+    for (int w = 0; w < PS_WARPS; ++w) {
+      most = max(most, sh.most[w]);
+      if (w < warp) {
+        xu += sh.sum_u[w];
+        xi += sh.sum_i[w];
+      }
+    }
+    sh.units[tid + 1] = xu;
+    sh.items[tid + 1] = xi;
+    if (tid == 0) {
+      sh.units[0] = 0;
+      sh.items[0] = 0;
+    }
     __syncthreads();
+    if (sh.items[PS_THREADS] <= (int)gridDim.x && most <= PS_WARPS * PS_ITEM_BLOCKS)
+      pad = (int64_t)PS_WARPS * max(PS_MIN_BLOCKS, pg_ceil(pg_ceil(most, PS_WARPS), 2) * 2);
   }
-  const int64_t total = sh.pre[PS_THREADS];
+  // blocks before the entries of thread j, in the list that is cut up: every item padded to a CTA's share, or none
+  auto before = [&](int j) -> int64_t { return pad ? (int64_t)sh.items[j] * pad : sh.units[j]; };
+  const int64_t total = before(PS_THREADS);
   const int64_t workers = (int64_t)gridDim.x * PS_WARPS;
-  const int64_t per_warp = max((total + workers - 1) / workers, (int64_t)PS_MIN_BLOCKS);
+  const int64_t per_warp = pad ? pad / PS_WARPS : max((total + workers - 1) / workers, (int64_t)PS_MIN_BLOCKS);
   const int64_t cta_begin = (int64_t)blockIdx.x * PS_WARPS * per_warp;
   if (cta_begin >= total) return;
   const int64_t cta_end = min(total, cta_begin + PS_WARPS * per_warp);
   int64_t u = min(total, cta_begin + warp * per_warp);
   const int64_t ue = min(total, u + per_warp);
 
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ps_ring) + warp * (PS_STAGES * 2 * TILE) + lane * 16;
-  const unsigned char* ring_g = ps_ring + warp * (PS_STAGES * 2 * TILE) + lane * 16;
-  float* slots = p.partial + (size_t)(blockIdx.x * (2 * PS_WARPS + 2)) * PS_SLOT_FLOATS;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ps_ring) + warp * (PS_RING * 2 * TILE) + lane * 16;
+  const unsigned char* ring_g = ps_ring + warp * (PS_RING * 2 * TILE) + lane * 16;
+  float* slots = p.partial + (size_t)(blockIdx.x * PS_SLOTS) * PS_SLOT_FLOATS;
 
   // ---- where this warp starts ----
   int ei = 0, index = 0, bo = 0;            // entry, item of the entry, block of the item
   int64_t entry_begin = 0;
   PgEntry e = {};
   Blocks vb = {};
-  int tiles = 1, items = 0;
+  int tiles = 1, items = 0, real = 1, blocks = 1;   // blocks of an item, and with its padding
+  auto next_entry = [&]() {                 // the first entry at or behind ei that has items; false = none
+    for (; ei < a.n; ++ei) {
+      e = per_thread == 1 ? sh.entry[ei] : pg_entry(p, a.seqs, a.starts, a.rows, ei);
+      items = entry_items(e, vb, tiles);
+      if (items == 0) continue;
+      real = max(1, vb.count());
+      blocks = pad ? (int)pad : real;
+      return true;
+    }
+    return false;
+  };
   if (u < ue) {
     int lo = 0, hi = PS_THREADS - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (sh.pre[mid] <= u) lo = mid; else hi = mid - 1;
+      if (before(mid) <= u) lo = mid; else hi = mid - 1;
     }
     ei = lo * per_thread;
-    entry_begin = sh.pre[lo];
-    for (; ei < a.n; ++ei) {
-      e = pg_entry(p, a.seqs, a.starts, a.rows, ei);
-      const int64_t nu = entry_units(e, vb, tiles);
-      if (u < entry_begin + nu) break;
-      entry_begin += nu;
+    entry_begin = before(lo);
+    while (next_entry() && u >= entry_begin + (int64_t)items * blocks) {
+      entry_begin += (int64_t)items * blocks;
+      ++ei;
     }
     if (ei >= a.n) u = ue;                  // cannot be, unless the lengths changed under the call
-    items = tiles * a.nl * p.heads;
-    const int blocks = max(1, vb.count());
     index = (int)((u - entry_begin) / blocks);
     bo = (int)((u - entry_begin) - (int64_t)index * blocks);
   }
 
   while (u < ue) {
     // ---- the item ----
-    const int blocks = max(1, vb.count());
     Item it;
     it.begin = entry_begin + (int64_t)index * blocks;
     it.blocks = blocks;
@@ -182,8 +229,52 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
     it.lj = index / tiles / p.heads;
     it.tok_row = e.row0;
     it.valid = min(R, e.count * p.group - it.row0);
-    const int first = bo, last = (int)min((int64_t)blocks, bo + (ue - u));
+    const int first = bo, end = (int)min((int64_t)blocks, bo + (ue - u));
+    const int last = vb.count() > 0 ? min(end, real) : first;       // what of it has tokens
     const int layer = a.layer0 + it.lj;
+
+    // ---- pages and magnitudes: lane i knows the tile of block `batch + i` and, one batch ahead, `batch + 32 + i` ----
+    const uint8_t* head_codes = p.codes + (((size_t)layer * p.pages) * p.heads + it.h) * ((size_t)2 * p.pt * D);
+    const float* head_mags = p.amax + (((size_t)layer * p.pages) * p.heads + it.h) * ((size_t)2 * (p.pt / kPageBlock));
+    struct Tile {
+      const uint8_t* codes;       // null = none
+      float ak, av;
+    };
+    auto lookup = [&](int b) {
+      Tile tl = {nullptr, 0.f, 0.f};
+      if (b + lane < last) {
+        const int tok = vb.at(b + lane) * kPageBlock, inner = (tok & (p.pt - 1)) / kPageBlock;
+        const int page = pg_page(p, e.seq, tok >> p.pt_shift);
+        if (page >= 0) {
+          const size_t slab = (size_t)page * p.heads * 2;
+          tl.codes = head_codes + slab * ((size_t)p.pt * D) + (size_t)inner * TILE;
+          const float* mg = head_mags + slab * (p.pt / kPageBlock) + inner;
+          tl.ak = __ldg(mg);
+          tl.av = __ldg(mg + p.pt / kPageBlock);
+        }
+      }
+      return tl;
+    };
+    Tile cur = lookup(first), nxt = {nullptr, 0.f, 0.f};
+    const size_t to_values = (size_t)p.pt * D;
+    // the tiles of blocks b and b + 1 on their way to ring slots `slot` and `slot + 1`
+    auto fetch = [&](const Tile& tl, int at, int slot) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint8_t* codes = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(tl.codes), at + k));
+        if (codes) {
+          codes += lane * 16;
+          const uint32_t dst = ring + (slot + k) * (2 * TILE);
+#pragma unroll
+          for (int i = 0; i < CH; ++i) cp_async16(dst + i * 512, codes + i * 512);
+          codes += to_values;
+#pragma unroll
+          for (int i = 0; i < CH; ++i) cp_async16(dst + TILE + i * 512, codes + i * 512);
+        }
+      }
+      cp_async_commit();
+    };
+    fetch(cur, 0, 0);
 
     // ---- its queries: operand fragments, the score factor and the position of the rows of this lane ----
     uint32_t qf[NT][D / 8];
@@ -248,153 +339,147 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
       l[nt][0] = l[nt][1] = 0.f;
     }
 
-    // lane i knows page and magnitudes of block `batch + i` of the item
-    int page_l = -1;
-    float ak_l = 0.f, av_l = 0.f;
-    auto lookup = [&](int batch) {
-      page_l = -1;
-      if (batch + lane < last && vb.count() > 0) {
-        const int tok = vb.at(batch + lane) * kPageBlock;
-        page_l = pg_page(p, e.seq, tok >> p.pt_shift);
-        if (page_l >= 0) {
-          const float* mg = p.amax + pg_mag(p, layer, page_l, it.h) + (tok & (p.pt - 1)) / kPageBlock;
-          ak_l = __ldg(mg);
-          av_l = __ldg(mg + p.pt / kPageBlock);
-        }
+    int slot = 0;
+    for (int b = first; b < last; b += 2) {
+      const int at = (b - first) & 31;                     // lane of block b
+      if (at == 0) {
+        if (b != first) cur = nxt;
+        nxt = b + 32 < last ? lookup(b + 32) : Tile{nullptr, 0.f, 0.f};
       }
-    };
-    auto fetch = [&](int b, int batch, int stage) {
-      const int page = __shfl_sync(0xffffffffu, page_l, (b - batch) & 31);
-      if (b < last && page >= 0) {
-        const int inner = ((vb.at(b) * kPageBlock) & (p.pt - 1)) / kPageBlock;
-        const uint8_t* k = p.codes + pg_slab(p, D, layer, page, it.h) + (size_t)inner * TILE + lane * 16;
-        const uint8_t* v = k + (size_t)p.pt * D;
-        const uint32_t dst = ring + stage * (2 * TILE);
+      fetch(at + 2 < 32 ? cur : nxt, (at + 2) & 31, slot ^ 2);
+      cp_async_wait<1>();
+      float ak[2], av[2];
+      bool here[2];
+      int j0[2];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) cp_async16(dst + i * 512, k + i * 512);
-#pragma unroll
-        for (int i = 0; i < CH; ++i) cp_async16(dst + TILE + i * 512, v + i * 512);
+      for (int k = 0; k < 2; ++k) {
+        ak[k] = __shfl_sync(0xffffffffu, cur.ak, at + k);
+        av[k] = __shfl_sync(0xffffffffu, cur.av, at + k);
+        here[k] = __shfl_sync(0xffffffffu, (int)(cur.codes != nullptr), at + k);
+        j0[k] = vb.at(b + k) * kPageBlock;
       }
-      cp_async_commit();
-    };
+      const unsigned char* tile = ring_g + slot * (2 * TILE);
+      slot ^= 2;
 
-    int stage = 0;
-    for (int batch = first; batch < last; batch += 32) {
-      lookup(batch);
-      const int stop = min(last, batch + 32);
-      // the ring restarts with every batch of 32 blocks
-      for (int s = 0; s < PS_STAGES - 1; ++s) fetch(batch + s < stop ? batch + s : last, batch, (stage + s) % PS_STAGES);
-      for (int b = batch; b < stop; ++b) {
-        const int ahead = b + PS_STAGES - 1;
-        fetch(ahead < stop ? ahead : last, batch, (stage + PS_STAGES - 1) % PS_STAGES);
-        cp_async_wait<PS_STAGES - 1>();
-        const int page = __shfl_sync(0xffffffffu, page_l, b - batch);
-        const float ak = __shfl_sync(0xffffffffu, ak_l, b - batch), av = __shfl_sync(0xffffffffu, av_l, b - batch);
-        const unsigned char* tile = ring_g + stage * (2 * TILE);
-        stage = stage + 1 == PS_STAGES ? 0 : stage + 1;
-        if (page < 0) continue;                                    // trimmed
-        const int j0 = vb.at(b) * kPageBlock;
-
-        // ---- scores: 16 tokens x 8 NT rows ----
-        float s[NT][4];
+      // ---- scores: 2 x 16 tokens x 8 NT rows ----
+      float s[2][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int half = 0; half < D / 64; ++half) {
-          const uint4 k0 = *reinterpret_cast<const uint4*>(tile + half * 512);
-          const uint4 k1 = *reinterpret_cast<const uint4*>(tile + (D / 64 + half) * 512);
-          const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+        for (int nt = 0; nt < NT; ++nt) s[k][nt][0] = s[k][nt][1] = s[k][nt][2] = s[k][nt][3] = 0.f;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
+      for (int half = 0; half < D / 64; ++half) {
+        uint4 kk[2][2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            kk[k][j] = *reinterpret_cast<const uint4*>(tile + k * (2 * TILE) + (j * (D / 64) + half) * 512);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t w0 = w == 0 ? kk[k][0].x : w == 1 ? kk[k][0].y : w == 2 ? kk[k][0].z : kk[k][0].w;
+            const uint32_t w1 = w == 0 ? kk[k][1].x : w == 1 ? kk[k][1].y : w == 2 ? kk[k][1].z : kk[k][1].w;
             uint32_t a0, a1, a2, a3;
-            pg_unpack4<E4M3>(w0[w], a0, a2);
-            pg_unpack4<E4M3>(w1[w], a1, a3);
+            pg_unpack4<E4M3>(w0, a0, a2);
+            pg_unpack4<E4M3>(w1, a1, a3);
             const int ks = half * 4 + w;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][2 * ks], qf[nt][2 * ks + 1]);
+            for (int nt = 0; nt < NT; ++nt) mma16816(s[k][nt], a0, a1, a2, a3, qf[nt][2 * ks], qf[nt][2 * ks + 1]);
           }
-        }
-        bool up = false;
-        const bool whole = all_rows && j0 + kPageBlock - 1 <= first_pos &&
-                           (!a.window || j0 > last_pos - a.window || j0 + kPageBlock <= a.sinks);
+      }
+      bool up = false;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bool whole = all_rows && here[k] && j0[k] + kPageBlock - 1 <= first_pos &&
+                           (!a.window || j0[k] > last_pos - a.window || j0[k] + kPageBlock <= a.sinks);
         // this lane's tokens: accumulator rows g and g + 8
-        const int ja = j0 + 4 * (g >> 1) + (g & 1), jb = ja + 2;
+        const int ja = j0[k] + 4 * (g >> 1) + (g & 1), jb = ja + 2;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[nt][i] *= ak * crow[nt][i & 1];
+          for (int i = 0; i < 4; ++i) s[k][nt][i] *= ak[k] * crow[nt][i & 1];
           if (!whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int j = i < 2 ? ja : jb, at = pos[nt][i & 1];
-              if (j > at || (a.window && j <= at - a.window && j >= a.sinks)) s[nt][i] = -INFINITY;
+              const int j = i < 2 ? ja : jb, at_row = pos[nt][i & 1];
+              if (!here[k] || j > at_row || (a.window && j <= at_row - a.window && j >= a.sinks)) s[k][nt][i] = -INFINITY;
             }
           }
-          up |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + 8.f || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + 8.f;
+          up |= fmaxf(s[k][nt][0], s[k][nt][2]) > m[nt][0] + 8.f || fmaxf(s[k][nt][1], s[k][nt][3]) > m[nt][1] + 8.f;
         }
-        if (__any_sync(0xffffffffu, up)) {
+      }
+      if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              float x = fmaxf(s[nt][c], s[nt][2 + c]);
+          for (int c = 0; c < 2; ++c) {
+            float x = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
 #pragma unroll
-              for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-              x = fmaxf(x, m[nt][c]);
-              const float f = x == m[nt][c] ? 1.f : pa_ex2(m[nt][c] - x);
-              m[nt][c] = x;
-              l[nt][c] *= f;
+            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+            x = fmaxf(x, m[nt][c]);
+            const float f = x == m[nt][c] ? 1.f : pa_ex2(m[nt][c] - x);
+            m[nt][c] = x;
+            l[nt][c] *= f;
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt) {
-                o[nt][mt][c] *= f;
-                o[nt][mt][2 + c] *= f;
-              }
+            for (int mt = 0; mt < MT; ++mt) {
+              o[nt][mt][c] *= f;
+              o[nt][mt][2 + c] *= f;
             }
-        }
-        if (av > 16.f * vref) {
-          const float now = __uint_as_float((__float_as_uint(av) & 0x7f800000u) + 0x00800000u);
-          ivref = __uint_as_float(0x7f000000u - __float_as_uint(now));
-          const float f = vref * ivref;
-          vref = now;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[nt][mt][i] *= f;
-        }
-        // ---- probabilities, times the value magnitude: second operand of the product with the values ----
-        const float r = av * ivref;
-        uint32_t ph[NT][2], pl[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float x[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float mm = m[nt][i & 1];
-            x[i] = pa_ex2(s[nt][i] - (mm == -INFINITY ? 0.f : mm));
           }
+      }
+      if (fmaxf(av[0], av[1]) > 16.f * vref) {
+        const float now = __uint_as_float((__float_as_uint(fmaxf(av[0], av[1])) & 0x7f800000u) + 0x00800000u);
+        ivref = __uint_as_float(0x7f000000u - __float_as_uint(now));
+        const float f = vref * ivref;
+        vref = now;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[nt][mt][i] *= f;
+      }
+      // ---- probabilities, times the value magnitude: second operand of the product with the values ----
+      uint32_t ph[2][NT][2], pl[2][NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float r = av[k] * ivref;
+          const float x[4] = {pa_ex2(s[k][nt][0] - m0), pa_ex2(s[k][nt][1] - m1), pa_ex2(s[k][nt][2] - m0), pa_ex2(s[k][nt][3] - m1)};
           l[nt][0] += x[0] + x[2];
           l[nt][1] += x[1] + x[3];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const float y0 = x[2 * i] * r, y1 = x[2 * i + 1] * r;
             const __half2 hi = __floats2half2_rn(y0, y1);
-            const float2 back = __half22float2(hi);
-            ph[nt][i] = movmatrix(*reinterpret_cast<const uint32_t*>(&hi));
-            pl[nt][i] = movmatrix(pack2(y0 - back.x, y1 - back.y));
+            ph[k][nt][i] = movmatrix(*reinterpret_cast<const uint32_t*>(&hi));
+            if (LO) {
+              const float2 back = __half22float2(hi);
+              pl[k][nt][i] = movmatrix(pack2(y0 - back.x, y1 - back.y));
+            }
           }
         }
-        // tokens behind the end may hold any byte; a NaN code would survive its zero probability
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        // tokens behind the end may hold any byte, a slot without a tile too; a NaN code would survive its zero probability
         uint32_t keep = 0xffffffffu;
-        if (E4M3 && j0 + kPageBlock > e.len) {
-          const int left = e.len - (j0 + 4 * t);
+        if (E4M3 && (!here[k] || j0[k] + kPageBlock > e.len)) {
+          const int left = here[k] ? e.len - (j0[k] + 4 * t) : 0;
           keep = left <= 0 ? 0u : (left >= 4 ? keep : keep >> (8 * (4 - left)));
         }
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-          const uint4 v4 = *reinterpret_cast<const uint4*>(tile + TILE + i * 512);
-          const uint32_t w[4] = {v4.x & keep, v4.y & keep, v4.z & keep, v4.w & keep};
+          const uint4 v4 = *reinterpret_cast<const uint4*>(tile + k * (2 * TILE) + TILE + i * 512);
+          uint32_t w[4] = {v4.x, v4.y, v4.z, v4.w};
+          if (E4M3) {
+#pragma unroll
+            for (int dd = 0; dd < 4; ++dd) w[dd] &= keep;
+          }
 #pragma unroll
           for (int dd = 0; dd < 4; dd += 2) {
             uint32_t a0, a1, a2, a3;
@@ -402,19 +487,19 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
             pg_unpack4<E4M3>(w[dd + 1], a1, a3);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              mma16816(o[nt][2 * i + dd / 2], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
-              mma16816(o[nt][2 * i + dd / 2], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+              mma16816(o[nt][2 * i + dd / 2], a0, a1, a2, a3, ph[k][nt][0], ph[k][nt][1]);
+              if (LO) mma16816(o[nt][2 * i + dd / 2], a0, a1, a2, a3, pl[k][nt][0], pl[k][nt][1]);
             }
           }
         }
       }
-      cp_async_wait<0>();
     }
+    cp_async_wait<0>();
 
     // ---- the item's rows, or a part of them ----
-    const bool complete = first == 0 && last == blocks;
+    const bool complete = first == 0 && end == blocks;
     const int which = first == 0 ? 1 : 0;
-    float* slot = slots + (size_t)(warp * 2 + which) * PS_SLOT_FLOATS;
+    float* slot_out = slots + (size_t)(warp * 2 + which) * PS_SLOT_FLOATS;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -440,12 +525,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
 #pragma unroll
           for (int i = 0; i < D / 8; i += 8) store8<T>(dst + i, f + i);
         } else {
-          float* dst = slot + rc * D + g * (D / 8);
+          float* dst = slot_out + rc * D + g * (D / 8);
 #pragma unroll
           for (int i = 0; i < D / 8; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
           if (g == 0) {
-            slot[R * D + 2 * rc] = m[nt][c];
-            slot[R * D + 2 * rc + 1] = sum;
+            slot_out[R * D + 2 * rc] = m[nt][c];
+            slot_out[R * D + 2 * rc + 1] = sum;
           }
         }
       }
@@ -455,24 +540,19 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
     }
 
     // ---- next ----
-    u += last - first;
+    u += end - first;
     bo = 0;
     if (++index == items && u < ue) {
       index = 0;
       entry_begin += (int64_t)items * blocks;
-      do {
-        if (++ei >= a.n) break;
-        e = pg_entry(p, a.seqs, a.starts, a.rows, ei);
-      } while (entry_units(e, vb, tiles) == 0);
-      if (ei >= a.n) break;                 // as above
-      items = tiles * a.nl * p.heads;
+      ++ei;
+      if (!next_entry()) break;             // as above
     }
   }
   __syncthreads();
 
-  // ---- merge inside the block: the warp that holds an item's first part in this block collects the others ----
-  auto merge_rows = [&](const Item& it, auto slot_of, int parts, int r, float4& f, float& mm, float& ll) {
-    // one row, a warp: lanes own four dimensions each (two halves of the warp alternate when D is 64)
+  // ---- merge: a warp takes a row, lanes own four dimensions each (with D 64 the upper half only helps with the maximum) ----
+  auto merge_row = [&](auto slot_of, int parts, int r, float4& f, float& mm, float& ll) {
     const int c4 = (lane % (D / 4)) * 4;
     mm = -INFINITY;
     for (int i = lane; i < parts; i += 32) mm = fmaxf(mm, __ldcg(slot_of(i) + R * D + 2 * r));
@@ -480,12 +560,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
     for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
     f = make_float4(0.f, 0.f, 0.f, 0.f);
     ll = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < parts; ++i) {
       const float* s = slot_of(i);
-      const float pm = __ldcg(s + R * D + 2 * r), pl = __ldcg(s + R * D + 2 * r + 1);
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(s + R * D + 2 * r));
       const float4 v = __ldcg(reinterpret_cast<const float4*>(s + r * D + c4));
-      const float w = pl == 0.f ? 0.f : pl * pa_ex2(pm - mm);
+      const float w = ml.y == 0.f ? 0.f : ml.y * pa_ex2(ml.x - mm);
       ll += w;
       f.x = fmaf(w, v.x, f.x);
       f.y = fmaf(w, v.y, f.y);
@@ -496,61 +576,71 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
     f = make_float4(f.x * inv, f.y * inv, f.z * inv, f.w * inv);
   };
   const int64_t per_cta = PS_WARPS * per_warp;
-  for (int which = 0; which < 2; ++which) {
-    if (!sh.has[warp][which] || (which == 0 && warp != 0)) continue;
-    const Item it = sh.part[warp][which];
+  // Inside the CTA: the items that begin in one of its warps (slot 1) or before it (slot 0 of warp 0), all rows dealt out
+  // to the warps in turn
+  bool outside = false;
+  int turn = 0;
+  for (int k = -1; k < PS_WARPS; ++k) {
+    const int w0 = max(k, 0), wh = k < 0 ? 0 : 1;
+    if (!sh.has[w0][wh]) continue;
+    const Item it = sh.part[w0][wh];
     const int64_t end = it.begin + it.blocks;
     const int wl = (int)((min(end, cta_end) - 1 - cta_begin) / per_warp);
     const bool inside = it.begin >= cta_begin && end <= cta_end;
-    float* cta_slot = slots + (size_t)(2 * PS_WARPS + which) * PS_SLOT_FLOATS;
+    outside |= !inside;
+    float* cta_slot = slots + (size_t)(2 * PS_WARPS + wh) * PS_SLOT_FLOATS;
     const float* base = slots;
-    const int w0 = warp, wh = which;
     auto slot_of = [=](int i) { return base + (size_t)((w0 + i) * 2 + (i == 0 ? wh : 0)) * PS_SLOT_FLOATS; };
-    for (int r = 0; r < it.valid; ++r) {
+    for (int r = 0; r < it.valid; ++r, ++turn) {
+      if (turn % PS_WARPS != warp) continue;
       float4 f;
       float mm, ll;
-      merge_rows(it, slot_of, wl - warp + 1, r, f, mm, ll);
+      merge_row(slot_of, wl - w0 + 1, r, f, mm, ll);
       if (lane < D / 4) {
         if (inside) {
           store4(reinterpret_cast<T*>(a.out) + row_offset(p, a, D, it, r) + lane * 4, f);
         } else {
           *reinterpret_cast<float4*>(cta_slot + r * D + lane * 4) = f;
-          if (lane == 0) {
-            cta_slot[R * D + 2 * r] = mm;
-            cta_slot[R * D + 2 * r + 1] = ll;
-          }
+          if (lane == 0) *reinterpret_cast<float2*>(cta_slot + R * D + 2 * r) = make_float2(mm, ll);
         }
       }
     }
-    if (!inside) {
-      __threadfence();
-      __syncwarp();
-      if (lane == 0) {
+  }
+  if (!outside) return;                                      // the same for all threads
+  __threadfence();
+  __syncthreads();
+  // Over the CTAs: the last one to arrive does it
+  if (tid < 2) {
+    // the item that began before this CTA, and the one that goes on behind it
+    int w0 = tid == 0 ? 0 : PS_WARPS - 1;
+    if (tid == 1)
+      while (w0 >= 0 && !sh.has[w0][1]) --w0;
+    if (w0 >= 0 && sh.has[w0][tid]) {
+      const Item it = sh.part[w0][tid];
+      const int64_t end = it.begin + it.blocks;
+      if (it.begin < cta_begin || end > cta_end) {
         const int c0 = (int)(it.begin / per_cta), c1 = (int)((end - 1) / per_cta);
         if (atomicAdd(p.counters + c0, 1) == c1 - c0) {
           p.counters[c0] = 0;
           __threadfence();
-          sh.fin[which] = it;
-          sh.fin_on[which] = 1;
+          sh.last[tid] = w0 + 1;
         }
       }
     }
   }
   __syncthreads();
-
-  // ---- merge over the blocks: the last one to arrive does it, all its warps, a row each ----
   for (int which = 0; which < 2; ++which) {
-    if (!sh.fin_on[which]) continue;
-    const Item it = sh.fin[which];
+    if (!sh.last[which]) continue;
+    const Item it = sh.part[sh.last[which] - 1][which];
     const int c0 = (int)(it.begin / per_cta), c1 = (int)((it.begin + it.blocks - 1) / per_cta);
     const float* base = p.partial;
     auto slot_of = [=](int i) {
-      return base + ((size_t)(c0 + i) * (2 * PS_WARPS + 2) + 2 * PS_WARPS + (i == 0 ? 1 : 0)) * PS_SLOT_FLOATS;
+      return base + ((size_t)(c0 + i) * PS_SLOTS + 2 * PS_WARPS + (i == 0 ? 1 : 0)) * PS_SLOT_FLOATS;
     };
     for (int r = warp; r < it.valid; r += PS_WARPS) {
       float4 f;
       float mm, ll;
-      merge_rows(it, slot_of, c1 - c0 + 1, r, f, mm, ll);
+      merge_row(slot_of, c1 - c0 + 1, r, f, mm, ll);
       if (lane < D / 4) store4(reinterpret_cast<T*>(a.out) + row_offset(p, a, D, it, r) + lane * 4, f);
     }
   }
@@ -558,7 +648,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_blocks_per_sm(NT)) pages_step_k
 
 template <typename T, int D, int NT, bool E4M3>
 static int launch_step(const PgParams& p, const PaArgs& a, cudaStream_t s) {
-  constexpr size_t smem = (size_t)PS_WARPS * PS_STAGES * 2 * 16 * D;
+  constexpr size_t smem = (size_t)PS_WARPS * PS_RING * 2 * 16 * D;
   static std::atomic<unsigned long long> done{0};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return fail_cuda("cudaGetDevice");
@@ -568,8 +658,8 @@ static int launch_step(const PgParams& p, const PaArgs& a, cudaStream_t s) {
       return fail_cuda("shared memory opt-in of pages_step_kernel");
     if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  constexpr size_t block_bytes = (size_t)(2 * PS_WARPS + 2) * PS_SLOT_FLOATS * 4;
-  int grid = ps_blocks_per_sm(NT) * pg_sms();
+  constexpr size_t block_bytes = (size_t)PS_SLOTS * PS_SLOT_FLOATS * 4;
+  int grid = ps_ctas(NT, D) * pg_sms();
   const int most = (int)(LESS_PAGES_PARTIAL_BYTES / block_bytes);
   if (grid > most) grid = most;
   if (grid > kPgCounters) grid = kPgCounters;
