@@ -4,8 +4,10 @@
 //   code = rn(x * top / a)            top = 127 (int8) or 448 (e4m3), ties to even
 //   older tokens of the block, where a has grown:  code = rn(code * a_old / a)
 //
-// x * top and code * a_old are exact in fp32 (16-bit inputs), the quotient is correctly rounded, and a quotient that
-// is not a tie is further than 2^-19 (relative) from one: the codes are those of exact arithmetic.
+// The codes are those of exact arithmetic, without a division per value.  x * top and code * a_old are exact in fp32
+// (16-bit inputs); times the correctly rounded 1 / a, a quotient is off by at most 2^-23 relative.  A quotient that is
+// not a tie is at least 2^-19 from the nearest one (both are ratios of integers of at most 8 + 11 bits), so rounding to
+// 21 bits first (2^-21) lands ties exactly on themselves and nothing else on a tie; the second rounding is then right.
 // Infinities are written as the largest finite fp16 number (bf16: 2^100, so that x * top stays finite), NaN as 0:
 // one bad token must not take the other fifteen of its block with it.  Magnitudes below 2^-100 (bf16) become 0: the
 // attention divides by magnitudes.  Tokens of the last block behind the
@@ -54,17 +56,32 @@ __device__ __forceinline__ float pw_value(uint32_t code) {   // in units of amax
   return (float)(int8_t)code;
 }
 
+// four quotients -> four codes
 template <bool E4M3>
-__device__ __forceinline__ uint32_t pw_code(float x) {
-  if (E4M3) return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
-  return (uint32_t)__float2int_rn(x) & 0xffu;
+__device__ __forceinline__ uint32_t pw_codes(const float* num, float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float q = __fmul_rn(num[i], inv), c = __fmul_rn(q, 9.f);     // 2^3 + 1: the upper 21 bits of q
+    y[i] = __fsub_rn(c, __fsub_rn(c, q));
+  }
+  if (E4M3) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+  }
+  // + 1.5 * 2^23 rounds to an integer, whose low byte is the code
+  uint32_t b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(y[i], 12582912.f));
+  return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
 
 template <typename T, int D, bool E4M3>
 __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwArgs a) {
   constexpr int PER = D;                        // threads per (head, keys or values): one 16-byte piece each
   constexpr int HEADS = PW_THREADS / (2 * PER); // heads per turn
-  __shared__ float red[PW_THREADS / 32];
+  __shared__ float red[2][PW_THREADS / 32];
   const int tid = threadIdx.x, lane = tid & 31;
   const int slot = blockIdx.x;
   int lo = 0, hi = a.n - 1;                     // the last entry whose slots start at or before this one
@@ -81,88 +98,99 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwA
   }
   const int pos0 = (begin / kPageBlock + slot - pw_slot(a, lo)) * kPageBlock;
   if (pos0 >= e.len) return;
+  const int keep = begin - pos0;                         // tokens of the block older than the call (<= 0: none)
+  const int live = min(kPageBlock, e.len - pos0);
+  const int lj = blockIdx.z, layer = a.layer0 + lj;
+  const int piece = tid % PER, which = (tid / PER) & 1, c = piece >> 5, g = (piece >> 2) & 7, t = piece & 3;
+  const int token = 4 * (g >> 1) + 2 * (c / (D / 64)) + (g & 1);       // of a piece of keys
+
+  // a head's 16 new values of this thread, as they come
+  const int64_t stride = which ? a.v_stride : a.k_stride;
+  const T* src = reinterpret_cast<const T*>(which ? a.v : a.k) + (int64_t)(e.row0 - keep) * stride + (int64_t)lj * p.heads * D;
+  src += which ? (int64_t)(4 * t) * stride + g * (D / 8) + c * 4 : (int64_t)token * stride + t * (D / 4) + (c % (D / 64)) * 16;
+  auto fetch = [&](int h, uint2 (&raw)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) raw[k] = make_uint2(0, 0);
+    if (h >= p.heads) return;
+    const T* s = src + (int64_t)h * D;
+    if (which == 0) {
+      if (token >= keep && token < live) {
+        const uint4 x = __ldcs(reinterpret_cast<const uint4*>(s)), y = __ldcs(reinterpret_cast<const uint4*>(s) + 1);
+        raw[0] = make_uint2(x.x, x.y);
+        raw[1] = make_uint2(x.z, x.w);
+        raw[2] = make_uint2(y.x, y.y);
+        raw[3] = make_uint2(y.z, y.w);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (4 * t + k >= keep && 4 * t + k < live) raw[k] = __ldcs(reinterpret_cast<const uint2*>(s + (int64_t)k * stride));
+    }
+  };
+  uint2 raw[4], ahead[4];
+  const int h_first = (int)blockIdx.y * HEADS + tid / (2 * PER), h_step = (int)gridDim.y * HEADS;
+  fetch(h_first, raw);
+
   // nothing after an error; a sequence listed twice: the first entry counts
   bool again = __ldcg(p.status) != 0;
   for (int j = tid; j < lo; j += PW_THREADS) again |= __ldg(a.seqs + j) == e.seq;
-  if (__syncthreads_or(again)) return;
   const int page = pg_page(p, e.seq, pos0 >> p.pt_shift);
-  if (page < 0 || __ldcg(p.refs + page) != 1) {          // trimmed, or held by other sequences too
+  const int refs = page >= 0 ? __ldcg(p.refs + page) : 0;
+  if (__syncthreads_or(again)) return;
+  if (refs != 1) {                                       // trimmed, or held by other sequences too
     if (tid == 0) pg_status(p.status, page < 0 ? kPagesBounds : kPagesState, 41);
     return;
   }
   const int inner = (pos0 & (p.pt - 1)) / kPageBlock;
-  const int keep = begin - pos0;                         // tokens of the block older than the call (<= 0: none)
-  const int live = min(kPageBlock, e.len - pos0);
-  const int lj = blockIdx.z, layer = a.layer0 + lj;
 
-  const int piece = tid % PER, which = (tid / PER) & 1, c = piece >> 5, g = (piece >> 2) & 7, t = piece & 3;
-  for (int h0 = (int)blockIdx.y * HEADS; h0 < p.heads; h0 += (int)gridDim.y * HEADS) {
+  int turn = 0;
+  for (int h0 = (int)blockIdx.y * HEADS; h0 < p.heads; h0 += h_step, turn ^= 1) {
     const int h = h0 + tid / (2 * PER);
     const bool in = h < p.heads;
-    uint8_t* tile = nullptr;
-    float* mag = nullptr;
-    float x[16];
+    fetch(h + h_step, ahead);
+    uint8_t* tile = p.codes + pg_slab(p, D, layer, page, in ? h : 0) + ((size_t)which * p.pt + inner * kPageBlock) * D + piece * 16;
+    float* mag = p.amax + pg_mag(p, layer, page, in ? h : 0) + which * (p.pt / kPageBlock) + inner;
     uint4 was = make_uint4(0, 0, 0, 0);
-    float old = 0.f, m = 0.f;
-    if (in) {
-      tile = p.codes + pg_slab(p, D, layer, page, h) + ((size_t)which * p.pt + inner * kPageBlock) * D + piece * 16;
-      mag = p.amax + pg_mag(p, layer, page, h) + which * (p.pt / kPageBlock) + inner;
-      if (keep > 0) {
-        was = *reinterpret_cast<const uint4*>(tile);
-        old = *mag;
-      }
-      const int64_t stride = which ? a.v_stride : a.k_stride;
-      const T* src = reinterpret_cast<const T*>(which ? a.v : a.k) + (int64_t)(e.row0 - keep) * stride +
-                     (int64_t)(lj * p.heads + h) * D;
+    float old = 0.f;
+    if (in && keep > 0) {
+      was = *reinterpret_cast<const uint4*>(tile);
+      old = *mag;
+    }
+    float x[16], m = 0.f;
+    const T* y = reinterpret_cast<const T*>(raw);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
-      if (which == 0) {
-        const int token = 4 * (g >> 1) + 2 * (c / (D / 64)) + (g & 1);
-        if (token >= keep && token < live) {
-          const uint4* s4 = reinterpret_cast<const uint4*>(src + (int64_t)token * stride + t * (D / 4) + (c % (D / 64)) * 16);
-          uint4 u[2] = {__ldg(s4), __ldg(s4 + 1)};
-          const T* y = reinterpret_cast<const T*>(u);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = pw_load(y[i]);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int token = 4 * t + k;
-          if (token >= keep && token < live) {
-            uint2 u = __ldg(reinterpret_cast<const uint2*>(src + (int64_t)token * stride + g * (D / 8) + c * 4));
-            const T* y = reinterpret_cast<const T*>(&u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i * 4 + k] = pw_load(y[i]);
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+    for (int i = 0; i < 16; ++i) {
+      // values come token by token, four dimensions each; a stored value word is one dimension, four tokens
+      const float f = pw_load(y[which ? (i & 3) * 4 + (i >> 2) : i]);
+      x[i] = f;
+      m = fmaxf(m, fabsf(f));
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    __syncthreads();
-    if (lane == 0) red[tid >> 5] = m;
-    __syncthreads();
+    if (lane == 0) red[turn][tid >> 5] = m;
+    __syncthreads();                                     // the other half of red is free: it was read a turn ago
     m = old;
 #pragma unroll
-    for (int w = 0; w < PER / 32; ++w) m = fmaxf(m, red[tid / PER * (PER / 32) + w]);
+    for (int w = 0; w < PER / 32; ++w) m = fmaxf(m, red[turn][tid / PER * (PER / 32) + w]);
     if (m < 0x1p-100f) m = 0.f;                          // its codes come out as 0 too
     if (in) {
-      const float unit = m > 0.f ? m : 1.f, top = pg_top<E4M3>();
+      const float inv = __frcp_rn(m > 0.f ? m : 1.f);
       uint32_t out[4];
-      const uint32_t* wasw = reinterpret_cast<const uint32_t*>(&was);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int token = which ? 4 * t + (i & 3) : 4 * (g >> 1) + 2 * (c / (D / 64)) + (g & 1);
-        const float num = token < keep ? pw_value<E4M3>((wasw[i / 4] >> (8 * (i & 3))) & 0xffu) * old : x[i] * top;
-        const uint32_t code = pw_code<E4M3>(__fdiv_rn(num, unit));
-        out[i / 4] = (i & 3) ? out[i / 4] | code << (8 * (i & 3)) : code;
+      for (int i = 0; i < 16; ++i) x[i] *= pg_top<E4M3>();
+      if (keep > 0) {
+        const uint32_t* wasw = reinterpret_cast<const uint32_t*>(&was);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((which ? 4 * t + (i & 3) : token) < keep) x[i] = pw_value<E4M3>((wasw[i / 4] >> (8 * (i & 3))) & 0xffu) * old;
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i] = pw_codes<E4M3>(x + 4 * i, inv);
       *reinterpret_cast<uint4*>(tile) = make_uint4(out[0], out[1], out[2], out[3]);
       if (piece == 0) *mag = m;
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) raw[k] = ahead[k];
   }
 }
 
@@ -186,8 +214,12 @@ extern "C" int less_pages_write(const less_pages* d, int32_t layer_begin, int32_
   if ((((uintptr_t)k | (uintptr_t)v) & 15) || ((k_stride | v_stride) & 7)) return LESS_ERR_MISALIGNED;
   PwArgs a = {k, v, k_stride, v_stride, seqs, starts, n, rows, layer_begin};
   const bool bf16 = d->flags & LESS_PAGES_BF16, e4m3 = d->flags & LESS_PAGES_E4M3;
-  const int turn = PW_THREADS / (2 * d->head_dim);
-  const dim3 grid(rows / kPageBlock + 2 * n, pg_ceil(d->heads, turn), layer_count);
+  // Heads of a block are taken in turn by one CTA, so that what leads to its page is looked up once and the next head's
+  // rows are on their way; apart where that leaves the GPU empty
+  const int turns = pg_ceil(d->heads, PW_THREADS / (2 * d->head_dim)), slots = rows / kPageBlock + 2 * n;
+  int share = (int)((int64_t)slots * layer_count * turns / (16 * pg_sms()));
+  share = share < 1 ? 1 : share > turns ? turns : share;
+  const dim3 grid(slots, pg_ceil(turns, share), layer_count);
   if (grid.y > 65535) return LESS_ERR_INVALID_CONFIG;
   cudaStream_t s = (cudaStream_t)stream;
 #define PW_LAUNCH(T, D, E) pages_write_kernel<T, D, E><<<grid, PW_THREADS, 0, s>>>(p, a)
