@@ -76,88 +76,129 @@ __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// A listed sequence found twice: the first entry counts.  A bitmap in shared memory tells whether there is any such;
+// only then the first entries are worked out, in p.mark.
+constexpr int PO_BITS = 65536;
+struct Listed {
+  uint32_t seen[PO_BITS / 32];
+};
+// whether thread-owned entry i (of the block's strided loop) sets a bit that is set already; caller synchronises before
+__device__ __forceinline__ bool listed_again(Listed& l, const PgParams& p, int s) {
+  if (p.seqs > PO_BITS) return true;                     // too many to tell: work it out
+  return atomicOr(&l.seen[s >> 5], 1u << (s & 31)) >> (s & 31) & 1;
+}
+
+enum { kAnyBad = 1, kAnyAgain = 2, kAnyShrink = 4, kAnyGrow = 8 };
+
 __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
     pages_resize_kernel(PgParams p, int D, int n, const int32_t* seqs, const int32_t* want) {
   __shared__ int sums[PO_THREADS / 32];
+  __shared__ Listed listed;
   __shared__ int nmoves;
+  __shared__ uint32_t any;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x == 0) {
-    if (tid == 0) nmoves = 0;
+    if (tid == 0) {
+      nmoves = 0;
+      any = 0;
+    }
+    for (int i = tid; i < min(PO_BITS, p.seqs + 31) / 32; i += PO_THREADS) listed.seen[i] = 0;
+    uint32_t mine = __ldcg(p.status) != 0 ? kAnyBad : 0;
+    __syncthreads();
     // a list that holds a bad entry changes nothing
-    bool bad = __ldcg(p.status) != 0;
     for (int i = tid; i < n; i += PO_THREADS) {
-      const int s = seqs[i], w = want[i];
-      if (s < 0 || s >= p.seqs || w < 0 || w > p.seq_pages * p.pt || !pg_len_ok(p, __ldcg(p.lens + s))) {
+      const int s = __ldg(seqs + i), w = __ldg(want + i);
+      const int old = s >= 0 && s < p.seqs ? __ldcg(p.lens + s) : -1;
+      if (w < 0 || w > p.seq_pages * p.pt || !pg_len_ok(p, old)) {
         pg_status(p.status, kPagesBounds, 10);
-        bad = true;
+        mine |= kAnyBad;
       } else {
-        p.mark[s] = n;
+        if (listed_again(listed, p, s)) mine |= kAnyAgain;
+        mine |= w < old ? kAnyShrink : w > old ? kAnyGrow : 0;
       }
     }
-    bad = __syncthreads_or(bad);
-    if (!bad) {
-      for (int i = tid; i < n; i += PO_THREADS) atomicMin(p.mark + seqs[i], i);   // listed twice: the first entry counts
-      __syncthreads();
-      // pages behind the new ends
-      for (int i = warp; i < n; i += PO_THREADS / 32) {
-        const int s = seqs[i], w = want[i], old = __ldcg(p.lens + s);
-        __syncwarp();
-        if (__ldcg(p.mark + s) != i || w >= old) continue;
-        int32_t* row = p.table + (size_t)s * p.seq_pages;
-        for (int o = pg_ceil(w, p.pt) + lane; o < min(p.seq_pages, pg_ceil(old, p.pt)); o += 32) {
-          const int page = row[o];
-          if (page >= 0 && page < p.pages) atomicSub(p.refs + page, 1);
-          row[o] = -1;
-        }
-        if (lane == 0) p.lens[s] = w;
+    mine = __reduce_or_sync(0xffffffffu, mine);
+    if (lane == 0 && mine) atomicOr(&any, mine);
+    __syncthreads();
+    const uint32_t flags = any;
+    if (!(flags & kAnyBad)) {
+      const bool twice = flags & kAnyAgain;
+      if (twice) {
+        for (int i = tid; i < n; i += PO_THREADS) p.mark[seqs[i]] = n;
+        __syncthreads();
+        for (int i = tid; i < n; i += PO_THREADS) atomicMin(p.mark + seqs[i], i);
+        __syncthreads();
       }
-      __syncthreads();
-      // how many pages every entry lacks, and from where in the list of free pages it takes them
-      int total = 0;
-      bool lost = false;
-      for (int base = 0; base < n; base += PO_THREADS) {
-        const int i = base + tid;
-        int need = 0, split = 0;
-        if (i < n) {
-          const int s = seqs[i], w = want[i], old = __ldcg(p.lens + s);
-          if (__ldcg(p.mark + s) == i && w > old) {
-            if (old & (p.pt - 1)) {
-              const int held = __ldcg(p.table + (size_t)s * p.seq_pages + (old >> p.pt_shift));
-              lost |= held < 0 || held >= p.pages;         // cut back into pages that were trimmed
-              split = held >= 0 && held < p.pages && __ldcg(p.refs + held) > 1;
-            }
-            need = pg_ceil(w, p.pt) - pg_ceil(old, p.pt) + split;
-          }
-        }
-        int sum;
-        const int upto = block_scan(need, sums, &sum);
-        if (i < n) p.off[i] = (total + upto - need) * 2 + split;
-        total += sum;
-      }
-      lost = __syncthreads_or(lost);
-      const int free_pages = total ? take_free(p, total, p.fresh, sums) : 0;
-      if (lost || total > free_pages) {                    // then no sequence grows
-        if (tid == 0) pg_status(p.status, lost ? kPagesState : kPagesExhausted, 11);
-      } else {
+      auto counts = [&](int i, int s) { return !twice || __ldcg(p.mark + s) == i; };
+      if (flags & kAnyShrink) {
+        // pages behind the new ends
         for (int i = warp; i < n; i += PO_THREADS / 32) {
-          const int s = seqs[i], w = want[i], old = __ldcg(p.lens + s);
+          const int s = __ldg(seqs + i), w = __ldg(want + i), old = __ldcg(p.lens + s);
           __syncwarp();
-          if (__ldcg(p.mark + s) != i || w <= old) continue;
-          const int at = __ldcg(p.off + i), split = at & 1;
-          const int first = pg_ceil(old, p.pt) - split, need = pg_ceil(w, p.pt) - first;
-          int32_t* row = p.table + (size_t)s * p.seq_pages + first;
-          for (int k = lane; k < need; k += 32) {
-            const int page = __ldcg(p.fresh + (at >> 1) + k);
-            if (split && k == 0) {
-              const int held = row[0], m = atomicAdd(&nmoves, 1);
-              p.moves[1 + 2 * m] = held;
-              p.moves[2 + 2 * m] = page;
-              atomicSub(p.refs + held, 1);
-            }
-            row[k] = page;
-            p.refs[page] = 1;
+          if (w >= old || !counts(i, s)) continue;
+          int32_t* row = p.table + (size_t)s * p.seq_pages;
+          for (int o = pg_ceil(w, p.pt) + lane; o < min(p.seq_pages, pg_ceil(old, p.pt)); o += 32) {
+            const int page = row[o];
+            if (page >= 0 && page < p.pages) atomicSub(p.refs + page, 1);
+            row[o] = -1;
           }
           if (lane == 0) p.lens[s] = w;
+        }
+        __syncthreads();
+      }
+      if (flags & kAnyGrow) {
+        // how many pages every entry lacks, and from where in the list of free pages it takes them
+        int total = 0;
+        bool lost = false;
+        for (int base = 0; base < n; base += PO_THREADS) {
+          const int i = base + tid;
+          int need = 0, split = 0;
+          if (i < n) {
+            const int s = __ldg(seqs + i), w = __ldg(want + i), old = __ldcg(p.lens + s);
+            if (w > old && counts(i, s)) {
+              if (old & (p.pt - 1)) {
+                const int held = __ldcg(p.table + (size_t)s * p.seq_pages + (old >> p.pt_shift));
+                lost |= held < 0 || held >= p.pages;       // cut back into pages that were trimmed
+                split = held >= 0 && held < p.pages && __ldcg(p.refs + held) > 1;
+              }
+              need = pg_ceil(w, p.pt) - pg_ceil(old, p.pt) + split;
+            }
+          }
+          int sum;
+          const int upto = block_scan(need, sums, &sum);
+          if (i < n) p.off[i] = (total + upto - need) * 2 + split;
+          total += sum;
+        }
+        lost = __syncthreads_or(lost);
+        const int free_pages = total ? take_free(p, total, p.fresh, sums) : 0;
+        if (lost || total > free_pages) {                  // then no sequence grows
+          if (tid == 0) pg_status(p.status, lost ? kPagesState : kPagesExhausted, 11);
+        } else if (total == 0) {
+          for (int i = tid; i < n; i += PO_THREADS) {
+            const int s = __ldg(seqs + i);
+            if (counts(i, s)) p.lens[s] = __ldg(want + i);   // those that shrink have their lengths already
+          }
+        } else {
+          for (int i = warp; i < n; i += PO_THREADS / 32) {
+            const int s = __ldg(seqs + i), w = __ldg(want + i), old = __ldcg(p.lens + s);
+            __syncwarp();
+            if (w <= old || !counts(i, s)) continue;
+            const int at = __ldcg(p.off + i), split = at & 1;
+            const int first = pg_ceil(old, p.pt) - split, need = pg_ceil(w, p.pt) - first;
+            int32_t* row = p.table + (size_t)s * p.seq_pages + first;
+            for (int k = lane; k < need; k += 32) {
+              const int page = __ldcg(p.fresh + (at >> 1) + k);
+              if (split && k == 0) {
+                const int held = row[0], m = atomicAdd(&nmoves, 1);
+                p.moves[1 + 2 * m] = held;
+                p.moves[2 + 2 * m] = page;
+                atomicSub(p.refs + held, 1);
+              }
+              row[k] = page;
+              p.refs[page] = 1;
+            }
+            if (lane == 0) p.lens[s] = w;
+          }
         }
       }
     }
@@ -183,28 +224,43 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
 __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p, int n, const int32_t* src,
                                                                      const int32_t* dst) {
   __shared__ int sums[PO_THREADS / 32];
+  __shared__ Listed listed;
   const int tid = threadIdx.x;
-  bool bad = __ldcg(p.status) != 0;
+  for (int i = tid; i < min(PO_BITS, p.seqs + 31) / 32; i += PO_THREADS) listed.seen[i] = 0;
+  bool bad = __ldcg(p.status) != 0, again = false;
+  __syncthreads();
   for (int i = tid; i < n; i += PO_THREADS) {
-    const int a = src[i], b = dst[i];
+    const int a = __ldg(src + i), b = __ldg(dst + i);
     if (a < 0 || a >= p.seqs || b < 0 || b >= p.seqs || !pg_len_ok(p, __ldcg(p.lens + a))) {
       pg_status(p.status, kPagesBounds, 20);
       bad = true;
     } else {
-      p.mark[a] = n;
-      p.mark[b] = n;
-    }
-  }
-  bad = __syncthreads_or(bad);
-  if (!bad) {
-    for (int i = tid; i < n; i += PO_THREADS) atomicMin(p.mark + dst[i], i);
-    __syncthreads();
-    // a destination is empty, listed once, and no source
-    for (int i = tid; i < n; i += PO_THREADS)
-      if (__ldcg(p.mark + dst[i]) != i || __ldcg(p.mark + src[i]) != n || __ldcg(p.lens + dst[i]) != 0) {
+      if (__ldcg(p.lens + b) != 0) {                       // a destination is empty, listed once, and no source
         pg_status(p.status, kPagesState, 21);
         bad = true;
       }
+      again |= listed_again(listed, p, b);
+    }
+  }
+  const bool small = p.seqs <= PO_BITS;
+  bad = __syncthreads_or(bad);
+  again = __syncthreads_or(again);
+  if (!bad && !small) {
+    for (int i = tid; i < n; i += PO_THREADS) {
+      p.mark[src[i]] = n;
+      p.mark[dst[i]] = n;
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += PO_THREADS) atomicMin(p.mark + dst[i], i);
+    __syncthreads();
+  }
+  if (!bad) {
+    bad = small && again;
+    for (int i = tid; i < n; i += PO_THREADS) {
+      const int a = __ldg(src + i), b = __ldg(dst + i);
+      bad |= small ? listed.seen[a >> 5] >> (a & 31) & 1 : __ldcg(p.mark + b) != i || __ldcg(p.mark + a) != n;
+    }
+    if (bad) pg_status(p.status, kPagesState, 21);
     bad = __syncthreads_or(bad);
   }
   int total = 0;
@@ -213,8 +269,8 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
       const int i = base + tid;
       int held = -1;
       if (i < n) {
-        const int len = __ldcg(p.lens + src[i]);
-        if (len & (p.pt - 1)) held = __ldcg(p.table + (size_t)src[i] * p.seq_pages + (len >> p.pt_shift));
+        const int a = __ldg(src + i), len = __ldcg(p.lens + a);
+        if (len & (p.pt - 1)) held = __ldcg(p.table + (size_t)a * p.seq_pages + (len >> p.pt_shift));
         if (held >= p.pages) held = -1;
       }
       int sum;
