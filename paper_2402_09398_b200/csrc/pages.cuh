@@ -16,7 +16,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include "less.h"
+#include "less_internal.cuh"
 
 namespace less {
 
@@ -33,7 +33,7 @@ struct PgParams {
   int32_t* lens;
   int32_t* refs;
   int32_t* status;         // [4] first words of the workspace
-  int32_t* moves;          // [0] number of page moves of the call under way, then (source, destination) pairs
+  int32_t* moves;          // [0] number of page moves of the call under way, then (source, destination, tiles) of each
   int32_t* mark;           // [seqs]
   int32_t* off;            // [seqs]
   int32_t* fresh;          // [max(seqs, pages)]
@@ -121,6 +121,30 @@ __device__ __forceinline__ int pg_page(const PgParams& p, int seq, int ordinal) 
     return -1;
   }
   return page;
+}
+
+// Every kernel of the cache is launched as a programmatic dependent of the kernel before it in the stream: its CTAs come
+// up while that one drains and wait, before they read anything, until it is complete (pg_wait).  Each lets its own
+// dependents come up as soon as all its CTAs run.
+__device__ __forceinline__ void pg_wait() {
+  pdl_launch_dependents();
+  pdl_wait_primary();
+}
+
+template <typename... P, typename... A>
+inline int pg_launch(const char* name, void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+  return e == cudaSuccess ? check_launch(name) : fail_cuda(name, e);
 }
 
 // host: checks a description; on success fills the device view

@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   extern __shared__ __align__(16) unsigned char ps_ring[];
   __shared__ PsShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  pg_wait();
 
   // ---- the list of blocks: a thread counts the entries of a stretch of its own, one scan orders them ----
   const int per_thread = pg_ceil(a.n, PS_THREADS);
@@ -663,8 +664,7 @@ static int launch_step(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   const int most = (int)(LESS_PAGES_PARTIAL_BYTES / block_bytes);
   if (grid > most) grid = most;
   if (grid > kPgCounters) grid = kPgCounters;
-  pages_step_kernel<T, D, NT, E4M3><<<grid, PS_THREADS, smem, s>>>(p, a);
-  return check_launch("pages_step_kernel");
+  return pg_launch("pages_step_kernel", pages_step_kernel<T, D, NT, E4M3>, dim3(grid), PS_THREADS, smem, s, p, a);
 }
 
 template <typename T, bool E4M3>

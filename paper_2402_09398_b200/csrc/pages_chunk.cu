@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   if (smem_misaligned(pc_smem, p.status, 120)) return;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pg_wait();
   // ---- the item: late rows, which see most, first ----
   const int64_t slot = gridDim.y - 1 - blockIdx.y;
   int lo = 0, hi = a.n - 1;
@@ -556,8 +557,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   }
   const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n;
   if (slots > 65535) return LESS_ERR_INVALID_CONFIG;
-  pages_chunk_kernel<T, D, E4M3><<<dim3(p.heads * a.nl, (unsigned)slots), PC_THREADS, smem, s>>>(p, a);
-  return check_launch("pages_chunk_kernel");
+  return pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3>, dim3(p.heads * a.nl, (unsigned)slots), PC_THREADS, smem, s, p, a);
 }
 
 int launch_pages_chunk(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s) {

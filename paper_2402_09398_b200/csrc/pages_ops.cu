@@ -64,7 +64,23 @@ __device__ __forceinline__ int take_free(const PgParams& p, int want, int* list,
   return total;
 }
 
-// copies page src to page dst of one layer, 16 bytes per thread and turn
+// A page move: the first `tiles` stored tiles of every head's keys and values (the rest of a page that is still being
+// filled holds nothing), in 16-byte units
+struct Move {
+  int src, dst, run, units;                            // run: units of one head's keys
+};
+__device__ __forceinline__ Move load_move(const PgParams& p, int D, int m) {
+  Move v;
+  v.src = __ldcg(p.moves + 1 + 3 * m);
+  v.dst = __ldcg(p.moves + 2 + 3 * m);
+  v.run = __ldcg(p.moves + 3 + 3 * m) * D;             // kPageBlock * D / 16 per tile
+  v.units = p.heads * 2 * v.run;
+  return v;
+}
+__device__ __forceinline__ uint4* unit_at(const PgParams& p, int D, int layer, int page, const Move& v, int u) {
+  const int hw = u / v.run;
+  return reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, page, 0) + (size_t)hw * p.pt * D) + (u - hw * v.run);
+}
 __device__ __forceinline__ void copy_mags(const PgParams& p, int layer, int src, int dst, int tid, int threads) {
   const int m = p.heads * 2 * (p.pt / kPageBlock);
   const float* a = p.amax + pg_mag(p, layer, src, 0);
@@ -97,6 +113,7 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
   __shared__ int nmoves;
   __shared__ uint32_t any;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pg_wait();
   if (blockIdx.x == 0) {
     if (tid == 0) {
       nmoves = 0;
@@ -190,8 +207,9 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
               const int page = __ldcg(p.fresh + (at >> 1) + k);
               if (split && k == 0) {
                 const int held = row[0], m = atomicAdd(&nmoves, 1);
-                p.moves[1 + 2 * m] = held;
-                p.moves[2 + 2 * m] = page;
+                p.moves[1 + 3 * m] = held;
+                p.moves[2 + 3 * m] = page;
+                p.moves[3 + 3 * m] = pg_ceil(old & (p.pt - 1), kPageBlock);
                 atomicSub(p.refs + held, 1);
               }
               row[k] = page;
@@ -207,16 +225,13 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
   }
   cluster_sync_all();
   const int moves = __ldcg(p.moves);
-  const int units = p.heads * 2 * p.pt * D / 16;
-  for (int m = 0; m < moves; ++m) {
-    const int src = __ldcg(p.moves + 1 + 2 * m), dst = __ldcg(p.moves + 2 + 2 * m);
+  for (int m = 0; m < moves; ++m)
     for (int layer = 0; layer < p.layers; ++layer) {
-      const uint4* a = reinterpret_cast<const uint4*>(p.codes + pg_slab(p, D, layer, src, 0));
-      uint4* b = reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, dst, 0));
-      for (int u = blockIdx.x * PO_THREADS + tid; u < units; u += PO_CLUSTER * PO_THREADS) b[u] = a[u];
-      if ((int)blockIdx.x == layer % PO_CLUSTER) copy_mags(p, layer, src, dst, tid, PO_THREADS);
+      const Move v = load_move(p, D, m);
+      for (int u = blockIdx.x * PO_THREADS + tid; u < v.units; u += PO_CLUSTER * PO_THREADS)
+        *unit_at(p, D, layer, v.dst, v, u) = *unit_at(p, D, layer, v.src, v, u);
+      if ((int)blockIdx.x == layer % PO_CLUSTER) copy_mags(p, layer, v.src, v.dst, tid, PO_THREADS);
     }
-  }
 }
 
 // Fork, the plan: which pairs need a copy of the page that is still being filled, and which free page each gets.
@@ -226,6 +241,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
   __shared__ int sums[PO_THREADS / 32];
   __shared__ Listed listed;
   const int tid = threadIdx.x;
+  pg_wait();
   for (int i = tid; i < min(PO_BITS, p.seqs + 31) / 32; i += PO_THREADS) listed.seen[i] = 0;
   bool bad = __ldcg(p.status) != 0, again = false;
   __syncthreads();
@@ -267,16 +283,20 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
   if (!bad) {
     for (int base = 0; base < n; base += PO_THREADS) {
       const int i = base + tid;
-      int held = -1;
+      int held = -1, len = 0;
       if (i < n) {
-        const int a = __ldg(src + i), len = __ldcg(p.lens + a);
+        const int a = __ldg(src + i);
+        len = __ldcg(p.lens + a);
         if (len & (p.pt - 1)) held = __ldcg(p.table + (size_t)a * p.seq_pages + (len >> p.pt_shift));
         if (held >= p.pages) held = -1;
       }
       int sum;
       const int at = total + block_scan(held >= 0, sums, &sum) - 1;
       if (i < n) p.off[i] = held >= 0 ? at : -1;
-      if (held >= 0) p.moves[1 + 2 * at] = held;
+      if (held >= 0) {
+        p.moves[1 + 3 * at] = held;
+        p.moves[3 + 3 * at] = pg_ceil(len & (p.pt - 1), kPageBlock);
+      }
       total += sum;
     }
     const int free_pages = total ? take_free(p, total, p.fresh, sums) : 0;
@@ -286,7 +306,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
     } else {
       for (int k = tid; k < total; k += PO_THREADS) {
         const int page = __ldcg(p.fresh + k);
-        p.moves[2 + 2 * k] = page;
+        p.moves[2 + 3 * k] = page;
         p.refs[page] = 1;
       }
     }
@@ -299,6 +319,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
 __global__ void __launch_bounds__(PO_THREADS) pages_compact_plan_kernel(PgParams p) {
   __shared__ int sums[PO_THREADS / 32];
   const int tid = threadIdx.x;
+  pg_wait();
   if (__ldcg(p.status) != 0) {
     if (tid == 0) p.moves[0] = -1;
     return;
@@ -319,13 +340,16 @@ __global__ void __launch_bounds__(PO_THREADS) pages_compact_plan_kernel(PgParams
   int all, h = block_scan(holes, sums, &all) - holes, m = block_scan(movers, sums, &all) - movers;
   for (int i = begin; i < end; ++i) {
     const bool used = __ldcg(p.refs + i) > 0;
-    if (!used && i < live) p.moves[2 + 2 * h++] = i;
-    if (used && i >= live) p.moves[1 + 2 * m++] = i;
+    if (!used && i < live) p.moves[2 + 3 * h++] = i;
+    if (used && i >= live) {
+      p.moves[3 + 3 * m] = p.pt / kPageBlock;
+      p.moves[1 + 3 * m++] = i;
+    }
     p.fresh[i] = i;
   }
   __syncthreads();
   for (int k = tid; k < all; k += PO_THREADS) {
-    const int a = __ldcg(p.moves + 1 + 2 * k), b = __ldcg(p.moves + 2 + 2 * k);
+    const int a = __ldcg(p.moves + 1 + 3 * k), b = __ldcg(p.moves + 2 + 3 * k);
     p.fresh[a] = b;
     p.refs[b] = __ldcg(p.refs + a);
     p.refs[a] = 0;
@@ -340,7 +364,9 @@ constexpr int PM_THREADS = 256, PM_UNITS = 1024;       // 16-byte units per piec
 template <bool FORK>
 __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int D, int n, const int32_t* src,
                                                                 const int32_t* dst) {
-  const int moves = __ldcg(p.moves), tid = threadIdx.x;
+  const int tid = threadIdx.x;
+  pg_wait();
+  const int moves = __ldcg(p.moves);
   if (moves < 0) return;
   const int rows = FORK ? n : p.seqs;
   for (int i = blockIdx.x; i < rows; i += gridDim.x) {
@@ -355,7 +381,7 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
           page = __ldcg(from + o);
           if (page >= 0 && page < p.pages) atomicAdd(p.refs + page, 1);
         } else if (o == whole && at >= 0) {
-          page = __ldcg(p.moves + 2 + 2 * at);
+          page = __ldcg(p.moves + 2 + 3 * at);
         }
         to[o] = page;
       }
@@ -368,28 +394,32 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
       }
     }
   }
-  const int units = p.heads * 2 * p.pt * D / 16, pieces = pg_ceil(units, PM_UNITS);
-  const int64_t work = (int64_t)moves * p.layers * pieces;
+  // pieces of a whole page; a move with fewer tiles has fewer
+  const int pieces = pg_ceil(p.heads * 2 * p.pt * D / 16, PM_UNITS), per_move = p.layers * pieces;
+  const int64_t work = (int64_t)moves * per_move;
   for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
-    const int64_t ml = w / pieces;
-    const int piece = (int)(w - ml * pieces), m = (int)(ml / p.layers), layer = (int)(ml - (int64_t)m * p.layers);
-    const int a = __ldcg(p.moves + 1 + 2 * m), b = __ldcg(p.moves + 2 + 2 * m);
-    const uint4* from = reinterpret_cast<const uint4*>(p.codes + pg_slab(p, D, layer, a, 0)) + piece * PM_UNITS;
-    uint4* to = reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, b, 0)) + piece * PM_UNITS;
-    const int left = min(PM_UNITS, units - piece * PM_UNITS);
-    uint4 v[PM_UNITS / PM_THREADS];
+    // 64-bit divisions only where the numbers need them
+    const int m = work <= 0x7fffffff ? (int)w / per_move : (int)(w / per_move);
+    const int rest = (int)(w - (int64_t)m * per_move), layer = rest / pieces, first = (rest - layer * pieces) * PM_UNITS;
+    const Move v = load_move(p, D, m);
+    uint4 x[PM_UNITS / PM_THREADS];
 #pragma unroll
-    for (int k = 0; k < PM_UNITS / PM_THREADS; ++k)
-      if (tid + k * PM_THREADS < left) v[k] = __ldcs(from + tid + k * PM_THREADS);
+    for (int k = 0; k < PM_UNITS / PM_THREADS; ++k) {
+      const int u = first + tid + k * PM_THREADS;
+      if (u < v.units) x[k] = __ldcs(unit_at(p, D, layer, v.src, v, u));
+    }
 #pragma unroll
-    for (int k = 0; k < PM_UNITS / PM_THREADS; ++k)
-      if (tid + k * PM_THREADS < left) __stcs(to + tid + k * PM_THREADS, v[k]);
-    if (piece == 0) copy_mags(p, layer, a, b, tid, PM_THREADS);
+    for (int k = 0; k < PM_UNITS / PM_THREADS; ++k) {
+      const int u = first + tid + k * PM_THREADS;
+      if (u < v.units) __stcs(unit_at(p, D, layer, v.dst, v, u), x[k]);
+    }
+    if (first == 0) copy_mags(p, layer, v.src, v.dst, tid, PM_THREADS);
   }
 }
 
 // Trim: a block per entry; an entry listed twice finds the pages gone (the exchange hands each out once)
 __global__ void __launch_bounds__(128) pages_trim_kernel(PgParams p, int n, const int32_t* seqs, int sinks, int window) {
+  pg_wait();
   const int s = seqs[blockIdx.x];
   if (__ldcg(p.status) != 0) return;
   if (s < 0 || s >= p.seqs) {
@@ -423,7 +453,7 @@ static PgLayout pg_layout(const less_pages* d) {
   };
   const size_t most = (size_t)(d->pages > d->seqs ? d->pages : d->seqs);
   l.counters = take(kPgCounters * 4);
-  l.moves = take((1 + 2 * most) * 4);
+  l.moves = take((1 + 3 * most) * 4);
   l.mark = take((size_t)d->seqs * 4);
   l.off = take((size_t)d->seqs * 4);
   l.fresh = take(most * 4);
@@ -521,8 +551,8 @@ int less_pages_resize(const less_pages* d, int32_t n, const int32_t* seqs, const
   if (n == 0) return LESS_OK;
   if (!seqs || !lens) return LESS_ERR_NULL_POINTER;
   if (((uintptr_t)seqs | (uintptr_t)lens) & 3) return LESS_ERR_MISALIGNED;
-  pages_resize_kernel<<<PO_CLUSTER, PO_THREADS, 0, (cudaStream_t)stream>>>(p, d->head_dim, n, seqs, lens);
-  return check_launch("pages_resize_kernel");
+  return pg_launch("pages_resize_kernel", pages_resize_kernel, dim3(PO_CLUSTER), PO_THREADS, 0, (cudaStream_t)stream, p, d->head_dim, n, seqs,
+                   lens);
 }
 
 int less_pages_fork(const less_pages* d, int32_t n, const int32_t* src, const int32_t* dst, void* stream) {
@@ -533,13 +563,11 @@ int less_pages_fork(const less_pages* d, int32_t n, const int32_t* src, const in
   if (n == 0) return LESS_OK;
   if (!src || !dst) return LESS_ERR_NULL_POINTER;
   if (((uintptr_t)src | (uintptr_t)dst) & 3) return LESS_ERR_MISALIGNED;
-  pages_fork_plan_kernel<<<1, PO_THREADS, 0, (cudaStream_t)stream>>>(p, n, src, dst);
-  rc = check_launch("pages_fork_plan_kernel");
+  rc = pg_launch("pages_fork_plan_kernel", pages_fork_plan_kernel, dim3(1), PO_THREADS, 0, (cudaStream_t)stream, p, n, src, dst);
   if (rc != LESS_OK) return rc;
   const int64_t pieces = (int64_t)n * (1 + (int64_t)d->layers * pg_ceil(d->heads * 2 * d->page_tokens * d->head_dim / 16, PM_UNITS));
   const int grid = (int)(pieces < 8 * pg_sms() ? pieces : 8 * pg_sms());
-  pages_move_kernel<true><<<grid, PM_THREADS, 0, (cudaStream_t)stream>>>(p, d->head_dim, n, src, dst);
-  return check_launch("pages_move_kernel");
+  return pg_launch("pages_move_kernel", pages_move_kernel<true>, dim3(grid), PM_THREADS, 0, (cudaStream_t)stream, p, d->head_dim, n, src, dst);
 }
 
 int less_pages_trim(const less_pages* d, int32_t n, const int32_t* seqs, int32_t sinks, int32_t window, void* stream) {
@@ -551,19 +579,17 @@ int less_pages_trim(const less_pages* d, int32_t n, const int32_t* seqs, int32_t
   if (n == 0) return LESS_OK;
   if (!seqs) return LESS_ERR_NULL_POINTER;
   if ((uintptr_t)seqs & 3) return LESS_ERR_MISALIGNED;
-  pages_trim_kernel<<<n, 128, 0, (cudaStream_t)stream>>>(p, n, seqs, sinks, window);
-  return check_launch("pages_trim_kernel");
+  return pg_launch("pages_trim_kernel", pages_trim_kernel, dim3(n), 128, 0, (cudaStream_t)stream, p, n, seqs, sinks, window);
 }
 
 int less_pages_compact(const less_pages* d, void* stream) {
   PgParams p;
   int rc = pg_view(d, &p);
   if (rc != LESS_OK) return rc;
-  pages_compact_plan_kernel<<<1, PO_THREADS, 0, (cudaStream_t)stream>>>(p);
-  rc = check_launch("pages_compact_plan_kernel");
+  rc = pg_launch("pages_compact_plan_kernel", pages_compact_plan_kernel, dim3(1), PO_THREADS, 0, (cudaStream_t)stream, p);
   if (rc != LESS_OK) return rc;
-  pages_move_kernel<false><<<8 * pg_sms(), PM_THREADS, 0, (cudaStream_t)stream>>>(p, d->head_dim, 0, nullptr, nullptr);
-  return check_launch("pages_move_kernel");
+  return pg_launch("pages_move_kernel", pages_move_kernel<false>, dim3(8 * pg_sms()), PM_THREADS, 0, (cudaStream_t)stream, p, d->head_dim, 0,
+                   (const int32_t*)nullptr, (const int32_t*)nullptr);
 }
 
 int less_pages_poll_status(const less_pages* d, void* stream) {

@@ -83,6 +83,7 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwA
   constexpr int HEADS = PW_THREADS / (2 * PER); // heads per turn
   __shared__ float red[2][PW_THREADS / 32];
   const int tid = threadIdx.x, lane = tid & 31;
+  pg_wait();
   const int slot = blockIdx.x;
   int lo = 0, hi = a.n - 1;                     // the last entry whose slots start at or before this one
   while (lo < hi) {
@@ -194,6 +195,107 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwA
   }
 }
 
+// One new token per sequence, a warp per (sequence, layer, head), which puts both tiles of the block back: older tokens
+// as they were or, if the magnitude has grown, rounded again, zeros behind the end, and then the token's own codes (a
+// lane's four dimensions of the keys are four neighbouring bytes, those of the values lie four bytes apart).  What counts
+// is the chain of loads that leads to the tiles: all that does not depend on one another is asked for at once.
+template <typename T, int D, bool E4M3>
+__global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p, PwArgs a, int nl) {
+  constexpr int PL = D / 32, PIECES = D / 32;   // values of a lane; 16-byte pieces of a lane in a tile
+  const int lane = threadIdx.x & 31;
+  pg_wait();
+  const int64_t w = (int64_t)blockIdx.x * (PW_THREADS / 32) + (threadIdx.x >> 5);
+  const int per = nl * p.heads, i = (int)(w / per), rest = (int)(w - (int64_t)i * per), lj = rest / p.heads, h = rest - lj * p.heads;
+  if (i >= a.n) return;
+  T raw[2][PL];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const T* src = reinterpret_cast<const T*>(which ? a.v : a.k) + (int64_t)i * (which ? a.v_stride : a.k_stride) +
+                   (int64_t)(lj * p.heads + h) * D + lane * PL;
+    if (PL == 4) *reinterpret_cast<uint2*>(raw[which]) = __ldcs(reinterpret_cast<const uint2*>(src));
+    else *reinterpret_cast<uint32_t*>(raw[which]) = __ldcs(reinterpret_cast<const uint32_t*>(src));
+  }
+  bool again = __ldcg(p.status) != 0;
+  const PgEntry e = pg_entry(p, a.seqs, nullptr, a.rows, i);
+  for (int j = lane; j < i; j += 32) again |= __ldg(a.seqs + j) == e.seq;
+  if (e.count == 0) return;
+  if (e.len == 0) {
+    if (lane == 0) pg_status(p.status, kPagesBounds, 42);
+    return;
+  }
+  const int pos = e.len - 1, page = pg_page(p, e.seq, pos >> p.pt_shift);
+  if (__any_sync(0xffffffffu, again)) return;
+  if (page < 0 || __ldcg(p.refs + page) != 1) {          // trimmed, or held by other sequences too
+    if (lane == 0) pg_status(p.status, page < 0 ? kPagesBounds : kPagesState, 43);
+    return;
+  }
+  const int inner = (pos & (p.pt - 1)) / kPageBlock, token = pos % kPageBlock, layer = a.layer0 + lj;
+  float* mags = p.amax + pg_mag(p, layer, page, h) + inner;
+  uint8_t* tiles = p.codes + pg_slab(p, D, layer, page, h) + (size_t)inner * kPageBlock * D;
+  float old[2] = {0.f, 0.f};
+  uint4 was[2][PIECES];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (token) old[which] = __ldcg(mags + which * (p.pt / kPageBlock));
+#pragma unroll
+    for (int c = 0; c < PIECES; ++c)
+      was[which][c] = token ? *reinterpret_cast<const uint4*>(tiles + (size_t)which * p.pt * D + c * 512 + lane * 16) : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    uint8_t* tile = tiles + (size_t)which * p.pt * D;
+    float x[4] = {0.f, 0.f, 0.f, 0.f}, m = 0.f;
+#pragma unroll
+    for (int k = 0; k < PL; ++k) {
+      x[k] = pw_load(raw[which][k]);
+      m = fmaxf(m, fabsf(x[k]));
+      x[k] *= pg_top<E4M3>();
+    }
+    // magnitudes are not negative: their order is that of their bits
+    m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
+    m = fmaxf(m, old[which]);
+    if (m < 0x1p-100f) m = 0.f;
+    const float inv = __frcp_rn(m > 0.f ? m : 1.f);
+    const uint32_t mine = pw_codes<E4M3>(x, inv);
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int c = 0; c < PIECES; ++c) {
+      // which of a word's four codes are older tokens': of the keys all or none, of the values the first few
+      const int row = 4 * (g >> 1) + 2 * (c / (D / 64)) + (g & 1), older = which ? min(max(token - 4 * t, 0), 4) : row < token ? 4 : 0;
+      const uint32_t keep = older == 4 ? 0xffffffffu : (1u << (8 * older)) - 1;
+      const uint32_t w[4] = {was[which][c].x & keep, was[which][c].y & keep, was[which][c].z & keep, was[which][c].w & keep};
+      uint4 out = make_uint4(w[0], w[1], w[2], w[3]);
+      if (m != old[which]) {
+        uint32_t again[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float y[4];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) y[b] = b < older ? pw_value<E4M3>((w[q] >> (8 * b)) & 0xffu) * old[which] : 0.f;
+          again[q] = pw_codes<E4M3>(y, inv);
+        }
+        out = make_uint4(again[0], again[1], again[2], again[3]);
+      }
+      *reinterpret_cast<uint4*>(tile + c * 512 + lane * 16) = out;
+    }
+    if (lane == 0 && (m != old[which] || token == 0)) mags[which * (p.pt / kPageBlock)] = m;
+    __syncwarp();                                        // the token's codes go on top, from other lanes
+    // the token's codes: dimensions lane * PL ..
+    const int d = lane * PL;
+    if (which == 0) {
+      const int gk = 2 * (token >> 2) + (token & 1), j = token >> 1 & 1, tk = d / (D / 4), r = d % (D / 4);
+      uint8_t* at = tile + (32 * (j * (D / 64) + r / 16) + 4 * gk + tk) * 16 + r % 16;
+      if (PL == 4) *reinterpret_cast<uint32_t*>(at) = mine;
+      else *reinterpret_cast<uint16_t*>(at) = (uint16_t)mine;
+    } else {
+      const int gv = d / (D / 8), r = d % (D / 8);
+      uint8_t* at = tile + (32 * (r / 4) + 4 * gv + (token >> 2)) * 16 + (r % 4) * 4 + (token & 3);
+#pragma unroll
+      for (int k = 0; k < PL; ++k) at[4 * k] = (uint8_t)(mine >> (8 * k));
+    }
+  }
+}
+
 }  // namespace less
 
 using namespace less;
@@ -202,7 +304,7 @@ extern "C" int less_pages_write(const less_pages* d, int32_t layer_begin, int32_
                                 const int32_t* seqs, const int32_t* starts, int32_t rows, const void* k,
                                 int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
   PgParams p;
-  const int rc = pg_view(d, &p);
+  int rc = pg_view(d, &p);
   if (rc != LESS_OK) return rc;
   if (layer_begin < 0 || layer_count < 1 || layer_begin > d->layers - layer_count) return LESS_ERR_BAD_LAYER_RANGE;
   if (n < 0 || n > (1 << 24) || rows < 0 || (!starts && rows != n)) return LESS_ERR_INVALID_CONFIG;
@@ -220,14 +322,17 @@ extern "C" int less_pages_write(const less_pages* d, int32_t layer_begin, int32_
   int share = (int)((int64_t)slots * layer_count * turns / (16 * pg_sms()));
   share = share < 1 ? 1 : share > turns ? turns : share;
   const dim3 grid(slots, pg_ceil(turns, share), layer_count);
-  if (grid.y > 65535) return LESS_ERR_INVALID_CONFIG;
+  const int64_t one = ((int64_t)n * layer_count * d->heads + PW_THREADS / 32 - 1) / (PW_THREADS / 32);
+  if (grid.y > 65535 || one > 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
   cudaStream_t s = (cudaStream_t)stream;
-#define PW_LAUNCH(T, D, E) pages_write_kernel<T, D, E><<<grid, PW_THREADS, 0, s>>>(p, a)
-#define PW_TYPES(D)                                                                         \
-  if (bf16) { if (e4m3) PW_LAUNCH(__nv_bfloat16, D, true); else PW_LAUNCH(__nv_bfloat16, D, false); } \
+#define PW_LAUNCH(T, D, E)                                                                                              \
+  rc = starts ? pg_launch("pages_write_kernel", pages_write_kernel<T, D, E>, grid, PW_THREADS, 0, s, p, a)               \
+              : pg_launch("pages_write_one_kernel", pages_write_one_kernel<T, D, E>, dim3(one), PW_THREADS, 0, s, p, a, layer_count)
+#define PW_TYPES(D)                                                                                                      \
+  if (bf16) { if (e4m3) PW_LAUNCH(__nv_bfloat16, D, true); else PW_LAUNCH(__nv_bfloat16, D, false); }                    \
   else { if (e4m3) PW_LAUNCH(__half, D, true); else PW_LAUNCH(__half, D, false); }
   if (d->head_dim == 128) { PW_TYPES(128) } else { PW_TYPES(64) }
 #undef PW_TYPES
 #undef PW_LAUNCH
-  return check_launch("pages_write_kernel");
+  return rc;
 }
