@@ -46,20 +46,24 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
 __device__ __forceinline__ int take_free(const PgParams& p, int want, int* list, int* warp_sums) {
   const int per = pg_ceil(pg_ceil(p.pages, PO_THREADS), 4) * 4;
   const int begin = min(p.pages, (int)threadIdx.x * per), end = min(p.pages, begin + per);
-  int mine = 0;
-  for (int i = begin; i < end; i += 4) {
+  auto group = [&](int i) {                            // bit k: page i + k is free
+    uint32_t f = 0;
     if (i + 4 <= end) {
       const int4 r = __ldcg(reinterpret_cast<const int4*>(p.refs + i));
-      mine += (r.x == 0) + (r.y == 0) + (r.z == 0) + (r.w == 0);
+      f = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
     } else {
-      for (int j = i; j < end; ++j) mine += __ldcg(p.refs + j) == 0;
+      for (int j = i; j < end; ++j) f |= (uint32_t)(__ldcg(p.refs + j) == 0) << (j - i);
     }
-  }
+    return f;
+  };
+  const uint32_t first = begin < end ? group(begin) : 0;
+  int mine = __popc(first);
+  for (int i = begin + 4; i < end; i += 4) mine += __popc(group(i));
   int total;
   int at = block_scan(mine, warp_sums, &total) - mine;
   if (mine)
-    for (int i = begin; i < end && at < want; ++i)
-      if (__ldcg(p.refs + i) == 0) list[at++] = i;
+    for (int i = begin; i < end && at < want; i += 4)
+      for (uint32_t f = i == begin ? first : group(i); f && at < want; f &= f - 1) list[at++] = i + __ffs(f) - 1;
   __syncthreads();
   return total;
 }
@@ -357,9 +361,9 @@ __global__ void __launch_bounds__(PO_THREADS) pages_compact_plan_kernel(PgParams
   if (tid == 0) p.moves[0] = all;
 }
 
-// Carries out a plan: the table rows (fork: n rows; compact: every row), then the page copies in pieces of 16 KB,
-// over the whole GPU.  Sources and destinations are disjoint (destinations were free).
-constexpr int PM_THREADS = 256, PM_UNITS = 1024;       // 16-byte units per piece
+// Carries out a plan: the table rows (fork: n rows; compact: every row), then the page copies, over the whole GPU.
+// Sources and destinations are disjoint (destinations were free).
+constexpr int PM_THREADS = 256, PM_UNITS = 8;          // 16-byte units of a lane on their way at once
 
 template <bool FORK>
 __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int D, int n, const int32_t* src,
@@ -394,26 +398,26 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
       }
     }
   }
-  // pieces of a whole page; a move with fewer tiles has fewer
-  const int pieces = pg_ceil(p.heads * 2 * p.pt * D / 16, PM_UNITS), per_move = p.layers * pieces;
+  // a warp per run of tiles (one head's keys or values of a page in one layer: contiguous, 1 to 32 KB)
+  const int lane = tid & 31, runs = p.heads * 2, per_move = p.layers * runs;
   const int64_t work = (int64_t)moves * per_move;
-  for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
+  for (int64_t w = (int64_t)blockIdx.x * (PM_THREADS / 32) + (tid >> 5); w < work; w += (int64_t)gridDim.x * (PM_THREADS / 32)) {
     // 64-bit divisions only where the numbers need them
     const int m = work <= 0x7fffffff ? (int)w / per_move : (int)(w / per_move);
-    const int rest = (int)(w - (int64_t)m * per_move), layer = rest / pieces, first = (rest - layer * pieces) * PM_UNITS;
+    const int rest = (int)(w - (int64_t)m * per_move), layer = rest / runs, hw = rest - layer * runs;
     const Move v = load_move(p, D, m);
-    uint4 x[PM_UNITS / PM_THREADS];
+    const uint4* from = reinterpret_cast<const uint4*>(p.codes + pg_slab(p, D, layer, v.src, 0) + (size_t)hw * p.pt * D);
+    uint4* to = reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, v.dst, 0) + (size_t)hw * p.pt * D);
+    if (hw == 0) copy_mags(p, layer, v.src, v.dst, lane, 32);
+    for (int u0 = 0; u0 < v.run; u0 += 32 * PM_UNITS) {
+      uint4 x[PM_UNITS];
 #pragma unroll
-    for (int k = 0; k < PM_UNITS / PM_THREADS; ++k) {
-      const int u = first + tid + k * PM_THREADS;
-      if (u < v.units) x[k] = __ldcs(unit_at(p, D, layer, v.src, v, u));
-    }
+      for (int k = 0; k < PM_UNITS; ++k)
+        if (u0 + 32 * k + lane < v.run) x[k] = __ldcs(from + u0 + 32 * k + lane);
 #pragma unroll
-    for (int k = 0; k < PM_UNITS / PM_THREADS; ++k) {
-      const int u = first + tid + k * PM_THREADS;
-      if (u < v.units) __stcs(unit_at(p, D, layer, v.dst, v, u), x[k]);
+      for (int k = 0; k < PM_UNITS; ++k)
+        if (u0 + 32 * k + lane < v.run) __stcs(to + u0 + 32 * k + lane, x[k]);
     }
-    if (first == 0) copy_mags(p, layer, v.src, v.dst, tid, PM_THREADS);
   }
 }
 
@@ -565,8 +569,8 @@ int less_pages_fork(const less_pages* d, int32_t n, const int32_t* src, const in
   if (((uintptr_t)src | (uintptr_t)dst) & 3) return LESS_ERR_MISALIGNED;
   rc = pg_launch("pages_fork_plan_kernel", pages_fork_plan_kernel, dim3(1), PO_THREADS, 0, (cudaStream_t)stream, p, n, src, dst);
   if (rc != LESS_OK) return rc;
-  const int64_t pieces = (int64_t)n * (1 + (int64_t)d->layers * pg_ceil(d->heads * 2 * d->page_tokens * d->head_dim / 16, PM_UNITS));
-  const int grid = (int)(pieces < 8 * pg_sms() ? pieces : 8 * pg_sms());
+  const int64_t ctas = n + (int64_t)n * d->layers * pg_ceil(d->heads * 2, PM_THREADS / 32);
+  const int grid = (int)(ctas < 8 * pg_sms() ? ctas : 8 * pg_sms());
   return pg_launch("pages_move_kernel", pages_move_kernel<true>, dim3(grid), PM_THREADS, 0, (cudaStream_t)stream, p, d->head_dim, n, src, dst);
 }
 

@@ -78,7 +78,7 @@ __device__ __forceinline__ uint32_t pw_codes(const float* num, float inv) {
 }
 
 template <typename T, int D, bool E4M3>
-__global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwArgs a) {
+__global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, PwArgs a) {
   constexpr int PER = D;                        // threads per (head, keys or values): one 16-byte piece each
   constexpr int HEADS = PW_THREADS / (2 * PER); // heads per turn
   __shared__ float red[2][PW_THREADS / 32];
@@ -128,9 +128,11 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwA
         if (4 * t + k >= keep && 4 * t + k < live) raw[k] = __ldcs(reinterpret_cast<const uint2*>(s + (int64_t)k * stride));
     }
   };
-  uint2 raw[4], ahead[4];
+  // two heads on their way beside the one that is worked on: 4 CTAs x 16 KB per SM
+  uint2 raw[4], ahead[2][4];
   const int h_first = (int)blockIdx.y * HEADS + tid / (2 * PER), h_step = (int)gridDim.y * HEADS;
   fetch(h_first, raw);
+  fetch(h_first + h_step, ahead[0]);
 
   // nothing after an error; a sequence listed twice: the first entry counts
   bool again = __ldcg(p.status) != 0;
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwA
   for (int h0 = (int)blockIdx.y * HEADS; h0 < p.heads; h0 += h_step, turn ^= 1) {
     const int h = h0 + tid / (2 * PER);
     const bool in = h < p.heads;
-    fetch(h + h_step, ahead);
+    fetch(h + 2 * h_step, ahead[1]);
     uint8_t* tile = p.codes + pg_slab(p, D, layer, page, in ? h : 0) + ((size_t)which * p.pt + inner * kPageBlock) * D + piece * 16;
     float* mag = p.amax + pg_mag(p, layer, page, in ? h : 0) + which * (p.pt / kPageBlock) + inner;
     uint4 was = make_uint4(0, 0, 0, 0);
@@ -191,7 +193,10 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_kernel(PgParams p, PwA
       if (piece == 0) *mag = m;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) raw[k] = ahead[k];
+    for (int k = 0; k < 4; ++k) {
+      raw[k] = ahead[0][k];
+      ahead[0][k] = ahead[1][k];
+    }
   }
 }
 
