@@ -4,10 +4,10 @@
 //   code = rn(x * top / a)            top = 127 (int8) or 448 (e4m3), ties to even
 //   older tokens of the block, where a has grown:  code = rn(code * a_old / a)
 //
-// The codes are those of exact arithmetic, without a division per value.  x * top and code * a_old are exact in fp32
-// (16-bit inputs); times the correctly rounded 1 / a, a quotient is off by at most 2^-23 relative.  A quotient that is
-// not a tie is at least 2^-19 from the nearest one (both are ratios of integers of at most 8 + 11 bits), so rounding to
-// 21 bits first (2^-21) lands ties exactly on themselves and nothing else on a tie; the second rounding is then right.
+// The codes are those of exact arithmetic, without a division per value.  A 16-bit value (an old code, exactly) times the
+// correctly rounded top / a (a_old / a) is off by at most 2^-23 relative.  A quotient that is not a tie is at least 2^-19
+// from the nearest one (both are ratios of integers of at most 8 + 11 bits), so rounding to 21 bits first (2^-21) lands
+// ties exactly on themselves and nothing else on a tie; the second rounding is then right.
 // Infinities are written as the largest finite fp16 number (bf16: 2^100, so that x * top stays finite), NaN as 0:
 // one bad token must not take the other fifteen of its block with it.  Magnitudes below 2^-100 (bf16) become 0: the
 // attention divides by magnitudes.  Tokens of the last block behind the
@@ -56,32 +56,63 @@ __device__ __forceinline__ float pw_value(uint32_t code) {   // in units of amax
   return (float)(int8_t)code;
 }
 
-// four quotients -> four codes
+// four values times a factor -> four codes
 template <bool E4M3>
-__device__ __forceinline__ uint32_t pw_codes(const float* num, float inv) {
-  float y[4];
+__device__ __forceinline__ uint32_t pw_codes(float x0, float x1, float x2, float x3, float factor) {
+  const uint64_t f = f32x2_pack(factor, factor), nine = f32x2_pack(9.f, 9.f), minus = f32x2_pack(-1.f, -1.f);
+  uint64_t y[2] = {f32x2_mul(f32x2_pack(x0, x1), f), f32x2_mul(f32x2_pack(x2, x3), f)};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float q = __fmul_rn(num[i], inv), c = __fmul_rn(q, 9.f);     // 2^3 + 1: the upper 21 bits of q
-    y[i] = __fsub_rn(c, __fsub_rn(c, q));
+  for (int i = 0; i < 2; ++i) {
+    const uint64_t c = f32x2_mul(y[i], nine);            // 2^3 + 1: c - (c - y) is y to 21 bits
+    y[i] = f32x2_fma(f32x2_fma(y[i], minus, c), minus, c);
   }
+  float a, b, c, d;
   if (E4M3) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3);
+    f32x2_unpack(y[0], a, b);
+    f32x2_unpack(y[1], c, d);
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
     return lo | hi << 16;
   }
   // + 1.5 * 2^23 rounds to an integer, whose low byte is the code
-  uint32_t b[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(y[i], 12582912.f));
-  return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  const uint64_t one = f32x2_pack(1.f, 1.f), magic = f32x2_pack(12582912.f, 12582912.f);
+  f32x2_unpack(f32x2_fma(y[0], one, magic), a, b);
+  f32x2_unpack(f32x2_fma(y[1], one, magic), c, d);
+  return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
+                     __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+}
+
+// two packed 16-bit values -> fp32
+template <typename T>
+__device__ __forceinline__ void pw_pair(uint32_t u, float& a, float& b);
+template <>
+__device__ __forceinline__ void pw_pair<__half>(uint32_t u, float& a, float& b) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
+  a = f.x;
+  b = f.y;
+}
+template <>
+__device__ __forceinline__ void pw_pair<__nv_bfloat16>(uint32_t u, float& a, float& b) {
+  a = __uint_as_float(u << 16);
+  b = __uint_as_float(u & 0xffff0000u);
+}
+// the largest finite value of pw_load, as bits: 65504, 2^100
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t pw_most_bits() { return std::is_same<T, __half>::value ? 0x7bffu : 0x7180u; }
+template <typename T>
+__device__ __forceinline__ uint32_t pw_clean(uint32_t u) {                // two values, each as pw_load takes it
+  T v[2];
+  *reinterpret_cast<uint32_t*>(v) = u;
+  v[0] = T(pw_load(v[0]));
+  v[1] = T(pw_load(v[1]));
+  return *reinterpret_cast<uint32_t*>(v);
 }
 
 template <typename T, int D, bool E4M3>
 __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, PwArgs a) {
   constexpr int PER = D;                        // threads per (head, keys or values): one 16-byte piece each
   constexpr int HEADS = PW_THREADS / (2 * PER); // heads per turn
-  __shared__ float red[2][PW_THREADS / 32];
+  __shared__ uint32_t red[2][PW_THREADS / 32];
   const int tid = threadIdx.x, lane = tid & 31;
   pg_wait();
   const int slot = blockIdx.x;
@@ -102,7 +133,11 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
   const int keep = begin - pos0;                         // tokens of the block older than the call (<= 0: none)
   const int live = min(kPageBlock, e.len - pos0);
   const int lj = blockIdx.z, layer = a.layer0 + lj;
-  const int piece = tid % PER, which = (tid / PER) & 1, c = piece >> 5, g = (piece >> 2) & 7, t = piece & 3;
+  // Which piece is whose: of the keys in stored order (a thread's 16 values are 32 bytes of one row), of the values such
+  // that neighbouring threads have neighbouring dimensions (four rows' 8 bytes each: whole sectors per warp)
+  const int which = (tid / PER) & 1, own = tid % PER;
+  const int c = which ? own % (D / 32) : own >> 5, t = which ? own / (D / 32) % 4 : own & 3, g = which ? own / (D / 8) : (own >> 2) & 7;
+  const int piece = 32 * c + 4 * g + t;
   const int token = 4 * (g >> 1) + 2 * (c / (D / 64)) + (g & 1);       // of a piece of keys
 
   // a head's 16 new values of this thread, as they come
@@ -116,7 +151,7 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
     const T* s = src + (int64_t)h * D;
     if (which == 0) {
       if (token >= keep && token < live) {
-        const uint4 x = __ldcs(reinterpret_cast<const uint4*>(s)), y = __ldcs(reinterpret_cast<const uint4*>(s) + 1);
+        const uint4 x = __ldg(reinterpret_cast<const uint4*>(s)), y = __ldg(reinterpret_cast<const uint4*>(s) + 1);
         raw[0] = make_uint2(x.x, x.y);
         raw[1] = make_uint2(x.z, x.w);
         raw[2] = make_uint2(y.x, y.y);
@@ -159,38 +194,62 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
       was = *reinterpret_cast<const uint4*>(tile);
       old = *mag;
     }
-    float x[16], m = 0.f;
-    const T* y = reinterpret_cast<const T*>(raw);
+    // the largest magnitude, as bits (not negative: their order is that of the bits); what is not finite is rare
+    uint32_t* word = reinterpret_cast<uint32_t*>(raw);
+    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      // values come token by token, four dimensions each; a stored value word is one dimension, four tokens
-      const float f = pw_load(y[which ? (i & 3) * 4 + (i >> 2) : i]);
-      x[i] = f;
-      m = fmaxf(m, fabsf(f));
+    for (int i = 0; i < 8; ++i) most = __vmaxu2(most, word[i] & 0x7fff7fffu);
+    most = max(most >> 16, most & 0xffffu);
+    if (most > pw_most_bits<T>()) {
+      most = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        word[i] = pw_clean<T>(word[i]);
+        most = __vmaxu2(most, word[i] & 0x7fff7fffu);
+      }
+      most = max(most >> 16, most & 0xffffu);
     }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if (lane == 0) red[turn][tid >> 5] = m;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) red[turn][tid >> 5] = most;
     __syncthreads();                                     // the other half of red is free: it was read a turn ago
-    m = old;
+    most = 0;
 #pragma unroll
-    for (int w = 0; w < PER / 32; ++w) m = fmaxf(m, red[turn][tid / PER * (PER / 32) + w]);
+    for (int w = 0; w < PER / 32; ++w) most = max(most, red[turn][tid / PER * (PER / 32) + w]);
+    float m, unused;
+    pw_pair<T>(most, m, unused);
+    m = fmaxf(m, old);
     if (m < 0x1p-100f) m = 0.f;                          // its codes come out as 0 too
     if (in) {
-      const float inv = __frcp_rn(m > 0.f ? m : 1.f);
+      const float unit = m > 0.f ? m : 1.f, factor = __fdiv_rn(pg_top<E4M3>(), unit);
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pw_pair<T>(word[i], x[2 * i], x[2 * i + 1]);
       uint32_t out[4];
+      if (which == 0) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] *= pg_top<E4M3>();
-      if (keep > 0) {
-        const uint32_t* wasw = reinterpret_cast<const uint32_t*>(&was);
+        for (int i = 0; i < 4; ++i) out[i] = pw_codes<E4M3>(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3], factor);
+      } else {                                           // token by token they came, a word is one dimension, four tokens
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if ((which ? 4 * t + (i & 3) : token) < keep) x[i] = pw_value<E4M3>((wasw[i / 4] >> (8 * (i & 3))) & 0xffu) * old;
+        for (int i = 0; i < 4; ++i) out[i] = pw_codes<E4M3>(x[i], x[4 + i], x[8 + i], x[12 + i], factor);
       }
+      if (keep > 0) {
+        // of a word's four codes, those of older tokens: of the keys all or none, of the values the first few
+        const int older = which ? min(max(keep - 4 * t, 0), 4) : token < keep ? 4 : 0;
+        const uint32_t mask = older == 4 ? 0xffffffffu : (1u << (8 * older)) - 1;
+        const float again = __fdiv_rn(old, unit);
+        const uint32_t ww[4] = {was.x, was.y, was.z, was.w};
+        if (older)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) out[i] = pw_codes<E4M3>(x + 4 * i, inv);
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w = ww[i] & mask;
+            if (m != old)
+              w = pw_codes<E4M3>(pw_value<E4M3>(w & 0xffu), pw_value<E4M3>(w >> 8 & 0xffu), pw_value<E4M3>(w >> 16 & 0xffu),
+                                 pw_value<E4M3>(w >> 24), again);
+            out[i] = (out[i] & ~mask) | (w & mask);
+          }
+      }
       *reinterpret_cast<uint4*>(tile) = make_uint4(out[0], out[1], out[2], out[3]);
-      if (piece == 0) *mag = m;
+      if (own == 0) *mag = m;
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -254,14 +313,13 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p,
     for (int k = 0; k < PL; ++k) {
       x[k] = pw_load(raw[which][k]);
       m = fmaxf(m, fabsf(x[k]));
-      x[k] *= pg_top<E4M3>();
     }
     // magnitudes are not negative: their order is that of their bits
     m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
     m = fmaxf(m, old[which]);
     if (m < 0x1p-100f) m = 0.f;
-    const float inv = __frcp_rn(m > 0.f ? m : 1.f);
-    const uint32_t mine = pw_codes<E4M3>(x, inv);
+    const float unit = m > 0.f ? m : 1.f, factor = __fdiv_rn(old[which], unit);
+    const uint32_t mine = pw_codes<E4M3>(x[0], x[1], x[2], x[3], __fdiv_rn(pg_top<E4M3>(), unit));
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) {
@@ -276,8 +334,8 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p,
         for (int q = 0; q < 4; ++q) {
           float y[4];
 #pragma unroll
-          for (int b = 0; b < 4; ++b) y[b] = b < older ? pw_value<E4M3>((w[q] >> (8 * b)) & 0xffu) * old[which] : 0.f;
-          again[q] = pw_codes<E4M3>(y, inv);
+          for (int b = 0; b < 4; ++b) y[b] = b < older ? pw_value<E4M3>((w[q] >> (8 * b)) & 0xffu) : 0.f;
+          again[q] = pw_codes<E4M3>(y[0], y[1], y[2], y[3], factor);
         }
         out = make_uint4(again[0], again[1], again[2], again[3]);
       }
