@@ -33,11 +33,11 @@ constexpr int PS_WARPS = 6, PS_THREADS = PS_WARPS * 32;
 // CTAs per SM: two (168 registers a thread, 96 KB of tiles per CTA) unless the rows' sums need more registers
 __host__ __device__ constexpr int ps_ctas(int NT, int D) { return NT * D <= 128 ? 2 : 1; }
 constexpr int PS_RING = 4;                     // tiles of a warp: two being worked on, two on their way
-constexpr int PS_MIN_BLOCKS = 4;               // blocks a warp takes at least: below that, merging costs more
-// With no more items than CTAs, none longer than this many blocks per warp, an item is one CTA's: no merging over CTAs
-constexpr int PS_ITEM_BLOCKS = 12;
-constexpr int PS_SLOT_FLOATS = 2112;           // rows x (D + 2) floats: 16 x 130 or 32 x 66
-constexpr int PS_SLOTS = 2 * PS_WARPS + 2;     // partial results of a CTA: two per warp, two of the CTA's own
+constexpr int PS_MIN_BLOCKS = 4;               // blocks a warp takes at least
+
+__device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {       // not negative; 32-bit where the numbers allow
+  return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -83,9 +83,9 @@ struct PsShared {
   int64_t sum_u[PS_WARPS];
   int sum_i[PS_WARPS];
   PgEntry entry[PS_THREADS];      // with no more entries than threads: the entries
-  Item part[PS_WARPS][2];         // the item that a warp's slot 0 / 1 holds a part of
-  int has[PS_WARPS][2];
-  int last[2];                    // whether this CTA merges its slot 0 / 1 item over all CTAs
+  Item part[PS_WARPS][2];         // the item that a warp holds a part of: begun before its stretch (0), or going on behind it
+  float* where[PS_WARPS][2];      // the part: rows x D values, then (maximum, sum) of the rows; null = none
+  int last[2];                    // whether this CTA merges the part-0 / part-1 item over all CTAs
 };
 
 // address of an item's row: rows are (token, query head of the group)
@@ -102,7 +102,6 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   constexpr int SLOT = R * (D + 2);
   // the rest of the probabilities matters next to an fp16 output (2^-12), not next to a bf16 one (2^-9)
   constexpr bool LO = std::is_same<T, __half>::value;
-  static_assert(SLOT <= PS_SLOT_FLOATS, "slot");
   extern __shared__ __align__(16) unsigned char ps_ring[];
   __shared__ PsShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -117,6 +116,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     tiles = (int)((nr + R - 1) / R);
     return tiles * a.nl * p.heads;
   };
+  int per_warp;
   int64_t pad = 0;
   {
     int64_t mu = 0;
@@ -151,8 +151,6 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       sh.sum_i[warp] = xi;
       sh.most[warp] = most;
     }
-    if (tid < 2 * PS_WARPS) sh.has[tid >> 1][tid & 1] = 0;
-    if (tid < 2) sh.last[tid] = 0;
     __syncthreads();
     for (int w = 0; w < PS_WARPS; ++w) {
       most = max(most, sh.most[w]);
@@ -168,23 +166,40 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       sh.items[0] = 0;
     }
     __syncthreads();
-    if (sh.items[PS_THREADS] <= (int)gridDim.x && most <= PS_WARPS * PS_ITEM_BLOCKS)
-      pad = (int64_t)PS_WARPS * max(PS_MIN_BLOCKS, pg_ceil(pg_ceil(most, PS_WARPS), 2) * 2);
+    // How the list is cut: every warp gets a stretch of the same length.  Where items are short they are padded to whole
+    // stretches of k warps each: then none is split, or only inside a CTA.  Times in blocks at full load, merging inside
+    // a CTA costs about 2 of them, over CTAs 8.
+    const int64_t workers = (int64_t)gridDim.x * PS_WARPS, items = sh.items[PS_THREADS], sum = sh.units[PS_THREADS];
+    per_warp = max(PS_MIN_BLOCKS, ((int)min((int64_t)1 << 24, div64(sum + workers - 1, workers)) + 1) & ~1);
+    int cost = per_warp + 8;
+#pragma unroll
+    for (int k = 1; k <= PS_WARPS; ++k) {
+      if (PS_WARPS % k) continue;
+      const int w = max(PS_MIN_BLOCKS, (pg_ceil(most, k) + 1) & ~1);
+      const int64_t rounds = div64(items * k + workers - 1, workers);
+      if (rounds > (k == 1 ? 64 : 1) || most > (1 << 20)) continue;
+      const int c = (int)rounds * w + (k > 1 ? 2 : 0);
+      if (c < cost) {
+        cost = c;
+        per_warp = (int)rounds * w;
+        pad = (int64_t)k * w;
+      }
+    }
   }
-  // blocks before the entries of thread j, in the list that is cut up: every item padded to a CTA's share, or none
+  // blocks before the entries of thread j, in the list that is cut up
   auto before = [&](int j) -> int64_t { return pad ? (int64_t)sh.items[j] * pad : sh.units[j]; };
-  const int64_t total = before(PS_THREADS);
-  const int64_t workers = (int64_t)gridDim.x * PS_WARPS;
-  const int64_t per_warp = pad ? pad / PS_WARPS : max((total + workers - 1) / workers, (int64_t)PS_MIN_BLOCKS);
-  const int64_t cta_begin = (int64_t)blockIdx.x * PS_WARPS * per_warp;
+  const int64_t total = before(PS_THREADS), per_cta = (int64_t)PS_WARPS * per_warp;
+  const int64_t cta_begin = (int64_t)blockIdx.x * per_cta, cta_end = min(total, cta_begin + per_cta);
   if (cta_begin >= total) return;
-  const int64_t cta_end = min(total, cta_begin + PS_WARPS * per_warp);
-  int64_t u = min(total, cta_begin + warp * per_warp);
+  int64_t u = min(total, cta_begin + (int64_t)warp * per_warp);
   const int64_t ue = min(total, u + per_warp);
+  if (lane < 2) sh.where[warp][lane] = nullptr;
+  if (tid < 2) sh.last[tid] = 0;
 
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ps_ring) + warp * (PS_RING * 2 * TILE) + lane * 16;
   const unsigned char* ring_g = ps_ring + warp * (PS_RING * 2 * TILE) + lane * 16;
-  float* slots = p.partial + (size_t)(blockIdx.x * PS_SLOTS) * PS_SLOT_FLOATS;
+  float* slots = p.partial + (size_t)(blockIdx.x * PS_WARPS) * SLOT;            // a warp's part 0
+  float* cta_slots = p.partial + (size_t)gridDim.x * PS_WARPS * SLOT;           // a CTA's two parts
 
   // ---- where this warp starts ----
   int ei = 0, index = 0, bo = 0;            // entry, item of the entry, block of the item
@@ -216,7 +231,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       ++ei;
     }
     if (ei >= a.n) u = ue;                  // cannot be, unless the lengths changed under the call
-    index = (int)((u - entry_begin) / blocks);
+    index = (int)div64(u - entry_begin, blocks);
     bo = (int)((u - entry_begin) - (int64_t)index * blocks);
   }
 
@@ -500,7 +515,11 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     // ---- the item's rows, or a part of them ----
     const bool complete = first == 0 && end == blocks;
     const int which = first == 0 ? 1 : 0;
-    float* slot_out = slots + (size_t)(warp * 2 + which) * PS_SLOT_FLOATS;
+    // the ring is free again with the last item of a warp's stretch
+    const bool done = u + (end - first) == ue;
+    float* slot_out = SLOT * 4 <= PS_RING * 2 * TILE && done ? reinterpret_cast<float*>(ps_ring + warp * (PS_RING * 2 * TILE))
+                                                             : slots + (size_t)warp * SLOT;
+    __syncwarp();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -537,7 +556,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       }
     if (!complete && lane == 0) {
       sh.part[warp][which] = it;
-      sh.has[warp][which] = 1;
+      sh.where[warp][which] = slot_out;
     }
 
     // ---- next ----
@@ -552,57 +571,81 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   }
   __syncthreads();
 
-  // ---- merge: a warp takes a row, lanes own four dimensions each (with D 64 the upper half only helps with the maximum) ----
-  auto merge_row = [&](auto slot_of, int parts, int r, float4& f, float& mm, float& ll) {
-    const int c4 = (lane % (D / 4)) * 4;
-    mm = -INFINITY;
-    for (int i = lane; i < parts; i += 32) mm = fmaxf(mm, __ldcg(slot_of(i) + R * D + 2 * r));
+  // ---- merge: a warp takes a row, lanes own four dimensions each (with D 64 the upper half repeats the lower) ----
+  // `far`: the parts come from other CTAs of this launch, so they are read past L1 (lines may be there from before)
+  auto merge_row = [&](auto far, auto part_of, int parts, int r, float4& f, float& mm, float& ll) {
+    auto load2 = [&](const float* s) {
+      const float2* v = reinterpret_cast<const float2*>(s + R * D + 2 * r);
+      return decltype(far)::value ? __ldcg(v) : *v;
+    };
+    auto load4 = [&](const float* s) {
+      const float4* v = reinterpret_cast<const float4*>(s + r * D + (lane % (D / 4)) * 4);
+      return decltype(far)::value ? __ldcg(v) : *v;
+    };
+
+    float pm = -INFINITY, pl = 0.f;                     // of part `lane`, the first 32
+    if (lane < parts) {
+      const float2 ml = load2(part_of(lane));
+      pm = ml.x;
+      pl = ml.y;
+    }
+    mm = pm;
+    for (int i = lane + 32; i < parts; i += 32) mm = fmaxf(mm, load2(part_of(i)).x);
 #pragma unroll
     for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
     f = make_float4(0.f, 0.f, 0.f, 0.f);
     ll = 0.f;
+    for (int base = 0; base < parts; base += 32) {
+      if (base) {
+        pm = -INFINITY;
+        pl = 0.f;
+        if (base + lane < parts) {
+          const float2 ml = load2(part_of(base + lane));
+          pm = ml.x;
+          pl = ml.y;
+        }
+      }
+      const float w = pl == 0.f ? 0.f : pl * pa_ex2(pm - mm);
+      const int n = min(32, parts - base);
 #pragma unroll 8
-    for (int i = 0; i < parts; ++i) {
-      const float* s = slot_of(i);
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(s + R * D + 2 * r));
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(s + r * D + c4));
-      const float w = ml.y == 0.f ? 0.f : ml.y * pa_ex2(ml.x - mm);
-      ll += w;
-      f.x = fmaf(w, v.x, f.x);
-      f.y = fmaf(w, v.y, f.y);
-      f.z = fmaf(w, v.z, f.z);
-      f.w = fmaf(w, v.w, f.w);
+      for (int i = 0; i < n; ++i) {
+        const float4 v = load4(part_of(base + i));
+        const float wi = __shfl_sync(0xffffffffu, w, i);
+        ll += wi;
+        f.x = fmaf(wi, v.x, f.x);
+        f.y = fmaf(wi, v.y, f.y);
+        f.z = fmaf(wi, v.z, f.z);
+        f.w = fmaf(wi, v.w, f.w);
+      }
     }
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
     f = make_float4(f.x * inv, f.y * inv, f.z * inv, f.w * inv);
   };
-  const int64_t per_cta = PS_WARPS * per_warp;
-  // Inside the CTA: the items that begin in one of its warps (slot 1) or before it (slot 0 of warp 0), all rows dealt out
-  // to the warps in turn
+  // Inside the CTA: the items that go on behind one of its warps (part 1), or begin before the first (part 0 of warp 0),
+  // all rows dealt out to the warps in turn
   bool outside = false;
   int turn = 0;
   for (int k = -1; k < PS_WARPS; ++k) {
     const int w0 = max(k, 0), wh = k < 0 ? 0 : 1;
-    if (!sh.has[w0][wh]) continue;
+    if (!sh.where[w0][wh]) continue;
     const Item it = sh.part[w0][wh];
     const int64_t end = it.begin + it.blocks;
-    const int wl = (int)((min(end, cta_end) - 1 - cta_begin) / per_warp);
+    const int wl = (int)div64(min(end, cta_end) - 1 - cta_begin, per_warp);
     const bool inside = it.begin >= cta_begin && end <= cta_end;
     outside |= !inside;
-    float* cta_slot = slots + (size_t)(2 * PS_WARPS + wh) * PS_SLOT_FLOATS;
-    const float* base = slots;
-    auto slot_of = [=](int i) { return base + (size_t)((w0 + i) * 2 + (i == 0 ? wh : 0)) * PS_SLOT_FLOATS; };
+    float* mine = cta_slots + (size_t)(2 * blockIdx.x + wh) * SLOT;
+    auto part_of = [&](int i) { return (const float*)sh.where[w0 + i][i == 0 ? wh : 0]; };
     for (int r = 0; r < it.valid; ++r, ++turn) {
       if (turn % PS_WARPS != warp) continue;
       float4 f;
       float mm, ll;
-      merge_row(slot_of, wl - w0 + 1, r, f, mm, ll);
+      merge_row(std::false_type{}, part_of, wl - w0 + 1, r, f, mm, ll);
       if (lane < D / 4) {
         if (inside) {
           store4(reinterpret_cast<T*>(a.out) + row_offset(p, a, D, it, r) + lane * 4, f);
         } else {
-          *reinterpret_cast<float4*>(cta_slot + r * D + lane * 4) = f;
-          if (lane == 0) *reinterpret_cast<float2*>(cta_slot + R * D + 2 * r) = make_float2(mm, ll);
+          *reinterpret_cast<float4*>(mine + r * D + lane * 4) = f;
+          if (lane == 0) *reinterpret_cast<float2*>(mine + R * D + 2 * r) = make_float2(mm, ll);
         }
       }
     }
@@ -615,12 +658,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     // the item that began before this CTA, and the one that goes on behind it
     int w0 = tid == 0 ? 0 : PS_WARPS - 1;
     if (tid == 1)
-      while (w0 >= 0 && !sh.has[w0][1]) --w0;
-    if (w0 >= 0 && sh.has[w0][tid]) {
+      while (w0 >= 0 && !sh.where[w0][1]) --w0;
+    if (w0 >= 0 && sh.where[w0][tid]) {
       const Item it = sh.part[w0][tid];
       const int64_t end = it.begin + it.blocks;
       if (it.begin < cta_begin || end > cta_end) {
-        const int c0 = (int)(it.begin / per_cta), c1 = (int)((end - 1) / per_cta);
+        const int c0 = (int)div64(it.begin, per_cta), c1 = (int)div64(end - 1, per_cta);
         if (atomicAdd(p.counters + c0, 1) == c1 - c0) {
           p.counters[c0] = 0;
           __threadfence();
@@ -633,15 +676,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   for (int which = 0; which < 2; ++which) {
     if (!sh.last[which]) continue;
     const Item it = sh.part[sh.last[which] - 1][which];
-    const int c0 = (int)(it.begin / per_cta), c1 = (int)((it.begin + it.blocks - 1) / per_cta);
-    const float* base = p.partial;
-    auto slot_of = [=](int i) {
-      return base + ((size_t)(c0 + i) * PS_SLOTS + 2 * PS_WARPS + (i == 0 ? 1 : 0)) * PS_SLOT_FLOATS;
-    };
+    const int c0 = (int)div64(it.begin, per_cta), c1 = (int)div64(it.begin + it.blocks - 1, per_cta);
+    auto part_of = [&](int i) { return cta_slots + (size_t)(2 * (c0 + i) + (i == 0 ? 1 : 0)) * SLOT; };
     for (int r = warp; r < it.valid; r += PS_WARPS) {
       float4 f;
       float mm, ll;
-      merge_row(slot_of, c1 - c0 + 1, r, f, mm, ll);
+      merge_row(std::true_type{}, part_of, c1 - c0 + 1, r, f, mm, ll);
       if (lane < D / 4) store4(reinterpret_cast<T*>(a.out) + row_offset(p, a, D, it, r) + lane * 4, f);
     }
   }
@@ -659,9 +699,10 @@ static int launch_step(const PgParams& p, const PaArgs& a, cudaStream_t s) {
       return fail_cuda("shared memory opt-in of pages_step_kernel");
     if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  constexpr size_t block_bytes = (size_t)PS_SLOTS * PS_SLOT_FLOATS * 4;
+  // a part of each warp, and two of the CTA; a counter per CTA
+  constexpr size_t cta_bytes = (size_t)(PS_WARPS + 2) * 8 * NT * (D + 2) * 4;
   int grid = ps_ctas(NT, D) * pg_sms();
-  const int most = (int)(LESS_PAGES_PARTIAL_BYTES / block_bytes);
+  const int most = (int)(LESS_PAGES_PARTIAL_BYTES / cta_bytes);
   if (grid > most) grid = most;
   if (grid > kPgCounters) grid = kPgCounters;
   return pg_launch("pages_step_kernel", pages_step_kernel<T, D, NT, E4M3>, dim3(grid), PS_THREADS, smem, s, p, a);
