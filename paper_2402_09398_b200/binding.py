@@ -519,77 +519,83 @@ class PagedCache:
         desc.workspace, desc.workspace_bytes = self.workspace.data_ptr(), nbytes
         self.desc = desc
         self.scale = head_dim ** -0.5
+        self.layers, self.heads, self.group, self.head_dim = layers, heads, group, head_dim
         self._index = self.device.index
+        self._lib = lib()
         if empty:
             self.reset()
 
-    # -- helpers ----------------------------------------------------------- #
+    # -- helpers (a call takes a few microseconds on the host: the checks below are the cheap forms) ---------- #
     def _call(self, fn, where, *args, stream=None):
-        if torch.cuda.current_device() == self._index:
-            s = torch.cuda.current_stream(self._index) if stream is None else stream
-            rc = fn(self.desc, *args, s.cuda_stream)
+        if torch._C._cuda_getDevice() == self._index:
+            rc = fn(self.desc, *args, torch._C._cuda_getCurrentRawStream(self._index) if stream is None
+                    else stream.cuda_stream)
         else:
             with torch.cuda.device(self._index):
-                s = torch.cuda.current_stream(self._index) if stream is None else stream
-                rc = fn(self.desc, *args, s.cuda_stream)
+                rc = fn(self.desc, *args, torch._C._cuda_getCurrentRawStream(self._index) if stream is None
+                        else stream.cuda_stream)
         if rc != LESS_OK:
             raise LessError(rc, where)
 
     def _list(self, t: torch.Tensor, name: str, n: Optional[int] = None) -> int:
-        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 or not t.is_contiguous():
+        if t.dtype is not torch.int32 or t.get_device() != self._index or t.dim() != 1 or not t.is_contiguous():
             raise ValueError(f"{name}: a contiguous 1-d int32 tensor on {self.device} is wanted")
         if n is not None and t.shape[0] != n:
             raise ValueError(f"{name}: {n} values are wanted, got {t.shape[0]}")
         return t.data_ptr()
 
     def _rows(self, t: torch.Tensor, name: str, heads: int):
-        d = self.desc
-        if t.dtype != self.dtype or t.device != self.device or t.dim() != 4:
+        if t.dtype is not self.dtype or t.get_device() != self._index or t.dim() != 4:
             raise ValueError(f"{name}: a [rows, layers, heads, D] tensor of {self.dtype} on {self.device} is wanted")
         rows, layers, h, dim = t.shape
-        if h != heads or dim != d.head_dim or layers > d.layers:
-            raise ValueError(f"{name}: [rows, layers, {heads}, {d.head_dim}] is wanted, got {tuple(t.shape)}")
-        if rows and (t.stride(3) != 1 or (h > 1 and t.stride(2) != dim) or (layers > 1 and t.stride(1) != h * dim)):
+        if h != heads or dim != self.head_dim or layers > self.layers:
+            raise ValueError(f"{name}: [rows, layers, {heads}, {self.head_dim}] is wanted, got {tuple(t.shape)}")
+        if rows <= 1 or t.is_contiguous():
+            stride = layers * h * dim
+            if rows == 0 or t.is_contiguous():
+                return rows, layers, stride
+        else:
+            stride = t.stride(0)
+        if t.stride(3) != 1 or (h > 1 and t.stride(2) != dim) or (layers > 1 and t.stride(1) != h * dim):
             raise ValueError(f"{name}: everything but the rows has to be contiguous")
-        stride = t.stride(0) if rows > 1 else layers * h * dim
         return rows, layers, stride
 
     # -- the maps ---------------------------------------------------------- #
     def reset(self, stream=None):
         """Empties the cache."""
-        self._call(lib().less_pages_reset, "less_pages_reset", stream=stream)
+        self._call(self._lib.less_pages_reset, "less_pages_reset", stream=stream)
 
     def resize(self, seqs, lens, stream=None):
         """Sequences get new lengths: pages are taken or released (0 frees a sequence)."""
         n = seqs.shape[0]
-        self._call(lib().less_pages_resize, "less_pages_resize", n, self._list(seqs, "seqs"),
+        self._call(self._lib.less_pages_resize, "less_pages_resize", n, self._list(seqs, "seqs"),
                    self._list(lens, "lens", n), stream=stream)
 
     def fork(self, src, dst, stream=None):
         """The empty sequences dst become copies of src (whole pages shared)."""
         n = src.shape[0]
-        self._call(lib().less_pages_fork, "less_pages_fork", n, self._list(src, "src"), self._list(dst, "dst", n),
+        self._call(self._lib.less_pages_fork, "less_pages_fork", n, self._list(src, "src"), self._list(dst, "dst", n),
                    stream=stream)
 
     def trim(self, seqs, sinks, window, stream=None):
         """Releases the pages between the first `sinks` tokens and the last `window`."""
-        self._call(lib().less_pages_trim, "less_pages_trim", seqs.shape[0], self._list(seqs, "seqs"), sinks, window,
+        self._call(self._lib.less_pages_trim, "less_pages_trim", seqs.shape[0], self._list(seqs, "seqs"), sinks, window,
                    stream=stream)
 
     def compact(self, stream=None):
         """Moves the pages in use to the front of the pool."""
-        self._call(lib().less_pages_compact, "less_pages_compact", stream=stream)
+        self._call(self._lib.less_pages_compact, "less_pages_compact", stream=stream)
 
     # -- contents ---------------------------------------------------------- #
     def write(self, k, v, seqs, starts=None, layer_begin=0, stream=None):
         """k, v [rows, layers, heads, D]: the last tokens of the listed sequences (rows starts[i] .. starts[i + 1]
         belong to seqs[i]; without starts one row each)."""
         n = seqs.shape[0]
-        rows, layers, ks = self._rows(k, "k", self.desc.heads)
-        vrows, vlayers, vs = self._rows(v, "v", self.desc.heads)
+        rows, layers, ks = self._rows(k, "k", self.heads)
+        vrows, vlayers, vs = self._rows(v, "v", self.heads)
         if (vrows, vlayers) != (rows, layers):
             raise ValueError("k and v have the same shape")
-        self._call(lib().less_pages_write, "less_pages_write", layer_begin, layers, n, self._list(seqs, "seqs"),
+        self._call(self._lib.less_pages_write, "less_pages_write", layer_begin, layers, n, self._list(seqs, "seqs"),
                    None if starts is None else self._list(starts, "starts", n + 1), rows, k.data_ptr(), ks,
                    v.data_ptr(), vs, stream=stream)
 
@@ -597,14 +603,13 @@ class PagedCache:
                   stream=None):
         """q [rows, layers, heads * group, D]: attention of the last tokens of the listed sequences over the cache.
         max_new: the most new tokens of a sequence, as far as the host knows (default: all rows)."""
-        d = self.desc
         n = seqs.shape[0]
-        rows, layers, qs = self._rows(q, "q", d.heads * d.group)
+        rows, layers, qs = self._rows(q, "q", self.heads * self.group)
         if out is None:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype != self.dtype or out.device != self.device or not out.is_contiguous():
             raise ValueError("out: a contiguous tensor of q's shape and type is wanted")
-        self._call(lib().less_pages_attention, "less_pages_attention", layer_begin, layers, n,
+        self._call(self._lib.less_pages_attention, "less_pages_attention", layer_begin, layers, n,
                    self._list(seqs, "seqs"), None if starts is None else self._list(starts, "starts", n + 1), rows,
                    max(1, rows if max_new is None else max_new), q.data_ptr(), qs, window, sinks,
                    self.scale if scale is None else scale, out.data_ptr(), stream=stream)
