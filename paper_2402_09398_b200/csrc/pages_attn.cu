@@ -61,15 +61,6 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
   return y;
 }
 
-__device__ __forceinline__ void store4(__half* dst, float4 f) {
-  __half2 h[2] = {__floats2half2_rn(f.x, f.y), __floats2half2_rn(f.z, f.w)};
-  *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(h);
-}
-__device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 f) {
-  __nv_bfloat162 h[2] = {__floats2bfloat162_rn(f.x, f.y), __floats2bfloat162_rn(f.z, f.w)};
-  *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(h);
-}
-
 // One item: rows [row0, row0 + valid) of a (sequence, layer, head)'s tokens x group rows.
 struct Item {
   int64_t begin;                // first block in the list of all blocks
@@ -714,7 +705,6 @@ static int launch_step(const PgParams& p, const PaArgs& a, cudaStream_t s) {
 template <typename T, bool E4M3>
 static int launch_step_dim(const PgParams& p, const PaArgs& a, int dim, int rows, cudaStream_t s) {
   if (dim == 128) return rows > 8 ? launch_step<T, 128, 2, E4M3>(p, a, s) : launch_step<T, 128, 1, E4M3>(p, a, s);
-  if (rows > 16) return launch_step<T, 64, 4, E4M3>(p, a, s);
   return rows > 8 ? launch_step<T, 64, 2, E4M3>(p, a, s) : launch_step<T, 64, 1, E4M3>(p, a, s);
 }
 

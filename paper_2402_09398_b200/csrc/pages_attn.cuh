@@ -63,6 +63,15 @@ __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* dst, const 
   for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
   *reinterpret_cast<uint4*>(dst) = u;
 }
+__device__ __forceinline__ void store4(__half* dst, float4 f) {
+  __half2 h[2] = {__floats2half2_rn(f.x, f.y), __floats2half2_rn(f.z, f.w)};
+  *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(h);
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 f) {
+  __nv_bfloat162 h[2] = {__floats2bfloat162_rn(f.x, f.y), __floats2bfloat162_rn(f.z, f.w)};
+  *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(h);
+}
+
 // rows of an entry (tokens x query heads of a group) up to which it is the step kernel's
 constexpr int kStepRows = 32;
 

@@ -109,6 +109,13 @@ __device__ __forceinline__ int64_t pc_slot(const PgParams& p, const PaArgs& a, i
   return (int64_t)row * p.group / (2 * PC_ROWS) + i;
 }
 
+constexpr int PC_SPLIT_TILES = 4;                         // key tiles of a split CTA at least
+
+// where the CTA of (slot, head, split) leaves its part: rows x D values, then (reference, sum) of the rows
+__device__ __forceinline__ size_t pc_part(int64_t slot, int heads, int head, int splits, int split, int D) {
+  return ((size_t)(slot * heads + head) * splits + split) * ((size_t)2 * PC_ROWS * (D + 2));
+}
+
 // visibility of the 32 columns of a stored-tile pair, bit 16 e + r = token r of tile e
 __device__ __forceinline__ uint32_t pc_mask16(int j0, int pos, int window, int sinks) {
   const int hi = min(max(pos + 1 - j0, 0), 16);
@@ -121,7 +128,7 @@ __device__ __forceinline__ uint32_t pc_mask16(int j0, int pos, int window, int s
 }
 
 template <typename T, int D, bool E4M3>
-__global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, PaArgs a) {
+__global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, PaArgs a, int splits) {
   constexpr int QT = PC_ROWS * D * 2;                     // bytes of a Q tile
   constexpr int KT = PC_KEYS * D * 2;                     // of a K or V tile
   extern __shared__ __align__(1024) unsigned char pc_smem[];
@@ -150,11 +157,19 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   const int tok0 = (int)(row0 / p.group), tok1 = (int)((row0 + valid - 1) / p.group);
   const Blocks vb = visible_blocks(a, base + tok1 + 1, tok1 - tok0 + 1);
   const int units = base + tok1 < 0 ? 0 : vb.count();
-  const int nk = pg_ceil(units, PC_TILES);
+  // with few items the key tiles are dealt out to `splits` CTAs (blockIdx.z), whose results are joined by a second kernel
+  const int nk_all = pg_ceil(units, PC_TILES), share = max(pg_ceil(nk_all, splits), splits > 1 ? PC_SPLIT_TILES : 1);
+  const int kt0 = min(nk_all, (int)blockIdx.z * share), nk = min(share, nk_all - kt0);
+  float* part = p.partial + pc_part(slot, gridDim.x, blockIdx.x, splits, blockIdx.z, D);
   const int64_t head_row = ((int64_t)lj * p.heads + h) * p.group * D;
   T* out = reinterpret_cast<T*>(a.out);
 
   if (nk == 0) {                                          // nothing to see
+    if (splits > 1) {
+      for (int i = tid; i < valid; i += PC_THREADS)
+        *reinterpret_cast<float2*>(part + (size_t)2 * PC_ROWS * D + 2 * i) = make_float2(-INFINITY, 0.f);
+      return;
+    }
     for (int i = tid; i < valid * (D / 8); i += PC_THREADS) {
       const int64_t rr = row0 + i / (D / 8);
       const int tok = (int)(rr / p.group), hd = (int)(rr - (int64_t)tok * p.group);
@@ -327,6 +342,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       if (!*abortp) {
         const float inv = l == 0.f ? 0.f : 1.f / l, unit = 1.f / pg_top<E4M3>();
         T* dst = out + (int64_t)(e.row0 + tok) * a.nl * p.heads * p.group * D + head_row + hd * D;
+        if (splits > 1 && r < valid) *reinterpret_cast<float2*>(part + (size_t)2 * PC_ROWS * D + 2 * r) = make_float2(M, l);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
@@ -336,8 +352,14 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
 #pragma unroll
           for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(o[i]) * inv * unit;
           if (r < valid) {
+            if (splits > 1) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) store8<T>(dst + 32 * c + i, f + i);
+              for (int i = 0; i < 32; i += 4)
+                *reinterpret_cast<float4*>(part + (size_t)r * D + 32 * c + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; i += 8) store8<T>(dst + 32 * c + i, f + i);
+            }
           }
         }
       }
@@ -357,7 +379,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     int page_l = -1, j_l = 0;
     float ak_l = 0.f, av_l = 0.f, vlast = 1.f;
     auto lookup = [&](int batch) {
-      const int u = (batch + (lane & ~1)) * PC_TILES + 2 * dw + (lane & 1);
+      const int u = (kt0 + batch + (lane & ~1)) * PC_TILES + 2 * dw + (lane & 1);
       page_l = -1;
       j_l = 0;
       if (u < units) {
@@ -543,6 +565,51 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   if (warp == 12) tmem_dealloc(tmem, 512);
 }
 
+// Joins the parts of split items: a warp per row of the output and head
+template <typename T, int D>
+__global__ void __launch_bounds__(256) pages_chunk_join_kernel(PgParams p, PaArgs a, int splits) {
+  pg_wait();
+  const int lane = threadIdx.x & 31, heads = a.nl * p.heads;
+  const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), per_row = (int64_t)heads * p.group;
+  const int row = (int)(w / per_row);
+  if (row >= a.rows) return;
+  const int head = (int)(w - row * per_row) / p.group, g = (int)(w - row * per_row) - head * p.group;
+  int lo = 0, hi = a.n - 1;                               // the last entry that starts at or before this row
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if ((a.starts ? __ldg(a.starts + mid) : mid) <= row) lo = mid; else hi = mid - 1;
+  }
+  const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, lo);
+  if ((int64_t)e.count * p.group <= a.max_rows || row < e.row0 || row >= e.row0 + e.count) return;
+  const int64_t rr = (int64_t)(row - e.row0) * p.group + g, slot = pc_slot(p, a, lo) + rr / (2 * PC_ROWS);
+  const int r = (int)(rr % (2 * PC_ROWS)), c4 = (lane % (D / 4)) * 4;
+  const float* part = p.partial + pc_part(slot, heads, head, splits, 0, D);
+  constexpr size_t STEP = (size_t)2 * PC_ROWS * (D + 2);
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < splits) ml = __ldcg(reinterpret_cast<const float2*>(part + lane * STEP + (size_t)2 * PC_ROWS * D + 2 * r));
+  float m = ml.y == 0.f ? -INFINITY : ml.x;
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  const float weight = ml.y == 0.f ? 0.f : ml.y * pa_ex2(ml.x - m);
+  float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+  float sum = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float ws = __shfl_sync(0xffffffffu, weight, s);
+    if (ws == 0.f) continue;                              // its values were not written
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(part + s * STEP + (size_t)r * D + c4));
+    sum += ws;
+    f.x = fmaf(ws, v.x, f.x);
+    f.y = fmaf(ws, v.y, f.y);
+    f.z = fmaf(ws, v.z, f.z);
+    f.w = fmaf(ws, v.w, f.w);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (lane < D / 4)
+    store4(reinterpret_cast<T*>(a.out) + ((int64_t)row * per_row + (int64_t)head * p.group + g) * D + c4,
+           make_float4(f.x * inv, f.y * inv, f.z * inv, f.w * inv));
+}
+
 template <typename T, int D, bool E4M3>
 static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   constexpr size_t smem = (size_t)(2 * PC_ROWS + 2 * PC_STAGES * PC_KEYS) * D * 2 + sizeof(PcShared);
@@ -555,9 +622,23 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
       return fail_cuda("shared memory opt-in of pages_chunk_kernel");
     if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n;
+  const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n, heads = (int64_t)p.heads * a.nl;
   if (slots > 65535) return LESS_ERR_INVALID_CONFIG;
-  return pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3>, dim3(p.heads * a.nl, (unsigned)slots), PC_THREADS, smem, s, p, a);
+  // Items that are sure to exist; with fewer of them than multiprocessors their keys are split (measured: two sequences of
+  // 30 000 tokens, eight KV heads, 48 rows each: 508 us unsplit, 75 us in nine parts)
+  int64_t items = (int64_t)a.rows * p.group / (2 * PC_ROWS);
+  if (items < a.n) items = a.n;
+  int64_t splits = pg_sms() / (items * heads);
+  const int64_t room = (int64_t)(LESS_PAGES_PARTIAL_BYTES / ((size_t)2 * PC_ROWS * (D + 2) * 4)) / (slots * heads);
+  splits = splits > 32 ? 32 : splits;
+  splits = splits > room ? room : splits;
+  splits = splits < 1 ? 1 : splits;
+  const int rc = pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3>, dim3((unsigned)heads, (unsigned)slots, (unsigned)splits),
+                           PC_THREADS, smem, s, p, a, (int)splits);
+  if (rc != LESS_OK || splits == 1) return rc;
+  const int64_t warps = (int64_t)a.rows * heads * p.group;
+  return pg_launch("pages_chunk_join_kernel", pages_chunk_join_kernel<T, D>, dim3((unsigned)((warps + 7) / 8)), 256, 0, s, p, a,
+                   (int)splits);
 }
 
 int launch_pages_chunk(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s) {

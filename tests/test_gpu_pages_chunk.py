@@ -106,3 +106,15 @@ def test_a_bad_query_stays_in_its_row_of_a_tile():
     bad = c.attention(q, ints([0]), ints([0, 200]))
     keep = torch.arange(200, device=DEV) != 77
     assert torch.equal(bad[keep], good[keep]) and not torch.isfinite(bad[77]).all()
+
+
+@pytest.mark.parametrize("dim,heads,group,new,window", [(128, 1, 4, 12, 0), (64, 2, 71, 1, 0), (128, 1, 128, 1, 500), (64, 1, 1, 300, 0)])
+def test_keys_split_over_ctas(dim, heads, group, new, window):
+    """Few rows, many keys: the key tiles of an item go to several CTAs, whose parts are joined."""
+    lens = [3000, 1, 700]
+    c, m = make(heads=heads, dim=dim, group=group, pt=64, pages=70, seqs=3, seq_pages=48, dtype=torch.bfloat16)
+    fill(c, m, lens)
+    n = [min(new, k) for k in lens]
+    first = attend(c, m, [0, 1, 2], starts_of(n), max_new=new, window=window, sinks=3 if window else 0)
+    again = attend(c, m, [0, 1, 2], starts_of(n), max_new=new, window=window, sinks=3 if window else 0)
+    assert np.array_equal(first, again)
