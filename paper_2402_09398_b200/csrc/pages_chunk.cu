@@ -34,7 +34,7 @@ constexpr int PC_SOFT_WARPS = 8, PC_DEQ_WARPS = 4;
 constexpr int PC_THREADS = (PC_SOFT_WARPS + PC_DEQ_WARPS + 2) * 32;
 constexpr int PC_STAGES = 4, PC_META = 8;
 
-struct PcMeta {                                           // of the stored tiles of a key tile
+struct __align__(16) PcMeta {                                           // of the stored tiles of a key tile
   float k1[PC_TILES];                                     // a_k / top
   float lav[PC_TILES], iav[PC_TILES];                     // log2 a_v, 1 / a_v
   int j0[PC_TILES];                                       // position of the first token, 2^30 = no tile
@@ -262,13 +262,13 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         const int buf = kt & 1;
         const uint32_t scol = lane_addr + (2 * x + buf) * PC_KEYS;
         wait_or_give_up(&sh->s_full[x][buf], (kt >> 1) & 1, abortp, status, 122);
-        if (__any_sync(0xffffffffu, *abortp)) break;
+        __syncwarp();                                     // after a give-up all waits return at once: no way out needed
         tc_fence_after_sync();
         const PcMeta& meta = sh->meta[kt % PC_META];
-        uint32_t part = 0;
-#pragma unroll
-        for (int i = 0; i < PC_TILES; ++i) part |= meta.part[i];
-        const bool masked = part >> x & 1;
+        const uint4 part = *reinterpret_cast<const uint4*>(meta.part);
+        const float4 k1 = *reinterpret_cast<const float4*>(meta.k1), lav = *reinterpret_cast<const float4*>(meta.lav),
+                     iav = *reinterpret_cast<const float4*>(meta.iav);
+        const bool masked = (part.x | part.y | part.z | part.w) >> x & 1;
 
         uint32_t pk[PC_KEYS / 2];
         float most, add;
@@ -279,8 +279,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           for (int c = 0; c < PC_KEYS / 32; ++c) {        // a pair of stored tiles: 4 columns of one, 4 of the other, ...
             uint32_t s[32];
             tmem_ld32(scol + 32 * c, s);
-            const float ke = meta.k1[2 * c] * crow, ko = meta.k1[2 * c + 1] * crow;
-            const float be = meta.lav[2 * c] - ref, bo = meta.lav[2 * c + 1] - ref;
+            const float ke = (c ? k1.z : k1.x) * crow, ko = (c ? k1.w : k1.y) * crow;
+            const float be = (c ? lav.z : lav.x) - ref, bo = (c ? lav.w : lav.y) - ref;
             uint32_t m = 0xffffffffu;
             if (decltype(with_mask)::value)
               m = pc_mask16(meta.j0[2 * c], pos, a.window, a.sinks) |
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
             for (int i = 0; i < 16; ++i) {                // columns 2 i, 2 i + 1
               const int ev = (i >> 1) & 1, tokbit = 16 * ev + 4 * (i >> 2) + 2 * (i & 1);
               float y0, y1;
-              f32x2_unpack(f32x2_fma((uint64_t)s[2 * i] | (uint64_t)s[2 * i + 1] << 32, k2[ev], b2[ev]), y0, y1);
+              f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), k2[ev], b2[ev]), y0, y1);
               if (decltype(with_mask)::value) {
                 y0 = m >> tokbit & 1 ? y0 : -INFINITY;
                 y1 = m >> (tokbit + 1) & 1 ? y1 : -INFINITY;
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
             float e0, e1, o0, o1;
             f32x2_unpack(sum[0], e0, e1);
             f32x2_unpack(sum[1], o0, o1);
-            add = fmaf(e0 + e1, meta.iav[2 * c], fmaf(o0 + o1, meta.iav[2 * c + 1], add));
+            add = fmaf(e0 + e1, c ? iav.z : iav.x, fmaf(o0 + o1, c ? iav.w : iav.y, add));
           }
         };
         for (bool again = false;; again = true) {
@@ -625,7 +625,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n, heads = (int64_t)p.heads * a.nl;
   if (slots > 65535) return LESS_ERR_INVALID_CONFIG;
   // Items that are sure to exist; with fewer of them than multiprocessors their keys are split (measured: two sequences of
-  // 30 000 tokens, eight KV heads, 48 rows each: 508 us unsplit, 75 us in nine parts)
+  // 30 000 tokens, eight KV heads, 48 rows each: 508 us unsplit, 85 us in nine parts)
   int64_t items = (int64_t)a.rows * p.group / (2 * PC_ROWS);
   if (items < a.n) items = a.n;
   int64_t splits = pg_sms() / (items * heads);
