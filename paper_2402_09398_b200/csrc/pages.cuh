@@ -125,10 +125,11 @@ __device__ __forceinline__ int pg_page(const PgParams& p, int seq, int ordinal) 
 
 // Every kernel of the cache is launched as a programmatic dependent of the kernel before it in the stream: its CTAs come
 // up while that one drains and wait, before they read anything, until it is complete (pg_wait).  Each lets its own
-// dependents come up as soon as all its CTAs run.
+// dependents come up once all its CTAs run.  So a kernel may be on an SM whose L1 still takes lines for the one before:
+// whatever a kernel of the cache writes (maps, codes, magnitudes, partial results) is read past L1, with __ldcg.
 __device__ __forceinline__ void pg_wait() {
-  pdl_launch_dependents();
   pdl_wait_primary();
+  pdl_launch_dependents();
 }
 
 template <typename... P, typename... A>

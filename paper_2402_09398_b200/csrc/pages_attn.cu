@@ -81,6 +81,18 @@ struct PsShared {
   int last[2];                    // whether this CTA merges the part-0 / part-1 item over all CTAs
 };
 
+// a part lies in shared or in global memory; there it may come from another CTA of this launch: past L1
+__device__ __forceinline__ float2 load_part2(const float* s) {
+  float2 v;
+  asm volatile("ld.relaxed.gpu.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(s) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 load_part4(const float* s) {
+  float4 v;
+  asm volatile("ld.relaxed.gpu.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(s) : "memory");
+  return v;
+}
+
 // address of an item's row: rows are (token, query head of the group)
 __device__ __forceinline__ int64_t row_offset(const PgParams& p, const PaArgs& a, int D, const Item& it, int r) {
   const int rr = it.row0 + r, tok = rr / p.group, hd = rr - tok * p.group;
@@ -259,8 +271,8 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
           const size_t slab = (size_t)page * p.heads * 2;
           tl.codes = head_codes + slab * ((size_t)p.pt * D) + (size_t)inner * TILE;
           const float* mg = head_mags + slab * (p.pt / kPageBlock) + inner;
-          tl.ak = __ldg(mg);
-          tl.av = __ldg(mg + p.pt / kPageBlock);
+          tl.ak = __ldcg(mg);
+          tl.av = __ldcg(mg + p.pt / kPageBlock);
         }
       }
       return tl;
@@ -301,7 +313,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
         const T* src = reinterpret_cast<const T*>(a.q) + (int64_t)(e.row0 + tok) * a.q_stride +
                        ((int64_t)it.lj * p.heads + it.h) * p.group * D + hd * D + t * (D / 4);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(src) + i);
+        for (int i = 0; i < D / 32; ++i) w[i] = __ldcg(reinterpret_cast<const uint4*>(src) + i);
       }
       float up = 1.f;
       if (!std::is_same<T, __half>::value) {
@@ -566,16 +578,9 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   __syncthreads();
 
   // ---- merge: a warp takes a row, lanes own four dimensions each (with D 64 the upper half repeats the lower) ----
-  // `far`: the parts come from other CTAs of this launch, so they are read past L1 (lines may be there from before)
-  auto merge_row = [&](auto far, auto part_of, int parts, int r, float4& f, float& mm, float& ll) {
-    auto load2 = [&](const float* s) {
-      const float2* v = reinterpret_cast<const float2*>(s + R * D + 2 * r);
-      return decltype(far)::value ? __ldcg(v) : *v;
-    };
-    auto load4 = [&](const float* s) {
-      const float4* v = reinterpret_cast<const float4*>(s + r * D + (lane % (D / 4)) * 4);
-      return decltype(far)::value ? __ldcg(v) : *v;
-    };
+  auto merge_row = [&](auto part_of, int parts, int r, float4& f, float& mm, float& ll) {
+    auto load2 = [&](const float* s) { return load_part2(s + R * D + 2 * r); };
+    auto load4 = [&](const float* s) { return load_part4(s + r * D + (lane % (D / 4)) * 4); };
 
     constexpr int N = 16;                               // parts on their way at once
     float4 v[N];
@@ -633,7 +638,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       if (turn % PS_WARPS != warp) continue;
       float4 f;
       float mm, ll;
-      merge_row(std::false_type{}, part_of, wl - w0 + 1, r, f, mm, ll);
+      merge_row(part_of, wl - w0 + 1, r, f, mm, ll);
       if (lane < D / 4) {
         if (inside) {
           store4(reinterpret_cast<T*>(a.out) + row_offset(p, a, D, it, r) + lane * 4, f);
@@ -675,7 +680,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     for (int r = warp; r < it.valid; r += PS_WARPS) {
       float4 f;
       float mm, ll;
-      merge_row(std::true_type{}, part_of, c1 - c0 + 1, r, f, mm, ll);
+      merge_row(part_of, c1 - c0 + 1, r, f, mm, ll);
       if (lane < D / 4) store4(reinterpret_cast<T*>(a.out) + row_offset(p, a, D, it, r) + lane * 4, f);
     }
   }

@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           float most = 0.f;
 #pragma unroll
           for (int c = 0; c < D / 8; ++c) {
-            const uint4 w = __ldg(src + c);
+            const uint4 w = __ldcg(src + c);
             const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         }
 #pragma unroll
         for (int c = 0; c < D / 8; ++c) {
-          uint4 w = r < valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+          uint4 w = r < valid ? __ldcg(src + c) : make_uint4(0, 0, 0, 0);
           if (!std::is_same<T, __half>::value) {
             const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&w);
             uint32_t u[4];
@@ -387,8 +387,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         page_l = pg_page(p, e.seq, j_l >> p.pt_shift);
         if (page_l >= 0) {
           const float* mg = p.amax + pg_mag(p, layer, page_l, h) + (j_l & (p.pt - 1)) / kPageBlock;
-          ak_l = __ldg(mg);
-          av_l = __ldg(mg + p.pt / kPageBlock);
+          ak_l = __ldcg(mg);
+          av_l = __ldcg(mg + p.pt / kPageBlock);
         }
       }
     };
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
 #pragma unroll
           for (int i = 0; i < KP; ++i) {
             const int piece = values ? i ^ (g & 1) : (D == 128 ? i ^ (t >> 1) : i);
-            reg[i] = __ldg(reinterpret_cast<const uint4*>(s + piece * 512));
+            reg[i] = __ldcg(reinterpret_cast<const uint4*>(s + piece * 512));
           }
           // tokens behind the end may hold any byte; a NaN code would survive its zero probability
           if (E4M3 && values && j + kPageBlock > e.len) {

@@ -43,27 +43,31 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
 
 // The lowest `want` free pages (refs == 0) go to list[0 .. want) in ascending order; returns how many are free.
 // A thread looks over a stretch of its own, so the order needs one scan.  Whole block.
-__device__ __forceinline__ int take_free(const PgParams& p, int want, int* list, int* warp_sums) {
-  const int per = pg_ceil(pg_ceil(p.pages, PO_THREADS), 4) * 4;
-  const int begin = min(p.pages, (int)threadIdx.x * per), end = min(p.pages, begin + per);
-  auto group = [&](int i) {                            // bit k: page i + k is free
-    uint32_t f = 0;
-    if (i + 4 <= end) {
-      const int4 r = __ldcg(reinterpret_cast<const int4*>(p.refs + i));
-      f = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
-    } else {
-      for (int j = i; j < end; ++j) f |= (uint32_t)(__ldcg(p.refs + j) == 0) << (j - i);
-    }
-    return f;
-  };
-  const uint32_t first = begin < end ? group(begin) : 0;
+// `first`: free_group of the thread's first four pages, which a caller that changes no counts before may ask for early.
+__device__ __forceinline__ uint32_t free_group(const PgParams& p, int i, int end) {   // bit k: page i + k is free
+  uint32_t f = 0;
+  if (i + 4 <= end) {
+    const int4 r = __ldcg(reinterpret_cast<const int4*>(p.refs + i));
+    f = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
+  } else {
+    for (int j = i; j < end; ++j) f |= (uint32_t)(__ldcg(p.refs + j) == 0) << (j - i);
+  }
+  return f;
+}
+__device__ __forceinline__ int pages_per_thread(const PgParams& p) { return pg_ceil(pg_ceil(p.pages, PO_THREADS), 4) * 4; }
+__device__ __forceinline__ uint32_t first_group(const PgParams& p) {
+  const int begin = min(p.pages, (int)threadIdx.x * pages_per_thread(p));
+  return free_group(p, begin, min(p.pages, begin + pages_per_thread(p)));
+}
+__device__ __forceinline__ int take_free(const PgParams& p, uint32_t first, int want, int* list, int* warp_sums) {
+  const int per = pages_per_thread(p), begin = min(p.pages, (int)threadIdx.x * per), end = min(p.pages, begin + per);
   int mine = __popc(first);
-  for (int i = begin + 4; i < end; i += 4) mine += __popc(group(i));
+  for (int i = begin + 4; i < end; i += 4) mine += __popc(free_group(p, i, end));
   int total;
   int at = block_scan(mine, warp_sums, &total) - mine;
   if (mine)
     for (int i = begin; i < end && at < want; i += 4)
-      for (uint32_t f = i == begin ? first : group(i); f && at < want; f &= f - 1) list[at++] = i + __ffs(f) - 1;
+      for (uint32_t f = i == begin ? first : free_group(p, i, end); f && at < want; f &= f - 1) list[at++] = i + __ffs(f) - 1;
   __syncthreads();
   return total;
 }
@@ -89,7 +93,7 @@ __device__ __forceinline__ void copy_mags(const PgParams& p, int layer, int src,
   const int m = p.heads * 2 * (p.pt / kPageBlock);
   const float* a = p.amax + pg_mag(p, layer, src, 0);
   float* b = p.amax + pg_mag(p, layer, dst, 0);
-  for (int i = tid; i < m; i += threads) b[i] = a[i];
+  for (int i = tid; i < m; i += threads) b[i] = __ldcg(a + i);
 }
 
 __device__ __forceinline__ void cluster_sync_all() {
@@ -159,7 +163,7 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
           if (w >= old || !counts(i, s)) continue;
           int32_t* row = p.table + (size_t)s * p.seq_pages;
           for (int o = pg_ceil(w, p.pt) + lane; o < min(p.seq_pages, pg_ceil(old, p.pt)); o += 32) {
-            const int page = row[o];
+            const int page = __ldcg(row + o);
             if (page >= 0 && page < p.pages) atomicSub(p.refs + page, 1);
             row[o] = -1;
           }
@@ -191,7 +195,7 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
           total += sum;
         }
         lost = __syncthreads_or(lost);
-        const int free_pages = total ? take_free(p, total, p.fresh, sums) : 0;
+        const int free_pages = total ? take_free(p, first_group(p), total, p.fresh, sums) : 0;
         if (lost || total > free_pages) {                  // then no sequence grows
           if (tid == 0) pg_status(p.status, lost ? kPagesState : kPagesExhausted, 11);
         } else if (total == 0) {
@@ -210,7 +214,7 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
             for (int k = lane; k < need; k += 32) {
               const int page = __ldcg(p.fresh + (at >> 1) + k);
               if (split && k == 0) {
-                const int held = row[0], m = atomicAdd(&nmoves, 1);
+                const int held = __ldcg(row), m = atomicAdd(&nmoves, 1);
                 p.moves[1 + 3 * m] = held;
                 p.moves[2 + 3 * m] = page;
                 p.moves[3 + 3 * m] = pg_ceil(old & (p.pt - 1), kPageBlock);
@@ -233,7 +237,7 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
     for (int layer = 0; layer < p.layers; ++layer) {
       const Move v = load_move(p, D, m);
       for (int u = blockIdx.x * PO_THREADS + tid; u < v.units; u += PO_CLUSTER * PO_THREADS)
-        *unit_at(p, D, layer, v.dst, v, u) = *unit_at(p, D, layer, v.src, v, u);
+        *unit_at(p, D, layer, v.dst, v, u) = __ldcg(unit_at(p, D, layer, v.src, v, u));
       if ((int)blockIdx.x == layer % PO_CLUSTER) copy_mags(p, layer, v.src, v.dst, tid, PO_THREADS);
     }
 }
@@ -247,6 +251,9 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
   const int tid = threadIdx.x;
   pg_wait();
   for (int i = tid; i < min(PO_BITS, p.seqs + 31) / 32; i += PO_THREADS) listed.seen[i] = 0;
+  // asked for before they are needed: what is free, and (of the first entries) what is copied
+  const uint32_t free4 = first_group(p);
+  int held0 = -1, len0 = 0;
   bool bad = __ldcg(p.status) != 0, again = false;
   __syncthreads();
   for (int i = tid; i < n; i += PO_THREADS) {
@@ -255,6 +262,10 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
       pg_status(p.status, kPagesBounds, 20);
       bad = true;
     } else {
+      if (i == tid) {
+        len0 = __ldcg(p.lens + a);
+        if (len0 & (p.pt - 1)) held0 = __ldcg(p.table + (size_t)a * p.seq_pages + (len0 >> p.pt_shift));
+      }
       if (__ldcg(p.lens + b) != 0) {                       // a destination is empty, listed once, and no source
         pg_status(p.status, kPagesState, 21);
         bad = true;
@@ -263,8 +274,8 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
     }
   }
   const bool small = p.seqs <= PO_BITS;
-  bad = __syncthreads_or(bad);
-  again = __syncthreads_or(again);
+  bad = __syncthreads_or(bad || (small && again));         // (twice among the destinations)
+  if (small && again) pg_status(p.status, kPagesState, 21);
   if (!bad && !small) {
     for (int i = tid; i < n; i += PO_THREADS) {
       p.mark[src[i]] = n;
@@ -275,7 +286,6 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
     __syncthreads();
   }
   if (!bad) {
-    bad = small && again;
     for (int i = tid; i < n; i += PO_THREADS) {
       const int a = __ldg(src + i), b = __ldg(dst + i);
       bad |= small ? listed.seen[a >> 5] >> (a & 31) & 1 : __ldcg(p.mark + b) != i || __ldcg(p.mark + a) != n;
@@ -287,13 +297,14 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
   if (!bad) {
     for (int base = 0; base < n; base += PO_THREADS) {
       const int i = base + tid;
-      int held = -1, len = 0;
-      if (i < n) {
+      int held = held0, len = len0;
+      if (base && i < n) {
+        held = -1;
         const int a = __ldg(src + i);
         len = __ldcg(p.lens + a);
         if (len & (p.pt - 1)) held = __ldcg(p.table + (size_t)a * p.seq_pages + (len >> p.pt_shift));
-        if (held >= p.pages) held = -1;
       }
+      if (i >= n || held >= p.pages) held = -1;
       int sum;
       const int at = total + block_scan(held >= 0, sums, &sum) - 1;
       if (i < n) p.off[i] = held >= 0 ? at : -1;
@@ -303,7 +314,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
       }
       total += sum;
     }
-    const int free_pages = total ? take_free(p, total, p.fresh, sums) : 0;
+    const int free_pages = total ? take_free(p, free4, total, p.fresh, sums) : 0;
     if (total > free_pages) {
       if (tid == 0) pg_status(p.status, kPagesExhausted, 22);
       bad = true;
@@ -393,7 +404,7 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
     } else {
       int32_t* row = p.table + (size_t)i * p.seq_pages;
       for (int o = tid; o < p.seq_pages; o += PM_THREADS) {
-        const int page = row[o];
+        const int page = __ldcg(row + o);
         if (page >= 0 && page < p.pages) row[o] = __ldcg(p.fresh + page);
       }
     }
@@ -413,7 +424,7 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
       uint4 x[PM_UNITS];
 #pragma unroll
       for (int k = 0; k < PM_UNITS; ++k)
-        if (u0 + 32 * k + lane < v.run) x[k] = __ldcs(from + u0 + 32 * k + lane);
+        if (u0 + 32 * k + lane < v.run) x[k] = __ldcg(from + u0 + 32 * k + lane);
 #pragma unroll
       for (int k = 0; k < PM_UNITS; ++k)
         if (u0 + 32 * k + lane < v.run) __stcs(to + u0 + 32 * k + lane, x[k]);

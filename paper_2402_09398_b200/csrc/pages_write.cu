@@ -191,8 +191,8 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
     uint4 was = make_uint4(0, 0, 0, 0);
     float old = 0.f;
     if (in && keep > 0) {
-      was = *reinterpret_cast<const uint4*>(tile);
-      old = *mag;
+      was = __ldcg(reinterpret_cast<const uint4*>(tile));
+      old = __ldcg(mag);
     }
     // the largest magnitude, as bits (not negative: their order is that of the bits); what is not finite is rare
     uint32_t* word = reinterpret_cast<uint32_t*>(raw);
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p,
     if (token) old[which] = __ldcg(mags + which * (p.pt / kPageBlock));
 #pragma unroll
     for (int c = 0; c < PIECES; ++c)
-      was[which][c] = token ? *reinterpret_cast<const uint4*>(tiles + (size_t)which * p.pt * D + c * 512 + lane * 16) : make_uint4(0, 0, 0, 0);
+      was[which][c] = token ? __ldcg(reinterpret_cast<const uint4*>(tiles + (size_t)which * p.pt * D + c * 512 + lane * 16)) : make_uint4(0, 0, 0, 0);
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
