@@ -33,7 +33,7 @@ struct PgParams {
   int32_t* lens;
   int32_t* refs;
   int32_t* status;         // [4] first words of the workspace
-  int32_t* moves;          // [0] number of page moves of the call under way, then (source, destination, tiles) of each
+  int32_t* moves;          // [0] number of page moves of the call under way, then (source, destination) of each
   int32_t* mark;           // [seqs]
   int32_t* off;            // [seqs]
   int32_t* fresh;          // [max(seqs, pages)]

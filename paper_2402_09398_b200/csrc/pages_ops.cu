@@ -72,23 +72,6 @@ __device__ __forceinline__ int take_free(const PgParams& p, uint32_t first, int 
   return total;
 }
 
-// A page move: the first `tiles` stored tiles of every head's keys and values (the rest of a page that is still being
-// filled holds nothing), in 16-byte units
-struct Move {
-  int src, dst, run, units;                            // run: units of one head's keys
-};
-__device__ __forceinline__ Move load_move(const PgParams& p, int D, int m) {
-  Move v;
-  v.src = __ldcg(p.moves + 1 + 3 * m);
-  v.dst = __ldcg(p.moves + 2 + 3 * m);
-  v.run = __ldcg(p.moves + 3 + 3 * m) * D;             // kPageBlock * D / 16 per tile
-  v.units = p.heads * 2 * v.run;
-  return v;
-}
-__device__ __forceinline__ uint4* unit_at(const PgParams& p, int D, int layer, int page, const Move& v, int u) {
-  const int hw = u / v.run;
-  return reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, page, 0) + (size_t)hw * p.pt * D) + (u - hw * v.run);
-}
 __device__ __forceinline__ void copy_mags(const PgParams& p, int layer, int src, int dst, int tid, int threads) {
   const int m = p.heads * 2 * (p.pt / kPageBlock);
   const float* a = p.amax + pg_mag(p, layer, src, 0);
@@ -215,9 +198,8 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
               const int page = __ldcg(p.fresh + (at >> 1) + k);
               if (split && k == 0) {
                 const int held = __ldcg(row), m = atomicAdd(&nmoves, 1);
-                p.moves[1 + 3 * m] = held;
-                p.moves[2 + 3 * m] = page;
-                p.moves[3 + 3 * m] = pg_ceil(old & (p.pt - 1), kPageBlock);
+                p.moves[1 + 2 * m] = held;
+                p.moves[2 + 2 * m] = page;
                 atomicSub(p.refs + held, 1);
               }
               row[k] = page;
@@ -235,10 +217,11 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
   const int moves = __ldcg(p.moves);
   for (int m = 0; m < moves; ++m)
     for (int layer = 0; layer < p.layers; ++layer) {
-      const Move v = load_move(p, D, m);
-      for (int u = blockIdx.x * PO_THREADS + tid; u < v.units; u += PO_CLUSTER * PO_THREADS)
-        *unit_at(p, D, layer, v.dst, v, u) = __ldcg(unit_at(p, D, layer, v.src, v, u));
-      if ((int)blockIdx.x == layer % PO_CLUSTER) copy_mags(p, layer, v.src, v.dst, tid, PO_THREADS);
+      const int src = __ldcg(p.moves + 1 + 2 * m), dst = __ldcg(p.moves + 2 + 2 * m), units = p.heads * 2 * p.pt * D / 16;
+      const uint4* from = reinterpret_cast<const uint4*>(p.codes + pg_slab(p, D, layer, src, 0));
+      uint4* to = reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, dst, 0));
+      for (int u = blockIdx.x * PO_THREADS + tid; u < units; u += PO_CLUSTER * PO_THREADS) to[u] = __ldcg(from + u);
+      if ((int)blockIdx.x == layer % PO_CLUSTER) copy_mags(p, layer, src, dst, tid, PO_THREADS);
     }
 }
 
@@ -308,10 +291,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
       int sum;
       const int at = total + block_scan(held >= 0, sums, &sum) - 1;
       if (i < n) p.off[i] = held >= 0 ? at : -1;
-      if (held >= 0) {
-        p.moves[1 + 3 * at] = held;
-        p.moves[3 + 3 * at] = pg_ceil(len & (p.pt - 1), kPageBlock);
-      }
+      if (held >= 0) p.moves[1 + 2 * at] = held;
       total += sum;
     }
     const int free_pages = total ? take_free(p, free4, total, p.fresh, sums) : 0;
@@ -321,7 +301,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
     } else {
       for (int k = tid; k < total; k += PO_THREADS) {
         const int page = __ldcg(p.fresh + k);
-        p.moves[2 + 3 * k] = page;
+        p.moves[2 + 2 * k] = page;
         p.refs[page] = 1;
       }
     }
@@ -355,16 +335,13 @@ __global__ void __launch_bounds__(PO_THREADS) pages_compact_plan_kernel(PgParams
   int all, h = block_scan(holes, sums, &all) - holes, m = block_scan(movers, sums, &all) - movers;
   for (int i = begin; i < end; ++i) {
     const bool used = __ldcg(p.refs + i) > 0;
-    if (!used && i < live) p.moves[2 + 3 * h++] = i;
-    if (used && i >= live) {
-      p.moves[3 + 3 * m] = p.pt / kPageBlock;
-      p.moves[1 + 3 * m++] = i;
-    }
+    if (!used && i < live) p.moves[2 + 2 * h++] = i;
+    if (used && i >= live) p.moves[1 + 2 * m++] = i;
     p.fresh[i] = i;
   }
   __syncthreads();
   for (int k = tid; k < all; k += PO_THREADS) {
-    const int a = __ldcg(p.moves + 1 + 3 * k), b = __ldcg(p.moves + 2 + 3 * k);
+    const int a = __ldcg(p.moves + 1 + 2 * k), b = __ldcg(p.moves + 2 + 2 * k);
     p.fresh[a] = b;
     p.refs[b] = __ldcg(p.refs + a);
     p.refs[a] = 0;
@@ -396,7 +373,7 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
           page = __ldcg(from + o);
           if (page >= 0 && page < p.pages) atomicAdd(p.refs + page, 1);
         } else if (o == whole && at >= 0) {
-          page = __ldcg(p.moves + 2 + 3 * at);
+          page = __ldcg(p.moves + 2 + 2 * at);
         }
         to[o] = page;
       }
@@ -409,25 +386,25 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
       }
     }
   }
-  // a warp per run of tiles (one head's keys or values of a page in one layer: contiguous, 1 to 32 KB)
-  const int lane = tid & 31, runs = p.heads * 2, per_move = p.layers * runs;
+  // a warp per run (one head's keys or values of a page in one layer, 1 to 32 KB)
+  const int lane = tid & 31, runs = p.heads * 2, per_move = p.layers * runs, run = p.pt * D / 16;
   const int64_t work = (int64_t)moves * per_move;
   for (int64_t w = (int64_t)blockIdx.x * (PM_THREADS / 32) + (tid >> 5); w < work; w += (int64_t)gridDim.x * (PM_THREADS / 32)) {
     // 64-bit divisions only where the numbers need them
     const int m = work <= 0x7fffffff ? (int)w / per_move : (int)(w / per_move);
     const int rest = (int)(w - (int64_t)m * per_move), layer = rest / runs, hw = rest - layer * runs;
-    const Move v = load_move(p, D, m);
-    const uint4* from = reinterpret_cast<const uint4*>(p.codes + pg_slab(p, D, layer, v.src, 0) + (size_t)hw * p.pt * D);
-    uint4* to = reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, v.dst, 0) + (size_t)hw * p.pt * D);
-    if (hw == 0) copy_mags(p, layer, v.src, v.dst, lane, 32);
-    for (int u0 = 0; u0 < v.run; u0 += 32 * PM_UNITS) {
+    const int src_page = __ldcg(p.moves + 1 + 2 * m), dst_page = __ldcg(p.moves + 2 + 2 * m);
+    const uint4* from = reinterpret_cast<const uint4*>(p.codes + pg_slab(p, D, layer, src_page, 0)) + (size_t)hw * run;
+    uint4* to = reinterpret_cast<uint4*>(p.codes + pg_slab(p, D, layer, dst_page, 0)) + (size_t)hw * run;
+    if (hw == 0) copy_mags(p, layer, src_page, dst_page, lane, 32);
+    for (int u0 = 0; u0 < run; u0 += 32 * PM_UNITS) {
       uint4 x[PM_UNITS];
 #pragma unroll
       for (int k = 0; k < PM_UNITS; ++k)
-        if (u0 + 32 * k + lane < v.run) x[k] = __ldcg(from + u0 + 32 * k + lane);
+        if (u0 + 32 * k + lane < run) x[k] = __ldcg(from + u0 + 32 * k + lane);
 #pragma unroll
       for (int k = 0; k < PM_UNITS; ++k)
-        if (u0 + 32 * k + lane < v.run) __stcs(to + u0 + 32 * k + lane, x[k]);
+        if (u0 + 32 * k + lane < run) __stcs(to + u0 + 32 * k + lane, x[k]);
     }
   }
 }
@@ -468,7 +445,7 @@ static PgLayout pg_layout(const less_pages* d) {
   };
   const size_t most = (size_t)(d->pages > d->seqs ? d->pages : d->seqs);
   l.counters = take(kPgCounters * 4);
-  l.moves = take((1 + 3 * most) * 4);
+  l.moves = take((1 + 2 * most) * 4);
   l.mark = take((size_t)d->seqs * 4);
   l.off = take((size_t)d->seqs * 4);
   l.fresh = take(most * 4);
