@@ -171,7 +171,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, lo);
   const int64_t rows = (int64_t)e.count * p.group;
   const int64_t row0 = (slot - pc_slot(p, a, lo)) * (2 * PC_ROWS);
-  if (rows <= a.max_rows || row0 >= rows) return;         // the step kernel's, or no rows left
+  // the step kernel's, or a slot before the first entry's (its rows need not start at 0), or no rows left
+  if (rows <= a.max_rows || row0 < 0 || row0 >= rows) return;
   const int valid = (int)min(rows - row0, (int64_t)2 * PC_ROWS), nx = valid > PC_ROWS ? 2 : 1;
   const int lj = blockIdx.x / p.heads, h = blockIdx.x - lj * p.heads, layer = a.layer0 + lj;
   const int base = e.len - e.count;                       // position of the entry's first token

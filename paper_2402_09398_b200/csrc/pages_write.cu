@@ -123,13 +123,15 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
   }
   const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, lo);
   const int begin = e.len - e.count;            // first new position
-  if (e.count == 0) return;
+  const int first = pw_slot(a, lo);
+  if (e.count == 0 || slot < first) return;     // slots before the first entry's: its rows need not start at 0
   if (begin < 0) {
     if (tid == 0) pg_status(p.status, kPagesBounds, 40);
     return;
   }
-  const int pos0 = (begin / kPageBlock + slot - pw_slot(a, lo)) * kPageBlock;
-  if (pos0 >= e.len) return;
+  const int64_t block = begin / kPageBlock + (int64_t)(slot - first);
+  if (block * kPageBlock >= e.len) return;
+  const int pos0 = (int)block * kPageBlock;
   const int keep = begin - pos0;                         // tokens of the block older than the call (<= 0: none)
   const int live = min(kPageBlock, e.len - pos0);
   const int lj = blockIdx.z, layer = a.layer0 + lj;

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_pages import DEV, attend, fill, ints, make
+from test_gpu_pages import DEV, HALF_STEP, attend, fill, ints, make, same_contents
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +118,28 @@ def test_keys_split_over_ctas(dim, heads, group, new, window):
     first = attend(c, m, [0, 1, 2], starts_of(n), max_new=new, window=window, sinks=3 if window else 0)
     again = attend(c, m, [0, 1, 2], starts_of(n), max_new=new, window=window, sinks=3 if window else 0)
     assert np.array_equal(first, again)
+
+
+@pytest.mark.parametrize("skip", [1, 17, 700])
+@pytest.mark.parametrize("new", [[3, 1], [90, 40]])
+def test_rows_before_the_first_entry(skip, new):
+    """starts[0] > 0: the rows before it belong to nobody; they are not read, and the output keeps its own."""
+    lens = [100, 45]
+    c, m = make(heads=2, group=4, pt=16, pages=40)
+    fill(c, m, lens)
+    want_k = np.random.default_rng(3).normal(size=(sum(new), 1, 2, 128)).astype(np.float16)
+    want_v = np.random.default_rng(4).normal(size=(sum(new), 1, 2, 128)).astype(np.float16)
+    pad = lambda x: torch.cat([torch.full((skip, *x.shape[1:]), float("nan"), dtype=c.dtype), torch.from_numpy(x)]).to(DEV)
+    starts = starts_of(new)
+    late = ints([skip + s for s in starts])
+    c.write(pad(want_k), pad(want_v), ints([0, 1]), late)
+    m.write([0, 1], starts, want_k.astype(np.float64), want_v.astype(np.float64))
+    same_contents(c, m)
+    q = np.random.default_rng(5).normal(size=(sum(new), 1, 8, 128)).astype(np.float16)
+    out = torch.full((skip + sum(new), 1, 8, 128), 7.0, dtype=c.dtype, device=DEV)
+    c.attention(pad(q), ints([0, 1]), late, max_new=max(new), out=out)
+    assert (out[:skip] == 7.0).all()
+    want, bound = m.attention(q.astype(np.float64), [0, 1], starts)
+    err = np.abs(out[skip:].double().cpu().numpy() - want)
+    assert (err <= HALF_STEP[c.dtype] * np.abs(want) + bound + 2.0 ** -24).all()
+    assert c.poll_status() == 0
