@@ -33,13 +33,15 @@ constexpr int PC_TILES = PC_KEYS / kPageBlock;            // stored tiles of a k
 constexpr int PC_SOFT_WARPS = 8, PC_DEQ_WARPS = 4;
 constexpr int PC_THREADS = (PC_SOFT_WARPS + PC_DEQ_WARPS + 2) * 32;
 constexpr int PC_STAGES = 4, PC_META = 8;
+constexpr float PC_LOW = 0x1p-100f;                       // least magnitude of values; all-zero blocks count as that
+constexpr float PC_WIDE = 64.f;                           // log2 of magnitudes that far apart need care (see the softmax)
 constexpr int PC_POLY = 1;                                // of eight pairs of exponentials, those on the FMA pipe (see ex2_poly)
 
 struct __align__(16) PcMeta {                                           // of the stored tiles of a key tile
   float k1[PC_TILES];                                     // a_k / top
   float lav[PC_TILES], iav[PC_TILES];                     // log2 a_v, 1 / a_v
   int j0[PC_TILES];                                       // position of the first token, 2^30 = no tile
-  uint32_t part[PC_TILES];                                // bit x: row tile x does not see all of it
+  uint32_t part[PC_TILES];                                // bit x: row tile x does not see all of it; [0] bit 2: PC_WIDE
 };
 
 struct PcShared {
@@ -338,12 +340,36 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         };
         for (bool again = false;; again = true) {
           const float ref = M == -INFINITY ? 0.f : M;
-          if (masked) pass(std::true_type{}, ref); else pass(std::false_type{}, ref);
+          if (masked) {
+            pass(std::true_type{}, ref);
+            // P / a_v is the probability as long as P does not underflow, which it does beside values 2^126 larger.  In a
+            // tile with a block 2^64 below the largest magnitude so far (an all-zero one beside others, as a rule) the
+            // probabilities are summed from exponentials without a_v; nearer ones lose less than 2^-62 of the sum each.
+            // Only masked tiles look (a bit that the issuing warp sets makes such a tile one): after either kind of pass
+            // the same loop took 14 % of the whole, through registers.
+            if (part.x & 4) {
+              add = 0.f;
+#pragma unroll 1
+              for (int c = 0; c < PC_KEYS / 8; ++c) {     // four tokens of each tile of a pair
+                uint32_t s[8];
+                tmem_ld8(scol + 8 * c, s);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  const int b = 2 * (c >> 2) + (i >> 2);
+                  if (pc_mask16(meta.j0[b], pos, a.window, a.sinks) >> (4 * (c & 3) + (i & 3)) & 1)
+                    add += pa_ex2(fmaf(__uint_as_float(s[i]), meta.k1[b] * crow, -ref));
+                }
+              }
+            }
+          } else {
+            pass(std::false_type{}, ref);
+          }
           const bool up = M == -INFINITY ? most > -INFINITY : most > 8.f;
           if (again || !__any_sync(0xffffffffu, up)) break;
-          const float f = M == -INFINITY || !up ? 1.f : pa_ex2(-most);
+          const float root = M == -INFINITY || !up ? 1.f : pa_ex2(-0.5f * most), f = root * root;
           if (up) M = ref + most;
-          l *= f;
+          l = l * root * root;                            // f itself may underflow where l / a_v is large
           if (kt) {
             wait_or_give_up(&sh->pv_done[x][(kt - 1) & 1], ((kt - 1) >> 1) & 1, abortp, status, 123);
             tc_fence_after_sync();
@@ -437,7 +463,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           kav[b] = av;
         }
         uint4(&reg)[KP] = values ? vreg[b] : kreg[b];
-        // values of magnitude 0 are zeros whatever their codes are: the exponent then carries another magnitude
+        // values of magnitude 0 are zeros whatever their codes are: the exponent then carries PC_LOW
         if (page >= 0 && (!values || av > 0.f)) {
           const uint8_t* s = p.codes + pg_slab(p, D, layer, page, h) + (size_t)(j & (p.pt - 1)) * D + lane * 16;
           if (values) s += (size_t)p.pt * D;
@@ -495,8 +521,9 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         const int page = b ? kpage[1] : kpage[0], j = b ? kj[1] : kj[0];
         const float ak = b ? kak[1] : kak[0], av = b ? kav[1] : kav[0];
         PcMeta& m = sh->meta[kt % PC_META];
-        // values that are all zero may have any magnitude: the last one seen
-        if (page >= 0 && av > 0.f) vlast = fmaxf(av, 0x1p-100f);
+        // values that are all zero may have any magnitude: the least, so that they do not set the reference of others.
+        // A tile that is not there repeats the last one.
+        if (page >= 0) vlast = fmaxf(av, PC_LOW);
         m.k1[i] = page >= 0 ? ak * (1.f / pg_top<E4M3>()) : 0.f;
         m.lav[i] = log2f(vlast);
         m.iav[i] = 1.f / vlast;
@@ -545,6 +572,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     const uint64_t ad = smem_desc(smem_u32(qres), 16, 1024, kLayoutSw128);
     const uint64_t bd = smem_desc(smem_u32(kring), 16, 1024, kLayoutSw128);
     wait_or_give_up(&sh->q_full, 0, abortp, status, 127);
+    float lav_most = -INFINITY;
     for (int kt = 0; kt < nk; ++kt) {
       const int st = kt % PC_STAGES;
       wait_or_give_up(&sh->k_full[st], (kt / PC_STAGES) & 1, abortp, status, 128);
@@ -558,6 +586,12 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         for (int ks = 0; ks < D / 16; ++ks)
           mma_ss_if(on, s0, desc_at(a0, (ks >> 2) * (PC_ROWS * 128 >> 4) + (ks & 3) * 2),
                     desc_at(b0, (ks >> 2) * (PC_KEYS * 128 >> 4) + (ks & 3) * 2), idesc, ks ? 1u : 0u);
+        if (x == 0) {                                     // this warp meets the key tiles in order: it compares magnitudes
+          const float4 lav = *reinterpret_cast<const float4*>(sh->meta[kt % PC_META].lav);
+          lav_most = fmaxf(lav_most, fmaxf(fmaxf(lav.x, lav.y), fmaxf(lav.z, lav.w)));
+          if (on && fminf(fminf(lav.x, lav.y), fminf(lav.z, lav.w)) < lav_most - PC_WIDE) sh->meta[kt % PC_META].part[0] = 7;
+          __syncwarp();
+        }
         mma_commit_if(on, &sh->s_full[x][kt & 1]);
         if (on) mbar_arrive(&sh->s_full[x][kt & 1]);      // passes on what came with k_full (the magnitudes)
         __syncwarp();
@@ -618,7 +652,7 @@ __global__ void __launch_bounds__(256) pages_chunk_join_kernel(PgParams p, PaArg
   float m = ml.y == 0.f ? -INFINITY : ml.x;
 #pragma unroll
   for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  const float weight = ml.y == 0.f ? 0.f : ml.y * pa_ex2(ml.x - m);
+  const float root = ml.y == 0.f ? 0.f : pa_ex2(0.5f * (ml.x - m)), weight = ml.y * root * root;   // as in the softmax
   float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
   float sum = 0.f;
 #pragma unroll 4

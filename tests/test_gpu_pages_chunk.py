@@ -143,3 +143,22 @@ def test_rows_before_the_first_entry(skip, new):
     err = np.abs(out[skip:].double().cpu().numpy() - want)
     assert (err <= HALF_STEP[c.dtype] * np.abs(want) + bound + 2.0 ** -24).all()
     assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("new", [12, 300])                  # 12: keys are split over CTAs
+@pytest.mark.parametrize("order", ["zero first", "small first", "large first", "zero among", "mixed"])
+def test_value_magnitudes_of_any_distance(order, new):
+    """A block's share of the probabilities does not depend on the size of its values, its values not on other blocks'."""
+    c, m = make(heads=1, dim=64, group=4, pt=16, pages=130, seqs=1, seq_pages=130, dtype=torch.bfloat16)
+    fill(c, m, [2000])
+    rng = np.random.default_rng(8)
+    b = np.arange(125)
+    e = {"zero first": np.where(b < 3, -np.inf, -30.0), "small first": np.where(b < 60, -95.0, 40.0),
+         "large first": np.where(b < 60, 40.0, -95.0), "zero among": np.where(b % 5 == 2, -np.inf, -30.0 - b % 3),
+         "mixed": rng.integers(-99, 90, 125).astype(float)}[order]
+    m.amax[0, m.table[0, :125], 0, 1, 0] = np.float32(np.exp2(e))
+    c.amax.copy_(torch.from_numpy(m.amax))
+    q = torch.from_numpy(rng.normal(size=(new, 1, 4, 64))).bfloat16()
+    got = c.attention(q.to(DEV), ints([0]), ints([0, new]), max_new=new).double().cpu().numpy()
+    want, bound = m.attention(q.double().numpy(), [0], [0, new])
+    assert (np.abs(got - want) <= HALF_STEP[c.dtype] * np.abs(want) + bound).all()
