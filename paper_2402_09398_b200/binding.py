@@ -7,6 +7,7 @@ torch is used for device memory and streams.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Dict, Optional, Sequence
@@ -605,8 +606,9 @@ class PagedCache:
         max_new: the most new tokens of a sequence, as far as the host knows (default: all rows)."""
         n = seqs.shape[0]
         rows, layers, qs = self._rows(q, "q", self.heads * self.group)
-        if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if out is None:                                  # memory of the stream that writes it
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype != self.dtype or out.device != self.device or not out.is_contiguous():
             raise ValueError("out: a contiguous tensor of q's shape and type is wanted")
         self._call(self._lib.less_pages_attention, "less_pages_attention", layer_begin, layers, n,

@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pg_wait();
   // ---- the item: late rows, which see most, first ----
-  const int64_t slot = gridDim.y - 1 - blockIdx.y;
+  const int heads = a.nl * p.heads, lh = (int)(blockIdx.x % heads);         // layer and head
+  const int64_t slot = gridDim.x / heads - 1 - blockIdx.x / heads;
   int lo = 0, hi = a.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -176,15 +177,15 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   // the step kernel's, or a slot before the first entry's (its rows need not start at 0), or no rows left
   if (rows <= a.max_rows || row0 < 0 || row0 >= rows) return;
   const int valid = (int)min(rows - row0, (int64_t)2 * PC_ROWS), nx = valid > PC_ROWS ? 2 : 1;
-  const int lj = blockIdx.x / p.heads, h = blockIdx.x - lj * p.heads, layer = a.layer0 + lj;
+  const int lj = lh / p.heads, h = lh - lj * p.heads, layer = a.layer0 + lj;
   const int base = e.len - e.count;                       // position of the entry's first token
   const int tok0 = (int)(row0 / p.group), tok1 = (int)((row0 + valid - 1) / p.group);
   const Blocks vb = visible_blocks(a, base + tok1 + 1, tok1 - tok0 + 1);
   const int units = base + tok1 < 0 ? 0 : vb.count();
-  // with few items the key tiles are dealt out to `splits` CTAs (blockIdx.z), whose results are joined by a second kernel
+  // with few items the key tiles are dealt out to `splits` CTAs (blockIdx.y), whose results are joined by a second kernel
   const int nk_all = pg_ceil(units, PC_TILES), share = max(pg_ceil(nk_all, splits), splits > 1 ? PC_SPLIT_TILES : 1);
-  const int kt0 = min(nk_all, (int)blockIdx.z * share), nk = min(share, nk_all - kt0);
-  float* part = p.partial + pc_part(slot, gridDim.x, blockIdx.x, splits, blockIdx.z, D);
+  const int kt0 = min(nk_all, (int)blockIdx.y * share), nk = min(share, nk_all - kt0);
+  float* part = p.partial + pc_part(slot, heads, lh, splits, blockIdx.y, D);
   const int64_t head_row = ((int64_t)lj * p.heads + h) * p.group * D;
   T* out = reinterpret_cast<T*>(a.out);
 
@@ -685,7 +686,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
     if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
   const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n, heads = (int64_t)p.heads * a.nl;
-  if (slots > 65535) return LESS_ERR_INVALID_CONFIG;
+  if (slots * heads > 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
   // Items that are sure to exist; with fewer of them than multiprocessors their keys are split (measured: two sequences of
   // 30 000 tokens, eight KV heads, 48 rows each: 508 us unsplit, 85 us in nine parts)
   int64_t items = (int64_t)a.rows * p.group / (2 * PC_ROWS);
@@ -695,7 +696,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   splits = splits > 32 ? 32 : splits;
   splits = splits > room ? room : splits;
   splits = splits < 1 ? 1 : splits;
-  const int rc = pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3>, dim3((unsigned)heads, (unsigned)slots, (unsigned)splits),
+  const int rc = pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3>, dim3((unsigned)(slots * heads), (unsigned)splits),
                            PC_THREADS, smem, s, p, a, (int)splits);
   if (rc != LESS_OK || splits == 1) return rc;
   const int64_t warps = (int64_t)a.rows * heads * p.group;

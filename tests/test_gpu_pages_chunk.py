@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_pages import DEV, HALF_STEP, attend, fill, ints, make, same_contents
+from test_gpu_pages import DEV, HALF_STEP, attend, fill, ints, make, same_contents, same_maps
 
 pytestmark = pytest.mark.gpu
 
@@ -162,3 +162,46 @@ def test_value_magnitudes_of_any_distance(order, new):
     got = c.attention(q.to(DEV), ints([0]), ints([0, new]), max_new=new).double().cpu().numpy()
     want, bound = m.attention(q.double().numpy(), [0], [0, new])
     assert (np.abs(got - want) <= HALF_STEP[c.dtype] * np.abs(want) + bound).all()
+
+
+def test_more_entries_than_a_grid_dimension_and_than_the_bitmap():
+    """70 000 sequences, nearly all of them empty, all in one call; lists with duplicates among them."""
+    n = 70000
+    c, m = make(heads=1, dim=64, group=1, pt=16, pages=80, seqs=n, seq_pages=8)
+    live, lens = [0, 65536, 7, 65535, n - 1], [100, 70, 16, 128, 1]
+    c.resize(ints(live + [7, 0]), ints(lens + [99, 3]))
+    assert m.resize(live + [7, 0], lens + [99, 3])
+    same_maps(c, m)
+    rng = np.random.default_rng(2)
+    k, v = (rng.normal(size=(sum(lens), 1, 1, 64)).astype(np.float16) for _ in range(2))
+    c.write(torch.from_numpy(k).to(DEV), torch.from_numpy(v).to(DEV), ints(live), ints(starts_of(lens)))
+    m.write(live, starts_of(lens), k.astype(np.float64), v.astype(np.float64))
+    c.fork(ints([0, 65536]), ints([1, 66000]))
+    m.fork([0, 65536], [1, 66000])
+    same_contents(c, m)
+    for src, dst in (([0, 0], [5, 5]), ([0, 9], [9, 11])):  # a destination twice; one that is a source
+        assert c.poll_status() == 0
+        c.fork(ints(src), ints(dst))
+        assert c.poll_status() == -10
+        same_maps(c, m)
+    order = rng.permutation(n)
+    new = np.ones(n, int)
+    new[np.isin(order, [0, 65536, 66000])] = 70
+    attend(c, m, order.tolist(), starts_of(new), max_new=70)
+
+
+def test_results_belong_to_the_stream_that_writes_them():
+    c, m = make(heads=2, group=2, pages=20)
+    fill(c, m, [200])
+    q = torch.randn(1, 1, 4, 128, device=DEV).half()
+    want = c.attention(q, ints([0]))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = c.attention(q, ints([0]), stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    place = got.data_ptr()
+    del got                                                 # back to that stream's memory, not to the current one's
+    assert torch.empty_like(want).data_ptr() != place
+    with torch.cuda.stream(side):
+        assert torch.empty_like(want).data_ptr() == place
