@@ -205,3 +205,52 @@ def test_results_belong_to_the_stream_that_writes_them():
     assert torch.empty_like(want).data_ptr() != place
     with torch.cuda.stream(side):
         assert torch.empty_like(want).data_ptr() == place
+
+
+def test_a_sequence_listed_twice():
+    c, m = make(heads=2, group=4, pages=30)
+    fill(c, m, [300, 200])
+    attend(c, m, [1, 0, 1, 1], starts_of([1, 1, 1, 1]), max_new=1, tail=0)
+    attend(c, m, [1, 0, 1, 0], starts_of([60, 3, 60, 80]), max_new=80, window=50, sinks=3)
+
+
+def test_offsets_beyond_32_bits():
+    """The same contents at the end of a pool of 5 GB and in a small one: the same bits."""
+    from paper_2402_09398_b200 import binding as B
+    lens, far = [500, 77, 130], 20000 - 20
+    caches = []
+    for pages in (20000, 20):
+        c = B.PagedCache(2, 8, 128, pages, 4, 8, group=4, page_tokens=64, dtype=torch.bfloat16)
+        c.refs[:pages - 20] = 1
+        c.codes[:, pages - 20:] = 0                         # bytes that no token owns compare equal
+        c.amax[:, pages - 20:] = 0
+        c.resize(ints([0, 1, 2]), ints(lens))
+        caches.append(c)
+    big, small = caches
+    assert big.codes.numel() > 2 ** 32 and torch.equal(big.table[:3] - far * (big.table[:3] >= 0).int(), small.table[:3])
+    starts = ints(starts_of(lens))
+    k, v = (torch.randn(sum(lens), 2, 8, 128, device=DEV).bfloat16() for _ in range(2))
+    q = torch.randn(sum(lens), 2, 32, 128, device=DEV).bfloat16()
+    for c in caches:
+        c.write(k, v, ints([0, 1, 2]), starts)
+        c.fork(ints([1]), ints([3]))
+        c.resize(ints([3, 2]), ints([78, 131]))
+        c.write(k[:2], v[:2], ints([3, 2]))
+    assert torch.equal(big.lens, small.lens)
+
+    def same(pages):
+        if pages:
+            assert torch.equal(big.refs[far:], small.refs)
+            assert torch.equal(big.codes[:, far:], small.codes) and torch.equal(big.amax[:, far:], small.amax)
+        for args in ((q[:4], ints([0, 1, 2, 3]), None, 1), (q, ints([0, 1, 2]), starts, 500)):
+            a, b = (c.attention(*args) for c in caches)
+            assert torch.isfinite(b).all() and torch.equal(a, b)
+        assert [c.poll_status() for c in caches] == [0, 0]
+
+    same(True)
+    big.refs[:far] = 0
+    for c in caches:
+        c.resize(ints([1]), ints([0]))
+        c.compact()
+    assert int(big.table.max()) < 20
+    same(False)
