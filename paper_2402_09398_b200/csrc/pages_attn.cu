@@ -740,11 +740,12 @@ extern "C" int less_pages_attention(const less_pages* d, int32_t layer_begin, in
   const int64_t most = (int64_t)max_new * d->group;
   int r = most > 0x7fffffff ? 0x7fffffff : (int)most;
   cudaStream_t s = (cudaStream_t)stream;
-  if (r > kStepRows) {
-    a.max_rows = kStepRows;
+  const int step_rows = (int64_t)n * layer_count * d->heads * 2 <= pg_sms() ? kStepRowsFew : kStepRows;
+  if (r > step_rows) {
+    a.max_rows = step_rows;
     rc = launch_pages_chunk(p, a, d->head_dim, d->flags, s);
-    if (rc != LESS_OK || !starts || d->group > kStepRows) return rc;   // without starts all entries are alike
-    r = kStepRows;
+    if (rc != LESS_OK || !starts || d->group > step_rows) return rc;   // without starts all entries are alike
+    r = step_rows;
   }
   if (d->flags & LESS_PAGES_BF16)
     return (d->flags & LESS_PAGES_E4M3) ? launch_step_dim<__nv_bfloat16, true>(p, a, d->head_dim, r, s)

@@ -72,8 +72,15 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 f) {
   *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(h);
 }
 
-// rows of an entry (tokens x query heads of a group) up to which it is the step kernel's
-constexpr int kStepRows = 32;
+// Rows of an entry (tokens x query heads of a group) up to which it is the step kernel's, which takes 16 at a time: more
+// and it reads the codes again.  With fewer items (entries, layers, KV heads) than every second multiprocessor it is
+// slower than the many-token kernel, whose keys are then split, from there on; with more only behind 32.
+// Measured, step against many-token kernel, 8 KV heads x 8 queries of D 128 unless said:
+//   24 rows (one KV head, D 64): 16 sequences of 1000: 27 / 14 us
+//   32 rows:  one of 500: 17 / 20 us; one of 2000: 31 / 21; four of 1000: 32 / 21; 64 of 100: 27 / 44;
+//             128 of 2000: 280 / 294; 64 of 1000, 32 KV heads x 1: 289 / 344
+//   48 rows:  two of 30 000: 111 / 80; 16 of 2000: 79 / 44
+constexpr int kStepRows = 32, kStepRowsFew = 16;
 
 int launch_pages_chunk(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);
 

@@ -181,7 +181,7 @@ class Model:
 
         The bound: 8 (D / 16) accumulations of a score round to 2^-22 of at most scale * sum |q| |k| each (the tensor
         cores' fp32 sums may truncate), so a probability is off by that much relative, an output by twice that of the
-        largest |v|; exponentials and the two sums add less than 2^-19 of it.  An entry of more than 32 rows (tokens x
+        largest |v|; exponentials and the two sums add less than 2^-19 of it.  An entry of more than 16 rows (tokens x
         query heads of a KV head), and any entry with bf16 output, may have its probabilities rounded to fp16 once: half
         a step is 2^-11 of each p or, below 2^-14 of the row's largest, 2^-25.  With |p' - p| <= 2^-11 p + 2^-25 the sum
         of p' v moves by at most (2^-11 + n 2^-25) max |v| times the sum of p (which is at least the largest p = 1):
@@ -214,7 +214,7 @@ class Model:
                         reach = np.where(ok, np.abs(qq) @ np.abs(k).T * scale, 0.0).max(1)
                         most = np.abs(v).max() if v.size else 0.0
                         rel = 2 * (self.D // 16) * reach * 2.0 ** -22 + 2.0 ** -19
-                        if m * self.G > 32 or self.bf16:
+                        if m * self.G > 16 or self.bf16:
                             rel = rel + 2.0 ** -11 + n * 2.0 ** -25
                         bound[starts[i]:starts[i + 1], lj, h * self.G + g] = (rel * most)[:, None]
         return out, bound
