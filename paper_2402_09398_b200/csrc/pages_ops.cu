@@ -10,8 +10,8 @@
 //
 // Measured, launches included: four children of one sequence freed and forked again, with growth (three calls, four
 // launches) 15 us; 96 children of 32 sequences in eight layers, 8 heads (203 MB of pages copied): 40 us; a pool of 64
-// sequences, a quarter of it ended, trimmed and closed up (194 MB): 57 us.  Plans take 4 to 6 us each, chains of loads
-// and scans; page copies run at 5 to 6 TB/s.
+// sequences, a quarter of it ended, trimmed and closed up (196 MB): 57 us.  A plan is a chain of loads and scans in one
+// block, some microseconds in which the rest of the GPU waits.
 #include <atomic>
 #include <string.h>
 
