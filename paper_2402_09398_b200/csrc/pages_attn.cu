@@ -13,16 +13,14 @@
 //   - A tile lies in memory in the order of the mma operand fragments (pages.cuh), so a lane copies (cp.async) and
 //     reads back the very bytes it needs: no barrier, no transposition, no bank conflicts.
 //   - Scores are computed transposed (m16n8k16: 16 tokens x 16 dimensions of K times 8 query rows): eight rows fill an
-//     instruction, and the codes, converted to fp16 exactly, are never scaled - the magnitude of a key block
-//     multiplies its scores, that of a value block its probabilities.
-//   - The running maximum of a row is only a reference: it is replaced, and the sums rescaled, when a score exceeds it
-//     by 2^8, which one vote per block finds; a block costs no shuffles otherwise.
+//     instruction, and the codes, converted to fp16 exactly, are never scaled - the magnitude of a key block is part of
+//     the factor that turns a score into an exponent, that of a value block, as log2 a_v, part of the exponent.
+//   - The running maximum of a row's exponents is only a reference: it is replaced, and the sums rescaled, when an exponent
+//     exceeds it by 8, which one vote per pair of blocks finds; a block costs no shuffles otherwise.
 // Roundings: bf16 queries become fp16 after division by a power of two of their row (11 bits are enough for 8; what
-// lies 2^-14 below the row's largest loses bits, 2^-25 of the largest at most).  Probabilities times magnitude go
-// into the second product as fp16 high part plus fp16 rest (22 bits), relative to a power of two of the largest value
-// magnitude so far, so the sums are as good as fp32 wherever magnitudes of a context lie within 2^14 of each other.
-// Next to a bf16 output, which is rounded to 2^-9, the rest is left out: 2^-12 of each probability.
-// The output is rounded once.
+// lies 2^-14 below the row's largest loses bits, 2^-25 of the largest at most).  P = p a_v, relative to the largest of the
+// row so far, goes into the second product as fp16 high part plus fp16 rest (22 bits); next to a bf16 output, which is
+// rounded to 2^-8, the rest is left out: 2^-11 of each.  The output is rounded once.
 //
 // Measured: 64 sequences of up to 4000 tokens, 8 KV heads x 4 queries of D 128 (264 MB): 66 us, 4.0 TB/s; two of 100 000
 // and more, 8 x 8 (474 MB): 97 us, 4.9 TB/s; 16 sequences, 40 heads, window 1024 (169 MB): 43 us, 3.9 TB/s.  Some 6 us
@@ -113,7 +111,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   constexpr int R = 8 * NT, MT = D / 16;
   constexpr int TILE = 16 * D, CH = TILE / 512;           // bytes of a tile; 16-byte pieces per lane
   constexpr int SLOT = R * (D + 2);
-  // the rest of the probabilities matters next to an fp16 output (2^-12), not next to a bf16 one (2^-9)
+  // the rest of the probabilities matters next to an fp16 output (2^-11), not next to a bf16 one (2^-8)
   constexpr bool LO = std::is_same<T, __half>::value;
   extern __shared__ __align__(16) unsigned char ps_ring[];
   __shared__ PsShared sh;
@@ -268,10 +266,10 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     const float* head_mags = p.amax + (((size_t)layer * p.pages) * p.heads + it.h) * ((size_t)2 * (p.pt / kPageBlock));
     struct Tile {
       const uint8_t* codes;       // null = none
-      float ak, av;
+      float ak, lav;              // magnitude of the keys, log2 of the values'
     };
     auto lookup = [&](int b) {
-      Tile tl = {nullptr, 0.f, 0.f};
+      Tile tl = {nullptr, 0.f, kNoValues};
       if (b + lane < last) {
         const int tok = vb.at(b + lane) * kPageBlock, inner = (tok & (p.pt - 1)) / kPageBlock;
         const int page = pg_page(p, e.seq, tok >> p.pt_shift);
@@ -280,12 +278,13 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
           tl.codes = head_codes + slab * ((size_t)p.pt * D) + (size_t)inner * TILE;
           const float* mg = head_mags + slab * (p.pt / kPageBlock) + inner;
           tl.ak = __ldcg(mg);
-          tl.av = __ldcg(mg + p.pt / kPageBlock);
+          const float av = __ldcg(mg + p.pt / kPageBlock);
+          if (av >= kLeastValue) tl.lav = log2f(av);
         }
       }
       return tl;
     };
-    Tile cur = lookup(first), nxt = {nullptr, 0.f, 0.f};
+    Tile cur = lookup(first), nxt = {nullptr, 0.f, kNoValues};
     const size_t to_values = (size_t)p.pt * D;
     // the tiles of blocks b and b + 1 on their way to ring slots `slot` and `slot + 1`
     auto fetch = [&](const Tile& tl, int at, int slot) {
@@ -358,7 +357,6 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     const bool all_rows = it.valid == R;
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
-    float vref = 0x1p-126f, ivref = 0x1p126f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -374,17 +372,17 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       const int at = (b - first) & 31;                     // lane of block b
       if (at == 0) {
         if (b != first) cur = nxt;
-        nxt = b + 32 < last ? lookup(b + 32) : Tile{nullptr, 0.f, 0.f};
+        nxt = b + 32 < last ? lookup(b + 32) : Tile{nullptr, 0.f, kNoValues};
       }
       fetch(at + 2 < 32 ? cur : nxt, (at + 2) & 31, slot ^ 2);
       cp_async_wait<1>();
-      float ak[2], av[2];
+      float ak[2], lav[2];
       bool here[2];
       int j0[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         ak[k] = __shfl_sync(0xffffffffu, cur.ak, at + k);
-        av[k] = __shfl_sync(0xffffffffu, cur.av, at + k);
+        lav[k] = __shfl_sync(0xffffffffu, cur.lav, at + k);
         here[k] = __shfl_sync(0xffffffffu, (int)(cur.codes != nullptr), at + k);
         j0[k] = vb.at(b + k) * kPageBlock;
       }
@@ -429,7 +427,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[k][nt][i] *= ak[k] * crow[nt][i & 1];
+          for (int i = 0; i < 4; ++i) s[k][nt][i] = fmaf(s[k][nt][i], ak[k] * crow[nt][i & 1], lav[k]);
           if (!whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -448,10 +446,11 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
             float x = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-            x = fmaxf(x, m[nt][c]);
-            const float f = x == m[nt][c] ? 1.f : pa_ex2(m[nt][c] - x);
+            if (!(x > m[nt][c])) continue;
+            x = rintf(x);
+            const float f = pa_pow2(m[nt][c] - x);
+            l[nt][c] = pa_scaled(l[nt][c], m[nt][c] - x);
             m[nt][c] = x;
-            l[nt][c] *= f;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
               o[nt][mt][c] *= f;
@@ -459,47 +458,40 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
             }
           }
       }
-      if (fmaxf(av[0], av[1]) > 16.f * vref) {
-        const float now = __uint_as_float((__float_as_uint(fmaxf(av[0], av[1])) & 0x7f800000u) + 0x00800000u);
-        ivref = __uint_as_float(0x7f000000u - __float_as_uint(now));
-        const float f = vref * ivref;
-        vref = now;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[nt][mt][i] *= f;
-      }
-      // ---- probabilities, times the value magnitude: second operand of the product with the values ----
+      // ---- probabilities times the value magnitude: second operand of the product with the values ----
       uint32_t ph[2][NT][2], pl[2][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const float r = av[k] * ivref;
-          const float x[4] = {pa_ex2(s[k][nt][0] - m0), pa_ex2(s[k][nt][1] - m1), pa_ex2(s[k][nt][2] - m0), pa_ex2(s[k][nt][3] - m1)};
-          l[nt][0] += x[0] + x[2];
-          l[nt][1] += x[1] + x[3];
+          const float back = lav[k] + kSumBits;
+          const uint32_t some = lav[k] == kNoValues ? 0u : 0xffffffffu;
+          float x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float y = s[k][nt][i] - (i & 1 ? m1 : m0);
+            x[i] = pa_ex2(y);
+            l[nt][i & 1] += pa_ex2(y - back);
+          }
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float y0 = x[2 * i] * r, y1 = x[2 * i + 1] * r;
-            const __half2 hi = __floats2half2_rn(y0, y1);
-            ph[k][nt][i] = movmatrix(*reinterpret_cast<const uint32_t*>(&hi));
+            const __half2 hi = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+            ph[k][nt][i] = movmatrix(*reinterpret_cast<const uint32_t*>(&hi) & some);
             if (LO) {
-              const float2 back = __half22float2(hi);
-              pl[k][nt][i] = movmatrix(pack2(y0 - back.x, y1 - back.y));
+              const float2 high = __half22float2(hi);
+              pl[k][nt][i] = movmatrix(pack2(x[2 * i] - high.x, x[2 * i + 1] - high.y) & some);
             }
           }
         }
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        // tokens behind the end may hold any byte, a slot without a tile too; a NaN code would survive its zero probability
+        // tokens behind the end may hold any byte, a slot without a tile or values of magnitude 0 too; a NaN code would
+        // survive its zero probability
         uint32_t keep = 0xffffffffu;
-        if (E4M3 && (!here[k] || j0[k] + kPageBlock > e.len)) {
-          const int left = here[k] ? e.len - (j0[k] + 4 * t) : 0;
+        if (E4M3 && (!here[k] || lav[k] == kNoValues || j0[k] + kPageBlock > e.len)) {
+          const int left = here[k] && lav[k] != kNoValues ? e.len - (j0[k] + 4 * t) : 0;
           keep = left <= 0 ? 0u : (left >= 4 ? keep : keep >> (8 * (4 - left)));
         }
 #pragma unroll
@@ -543,12 +535,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int rc = nt * 8 + 2 * t + c;
         if (rc >= it.valid) continue;
-        const float inv = sum > 0.f ? 1.f / sum : 0.f, unit = vref / pg_top<E4M3>();
+        const float unit = (sum > 0.f ? 1.f / sum : 0.f) * (0x1p-24f / pg_top<E4M3>());
         float f[D / 8];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-          f[2 * mt] = o[nt][mt][c] * inv * unit;
-          f[2 * mt + 1] = o[nt][mt][2 + c] * inv * unit;
+          f[2 * mt] = o[nt][mt][c] * unit;
+          f[2 * mt + 1] = o[nt][mt][2 + c] * unit;
         }
         if (sum != sum) {                                    // a query that is not finite
 #pragma unroll
@@ -563,8 +555,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
 #pragma unroll
           for (int i = 0; i < D / 8; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
           if (g == 0) {
-            slot_out[R * D + 2 * rc] = m[nt][c];
-            slot_out[R * D + 2 * rc + 1] = sum;
+            *reinterpret_cast<float2*>(slot_out + R * D + 2 * rc) = pa_share(m[nt][c], sum);
           }
         }
       }

@@ -40,6 +40,27 @@ __device__ __forceinline__ float pa_ex2(float x) {
   return y;
 }
 
+// A row's sums are relative to 2^m of the row, a reference near the largest exponent so far.  m is a whole number, so that a
+// new reference changes the sums by exact powers of two.
+__device__ __forceinline__ float pa_scaled(float x, float d) { return scalbnf(x, (int)fmaxf(d, -1000.f)); }   // x 2^d
+__device__ __forceinline__ float pa_pow2(float d) { return pa_scaled(1.f, d); }
+// The exponents of P = p a_v include log2 a_v, so that what is rounded to fp16 is relative to the largest share of the sum,
+// wherever the magnitudes of other blocks lie; p itself, for the sum of the probabilities, is 2^-log2 a_v of it.
+// Magnitudes lie in [2^-100, 2^100] (less counts as values of zero): that sum is kept 2^-24 times as large, from 2^-117
+// of one token to 2^100 of each.
+constexpr float kLeastValue = 0x1p-100f, kNoValues = -101.f, kSumBits = 24.f;
+
+// (reference, sum) of a part of a row, the same but with the sum in [1, 2): a weight in joining the parts is then
+// sum 2^(reference - largest), which is lost only if it does not count.  Beyond 2^23 references are coarser than that.
+__device__ __forceinline__ float2 pa_share(float m, float sum) {
+  if (sum >= 0x1p-126f && sum < INFINITY && fabsf(m) < 0x1p23f) {
+    const int bits = __float_as_int(sum);
+    m += (float)((bits >> 23) - 127);
+    sum = __int_as_float((bits & 0x007fffff) | 0x3f800000);
+  }
+  return make_float2(m, sum);
+}
+
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
