@@ -15,12 +15,14 @@
 //   - Scores are computed transposed (m16n8k16: 16 tokens x 16 dimensions of K times 8 query rows): eight rows fill an
 //     instruction, and the codes, converted to fp16 exactly, are never scaled - the magnitude of a key block is part of
 //     the factor that turns a score into an exponent, that of a value block, as log2 a_v, part of the exponent.
-//   - The running maximum of a row's exponents is only a reference: it is replaced, and the sums rescaled, when an exponent
-//     exceeds it by 8, which one vote per pair of blocks finds; a block costs no shuffles otherwise.
+//   - A row's sums are relative to 2^m, m a reference near the largest exponent of late (pages_attn.cuh): it is moved, and
+//     the sums rescaled, when exponents leave a range around it, which one vote per pair of blocks finds; a pair costs no
+//     shuffles otherwise.
 // Roundings: bf16 queries become fp16 after division by a power of two of their row (11 bits are enough for 8; what
-// lies 2^-14 below the row's largest loses bits, 2^-25 of the largest at most).  P = p a_v, relative to the largest of the
-// row so far, goes into the second product as fp16 high part plus fp16 rest (22 bits); next to a bf16 output, which is
-// rounded to 2^-8, the rest is left out: 2^-11 of each.  The output is rounded once.
+// lies 2^-14 below the row's largest loses bits, 2^-25 of the largest at most).  P = p a_v / 2^m goes into the second
+// product as fp16 high part plus fp16 rest (22 bits); next to a bf16 output, which is rounded to 2^-8, the rest is left
+// out: 2^-11 of each.  Either way P below 2^-14 is off by up to 2^-25, at most 2^-18 of the largest P of the pair.  The
+// output is rounded once.
 //
 // Measured: 64 sequences of up to 4000 tokens, 8 KV heads x 4 queries of D 128 (264 MB): 66 us, 4.0 TB/s; two of 100 000
 // and more, 8 x 8 (474 MB): 97 us, 4.9 TB/s; 16 sequences, 40 heads, window 1024 (169 MB): 43 us, 3.9 TB/s.  Some 6 us
@@ -363,10 +365,11 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[nt][mt][i] = 0.f;
-      m[nt][0] = m[nt][1] = -INFINITY;
+      m[nt][0] = m[nt][1] = 0.f;
       l[nt][0] = l[nt][1] = 0.f;
     }
 
+    int low = 0;                                           // how far the references are below their highest: a byte per row of the lane
     int slot = 0;
     for (int b = first; b < last; b += 2) {
       const int at = (b - first) & 31;                     // lane of block b
@@ -417,7 +420,6 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
             for (int nt = 0; nt < NT; ++nt) mma16816(s[k][nt], a0, a1, a2, a3, qf[nt][2 * ks], qf[nt][2 * ks + 1]);
           }
       }
-      bool up = false;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const bool whole = all_rows && here[k] && j0[k] + kPageBlock - 1 <= first_pos &&
@@ -426,8 +428,11 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
         const int ja = j0[k] + 4 * (g >> 1) + (g & 1), jb = ja + 2;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          const uint64_t factor = f32x2_mul(f32x2_pack(ak[k], ak[k]), f32x2_pack(crow[nt][0], crow[nt][1]));
+          const uint64_t offset = f32x2_pack(lav[k] - m[nt][0], lav[k] - m[nt][1]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[k][nt][i] = fmaf(s[k][nt][i], ak[k] * crow[nt][i & 1], lav[k]);
+          for (int i = 0; i < 4; i += 2)
+            f32x2_unpack(f32x2_fma(f32x2_pack(s[k][nt][i], s[k][nt][i + 1]), factor, offset), s[k][nt][i], s[k][nt][i + 1]);
           if (!whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -435,10 +440,18 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
               if (!here[k] || j > at_row || (a.window && j <= at_row - a.window && j >= a.sinks)) s[k][nt][i] = -INFINITY;
             }
           }
-          up |= fmaxf(s[k][nt][0], s[k][nt][2]) > m[nt][0] + 8.f || fmaxf(s[k][nt][1], s[k][nt][3]) > m[nt][1] + 8.f;
         }
       }
-      if (__any_sync(0xffffffffu, up)) {
+      // the reference is set by the first pair, and follows: a row that it has left has a lane whose own keys lie outside
+      bool away = b == first;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float x = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
+          away |= x > kRefMost || (x < kRefLeast && x > -INFINITY);
+        }
+      if (__any_sync(0xffffffffu, away)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -446,15 +459,30 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
             float x = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-            if (!(x > m[nt][c])) continue;
-            x = rintf(x);
-            const float f = pa_pow2(m[nt][c] - x);
-            l[nt][c] = pa_scaled(l[nt][c], m[nt][c] - x);
-            m[nt][c] = x;
+            float d = 0.f;                                   // what the reference moves by
+            if (x > kRefMost || (x > -INFINITY && (x < kRefBack || b == first))) d = rintf(x) - kRefNew;
+            if (b != first && __any_sync(0xffffffffu, d != 0.f)) {
+              float big = fmaxf(l[nt][c], fabsf(o[nt][0][c]));
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              o[nt][mt][c] *= f;
-              o[nt][mt][2 + c] *= f;
+              for (int i = 4; i < 32; i <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, i));
+              if (big > 0.f) {                               // down by so much that no sum passes 2^104
+                const int sh = 16 * nt + 8 * c, is = low >> sh & 255;
+                d = fmaxf(d, (float)max(is - 60, min(0, (int)(__float_as_uint(big) >> 23) - 127 - 90)));
+                low = (low & ~(255 << sh)) | max(0, is - (int)d) << sh;
+              }
+              const float f = big > 0.f ? pa_pow2(-d) : 1.f;
+              l[nt][c] = pa_scaled(l[nt][c], -d);
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                o[nt][mt][c] *= f;
+                o[nt][mt][2 + c] *= f;
+              }
+            }
+            m[nt][c] += d;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              s[k][nt][c] -= d;
+              s[k][nt][2 + c] -= d;
             }
           }
       }
@@ -462,17 +490,18 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       uint32_t ph[2][NT][2], pl[2][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const float back = lav[k] + kSumBits;
+          const float back = -kSumBits - lav[k];
           const uint32_t some = lav[k] == kNoValues ? 0u : 0xffffffffu;
           float x[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float y = s[k][nt][i] - (i & 1 ? m1 : m0);
-            x[i] = pa_ex2(y);
-            l[nt][i & 1] += pa_ex2(y - back);
+          for (int i = 0; i < 4; i += 2) {
+            float p0, p1;
+            f32x2_unpack(f32x2_add(f32x2_pack(s[k][nt][i], s[k][nt][i + 1]), f32x2_pack(back, back)), p0, p1);
+            x[i] = pa_ex2(s[k][nt][i]);
+            x[i + 1] = pa_ex2(s[k][nt][i + 1]);
+            f32x2_unpack(f32x2_add(f32x2_pack(l[nt][0], l[nt][1]), f32x2_pack(pa_ex2(p0), pa_ex2(p1))), l[nt][0], l[nt][1]);
           }
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
@@ -535,7 +564,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int rc = nt * 8 + 2 * t + c;
         if (rc >= it.valid) continue;
-        const float unit = (sum > 0.f ? 1.f / sum : 0.f) * (0x1p-24f / pg_top<E4M3>());
+        const float unit = (sum > 0.f ? 1.f / sum : 0.f) * (0x1p-8f / pg_top<E4M3>());
         float f[D / 8];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {

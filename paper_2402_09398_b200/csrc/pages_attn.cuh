@@ -34,25 +34,41 @@ __device__ __forceinline__ Blocks visible_blocks(const PaArgs& a, int len, int c
   return b;
 }
 
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 __device__ __forceinline__ float pa_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
-// A row's sums are relative to 2^m of the row, a reference near the largest exponent so far.  m is a whole number, so that a
-// new reference changes the sums by exact powers of two.
-__device__ __forceinline__ float pa_scaled(float x, float d) { return scalbnf(x, (int)fmaxf(d, -1000.f)); }   // x 2^d
-__device__ __forceinline__ float pa_pow2(float d) { return pa_scaled(1.f, d); }
-// The exponents of P = p a_v include log2 a_v, so that what is rounded to fp16 is relative to the largest share of the sum,
-// wherever the magnitudes of other blocks lie; p itself, for the sum of the probabilities, is 2^-log2 a_v of it.
-// Magnitudes lie in [2^-100, 2^100] (less counts as values of zero): that sum is kept 2^-24 times as large, from 2^-117
-// of one token to 2^100 of each.
-constexpr float kLeastValue = 0x1p-100f, kNoValues = -101.f, kSumBits = 24.f;
+// Exponents are those of P = p a_v: they include log2 a_v, so that what is rounded to fp16 is relative to the largest shares
+// of a row's sum, wherever the magnitudes of other blocks lie.  The sums are relative to 2^m, a reference that follows the
+// keys in both directions: fp16 has its 11 bits down to 2^-14 and nothing below 2^-25, and beside a first token that holds
+// nearly all probability the others would vanish.  Where the largest exponent of the keys at hand is not within
+// [m - 7, m + 15], m is set 7 below it (to a whole number: the sums change by exact powers of two): P is at most 2^15, and
+// keys that it is too small for lose 2^-18 of the largest at hand.  A lane sees its own keys only, so m goes down from
+// 2 above it already once any row has to: rows just inside the range would call again and again.
+constexpr float kRefNew = 7.f, kRefMost = 15.f, kRefLeast = -7.f, kRefBack = 2.f;
+// The sum of the probabilities takes 2^(exponent - log2 a_v - 8): with magnitudes in [2^-100, 2^100] (less counts as
+// values of zero) 2^-102 of the token that has set m, 2^107 of any at most.
+constexpr float kLeastValue = 0x1p-100f, kNoValues = -101.f, kSumBits = 8.f;
+
+// 2^d for a whole number d; zero below 2^-126, 2^127 at most
+__device__ __forceinline__ float pa_pow2(float d) { return __int_as_float(((int)fminf(fmaxf(d, -127.f), 127.f) + 127) << 23); }
+__device__ __forceinline__ float pa_scaled(float x, float d) {         // x 2^d, |d| <= 254
+  const float half = floorf(0.5f * d);
+  return x * pa_pow2(half) * pa_pow2(d - half);
+}
 
 // (reference, sum) of a part of a row, the same but with the sum in [1, 2): a weight in joining the parts is then
 // sum 2^(reference - largest), which is lost only if it does not count.  Beyond 2^23 references are coarser than that.
 __device__ __forceinline__ float2 pa_share(float m, float sum) {
+  if (sum == 0.f) m = -INFINITY;                          // saw nothing
   if (sum >= 0x1p-126f && sum < INFINITY && fabsf(m) < 0x1p23f) {
     const int bits = __float_as_int(sum);
     m += (float)((bits >> 23) - 127);

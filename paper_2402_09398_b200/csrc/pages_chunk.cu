@@ -62,11 +62,6 @@ struct PcShared {
   int abort;
 };
 
-__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 // 2^y for two values on the FMA pipe, y >= -126 (smaller counts as that): y = n + f with n the nearest integer, 2^f by a
 // polynomial of degree 4 (least maximum of the relative error on [-1/2, 1/2]: 2.6e-6, 2^-18.6), n added to its exponent.
 // The exponential unit gives one result in eight cycles per warp, 16 per SM and cycle: of a key tile's exponentials it

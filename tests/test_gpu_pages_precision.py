@@ -127,3 +127,51 @@ def test_values_of_any_magnitude(dim, fmt, dtype, new, group, many, order):
     m.amax[0, m.table[0, :63], 0, 1, 0] = np.float32(np.exp2(rng.integers(-99, -90, 63) if dtype == torch.bfloat16 else -8.0))
     push(c, m)
     check(c, m, torch.from_numpy(rng.normal(size=(new, 1, group, dim))).to(dtype), [0], [0, new], many)
+
+
+def weak_tokens_beside_a_strong_one(dim, fmt, dtype, new, group, many, bits):
+    """The first token's values are zeros, so that what comes out is the share of all the others, 2^-bits of its own each."""
+    n = 4000
+    c, m = make(heads=1, dim=dim, group=group, pt=64, pages=64, seqs=1, seq_pages=64, fmt=fmt, dtype=dtype)
+    fill(c, m, [n])
+    rng = np.random.default_rng(bits)
+    set_first(m, 0, np.arange(n), 0, 0)
+    page = m.table[0, 0]
+    code = bits * np.log(2.0) / (20.0 * m.amax[0, page, 0, 0, 0]) * (127 if fmt == "int8" else 448)
+    set_first(m, 0, 0, 0, round(code) if fmt == "int8" else int(np.searchsorted(m.val[:127], code)))
+    m.codes[:, page, :, 1, m.at[1][0]] = 0
+    m.amax[:, m.table[0, :63], :, 1] *= 2.0 ** min(14, bits - 8)       # so that fp16 can hold what comes out
+    push(c, m)
+    check(c, m, queries(rng, new, m, dtype, 20.0 * dim ** 0.5), [0], [0, new], many)
+
+
+TYPES = [(64, "int8", torch.float16), (64, "e4m3", torch.bfloat16), (128, "int8", torch.bfloat16), (128, "e4m3", torch.float16)]
+
+
+@pytest.mark.parametrize("dim,fmt,dtype", TYPES)
+@pytest.mark.parametrize("new,group,many", SHAPES[:3])
+@pytest.mark.parametrize("bits", [12, 20, 27, 34])
+def test_first_token_that_holds_nearly_all_probability(dim, fmt, dtype, new, group, many, bits):
+    weak_tokens_beside_a_strong_one(dim, fmt, dtype, new, group, many, bits)
+
+
+@pytest.mark.parametrize("dim,fmt,dtype", TYPES)
+@pytest.mark.parametrize("new,group,many", SHAPES[:3])
+def test_strong_tokens_now_and_then(dim, fmt, dtype, new, group, many):
+    """The reference goes up and down many times, also by more than the sums have room for."""
+    strong_tokens_now_and_then(dim, fmt, dtype, new, group, many)
+
+
+def strong_tokens_now_and_then(dim, fmt, dtype, new, group, many):
+    n = 3000
+    c, m = make(heads=1, dim=dim, group=group, pt=16, pages=190, seqs=1, seq_pages=190, fmt=fmt, dtype=dtype)
+    fill(c, m, [n])
+    rng = np.random.default_rng(9)
+    top = 127 if fmt == "int8" else 0x7e
+    set_first(m, 0, np.arange(n), 0, 0)
+    for j in rng.integers(0, n - new, 25):                     # 4 to 120 bits above the others
+        set_first(m, 0, j, 0, int(rng.integers(top // 12, top + 1)))
+    set_first(m, 0, 40, 0, top)
+    m.amax[:, m.table[0, :188], :, 1] *= 2.0 ** 6
+    push(c, m)
+    check(c, m, queries(rng, new, m, dtype, 24.0 * dim ** 0.5), [0], [0, new], many)
