@@ -460,7 +460,8 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             float d = 0.f;                                   // what the reference moves by
-            if (x > kRefMost || (x > -INFINITY && (x < kRefBack || b == first))) d = rintf(x) - kRefNew;
+            if (x > kRefMost || (x > -INFINITY && (x < kRefBack || b == first)))
+              d = rintf(x) - (x > kRefMost && b != first ? kRefUp : kRefNew);
             if (b != first && __any_sync(0xffffffffu, d != 0.f)) {
               float big = fmaxf(l[nt][c], fabsf(o[nt][0][c]));
 #pragma unroll

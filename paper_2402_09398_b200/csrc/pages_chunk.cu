@@ -17,10 +17,11 @@
 // Codes are exact in fp16 and are never scaled.  The magnitude a_k of a key block is part of the factor that turns a
 // score into the exponent, and that of a value block, as log2 a_v, part of the exponent's offset:
 //   P = 2^(s a_k c + log2 a_v - M)            sum of the probabilities: sum over blocks of (sum P) / a_v
-// M is a running reference of a row: scores are exponentiated against the M at hand in one pass, and only if one
-// exceeds it by 2^8 - as a rule in the first tile alone - are O and the sums rescaled and the pass repeated.
-// Roundings: P (at most 2^8, the largest of a row at least near 1) is rounded once to fp16, 2^-11 of each with
-// independent signs, queries as in the step kernel, the output once.
+// M is a reference of a row that follows its keys up and down (pages_attn.cuh): scores are exponentiated against the M at
+// hand in one pass, and only if the largest exponent lies outside the range around it - as a rule in the first tile alone -
+// O and the sums are rescaled and the pass repeated.
+// Roundings: P is rounded once to fp16, 2^-11 of each with independent signs or, where it is below 2^-14, 2^-25, which is at
+// most 2^-18 of the largest of the key tile; queries as in the step kernel, the output once.
 //
 // Measured: five sequences of 700 to 8000 tokens, 1 to 2048 of them new, 8 KV heads x 4 queries of D 128: 605 to 641 us,
 // 813 to 860 TFLOP/s, half of the matrix rate; 8192 new tokens, 32 heads, window 1024: 265 us (129 GFLOP: 487 TFLOP/s,
@@ -43,7 +44,6 @@ constexpr int PC_TILES = PC_KEYS / kPageBlock;            // stored tiles of a k
 constexpr int PC_SOFT_WARPS = 8, PC_DEQ_WARPS = 4;
 constexpr int PC_THREADS = (PC_SOFT_WARPS + PC_DEQ_WARPS + 2) * 32;
 constexpr int PC_STAGES = 4, PC_META = 8;
-constexpr float PC_LOW = 0x1p-100f;                       // least magnitude of values; all-zero blocks count as that
 constexpr float PC_WIDE = 64.f;                           // log2 of magnitudes that far apart need care (see the softmax)
 constexpr int PC_POLY = 1;                                // of eight pairs of exponentials, those on the FMA pipe (see ex2_poly)
 
@@ -58,6 +58,7 @@ struct PcShared {
   uint64_t q_full, k_full[PC_STAGES], k_empty[PC_STAGES], v_full[PC_STAGES], v_empty[PC_STAGES];
   uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];     // [row tile][buffer]: key tiles alternate
   PcMeta meta[PC_META];
+  float lowest[2 * PC_ROWS];                              // how far down the references of the rows may go
   uint32_t tmem_base;
   int abort;
 };
@@ -371,11 +372,18 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           } else {
             pass(std::false_type{}, ref);
           }
-          const bool up = M == -INFINITY ? most > -INFINITY : most > 8.f;
-          if (again || !__any_sync(0xffffffffu, up)) break;
-          const float root = M == -INFINITY || !up ? 1.f : pa_ex2(-0.5f * most), f = root * root;
-          if (up) M = ref + most;
-          l = l * root * root;                            // f itself may underflow where l / a_v is large
+          const bool none = M == -INFINITY, up = most > (none ? -INFINITY : kRefMost);
+          const bool down = !none && most < kRefLeast && most > -INFINITY;
+          if (again || !__any_sync(0xffffffffu, up || down)) break;
+          float d = up || down ? rintf(most) - (up && !none ? kRefUp : kRefNew) : 0.f;   // what the reference moves by
+          const float lowest = none ? -INFINITY : sh->lowest[r];
+          // down by 40 below the highest, so that O has room, and no further than l has
+          if (down) d = fmaxf(d, fmaxf(lowest - M, (float)min(0, (int)(__float_as_uint(l) >> 23) - 127 - 90)));
+          if (up) sh->lowest[r] = fmaxf(lowest, ref + d - 40.f);
+          if (up || down) M = ref + d;
+          if (none) d = 0.f;
+          l = pa_scaled(l, -d);
+          const float f = pa_pow2(-d);
           if (kt) {
             wait_or_give_up(&sh->pv_done[x][(kt - 1) & 1], ((kt - 1) >> 1) & 1, abortp, status, 123);
             tc_fence_after_sync();
@@ -391,7 +399,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
             tmem_st_wait();
           }
         }
-        l += add;
+        l = fmaf(add, 0x1p-8f, l);                        // the sum is kept 2^-kSumBits times as large
         tmem_st32(scol, pk);
         tmem_st_wait();
         tc_fence_before_sync();
@@ -400,7 +408,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       wait_or_give_up(&sh->pv_done[x][(nk - 1) & 1], ((nk - 1) >> 1) & 1, abortp, status, 124);
       tc_fence_after_sync();
       if (!*abortp) {
-        const float inv = l == 0.f ? 0.f : 1.f / l, unit = 1.f / pg_top<E4M3>();
+        // (one factor instead of two here makes the whole loop above 10 % slower)
+        const float inv = l == 0.f ? 0.f : 1.f / l, unit = 0x1p-8f / pg_top<E4M3>();
         T* dst = out + (int64_t)(e.row0 + tok) * a.nl * p.heads * p.group * D + head_row + hd * D;
         if (splits > 1 && r < valid) *reinterpret_cast<float2*>(part + (size_t)2 * PC_ROWS * D + 2 * r) = make_float2(M, l);
 #pragma unroll
@@ -469,8 +478,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           kav[b] = av;
         }
         uint4(&reg)[KP] = values ? vreg[b] : kreg[b];
-        // values of magnitude 0 are zeros whatever their codes are: the exponent then carries PC_LOW
-        if (page >= 0 && (!values || av > 0.f)) {
+        // values of magnitude 0 are zeros whatever their codes are: the exponent then carries kLeastValue
+        if (page >= 0 && (!values || av >= kLeastValue)) {
           const uint8_t* s = p.codes + pg_slab(p, D, layer, page, h) + (size_t)(j & (p.pt - 1)) * D + lane * 16;
           if (values) s += (size_t)p.pt * D;
 #pragma unroll
@@ -529,7 +538,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         PcMeta& m = sh->meta[kt % PC_META];
         // values that are all zero may have any magnitude: the least, so that they do not set the reference of others.
         // A tile that is not there repeats the last one.
-        if (page >= 0) vlast = fmaxf(av, PC_LOW);
+        if (page >= 0) vlast = fmaxf(av, kLeastValue);
         m.k1[i] = page >= 0 ? ak * (1.f / pg_top<E4M3>()) : 0.f;
         m.lav[i] = log2f(vlast);
         m.iav[i] = 1.f / vlast;
@@ -633,7 +642,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   if (warp == 12) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of split items: a warp per row of the output and head.  Part weights are l 2^(M - m), kept in fp32, the
+// Joins the parts of split items: a warp per row of the output and head.  Part weights are l 2^(M - m), l in [1, 2), the
 // parts fp32 too; at most LESS_PAGES_PARTIAL_BYTES, which stay in L2.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) pages_chunk_join_kernel(PgParams p, PaArgs a, int splits) {
@@ -656,10 +665,11 @@ __global__ void __launch_bounds__(256) pages_chunk_join_kernel(PgParams p, PaArg
   constexpr size_t STEP = (size_t)2 * PC_ROWS * (D + 2);
   float2 ml = make_float2(-INFINITY, 0.f);
   if (lane < splits) ml = __ldcg(reinterpret_cast<const float2*>(part + lane * STEP + (size_t)2 * PC_ROWS * D + 2 * r));
-  float m = ml.y == 0.f ? -INFINITY : ml.x;
+  ml = pa_share(ml.x, ml.y);                              // (in the kernel before, ahead of the store, it takes 1 % of that)
+  float m = ml.x;
 #pragma unroll
   for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  const float root = ml.y == 0.f ? 0.f : pa_ex2(0.5f * (ml.x - m)), weight = ml.y * root * root;   // as in the softmax
+  const float weight = ml.y == 0.f ? 0.f : ml.y * pa_ex2(ml.x - m);
   float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
   float sum = 0.f;
 #pragma unroll 4

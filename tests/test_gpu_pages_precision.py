@@ -175,3 +175,16 @@ def strong_tokens_now_and_then(dim, fmt, dtype, new, group, many):
     m.amax[:, m.table[0, :188], :, 1] *= 2.0 ** 6
     push(c, m)
     check(c, m, queries(rng, new, m, dtype, 24.0 * dim ** 0.5), [0], [0, new], many)
+
+
+@pytest.mark.parametrize("dim,fmt,dtype", TYPES)
+@pytest.mark.parametrize("new,group,many", SHAPES[3:])
+@pytest.mark.parametrize("bits", [12, 20, 27, 34])
+def test_many_tokens_first_token_that_holds_nearly_all_probability(dim, fmt, dtype, new, group, many, bits):
+    weak_tokens_beside_a_strong_one(dim, fmt, dtype, new, group, many, bits)
+
+
+@pytest.mark.parametrize("dim,fmt,dtype", TYPES)
+@pytest.mark.parametrize("new,group,many", SHAPES[3:])
+def test_many_tokens_strong_tokens_now_and_then(dim, fmt, dtype, new, group, many):
+    strong_tokens_now_and_then(dim, fmt, dtype, new, group, many)
