@@ -333,9 +333,11 @@ int less_prompt_scores_noalloc(const void* Q, const void* K, int32_t n_inst, int
  *     value = code * amax / 127   (int8)         value = code * amax / 448   (e4m3, LESS_PAGES_E4M3)
  * All calls are asynchronous on the given stream, allocate nothing, read lengths and tables on the device, and can be
  * captured in a CUDA graph.  Lists (`seqs`, `lens`, `src`, `dst`, `starts`) are device int32 arrays.  Errors that only
- * the device can see (an index out of range, no free page) go to the status word that less_pages_poll_status reads;
- * until it has been read, calls that change the cache do nothing.  One call at a time per cache (its workspace is
- * shared by all of them, replays of captured ones included); different caches are independent.
+ * the device can see (an index out of range, no free page) go to the status that less_pages_poll_status reads; until it
+ * has been read, calls that change the cache do nothing.  Only less_pages_write and less_pages_trim, which refuse entries
+ * one by one, go on with the others, in that call and in writes and trims that directly follow (the layers of a step).
+ * One call at a time per cache (its workspace is shared by all of them, replays of captured ones included); different
+ * caches are independent.
  * Every function runs on the current device, which is the one the buffers are on. */
 enum {
   LESS_PAGES_E4M3 = 1u,   /* codes are e4m3 instead of int8 */
@@ -397,9 +399,10 @@ int less_pages_compact(const less_pages* cache, void* cuda_stream);
  * k, v: device fp16 / bf16 [rows, layer_count, heads, D], `stride` elements from row to row (a multiple of 8), for
  * layers [layer_begin, + layer_count).  code = round(x * top / amax), ties to even, with amax = the largest |x| of the
  * block (16 tokens x D of a layer and head); where a block holds older tokens, its amax only grows and their codes
- * are rounded again.  Infinities count as the largest finite value (bf16: 2^100), NaN and an amax below 2^-100 as 0.  Rows behind starts[n] are
- * not read; of a sequence listed twice the first entry counts; a page that other sequences hold too is not
- * written (LESS_ERR_BAD_STATE). */
+ * are rounded again.  Infinities count as the largest finite value (bf16: 2^100), NaN and an amax below 2^-100 as 0.
+ * Rows behind starts[n] are not read; of a sequence listed twice the first entry counts; a page that other sequences hold
+ * too is not written (LESS_ERR_BAD_STATE), nor one that less_pages_trim has released (LESS_ERR_DEVICE_BOUNDS).  Whatever
+ * is refused, every other token of the call is written. */
 int less_pages_write(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n, const int32_t* seqs,
                      const int32_t* starts, int32_t rows, const void* k, int64_t k_stride, const void* v,
                      int64_t v_stride, void* cuda_stream);

@@ -32,7 +32,7 @@ struct PgParams {
   int32_t* table;
   int32_t* lens;
   int32_t* refs;
-  int32_t* status;         // [4] first words of the workspace
+  int32_t* status;         // [4] first words of the workspace: code and place of an error; of an error of write or trim
   int32_t* moves;          // [0] number of page moves of the call under way, then (source, destination) of each
   int32_t* mark;           // [seqs]
   int32_t* off;            // [seqs]
@@ -45,6 +45,16 @@ constexpr int kPgCounters = 1024;
 
 __device__ __forceinline__ void pg_status(int32_t* status, int code, int where) {
   if (atomicCAS(status, 0, code) == 0) status[1] = where;
+}
+
+// Write and trim run on many CTAs, some of which find errors while others have not begun.  So that what they do does not
+// depend on which is first, they look at the first word and report to the second: an entry that is refused stops no other
+// one.  A call that is planned by one CTA sees both, and moves the second to the first.
+constexpr int kLateStatus = 2;
+__device__ __forceinline__ bool pg_stopped(const PgParams& p) {
+  const int4 s = __ldcg(reinterpret_cast<const int4*>(p.status));
+  if (s.z && threadIdx.x == 0) pg_status(p.status, s.z, s.w);
+  return (s.x | s.z) != 0;
 }
 
 __host__ __device__ __forceinline__ int pg_ceil(int a, int b) { return (a + b - 1) / b; }

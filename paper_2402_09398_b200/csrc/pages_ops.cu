@@ -116,7 +116,7 @@ __global__ void __cluster_dims__(PO_CLUSTER, 1, 1) __launch_bounds__(PO_THREADS)
       any = 0;
     }
     for (int i = tid; i < min(PO_BITS, p.seqs + 31) / 32; i += PO_THREADS) listed.seen[i] = 0;
-    uint32_t mine = __ldcg(p.status) != 0 ? kAnyBad : 0;
+    uint32_t mine = pg_stopped(p) ? kAnyBad : 0;
     __syncthreads();
     // a list that holds a bad entry changes nothing
     for (int i = tid; i < n; i += PO_THREADS) {
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_fork_plan_kernel(PgParams p,
   // asked for before they are needed: what is free, and (of the first entries) what is copied
   const uint32_t free4 = first_group(p);
   int held0 = -1, len0 = 0;
-  bool bad = __ldcg(p.status) != 0, again = false;
+  bool bad = pg_stopped(p), again = false;
   __syncthreads();
   for (int i = tid; i < n; i += PO_THREADS) {
     const int a = __ldg(src + i), b = __ldg(dst + i);
@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_compact_plan_kernel(PgParams
   __shared__ int sums[PO_THREADS / 32];
   const int tid = threadIdx.x;
   pg_wait();
-  if (__ldcg(p.status) != 0) {
+  if (pg_stopped(p)) {
     if (tid == 0) p.moves[0] = -1;
     return;
   }
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(128) pages_trim_kernel(PgParams p, int n, cons
   const int s = seqs[blockIdx.x];
   if (__ldcg(p.status) != 0) return;
   if (s < 0 || s >= p.seqs) {
-    if (threadIdx.x == 0) pg_status(p.status, kPagesBounds, 30);
+    if (threadIdx.x == 0) pg_status(p.status + kLateStatus, kPagesBounds, 30);
     return;
   }
   const int keep = __ldcg(p.lens + s) - window;          // first token that a window still covers
@@ -600,6 +600,7 @@ int less_pages_poll_status(const less_pages* d, void* stream) {
   if (cudaMemcpyAsync(st, p.status, 16, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
       cudaStreamSynchronize(s) != cudaSuccess)
     return fail_cuda("less_pages_poll_status");
+  if (st[0] == 0) st[0] = st[kLateStatus];
   if (st[0] == 0) return LESS_OK;
   if (cudaMemsetAsync(p.status, 0, 16, s) != cudaSuccess) return fail_cuda("less_pages_poll_status");
   if (st[0] == kPagesExhausted) return LESS_ERR_PAGES_EXHAUSTED;

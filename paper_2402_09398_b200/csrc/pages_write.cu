@@ -117,6 +117,8 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
   __shared__ uint32_t red[2][PW_THREADS / 32];
   const int tid = threadIdx.x, lane = tid & 31;
   pg_wait();
+  bool again = __ldcg(p.status) != 0;           // nothing after an error of an earlier call
+  p.status += kLateStatus;
   const int slot = blockIdx.x;
   int lo = 0, hi = a.n - 1;                     // the last entry whose slots start at or before this one
   while (lo < hi) {
@@ -173,8 +175,7 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
   fetch(h_first, raw);
   fetch(h_first + h_step, ahead[0]);
 
-  // nothing after an error; a sequence listed twice: the first entry counts
-  bool again = __ldcg(p.status) != 0;
+  // a sequence listed twice: the first entry counts
   for (int j = tid; j < lo; j += PW_THREADS) again |= __ldg(a.seqs + j) == e.seq;
   const int page = pg_page(p, e.seq, pos0 >> p.pt_shift);
   const int refs = page >= 0 ? __ldcg(p.refs + page) : 0;
@@ -285,6 +286,7 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p,
     else *reinterpret_cast<uint32_t*>(raw[which]) = __ldcs(reinterpret_cast<const uint32_t*>(src));
   }
   bool again = __ldcg(p.status) != 0;
+  p.status += kLateStatus;
   const PgEntry e = pg_entry(p, a.seqs, nullptr, a.rows, i);
   for (int j = lane; j < i; j += 32) again |= __ldg(a.seqs + j) == e.seq;
   if (e.count == 0) return;

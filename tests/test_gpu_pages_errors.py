@@ -1,0 +1,83 @@
+"""What the paged cache does beside an error: which entries of a call are carried out, and which calls after it."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_pages import DEV, ints, make, same_contents, same_maps
+
+pytestmark = pytest.mark.gpu
+BOUNDS, STATE = -8, -10
+
+
+def rows(rng, n, heads, dtype=torch.float16, dim=128):
+    return torch.from_numpy(rng.normal(size=(n, 2, heads, dim))).to(dtype)
+
+
+@pytest.mark.parametrize("bad,code", [(-1, BOUNDS), (70, BOUNDS), (64, STATE)])   # no sequence; one whose page is shared
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("at", [0, 30, 63])
+def test_write_carries_out_every_entry_but_the_refused_one(bad, code, many, at):
+    n, heads = 64, 3
+    c, m = make(layers=2, heads=heads, dim=128, pages=700, seqs=66, seq_pages=10, pt=16)
+    rng = np.random.default_rng(at)
+    new = [int(x) for x in rng.integers(1, 60, n)] if many else [1] * n
+    lens = [int(x) + k for x, k in zip(rng.integers(0, 80, n), new)]
+    c.resize(ints(range(n)), ints(lens))
+    m.resize(list(range(n)), lens)
+    c.resize(ints([64]), ints([32]))
+    m.resize([64], [32])
+    c.fork(ints([64]), ints([65]))
+    m.fork([64], [65])
+    # sequence `at`'s rows are the refused entry's: it keeps what it has
+    seqs = list(range(n))
+    seqs[at] = bad
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(int).tolist()
+    for k in range(20):
+        kk, vv = rows(rng, starts[-1], heads), rows(rng, starts[-1], heads)
+        c.write(kk.to(DEV), vv.to(DEV), ints(seqs), ints(starts) if many else None)
+        keep = [i for i in range(n) if i != at]
+        for i in keep:
+            m.write([i], [0, new[i]], *(x[starts[i]:starts[i + 1]].double().numpy() for x in (kk, vv)))
+        if k % 5 == 4:                                     # a write that follows goes on, others wait
+            c.resize(ints([0]), ints([0]))
+            c.write(vv.to(DEV), kk.to(DEV), ints(seqs), ints(starts) if many else None)
+            # (an entry with more tokens than its sequence has is out of bounds before its page is looked at)
+            assert c.poll_status() == (BOUNDS if new[at] > 32 else code) and c.poll_status() == 0
+            for i in range(n):
+                for b in range((lens[i] - new[i]) // 16 if i != at else 10 ** 9, -(-lens[i] // 16)):
+                    page, inner = m.table[i, b], 0
+                    assert np.array_equal(c.codes[:, page].cpu().numpy(), m.codes[:, page]), (i, b)
+                    assert np.array_equal(c.amax[:, page].double().cpu().numpy(), m.amax[:, page])
+            same_maps(c, m)
+
+
+def test_trim_carries_out_every_entry_but_the_refused_one():
+    n = 900
+    for k in range(10):
+        c, m = make(heads=1, dim=64, pages=n * 4, seqs=n, seq_pages=4, pt=16)
+        c.resize(ints(range(n)), ints([64] * n))
+        m.resize(list(range(n)), [64] * n)
+        order = np.random.default_rng(k).permutation(n).tolist()
+        c.trim(ints([n] + order[:-1]), 0, 20)
+        m.trim(order[:-1], 0, 20)
+        c.trim(ints(order[-1:]), 0, 20)                    # goes on as well
+        m.trim(order[-1:], 0, 20)
+        c.compact()                                        # does not
+        same_maps(c, m)
+        assert c.poll_status() == BOUNDS and c.poll_status() == 0
+
+
+def test_other_calls_wait_until_the_error_of_a_write_has_been_read():
+    c, m = make(heads=2, pages=20, seqs=5, seq_pages=4, pt=16)
+    c.resize(ints([0, 1]), ints([20, 30]))
+    m.resize([0, 1], [20, 30])
+    x = torch.ones(1, 1, 2, 128, device=DEV).half()
+    c.write(x, x, ints([9]))
+    c.fork(ints([0]), ints([2]))
+    c.write(x, x, ints([0]))                               # the fork has seen the error: from now on nothing is written
+    c.trim(ints([1]), 0, 1)
+    c.resize(ints([3]), ints([5]))
+    same_maps(c, m)
+    assert (c.codes == 0).all() and c.poll_status() == BOUNDS and c.poll_status() == 0
+    c.write(x, x, ints([0]))
+    assert (c.codes != 0).any() and c.poll_status() == 0
