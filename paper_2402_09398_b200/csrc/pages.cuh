@@ -123,6 +123,14 @@ __device__ __forceinline__ PgEntry pg_entry(const PgParams& p, const int32_t* se
   return e;
 }
 
+// Whether entry i starts behind its end.  Kernels that look entries up by their rows miss some then, so one CTA of them
+// looks at all.
+__device__ __forceinline__ bool pg_descends(const int32_t* starts, int i) { return starts && __ldg(starts + i + 1) < __ldg(starts + i); }
+__device__ __forceinline__ void pg_check_starts(const PgParams& p, const int32_t* starts, int n) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x)
+    if (pg_descends(starts, i)) pg_status(p.status, kPagesBounds, 4);
+}
+
 // page of the tokens [ordinal * pt, + pt) of a sequence, -1 = none
 __device__ __forceinline__ int pg_page(const PgParams& p, int seq, int ordinal) {
   const int page = __ldcg(p.table + (size_t)seq * p.seq_pages + ordinal);

@@ -169,9 +169,13 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pg_wait();
+  if (blockIdx.x == gridDim.x - 1) {                      // one CTA more than there are slots
+    if (blockIdx.y == 0) pg_check_starts(p, a.starts, a.n);
+    return;
+  }
   // ---- the item: late rows, which see most, first ----
   const int heads = a.nl * p.heads, lh = (int)(blockIdx.x % heads);         // layer and head
-  const int64_t slot = gridDim.x / heads - 1 - blockIdx.x / heads;
+  const int64_t slot = (gridDim.x - 1) / heads - 1 - blockIdx.x / heads;
   int lo = 0, hi = a.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -702,7 +706,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
     if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
   const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n, heads = (int64_t)p.heads * a.nl;
-  if (slots * heads > 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
+  if (slots * heads >= 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
   // Items that are sure to exist; with fewer of them than multiprocessors their keys are split (measured: two sequences of
   // 30 000 tokens, eight KV heads, 48 rows each: 508 us unsplit, 85 us in nine parts)
   int64_t items = (int64_t)a.rows * p.group / (2 * PC_ROWS);
@@ -712,7 +716,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   splits = splits > 32 ? 32 : splits;
   splits = splits > room ? room : splits;
   splits = splits < 1 ? 1 : splits;
-  const int rc = pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3>, dim3((unsigned)(slots * heads), (unsigned)splits),
+  const int rc = pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3>, dim3((unsigned)(slots * heads + 1), (unsigned)splits),
                            PC_THREADS, smem, s, p, a, (int)splits);
   if (rc != LESS_OK || splits == 1) return rc;
   const int64_t warps = (int64_t)a.rows * heads * p.group;

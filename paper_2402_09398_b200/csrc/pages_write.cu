@@ -120,6 +120,10 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
   bool again = __ldcg(p.status) != 0;           // nothing after an error of an earlier call
   p.status += kLateStatus;
   const int slot = blockIdx.x;
+  if (slot == (int)gridDim.x - 1) {             // one CTA more than there are slots
+    pg_check_starts(p, a.starts, a.n);
+    return;
+  }
   int lo = 0, hi = a.n - 1;                     // the last entry whose slots start at or before this one
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -393,7 +397,7 @@ extern "C" int less_pages_write(const less_pages* d, int32_t layer_begin, int32_
   const int turns = pg_ceil(d->heads, PW_THREADS / (2 * d->head_dim)), slots = rows / kPageBlock + 2 * n;
   const int64_t wave = 4 * pg_sms(), work = (int64_t)slots * layer_count * turns;
   const int share = work > wave * turns ? turns : (int)((work + wave - 1) / wave);
-  const dim3 grid(slots, pg_ceil(turns, share), layer_count);
+  const dim3 grid(slots + 1, pg_ceil(turns, share), layer_count);
   const int64_t one = ((int64_t)n * layer_count * d->heads + PW_THREADS / 32 - 1) / (PW_THREADS / 32);
   if (grid.y > 65535 || one > 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
   cudaStream_t s = (cudaStream_t)stream;

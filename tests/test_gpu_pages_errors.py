@@ -81,3 +81,19 @@ def test_other_calls_wait_until_the_error_of_a_write_has_been_read():
     assert (c.codes == 0).all() and c.poll_status() == BOUNDS and c.poll_status() == 0
     c.write(x, x, ints([0]))
     assert (c.codes != 0).any() and c.poll_status() == 0
+
+
+def test_starts_that_descend_are_reported():
+    """Also where the entry in question is one that a search for rows never meets."""
+    c, m = make(heads=1, group=71, dim=64, pages=300, seqs=4, seq_pages=64, pt=16)
+    c.resize(ints([0, 1, 2, 3]), ints([1000] * 4))
+    x = torch.zeros(1000, 1, 1, 64, device=DEV).half()
+    q = torch.zeros(1000, 1, 71, 64, device=DEV).half()
+    assert c.poll_status() == 0
+    for starts in ([0, 1000, 0, 500, 1000], [0, 0, 1000, 999, 1000], [500, 0, 1000, 1000, 1000]):
+        c.write(x, x, ints([0, 1, 2, 3]), ints(starts))
+        assert c.poll_status() == BOUNDS, starts
+        c.attention(q, ints([0, 1, 2, 3]), ints(starts), max_new=1000)
+        assert c.poll_status() == BOUNDS, starts
+        c.attention(q, ints([0, 1, 2, 3]), ints(starts), max_new=1)
+        assert c.poll_status() == BOUNDS, starts
