@@ -416,7 +416,7 @@ int less_pages_write(const less_pages* cache, int32_t layer_begin, int32_t layer
  * q: device [rows, layer_count, heads * group, D], q_stride elements from row to row (a multiple of 8); out: device
  * [rows, layer_count, heads * group, D], contiguous, q's type; rows behind starts[n] are left as they are.
  * max_new: the most new tokens any entry has, as far as the host knows; it chooses among kernels, whose results differ
- * in rounding only (with max_new * group > 16, (rows * group / 256 + n) * layer_count * heads has to be below 2^31).
+ * in rounding only ((rows * group / 8 + n) * layer_count * heads has to be below 2^31).
  * scale: > 0, 1 / sqrt(D) as a rule.  A sequence may be listed twice. */
 int less_pages_attention(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n,
                          const int32_t* seqs, const int32_t* starts, int32_t rows, int32_t max_new, const void* q,

@@ -139,6 +139,8 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       int tiles;
       const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, i);
       if (per_thread == 1) sh.entry[tid] = e;
+      // entries overlap then, and the items of all might not be counted in 32 bits (else the host has made sure of that)
+      if (pg_descends(a.starts, i)) most = 0x7fffffff;
       const int items = entry_items(e, b, tiles);
       if (items) {
         const int blocks = max(1, b.count());
@@ -172,6 +174,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
         xi += sh.sum_i[w];
       }
     }
+    if (most == 0x7fffffff) return;                        // pg_entry has reported it
     sh.units[tid + 1] = xu;
     sh.items[tid + 1] = xi;
     if (tid == 0) {
@@ -183,7 +186,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     // stretches of k warps each: then none is split, or only inside a CTA.  Times in blocks at full load, merging inside
     // a CTA costs about 2 of them, over CTAs 8.
     const int64_t workers = (int64_t)gridDim.x * PS_WARPS, items = sh.items[PS_THREADS], sum = sh.units[PS_THREADS];
-    per_warp = max(PS_MIN_BLOCKS, ((int)min((int64_t)1 << 24, div64(sum + workers - 1, workers)) + 1) & ~1);
+    per_warp = max(PS_MIN_BLOCKS, ((int)min((int64_t)1 << 30, div64(sum + workers - 1, workers)) + 1) & ~1);
     int cost = per_warp + 8;
 #pragma unroll
     for (int k = 1; k <= PS_WARPS; ++k) {
@@ -756,7 +759,9 @@ extern "C" int less_pages_attention(const less_pages* d, int32_t layer_begin, in
   if (layer_begin < 0 || layer_count < 1 || layer_begin > d->layers - layer_count) return LESS_ERR_BAD_LAYER_RANGE;
   if (n < 0 || n > (1 << 24) || rows < 0 || (!starts && rows != n) || max_new < 1) return LESS_ERR_INVALID_CONFIG;
   if (window < 0 || sinks < 0 || !(scale > 0.f) || scale > 3e38f) return LESS_ERR_INVALID_CONFIG;
+  // rows of a KV head, and items of all (8 rows or 16 each), are counted in 32 bits
   if ((int64_t)rows * d->group > 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
+  if (layer_count > 0x7fffffff / ((int64_t)rows * d->group / 8 + n + 1) / d->heads) return LESS_ERR_INVALID_CONFIG;
   if (n == 0 || rows == 0) return LESS_OK;
   if (!seqs || !q || !out) return LESS_ERR_NULL_POINTER;
   if (((uintptr_t)seqs | (uintptr_t)starts) & 3) return LESS_ERR_MISALIGNED;

@@ -97,3 +97,15 @@ def test_starts_that_descend_are_reported():
         assert c.poll_status() == BOUNDS, starts
         c.attention(q, ints([0, 1, 2, 3]), ints(starts), max_new=1)
         assert c.poll_status() == BOUNDS, starts
+
+
+def test_entries_that_overlap_more_often_than_can_be_counted():
+    """starts 0, 1024, 0, 1024, ...: 2^32 items of eight rows.  Nothing is done (an index of an item would be any number)."""
+    c, m = make(layers=16, heads=8, group=8, dim=64, pages=64, seqs=1, seq_pages=64, pt=16)
+    c.resize(ints([0]), ints([1000]))
+    q = torch.zeros(1024, 16, 64, 64, device=DEV).half()
+    n = 1 << 16
+    out = torch.full_like(q, 3.0)
+    c.attention(q, torch.zeros(n, dtype=torch.int32, device=DEV), ints([0, 1024] * (n // 2) + [0]), max_new=1, out=out)
+    assert c.poll_status() == BOUNDS
+    assert (out == 3.0).all()

@@ -135,3 +135,11 @@ def test_codes_of_the_model():
     want = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
     assert np.array_equal(pages_ref.encode(x.astype(np.float64), "e4m3"), want)
     assert pages_ref.encode(np.array([0.5, 1.5, 2.5, -0.5]), "int8").tolist() == [0, 2, 2, 0]
+
+
+def test_attention_of_more_items_than_can_be_counted(B):
+    d, p = desc(B, heads=64, group=2), 4096
+
+    def attn(rows, lc):
+        return B.less_pages_attention(d, 0, lc, 4, p, p, rows, 1, p, 2 * 64 * 2 * 128, 0, 0, 0.1, p, None)
+    assert attn(1 << 29, 1) == BAD and attn(1 << 27, 1) == BAD and attn(1 << 26, 2) == BAD
