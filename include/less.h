@@ -397,14 +397,13 @@ int less_pages_compact(const less_pages* cache, void* cuda_stream);
 /* Writes the last tokens of n sequences (less_pages_resize has made room): entry i's tokens are the rows [starts[i],
  * starts[i + 1]) of k and v (starts NULL: one row each), and go to positions [lens - count, lens) of sequence seqs[i].
  * starts ascends; where it does not (LESS_ERR_DEVICE_BOUNDS), any entry of the call may be left out.
- * starts ascends; where it does not (LESS_ERR_DEVICE_BOUNDS), any entry of the call may be left out.
  * k, v: device fp16 / bf16 [rows, layer_count, heads, D], `stride` elements from row to row (a multiple of 8), for
  * layers [layer_begin, + layer_count).  code = round(x * top / amax), ties to even, with amax = the largest |x| of the
  * block (16 tokens x D of a layer and head); where a block holds older tokens, its amax only grows and their codes
  * are rounded again.  Infinities count as the largest finite value (bf16: 2^100), NaN and an amax below 2^-100 as 0.
- * Rows behind starts[n] are not read; of a sequence listed twice the first entry counts; a page that other sequences hold
- * too is not written (LESS_ERR_BAD_STATE), nor one that less_pages_trim has released (LESS_ERR_DEVICE_BOUNDS).  Whatever
- * else is refused, every other token of the call is written. */
+ * n <= seqs.  Rows behind starts[n] are not read; of a sequence listed twice the first entry counts; a page that other
+ * sequences hold too is not written (LESS_ERR_BAD_STATE), nor one that less_pages_trim has released
+ * (LESS_ERR_DEVICE_BOUNDS).  Whatever else is refused, every other token of the call is written. */
 int less_pages_write(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n, const int32_t* seqs,
                      const int32_t* starts, int32_t rows, const void* k, int64_t k_stride, const void* v,
                      int64_t v_stride, void* cuda_stream);

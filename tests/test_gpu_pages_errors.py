@@ -109,3 +109,23 @@ def test_entries_that_overlap_more_often_than_can_be_counted():
     c.attention(q, torch.zeros(n, dtype=torch.int32, device=DEV), ints([0, 1024] * (n // 2) + [0]), max_new=1, out=out)
     assert c.poll_status() == BOUNDS
     assert (out == 3.0).all()
+
+
+@pytest.mark.parametrize("n", [2048, 2049, 5000])
+@pytest.mark.parametrize("many", [False, True])
+def test_first_entry_of_a_sequence_counts_in_long_lists(n, many):
+    """Also beside entries that name no sequence; a list of more than 2048 entries is looked up in another way."""
+    c, m = make(layers=1, heads=1, dim=64, pages=n, seqs=n, seq_pages=1, pt=16)
+    rng = np.random.default_rng(n)
+    lens = [int(x) for x in rng.integers(2, 17, n)]
+    c.resize(ints(range(n)), ints(lens))
+    m.resize(list(range(n)), lens)
+    seqs = rng.integers(0, n, n)
+    seqs[rng.integers(0, n, 3)] = (-1, n, 2 ** 31 - 1)
+    k, v = (torch.from_numpy(rng.normal(size=(n, 1, 1, 64))).half() for _ in range(2))
+    c.write(k.to(DEV), v.to(DEV), ints(seqs), ints(range(n + 1)) if many else None)
+    first = [i for i in np.unique(seqs, return_index=True)[1] if 0 <= seqs[i] < n]
+    for i in first:
+        m.write([int(seqs[i])], [0, 1], k[i:i + 1].double().numpy(), v[i:i + 1].double().numpy())
+    same_contents(c, m)
+    assert c.poll_status() == BOUNDS

@@ -143,3 +143,8 @@ def test_attention_of_more_items_than_can_be_counted(B):
     def attn(rows, lc):
         return B.less_pages_attention(d, 0, lc, 4, p, p, rows, 1, p, 2 * 64 * 2 * 128, 0, 0, 0.1, p, None)
     assert attn(1 << 29, 1) == BAD and attn(1 << 27, 1) == BAD and attn(1 << 26, 2) == BAD
+
+
+@pytest.mark.parametrize("starts", [None, 4096])
+def test_write_of_more_entries_than_sequences(B, starts):
+    assert B.less_pages_write(desc(B), 0, 1, 4, 4096, starts, 4, 4096, 512, 4096, 512, None) == BAD
