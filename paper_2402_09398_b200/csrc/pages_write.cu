@@ -7,7 +7,8 @@
 // The codes are those of exact arithmetic, without a division per value.  A 16-bit value (an old code, exactly) times the
 // correctly rounded top / a (a_old / a) is off by at most 2^-23 relative.  A quotient that is not a tie is at least 2^-19
 // from the nearest one (both are ratios of integers of at most 8 + 11 bits), so rounding to 21 bits first (2^-21) lands
-// ties exactly on themselves and nothing else on a tie; the second rounding is then right.
+// ties exactly on themselves and nothing else on a tie; the second rounding is then right.  (Magnitudes of more bits, which
+// only a cache that its owner has filled can have, go another way: pw_foreign_block.)
 // Infinities are written as the largest finite fp16 number (bf16: 2^100, so that x * top stays finite), NaN as 0:
 // one bad token must not take the other fifteen of its block with it.  Magnitudes below 2^-100 (bf16) become 0: the
 // attention divides by magnitudes.  Tokens of the last block behind the
@@ -100,6 +101,22 @@ __device__ __forceinline__ uint32_t pw_codes(float x0, float x1, float x2, float
                      __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
 
+// The same where a magnitude is not one of the 16-bit inputs' (a cache that the caller has filled): the quotient
+// value * num / m may then lie nearer to a tie than fp32 can tell.  y, to 21 bits, is a tie exactly or far from one; the
+// sign of value * num - y * m, which 64 bits hold exactly, says on which side of it the quotient is.
+__device__ __forceinline__ bool pw_foreign(float m) { return (__float_as_uint(m) & 0x1fffu) != 0; }   // more than 11 bits
+__device__ __forceinline__ float pw_beside(float x, float num, float m) {
+  const float q = __fdiv_rn(num, m) * x, c = __fmul_rn(q, 9.f), y = c - __fadd_rn(c, -q);
+  const double d = fma((double)x, (double)num, -(double)y * (double)m);
+  if (y == 0.f || d == 0.) return y;
+  return __int_as_float(__float_as_int(y) + ((d > 0.) == (y > 0.f) ? 1 : -1));
+}
+template <bool E4M3>
+__device__ __forceinline__ uint32_t pw_code_foreign(float x, float num, float m) {
+  const float y = pw_beside(x, num, m);
+  return E4M3 ? __nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3) : (uint32_t)__float2int_rn(y) & 0xffu;
+}
+
 // two packed 16-bit values -> fp32
 template <typename T>
 __device__ __forceinline__ void pw_pair(uint32_t u, float& a, float& b);
@@ -124,6 +141,41 @@ __device__ __forceinline__ uint32_t pw_clean(uint32_t u) {                // two
   v[0] = T(pw_load(v[0]));
   v[1] = T(pw_load(v[1]));
   return *reinterpret_cast<uint32_t*>(v);
+}
+
+// byte of (token, dimension) in a tile of keys or values (pages.cuh)
+template <int D>
+__device__ __forceinline__ int pw_byte(int which, int token, int d) {
+  const int c = which ? d % (D / 8) / 4 : (token >> 1 & 1) * (D / 64) + d % (D / 4) / 16;
+  const int g = which ? d / (D / 8) : 2 * (token >> 2) + (token & 1), t = which ? token >> 2 : d / (D / 4);
+  return (32 * c + 4 * g + t) * 16 + (which ? d % 4 * 4 + (token & 3) : d % 16);
+}
+// The keys or values of one block of one head, whatever the older magnitude is: by one warp, a byte at a time.  `src`: the
+// first of live - keep new tokens.
+template <typename T, int D, bool E4M3>
+__device__ __noinline__ void pw_foreign_block(const T* src, int64_t stride, int which, int keep, int live, uint8_t* tile, float* mag) {
+  const int lane = threadIdx.x & 31;
+  const float old = keep > 0 ? __ldcg(mag) : 0.f;
+  uint32_t most = 0;
+  for (int i = lane; i < (live - keep) * D; i += 32)
+    most = max(most, __float_as_uint(fabsf(pw_load(src[(int64_t)(i / D) * stride + i % D]))));
+  float m = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, most)), old);
+  if (m < 0x1p-100f) m = 0.f;
+  const float unit = m > 0.f ? m : 1.f;
+  for (int i = lane; i < kPageBlock * D; i += 32) {
+    const int token = i / D, d = i % D;
+    uint8_t* at = tile + pw_byte<D>(which, token, d);
+    uint32_t code = 0;
+    if (token < keep) {
+      code = __ldcg(at);
+      if (m != old) code = pw_code_foreign<E4M3>(pw_value<E4M3>(code), old, unit);
+    } else if (token < live) {
+      code = pw_code_foreign<E4M3>(pw_load(src[(int64_t)(token - keep) * stride + d]), pg_top<E4M3>(), unit);
+    }
+    *at = (uint8_t)code;
+  }
+  __syncwarp();                                          // all lanes have read the older magnitude
+  if (lane == 0) *mag = m;
 }
 
 template <typename T, int D, bool E4M3>
@@ -207,6 +259,24 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
     return;
   }
   const int inner = (pos0 & (p.pt - 1)) / kPageBlock;
+
+  if (keep > 0) {
+    // Older magnitudes are looked at before the loop, whose registers the other way would take (prompts: 135 us against 116)
+    auto head_of = [&](int i) { return ((int)blockIdx.y + i / HEADS * (int)gridDim.y) * HEADS + i % HEADS; };   // i-th of the CTA
+    bool foreign = false;
+    for (int i = tid; head_of(i >> 1) < p.heads; i += PW_THREADS)
+      foreign |= pw_foreign(__ldcg(p.amax + pg_mag(p, layer, page, head_of(i >> 1)) + (i & 1) * (p.pt / kPageBlock) + inner));
+    if (__syncthreads_or(foreign)) {
+      for (int i = tid >> 5; head_of(i >> 1) < p.heads; i += PW_THREADS / 32) {
+        const int h = head_of(i >> 1), kv = i & 1;
+        const int64_t step = kv ? a.v_stride : a.k_stride;
+        pw_foreign_block<T, D, E4M3>(reinterpret_cast<const T*>(kv ? a.v : a.k) + e.row0 * step + ((int64_t)lj * p.heads + h) * D, step, kv, keep, live,
+                                     p.codes + pg_slab(p, D, layer, page, h) + ((size_t)kv * p.pt + inner * kPageBlock) * D,
+                                     p.amax + pg_mag(p, layer, page, h) + kv * (p.pt / kPageBlock) + inner);
+      }
+      return;
+    }
+  }
 
   int turn = 0;
   for (int h0 = (int)blockIdx.y * HEADS; h0 < p.heads; h0 += h_step, turn ^= 1) {
@@ -335,6 +405,14 @@ __global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p,
 #pragma unroll
     for (int c = 0; c < PIECES; ++c)
       was[which][c] = token ? __ldcg(reinterpret_cast<const uint4*>(tiles + (size_t)which * p.pt * D + c * 512 + lane * 16)) : make_uint4(0, 0, 0, 0);
+  }
+  if (pw_foreign(old[0]) || pw_foreign(old[1])) {
+    for (int which = 0; which < 2; ++which) {
+      const int64_t stride = which ? a.v_stride : a.k_stride;
+      pw_foreign_block<T, D, E4M3>(reinterpret_cast<const T*>(which ? a.v : a.k) + (int64_t)i * stride + (int64_t)(lj * p.heads + h) * D, stride,
+                                   which, token, token + 1, tiles + (size_t)which * p.pt * D, mags + which * (p.pt / kPageBlock));
+    }
+    return;
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
