@@ -479,8 +479,10 @@ class PagedCache:
 
     Sequences are rows of `table`; lists of them and of lengths are int32 tensors on the cache's device.  `buffers`
     gives the cache tensors that exist already (codes, amax, table, lens, refs), contiguous, in the shapes below;
-    without it the cache starts empty.  Calls are asynchronous on the current stream (or `stream`); `poll_status`
-    tells what the device found wrong."""
+    without it the cache starts empty.  Calls are asynchronous on the current stream or on `stream`, and what they are
+    given may be dropped when they return: memory that `stream` still reads is not handed out again before it has.
+    (As with any call, `stream` has to wait for the stream that wrote the inputs.)  `poll_status` tells what the device
+    found wrong."""
 
     def __init__(self, layers, heads, head_dim, pages, seqs, seq_pages, group=1, page_tokens=64, fmt="int8",
                  dtype=torch.float16, device="cuda", buffers: Optional[Dict[str, torch.Tensor]] = None):
@@ -522,12 +524,21 @@ class PagedCache:
         self.scale = head_dim ** -0.5
         self.layers, self.heads, self.group, self.head_dim = layers, heads, group, head_dim
         self._index = self.device.index
+        self._streams = set()                            # those that the buffers are recorded on
         self._lib = lib()
         if empty:
             self.reset()
 
     # -- helpers (a call takes a few microseconds on the host: the checks below are the cheap forms) ---------- #
-    def _call(self, fn, where, *args, stream=None):
+    def _call(self, fn, where, *args, stream=None, keep=()):
+        if stream is not None:
+            for t in keep:
+                if t is not None:
+                    t.record_stream(stream)
+            if stream.cuda_stream not in self._streams:
+                self._streams.add(stream.cuda_stream)
+                for t in (self.codes, self.amax, self.table, self.lens, self.refs, self.workspace):
+                    t.record_stream(stream)
         if torch._C._cuda_getDevice() == self._index:
             rc = fn(self.desc, *args, torch._C._cuda_getCurrentRawStream(self._index) if stream is None
                     else stream.cuda_stream)
@@ -570,18 +581,18 @@ class PagedCache:
         """Sequences get new lengths: pages are taken or released (0 frees a sequence)."""
         n = seqs.shape[0]
         self._call(self._lib.less_pages_resize, "less_pages_resize", n, self._list(seqs, "seqs"),
-                   self._list(lens, "lens", n), stream=stream)
+                   self._list(lens, "lens", n), stream=stream, keep=(seqs, lens))
 
     def fork(self, src, dst, stream=None):
         """The empty sequences dst become copies of src (whole pages shared)."""
         n = src.shape[0]
         self._call(self._lib.less_pages_fork, "less_pages_fork", n, self._list(src, "src"), self._list(dst, "dst", n),
-                   stream=stream)
+                   stream=stream, keep=(src, dst))
 
     def trim(self, seqs, sinks, window, stream=None):
         """Releases the pages between the first `sinks` tokens and the last `window`."""
         self._call(self._lib.less_pages_trim, "less_pages_trim", seqs.shape[0], self._list(seqs, "seqs"), sinks, window,
-                   stream=stream)
+                   stream=stream, keep=(seqs,))
 
     def compact(self, stream=None):
         """Moves the pages in use to the front of the pool."""
@@ -598,7 +609,7 @@ class PagedCache:
             raise ValueError("k and v have the same shape")
         self._call(self._lib.less_pages_write, "less_pages_write", layer_begin, layers, n, self._list(seqs, "seqs"),
                    None if starts is None else self._list(starts, "starts", n + 1), rows, k.data_ptr(), ks,
-                   v.data_ptr(), vs, stream=stream)
+                   v.data_ptr(), vs, stream=stream, keep=(k, v, seqs, starts))
 
     def attention(self, q, seqs, starts=None, max_new=None, layer_begin=0, window=0, sinks=0, scale=None, out=None,
                   stream=None):
@@ -614,7 +625,7 @@ class PagedCache:
         self._call(self._lib.less_pages_attention, "less_pages_attention", layer_begin, layers, n,
                    self._list(seqs, "seqs"), None if starts is None else self._list(starts, "starts", n + 1), rows,
                    max(1, rows if max_new is None else max_new), q.data_ptr(), qs, window, sinks,
-                   self.scale if scale is None else scale, out.data_ptr(), stream=stream)
+                   self.scale if scale is None else scale, out.data_ptr(), stream=stream, keep=(q, seqs, starts, out))
         return out
 
     def poll_status(self, stream=None) -> int:

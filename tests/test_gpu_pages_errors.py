@@ -129,3 +129,42 @@ def test_first_entry_of_a_sequence_counts_in_long_lists(n, many):
         m.write([int(seqs[i])], [0, 1], k[i:i + 1].double().numpy(), v[i:i + 1].double().numpy())
     same_contents(c, m)
     assert c.poll_status() == BOUNDS
+
+
+@pytest.mark.parametrize("call", ["write", "attention", "resize"])
+def test_inputs_may_be_dropped_while_another_stream_waits_to_read_them(call):
+    c, m = make(heads=2, group=2, pages=40, seqs=4, seq_pages=12)
+    rng = np.random.default_rng(1)
+    k, v = (torch.from_numpy(rng.normal(size=(300, 1, 2, 128))).half() for _ in range(2))
+    q = torch.from_numpy(rng.normal(size=(300, 1, 4, 128))).half().to(DEV)
+    seqs, starts = ints([0, 1]), ints([0, 100, 300])
+    c.resize(seqs, ints([100, 200]))
+    m.resize([0, 1], [100, 200])
+    c.write(k.to(DEV), v.to(DEV), seqs, starts)
+    m.write([0, 1], [0, 100, 300], k.double().numpy(), v.double().numpy())
+    want = c.attention(q, seqs, starts, max_new=200)
+    side = torch.cuda.Stream()
+    kd, vd, qd, lens = v.to(DEV), k.to(DEV), q.clone(), ints([150, 200])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)                     # some 50 ms
+    if call == "write":
+        c.write(kd, vd, seqs, starts, stream=side)
+        m.write([0, 1], [0, 100, 300], v.double().numpy(), k.double().numpy())
+    elif call == "attention":
+        got = c.attention(qd, seqs, starts, max_new=200, stream=side)
+    else:
+        c.resize(seqs, lens, stream=side)
+        m.resize([0, 1], [150, 200])
+    old = [t.data_ptr() for t in (kd, vd, qd, lens)]
+    shapes = [(t.shape, t.dtype) for t in (kd, vd, qd, lens)]
+    del kd, vd, qd, lens
+    new = [torch.zeros(s, dtype=d, device=DEV) for s, d in shapes for _ in range(2)]     # on the current stream, at once
+    side.synchronize()
+    if call == "attention":
+        assert torch.equal(got, want)
+    else:
+        same_contents(c, m)
+    used = {"write": old[:2], "attention": old[2:3], "resize": old[3:]}[call]
+    assert not set(used) & {t.data_ptr() for t in new}
+    assert c.poll_status() == 0
