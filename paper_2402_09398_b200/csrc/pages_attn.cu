@@ -9,7 +9,7 @@
 //     of one long sequence and a ragged batch load it alike.  Lengths are read on the device.  What of an item a
 //     warp did not do alone is merged afterwards: in the block of warps first, then, by the block that arrives last,
 //     over blocks (a counter that the last one resets; the order of the sum is fixed).  Short items are padded to whole
-//     stretches instead, so that there is nothing to merge (one token of 250, 8 heads: 9.3 us, cut evenly 12.6).
+//     stretches instead, so that there is nothing to merge (one token of 250, 8 heads: 9.7 us, cut evenly 13.5).
 //   - A tile lies in memory in the order of the mma operand fragments (pages.cuh), so a lane copies (cp.async) and
 //     reads back the very bytes it needs: no barrier, no transposition, no bank conflicts.
 //   - Scores are computed transposed (m16n8k16: 16 tokens x 16 dimensions of K times 8 query rows): eight rows fill an
@@ -24,8 +24,8 @@
 // out: 2^-11 of each.  Either way P below 2^-14 is off by up to 2^-25, at most 2^-18 of the largest P of the pair.  The
 // output is rounded once.
 //
-// Measured: 64 sequences of up to 4000 tokens, 8 KV heads x 4 queries of D 128 (264 MB): 66 us, 4.0 TB/s; two of 100 000
-// and more, 8 x 8 (474 MB): 97 us, 4.9 TB/s; 16 sequences, 40 heads, window 1024 (169 MB): 43 us, 3.9 TB/s.  Some 6 us
+// Measured: 64 sequences of up to 4000 tokens, 8 KV heads x 4 queries of D 128 (264 MB): 68 us, 3.9 TB/s; two of 100 000
+// and more, 8 x 8 (474 MB): 96 us, 4.9 TB/s; 16 sequences, 40 heads, window 1024 (169 MB): 44 us, 3.8 TB/s.  Some 6 us
 // are the beginning (entries, cut, first pages: a chain of four loads), a few the merges; in between SMs differ (the same
 // number of bytes takes some of them a quarter longer).  Stretches handed out at run time instead cost 8 to 30 us
 // more at two long sequences: more parts to merge.
@@ -42,7 +42,7 @@ constexpr int PS_WARPS = 6, PS_THREADS = PS_WARPS * 32;
 // CTAs per SM: two (168 registers a thread, 96 KB of tiles per CTA) unless the rows' sums need more registers
 __host__ __device__ constexpr int ps_ctas(int NT, int D) { return NT * D <= 128 ? 2 : 1; }
 constexpr int PS_RING = 4;                     // tiles of a warp: two being worked on, two on their way
-constexpr int PS_MIN_BLOCKS = 4;               // blocks a warp takes at least (one token of 250: 2 the same, 8: 9.3 -> 13.2 us)
+constexpr int PS_MIN_BLOCKS = 4;               // blocks a warp takes at least (one token of 250: 2 the same, 8: 9.7 -> 13.3 us)
 
 __device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {       // not negative; 32-bit where the numbers allow
   return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
             for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             float d = 0.f;                                   // what the reference moves by
             if (x > kRefMost || (x > -INFINITY && (x < kRefBack || b == first)))
-              d = rintf(x) - (x > kRefMost && b != first ? kRefUp : kRefNew);
+              d = x - (x > kRefMost && b != first ? kRefUp : kRefNew);
             if (b != first && __any_sync(0xffffffffu, d != 0.f)) {
               float big = fmaxf(l[nt][c], fabsf(o[nt][0][c]));
 #pragma unroll
@@ -472,9 +472,9 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
               if (big > 0.f) {                               // down by so much that no sum passes 2^104
                 const int sh = 16 * nt + 8 * c, is = low >> sh & 255;
                 d = fmaxf(d, (float)max(is - 60, min(0, (int)(__float_as_uint(big) >> 23) - 127 - 90)));
-                low = (low & ~(255 << sh)) | max(0, is - (int)d) << sh;
+                low = (low & ~(255 << sh)) | max(0, is - __float2int_rd(d)) << sh;
               }
-              const float f = big > 0.f ? pa_pow2(-d) : 1.f;
+              const float f = big > 0.f ? pa_ex2(-d) : 1.f;
               l[nt][c] = pa_scaled(l[nt][c], -d);
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt) {

@@ -50,7 +50,8 @@ __device__ __forceinline__ float pa_ex2(float x) {
 // of a row's sum, wherever the magnitudes of other blocks lie.  The sums are relative to 2^m, a reference that follows the
 // keys in both directions: fp16 has its 11 bits down to 2^-14 and nothing below 2^-25, and beside a first token that holds
 // nearly all probability the others would vanish.  Where the largest exponent of the keys at hand is not within
-// [m - 7, m + 15], m is set 7 below it (to a whole number: the sums change by exact powers of two): P is at most 2^15, and
+// [m - 7, m + 15], m is set 7 below it: P is at most 2^15, the largest one 2^7 without rounding (a row whose sum is nearly
+// one key's would show that rounding), and
 // keys that it is too small for lose 2^-18 of the largest at hand.  Where a row that has a reference meets larger exponents,
 // they as a rule come alone: m then goes 12 below them, so that the next keys are not far below it (2048 new tokens at 8192,
 // one key block in a hundred four times as large: 10 us of 300 less than with 7).
@@ -61,20 +62,19 @@ constexpr float kRefNew = 7.f, kRefUp = 12.f, kRefMost = 15.f, kRefLeast = -7.f,
 // values of zero) 2^-102 of the token that has set m, 2^107 of any at most.
 constexpr float kLeastValue = 0x1p-100f, kNoValues = -101.f, kSumBits = 8.f;
 
-// 2^d for a whole number d; zero below 2^-126, 2^127 at most
-__device__ __forceinline__ float pa_pow2(float d) { return __int_as_float(((int)fminf(fmaxf(d, -127.f), 127.f) + 127) << 23); }
-__device__ __forceinline__ float pa_scaled(float x, float d) {         // x 2^d, |d| <= 254
-  const float half = floorf(0.5f * d);
-  return x * pa_pow2(half) * pa_pow2(d - half);
+__device__ __forceinline__ float pa_scaled(float x, float d) {         // x 2^d, also where 2^d alone is out of range
+  const float root = pa_ex2(0.5f * d);
+  return x * root * root;
 }
 
-// (reference, sum) of a part of a row, the same but with the sum in [1, 2): a weight in joining the parts is then
-// sum 2^(reference - largest), which is lost only if it does not count.  Beyond 2^23 references are coarser than that.
+// (reference, sum) of a part of a row, the same but with the sum in [1, 2) if it was far from that: a weight in joining the
+// parts is sum 2^(reference - largest), which is then lost only if it does not count, and times any value in range.  (The
+// new reference is rounded: to 2^-18 of the weight up to 64.  Beyond 2^23 references are coarser than the exponent.)
 __device__ __forceinline__ float2 pa_share(float m, float sum) {
   if (sum == 0.f) m = -INFINITY;                          // saw nothing
-  if (sum >= 0x1p-126f && sum < INFINITY && fabsf(m) < 0x1p23f) {
-    const int bits = __float_as_int(sum);
-    m += (float)((bits >> 23) - 127);
+  const int bits = __float_as_int(sum), ex = (bits >> 23) - 127;
+  if (sum >= 0x1p-126f && sum < INFINITY && abs(ex) > 20 && fabsf(m) < 0x1p23f) {
+    m += (float)ex;
     sum = __int_as_float((bits & 0x007fffff) | 0x3f800000);
   }
   return make_float2(m, sum);
@@ -116,10 +116,11 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 f) {
 // and it reads the codes again.  With fewer items (entries, layers, KV heads) than every second multiprocessor it is
 // slower than the many-token kernel, whose keys are then split, from there on; with more only behind 32.
 // Measured, step against many-token kernel, 8 KV heads x 8 queries of D 128 unless said:
-//   24 rows (one KV head, D 64): 16 sequences of 1000: 27 / 14 us
-//   32 rows:  one of 500: 17 / 20 us; one of 2000: 31 / 21; four of 1000: 32 / 21; 64 of 100: 27 / 44;
-//             128 of 2000: 280 / 294; 64 of 1000, 32 KV heads x 1: 289 / 344
-//   48 rows:  two of 30 000: 111 / 80; 16 of 2000: 79 / 44
+//   24 rows (one KV head, D 64): 16 sequences of 1000: 28 / 19 us
+//   32 rows:  one of 500: 18 / 20 us; one of 2000: 32 / 22; four of 1000: 34 / 22; 64 of 100: 28 / 46;
+//             128 of 2000: 280 / 304; 64 of 1000, 32 KV heads x 1: 292 / 360
+//   48 rows:  two of 30 000: 110 / 81; 16 of 2000: 79 / 46
+// (Few short sequences lose 2 us by it: the host does not know the lengths.)
 constexpr int kStepRows = 32, kStepRowsFew = 16;
 
 int launch_pages_chunk(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);

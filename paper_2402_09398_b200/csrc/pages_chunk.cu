@@ -23,8 +23,8 @@
 // Roundings: P is rounded once to fp16, 2^-11 of each with independent signs or, where it is below 2^-14, 2^-25, which is at
 // most 2^-18 of the largest of the key tile; queries as in the step kernel, the output once.
 //
-// Measured: five sequences of 700 to 8000 tokens, 1 to 2048 of them new, 8 KV heads x 4 queries of D 128: 605 to 641 us,
-// 813 to 860 TFLOP/s, half of the matrix rate; 8192 new tokens, 32 heads, window 1024: 265 us (129 GFLOP: 487 TFLOP/s,
+// Measured: five sequences of 700 to 8000 tokens, 1 to 2048 of them new, 8 KV heads x 4 queries of D 128: 613 to 650 us,
+// 800 to 850 TFLOP/s, half of the matrix rate; 8192 new tokens, 32 heads, window 1024: 265 us (129 GFLOP: 487 TFLOP/s,
 // 11 of a CTA's 38 us are its beginning and end).  A key tile of 256 rows takes some 2200 cycles: 1024 of the exponential
 // unit, 1250 or more of the tensor cores, and chains of waits between the roles; none is busy much more than half the time.
 // Measured and slower (2048 new tokens at 8192, 8 x 4 heads, 307 us then): key tiles of 128 with one score buffer
@@ -67,7 +67,7 @@ struct PcShared {
 // polynomial of degree 4 (least maximum of the relative error on [-1/2, 1/2]: 2.6e-6, 2^-18.6), n added to its exponent.
 // The exponential unit gives one result in eight cycles per warp, 16 per SM and cycle: of a key tile's exponentials it
 // takes as many cycles as the tensor cores of the products, so PC_POLY of every eight pairs are computed here (8 KV heads x 4,
-// 2048 new tokens at 8192: none 314 us, one 292, two 296, four 314: instruction slots are scarce too).
+// 2048 new tokens at 8192: none 280 us, one 277, two 304, four 342: instruction slots are scarce too).
 __device__ __forceinline__ void ex2_poly(float y0, float y1, float& p0, float& p1) {
   const uint64_t y = f32x2_pack(fmaxf(y0, -126.f), fmaxf(y1, -126.f)), magic = f32x2_pack(12582912.f, 12582912.f);
   const uint64_t t = f32x2_add(y, magic);                // n in the low bits
@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           const bool none = M == -INFINITY, up = most > (none ? -INFINITY : kRefMost);
           const bool down = !none && most < kRefLeast && most > -INFINITY;
           if (again || !__any_sync(0xffffffffu, up || down)) break;
-          float d = up || down ? rintf(most) - (up && !none ? kRefUp : kRefNew) : 0.f;   // what the reference moves by
+          float d = up || down ? most - (up && !none ? kRefUp : kRefNew) : 0.f;   // what the reference moves by
           const float lowest = none ? -INFINITY : sh->lowest[r];
           // down by 40 below the highest, so that O has room, and no further than l has
           if (down) d = fmaxf(d, fmaxf(lowest - M, (float)min(0, (int)(__float_as_uint(l) >> 23) - 127 - 90)));
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           if (up || down) M = ref + d;
           if (none) d = 0.f;
           l = pa_scaled(l, -d);
-          const float f = pa_pow2(-d);
+          const float f = pa_ex2(-d);
           if (kt) {
             wait_or_give_up(&sh->pv_done[x][(kt - 1) & 1], ((kt - 1) >> 1) & 1, abortp, status, 123);
             tc_fence_after_sync();
@@ -646,7 +646,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   if (warp == 12) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of split items: a warp per row of the output and head.  Part weights are l 2^(M - m), l in [1, 2), the
+// Joins the parts of split items: a warp per row of the output and head.  Part weights are l 2^(M - m), kept in fp32, the
 // parts fp32 too; at most LESS_PAGES_PARTIAL_BYTES, which stay in L2.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) pages_chunk_join_kernel(PgParams p, PaArgs a, int splits) {
@@ -708,7 +708,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n, heads = (int64_t)p.heads * a.nl;
   if (slots * heads >= 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
   // Items that are sure to exist; with fewer of them than multiprocessors their keys are split (measured: two sequences of
-  // 30 000 tokens, eight KV heads, 48 rows each: 508 us unsplit, 85 us in nine parts)
+  // 30 000 tokens, eight KV heads, 48 rows each: 489 us unsplit, 82 us in nine parts)
   int64_t items = (int64_t)a.rows * p.group / (2 * PC_ROWS);
   if (items < a.n) items = a.n;
   int64_t splits = pg_sms() / (items * heads);

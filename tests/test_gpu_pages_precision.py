@@ -188,3 +188,20 @@ def test_many_tokens_first_token_that_holds_nearly_all_probability(dim, fmt, dty
 @pytest.mark.parametrize("new,group,many", SHAPES[3:])
 def test_many_tokens_strong_tokens_now_and_then(dim, fmt, dtype, new, group, many):
     strong_tokens_now_and_then(dim, fmt, dtype, new, group, many)
+
+
+@pytest.mark.parametrize("dim,fmt,dtype", TYPES)
+@pytest.mark.parametrize("group,many", [(1, False), (8, False), (16, False), (40, True), (128, True)])
+def test_a_row_that_is_one_key(dim, fmt, dtype, group, many):
+    """One key, or one with nearly all probability: the largest P of a row is a power of two, so that the result is the value
+    but for 2^-15 (the bound of `expected` without the rounding of P) and the output's own rounding."""
+    n = 30
+    c, m = make(heads=1, dim=dim, group=group, pt=16, pages=2 * n, seqs=n, seq_pages=2, fmt=fmt, dtype=dtype)
+    fill(c, m, [1] * n)
+    rng = np.random.default_rng(group)
+    q = torch.from_numpy(rng.normal(size=(n, 1, group, dim))).to(dtype)
+    got = c.attention(q.to(DEV), ints(range(n))).double().cpu().numpy()
+    want = np.stack([m.rows(0, s, 0, 1, 1)[0] for s in range(n)])[:, :, None]
+    step = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(want), 2.0 ** -14))) - (10 if dtype == torch.float16 else 7))
+    assert (np.abs(got - want) <= step / 2 + 2.0 ** -15 * np.abs(want)).all()
+    assert c.poll_status() == 0
