@@ -482,7 +482,7 @@ class PagedCache:
     without it the cache starts empty.  Calls are asynchronous on the current stream or on `stream`, and what they are
     given may be dropped when they return: memory that `stream` still reads is not handed out again before it has.
     (As with any call, `stream` has to wait for the stream that wrote the inputs.)  `poll_status` tells what the device
-    found wrong."""
+    found wrong; until then calls that change the cache do nothing (write and trim go on with what is not refused)."""
 
     def __init__(self, layers, heads, head_dim, pages, seqs, seq_pages, group=1, page_tokens=64, fmt="int8",
                  dtype=torch.float16, device="cuda", buffers: Optional[Dict[str, torch.Tensor]] = None):

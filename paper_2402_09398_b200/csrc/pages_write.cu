@@ -16,7 +16,7 @@
 //
 // Bound by memory: 2 bytes read and 1 written per value.  A block of threads takes one 16-token block of one layer
 // for a few heads; a thread owns one 16-byte piece of the stored tile (pages.cuh), so the stores are contiguous.
-// Measured: 18 400 tokens of four layers, 8 heads of D 128 (452 MB): 113 us, 4.0 TB/s of 6.5; with a division per value
+// Measured: 18 400 tokens of four layers, 8 heads of D 128 (452 MB): 116 us, 3.9 TB/s of 6.5; with a division per value
 // 376, one head ahead 158, fp32 maxima 145.  The rest is the chain per head: loads, maximum over 4 warps, stores.
 #include <type_traits>
 
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(PW_THREADS, 4) pages_write_kernel(PgParams p, 
 // as they were or, if the magnitude has grown, rounded again, zeros behind the end, and then the token's own codes (a
 // lane's four dimensions of the keys are four neighbouring bytes, those of the values lie four bytes apart).  What counts
 // is the chain of loads that leads to the tiles: all that does not depend on one another is asked for at once.
-// Measured: 64 sequences, four layers, 8 heads: 9.3 us replayed, launch included; 0.2 us of memory traffic.
+// Measured: 64 sequences, four layers, 8 heads, resize before it: 10 us replayed, launches included; 0.2 us of memory traffic.
 template <typename T, int D, bool E4M3>
 __global__ void __launch_bounds__(PW_THREADS) pages_write_one_kernel(PgParams p, PwArgs a, int nl) {
   constexpr int PL = D / 32, PIECES = D / 32;   // values of a lane; 16-byte pieces of a lane in a tile
@@ -490,8 +490,9 @@ extern "C" int less_pages_write(const less_pages* d, int32_t layer_begin, int32_
   const bool bf16 = d->flags & LESS_PAGES_BF16, e4m3 = d->flags & LESS_PAGES_E4M3;
   // Heads of a block are taken in turn by one CTA, so that what leads to its page is looked up once and the next head's
   // rows are on their way: as many as make one wave of resident CTAs (4 per multiprocessor).  Measured, one turn a CTA /
-  // all heads in one / this rule, D 128: 200 tokens of 32 heads 5.0 / 19.5 / 5.1 us; 1000 of 32 13.1 / 19.4 / 9.5; four
-  // sequences of 2000, 8 heads 24.8 / 15.1 / 15.0; 18 400 tokens of four layers, 8 heads 235 / 113 / 113.
+  // all heads in one / this rule, D 128, with the resize: 200 tokens of 32 heads 8.3 / 27.9 / 8.3 us; 1000 of 32
+  // 17.7 / 29.5 / 13.3; four sequences of 2000, 8 heads 30.2 / 19.2 / 19.5; 18 400 tokens of four layers, 8 heads
+  // 233 / 116 / 116.
   const int turns = pg_ceil(d->heads, PW_THREADS / (2 * d->head_dim)), slots = rows / kPageBlock + 2 * n;
   const int64_t wave = 4 * pg_sms(), work = (int64_t)slots * layer_count * turns;
   const int share = work > wave * turns ? turns : (int)((work + wave - 1) / wave);
