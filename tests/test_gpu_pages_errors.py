@@ -168,3 +168,25 @@ def test_inputs_may_be_dropped_while_another_stream_waits_to_read_them(call):
     used = {"write": old[:2], "attention": old[2:3], "resize": old[3:]}[call]
     assert not set(used) & {t.data_ptr() for t in new}
     assert c.poll_status() == 0
+
+
+def test_calls_on_a_named_stream_can_be_captured():
+    c, m = make(heads=2, group=2, pages=40, seqs=4, seq_pages=12)
+    k = torch.randn(2, 1, 2, 128, device=DEV).half()
+    q, seqs, lens = torch.randn(2, 1, 4, 128, device=DEV).half(), ints([0, 1]), ints([0, 0])
+    out = torch.zeros_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        lens.add_(1)
+        c.resize(seqs, lens, stream=side)
+        c.write(k, k.neg(), seqs, stream=side)             # the graph's own memory, dropped at once
+        c.attention(q, seqs, out=out, stream=side)
+    for i in range(1, 40):
+        graph.replay()
+        m.resize([0, 1], [i, i])
+        m.write([0, 1], [0, 1, 2], k.double().cpu().numpy(), -k.double().cpu().numpy())
+    torch.cuda.synchronize()
+    same_contents(c, m)
+    assert torch.equal(out, c.attention(q, seqs)) and c.poll_status() == 0
