@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
                 d = fmaxf(d, (float)max(is - 60, min(0, (int)(__float_as_uint(big) >> 23) - 127 - 90)));
                 low = (low & ~(255 << sh)) | max(0, is - __float2int_rd(d)) << sh;
               }
+              d = (m[nt][c] + d) - m[nt][c];                 // as the reference is rounded
               const float f = big > 0.f ? pa_ex2(-d) : 1.f;
               l[nt][c] = pa_scaled(l[nt][c], -d);
 #pragma unroll

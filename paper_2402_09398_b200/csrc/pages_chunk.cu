@@ -384,7 +384,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           // down by 40 below the highest, so that O has room, and no further than l has
           if (down) d = fmaxf(d, fmaxf(lowest - M, (float)min(0, (int)(__float_as_uint(l) >> 23) - 127 - 90)));
           if (up) sh->lowest[r] = fmaxf(lowest, ref + d - 40.f);
-          if (up || down) M = ref + d;
+          if (up || down) {
+            M = ref + d;
+            d = M - ref;                                  // as it is rounded
+          }
           if (none) d = 0.f;
           l = pa_scaled(l, -d);
           const float f = pa_ex2(-d);
