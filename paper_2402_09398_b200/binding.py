@@ -10,7 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
-from typing import Dict, Optional, Sequence
+from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -35,6 +35,7 @@ EXPORTED = [
     "less_pages_workspace_bytes", "less_pages_reset", "less_pages_resize", "less_pages_fork",
     "less_pages_trim", "less_pages_compact", "less_pages_write", "less_pages_attention",
     "less_pages_poll_status",
+    "less_beams_workspace_bytes", "less_beam_select",
 ]
 LESS_NOALLOC_MAX_ROWS = 65536
 LESS_ERR_NOALLOC_TOO_LARGE = -12
@@ -42,6 +43,10 @@ LESS_ERR_PAGES_EXHAUSTED = -13
 LESS_PAGES_E4M3 = 1
 LESS_PAGES_BF16 = 2
 LESS_PAGE_BLOCK = 16
+LESS_BEAMS_BF16 = 1
+LESS_BEAMS_F32 = 2
+LESS_BEAMS_MOST_BEAMS = 64
+LESS_BEAMS_MOST_KEEP = 128
 
 KERNEL_NAMES = ["feature_map", "decode", "rowstat", "colsum", "attn_out", "select", "build", "finalize",
                 "psi", "gather", "masked_pack", "masked_out"]
@@ -64,6 +69,12 @@ class less_pages(C.Structure):
                 ("page_tokens", C.c_int32), ("pages", C.c_int32), ("seqs", C.c_int32), ("seq_pages", C.c_int32),
                 ("flags", C.c_uint32), ("codes", C.c_void_p), ("amax", C.c_void_p), ("table", C.c_void_p),
                 ("lens", C.c_void_p), ("refs", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class less_beams(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("beams", C.c_int32), ("vocab", C.c_int32), ("keep", C.c_int32),
+                ("end_token", C.c_int32), ("flags", C.c_uint32), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_size_t)]
 
 
@@ -141,6 +152,11 @@ def lib() -> C.CDLL:
         fn = getattr(L, "less_pages_" + name)
         fn.restype = C.c_int
         fn.argtypes = [pg] + args
+    bm = C.POINTER(less_beams)
+    L.less_beams_workspace_bytes.restype = sz
+    L.less_beams_workspace_bytes.argtypes = [bm]
+    L.less_beam_select.restype = C.c_int
+    L.less_beam_select.argtypes = [bm, vp, i64, vp, vp, vp, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -277,6 +293,16 @@ def less_pages_attention(cache: less_pages, layer_begin, layer_count, n, seqs, s
 
 def less_pages_poll_status(cache: less_pages, stream) -> int:
     return lib().less_pages_poll_status(cache, stream)
+
+
+def less_beams_workspace_bytes(beams: less_beams) -> int:
+    return int(lib().less_beams_workspace_bytes(C.byref(beams)))
+
+
+def less_beam_select(beams: less_beams, logits, row_stride, scores, ended, out_scores, out_tokens, out_parents,
+                     out_ended, stream) -> int:
+    return lib().less_beam_select(beams, logits, row_stride, scores, ended, out_scores, out_tokens, out_parents,
+                                  out_ended, stream)
 
 
 # --------------------------------------------------------------------------- #
@@ -632,3 +658,82 @@ class PagedCache:
         """What the device found wrong since the last poll (0 = nothing); clears it."""
         with torch.cuda.device(self._index):
             return less_pages_poll_status(self.desc, _stream_ptr(stream))
+
+
+class BeamChoice(NamedTuple):
+    """What a step of beam search chose: tensors [groups, keep], the largest value first."""
+    scores: torch.Tensor       # fp32, the values
+    tokens: torch.Tensor       # int32, -1 = no candidate
+    parents: torch.Tensor      # int32, group * beams + beam
+    ended: torch.Tensor        # bool, token == end_token
+
+
+class BeamSelect:
+    """The selection of beam search (less_beams): holds its workspace and forwards calls.
+
+    `keep` candidates per group (default: as many as beams, so that the choice is the next step's state and
+    `parents.view(-1)` is what `PagedCache.reorder` and `LessContext.reorder` take).  Calls are asynchronous on the
+    current stream or on `stream`; one at a time per holder."""
+
+    def __init__(self, groups, beams, vocab, keep=None, dtype=torch.float16, end_token=-1, device="cuda"):
+        flags = {torch.float16: 0, torch.bfloat16: LESS_BEAMS_BF16, torch.float32: LESS_BEAMS_F32}.get(dtype)
+        if flags is None:
+            raise ValueError(f"dtype is torch.float16, torch.bfloat16 or torch.float32, not {dtype}")
+        keep = beams if keep is None else keep
+        desc = less_beams(groups, beams, vocab, keep, end_token, flags)
+        nbytes = less_beams_workspace_bytes(desc)
+        if nbytes == 0:
+            raise LessError(-1, "less_beams_workspace_bytes")
+        if not torch.cuda.is_available():
+            raise RuntimeError("the LESS library needs a CUDA device (there is no CPU path)")
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        desc.workspace, desc.workspace_bytes = self.workspace.data_ptr(), nbytes
+        self.desc, self.dtype, self.device = desc, dtype, self.workspace.device
+        self.groups, self.beams, self.vocab, self.keep = groups, beams, vocab, keep
+        self._index = self.device.index
+        self._streams = set()                            # those that the workspace is recorded on
+        self._lib = lib()
+
+    def _pairs(self, t: torch.Tensor, name: str, dtypes) -> int:
+        if t.dtype not in dtypes or t.get_device() != self._index or t.shape != (self.groups, self.beams) or \
+                not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous [{self.groups}, {self.beams}] tensor of {dtypes[0]} on {self.device} "
+                             "is wanted")
+        return t.data_ptr()
+
+    def select(self, logits, scores, ended=None, stream=None) -> BeamChoice:
+        """logits [groups, beams, vocab] (any stride from beam to beam), scores fp32 [groups, beams] (-inf: no such
+        beam), ended bool [groups, beams] or None: the `keep` best continuations of every group."""
+        if logits.dtype is not self.dtype or logits.get_device() != self._index or \
+                logits.shape != (self.groups, self.beams, self.vocab):
+            raise ValueError(f"logits: a [{self.groups}, {self.beams}, {self.vocab}] tensor of {self.dtype} on "
+                             f"{self.device} is wanted")
+        s0, s1, s2 = logits.stride()
+        stride = s1 if self.beams > 1 else (s0 if self.groups > 1 else self.vocab)
+        if (s2 != 1 and self.vocab > 1) or (self.groups > 1 and s0 != self.beams * stride) or stride < self.vocab:
+            raise ValueError("logits: rows of contiguous elements, at one distance from beam to beam, are wanted")
+        scores_ptr = self._pairs(scores, "scores", (torch.float32,))
+        ended_ptr = None if ended is None else self._pairs(ended, "ended", (torch.bool, torch.uint8))
+        if ended is not None and self.desc.end_token < 0:
+            raise ValueError("beams that have ended need an end_token")
+        with torch.cuda.device(self._index) if torch._C._cuda_getDevice() != self._index else contextlib.nullcontext():
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                shape = (self.groups, self.keep)         # memory of the stream that writes it
+                out = BeamChoice(torch.empty(shape, dtype=torch.float32, device=self.device),
+                                 torch.empty(shape, dtype=torch.int32, device=self.device),
+                                 torch.empty(shape, dtype=torch.int32, device=self.device),
+                                 torch.empty(shape, dtype=torch.bool, device=self.device))
+            if stream is not None:
+                for t in (logits, scores, ended):
+                    if t is not None:
+                        t.record_stream(stream)
+                if stream.cuda_stream not in self._streams:
+                    self._streams.add(stream.cuda_stream)
+                    self.workspace.record_stream(stream)
+            rc = self._lib.less_beam_select(
+                self.desc, logits.data_ptr(), stride, scores_ptr, ended_ptr, out.scores.data_ptr(),
+                out.tokens.data_ptr(), out.parents.data_ptr(), out.ended.data_ptr(),
+                torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream)
+        if rc != LESS_OK:
+            raise LessError(rc, "less_beam_select")
+        return out
