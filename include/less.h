@@ -242,7 +242,8 @@ enum {
   LESS_KERNEL_GATHER = 9,
   LESS_KERNEL_MASKED_PACK = 10,
   LESS_KERNEL_MASKED_OUT = 11,
-  LESS_KERNEL_COUNT = 12
+  LESS_KERNEL_REORDER = 12,
+  LESS_KERNEL_COUNT = 13
 };
 int less_profile(less_ctx* ctx, int enable);
 int less_profile_read(less_ctx* ctx, float* ms_total_host, int64_t* launches_host);
@@ -267,6 +268,29 @@ int less_export_state(less_ctx* ctx, const int32_t* inst_host, int32_t n, void* 
                       size_t bytes, void* cuda_stream);
 int less_import_state(less_ctx* ctx, const int32_t* inst_host, int32_t n, const void* host_buf,
                       size_t bytes, void* cuda_stream);
+
+/* Beam search: row b of the batch becomes what row parents[b] was - slots, scores, psi, H and z of all layers and heads -
+ * in place.  parents: device int32 [batch] (what less_beam_select gives); the batch consists of groups of `beams` rows
+ * (beams <= 3072, batch a multiple), and a row's parent is of its own group: where one is not, no row changes and the
+ * status word reads LESS_ERR_DEVICE_BOUNDS.  The position is the context's and stays.  Asynchronous; can be captured. */
+int less_reorder(less_ctx* ctx, int32_t beams, const int32_t* parents, void* cuda_stream);
+
+/* Where the state lies in the arena, for copies on the device (instances in the order b, layer, head; N = heavy + recent
+ * slots, of which the first `count` are live).  Who writes here does so in the order of the stream that the context's
+ * calls run on.  The position is not in it. */
+typedef struct less_state {
+  void* K;            /* fp16 [I, N, D] */
+  void* V;            /* fp16 [I, N, D] */
+  int32_t* pos;       /* [I, slot_pitch]: absolute positions */
+  float* acc;         /* [I, slot_pitch]: H2O scores */
+  float* psi;         /* [I, N, R] */
+  float* H;           /* [I, R, D] */
+  float* z;           /* [I, R] */
+  int32_t* count;     /* [I]: live slots */
+  int32_t slots;      /* N */
+  int32_t slot_pitch; /* N rounded up to a multiple of 4 */
+} less_state;
+int less_state_view(less_ctx* ctx, less_state* out);
 
 /* phi(q_t) and psi(k_t) of the last decode step: host float [B*L*H*group, R]
  * and [B*L*H, R] (either may be NULL).  Synchronises the stream. */
@@ -384,6 +408,14 @@ int less_pages_resize(const less_pages* cache, int32_t n, const int32_t* seqs, c
  * filled is copied to the lowest free page (in the order of the list).  A source may be listed often, a destination
  * once and not as a source.  All or nothing: LESS_ERR_PAGES_EXHAUSTED, LESS_ERR_BAD_STATE. */
 int less_pages_fork(const less_pages* cache, int32_t n, const int32_t* src, const int32_t* dst, void* cuda_stream);
+
+/* A step of beam search: entry i, sequence seqs[i], becomes what entry parents[i], sequence seqs[parents[i]], was.  Whole
+ * pages are shared.  Of the children of a sequence one takes over the page that is still being filled (the sequence itself
+ * if it is its own child, else the first of the list), the others get copies of its 16-token blocks in use, in the lowest
+ * free pages, in the order of the list; pages that nobody holds any longer are released first.  A sequence is listed
+ * once; n <= seqs and 16384.  All or nothing: LESS_ERR_PAGES_EXHAUSTED, LESS_ERR_BAD_STATE (a sequence listed twice),
+ * LESS_ERR_DEVICE_BOUNDS. */
+int less_pages_reorder(const less_pages* cache, int32_t n, const int32_t* seqs, const int32_t* parents, void* cuda_stream);
 
 /* Releases the pages of the listed sequences that hold neither one of the first `sinks` tokens nor one of the last
  * `window` (>= 1): what less_pages_attention with these arguments never reads again. */

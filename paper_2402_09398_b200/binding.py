@@ -35,7 +35,8 @@ EXPORTED = [
     "less_pages_workspace_bytes", "less_pages_reset", "less_pages_resize", "less_pages_fork",
     "less_pages_trim", "less_pages_compact", "less_pages_write", "less_pages_attention",
     "less_pages_poll_status",
-    "less_beams_workspace_bytes", "less_beam_select",
+    "less_beams_workspace_bytes", "less_beam_select", "less_reorder", "less_state_view",
+    "less_pages_reorder",
 ]
 LESS_NOALLOC_MAX_ROWS = 65536
 LESS_ERR_NOALLOC_TOO_LARGE = -12
@@ -49,7 +50,7 @@ LESS_BEAMS_MOST_BEAMS = 64
 LESS_BEAMS_MOST_KEEP = 128
 
 KERNEL_NAMES = ["feature_map", "decode", "rowstat", "colsum", "attn_out", "select", "build", "finalize",
-                "psi", "gather", "masked_pack", "masked_out"]
+                "psi", "gather", "masked_pack", "masked_out", "reorder"]
 
 
 class less_config(C.Structure):
@@ -62,6 +63,12 @@ class less_config(C.Structure):
 class less_weights(C.Structure):
     _fields_ = [("w_phi1", C.c_void_p), ("w_phi2", C.c_void_p), ("w_psi1", C.c_void_p),
                 ("w_psi2", C.c_void_p), ("w_psi3", C.c_void_p), ("psi_scale", C.c_void_p)]
+
+
+class less_state(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("pos", C.c_void_p), ("acc", C.c_void_p), ("psi", C.c_void_p),
+                ("H", C.c_void_p), ("z", C.c_void_p), ("count", C.c_void_p), ("slots", C.c_int32),
+                ("slot_pitch", C.c_int32)]
 
 
 class less_pages(C.Structure):
@@ -145,6 +152,7 @@ def lib() -> C.CDLL:
     L.less_pages_workspace_bytes.restype = sz
     L.less_pages_workspace_bytes.argtypes = [pg]
     for name, args in (("reset", [vp]), ("resize", [i32, vp, vp, vp]), ("fork", [i32, vp, vp, vp]),
+                       ("reorder", [i32, vp, vp, vp]),
                        ("trim", [i32, vp, i32, i32, vp]), ("compact", [vp]),
                        ("write", [i32, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp]),
                        ("attention", [i32, i32, i32, vp, vp, i32, i32, vp, i64, i32, i32, C.c_float, vp, vp]),
@@ -152,6 +160,10 @@ def lib() -> C.CDLL:
         fn = getattr(L, "less_pages_" + name)
         fn.restype = C.c_int
         fn.argtypes = [pg] + args
+    L.less_reorder.restype = C.c_int
+    L.less_reorder.argtypes = [vp, i32, vp, vp]
+    L.less_state_view.restype = C.c_int
+    L.less_state_view.argtypes = [vp, C.POINTER(less_state)]
     bm = C.POINTER(less_beams)
     L.less_beams_workspace_bytes.restype = sz
     L.less_beams_workspace_bytes.argtypes = [bm]
@@ -231,6 +243,15 @@ def less_masked_attention(ctx, layer_begin, layer_count, seq_len, Q, K, V, exact
     return lib().less_masked_attention(ctx, layer_begin, layer_count, seq_len, Q, K, V, exact_until, out, stream)
 
 
+def less_reorder(ctx, beams, parents, stream) -> int:
+    return lib().less_reorder(ctx, beams, parents, stream)
+
+
+def less_state_view(ctx):
+    out = less_state()
+    return lib().less_state_view(ctx, C.byref(out)), out
+
+
 def less_read_feature_maps(ctx, phi_ptr, psi_ptr, stream) -> int:
     return lib().less_read_feature_maps(ctx, phi_ptr, psi_ptr, stream)
 
@@ -269,6 +290,10 @@ def less_pages_resize(cache: less_pages, n, seqs, lens, stream) -> int:
 
 def less_pages_fork(cache: less_pages, n, src, dst, stream) -> int:
     return lib().less_pages_fork(cache, n, src, dst, stream)
+
+
+def less_pages_reorder(cache: less_pages, n, seqs, parents, stream) -> int:
+    return lib().less_pages_reorder(cache, n, seqs, parents, stream)
 
 
 def less_pages_trim(cache: less_pages, n, seqs, sinks, window, stream) -> int:
@@ -454,6 +479,35 @@ class LessContext:
         _check(less_import_state(self.ctx, inst.ctypes.data, len(inst), buf.ctypes.data, buf.nbytes,
                                  _stream_ptr(stream)), "less_import_state")
 
+    def reorder(self, parents, beams=None, stream=None):
+        """Row b of the batch becomes what row parents[b] was (int32 [batch] on the device, or [groups, beams]); parents
+        are of the row's own group of `beams` rows (default: the whole batch is one group)."""
+        if parents.dtype is not torch.int32 or parents.device != self.arena.device or \
+                parents.numel() != self.cfg.batch or not parents.is_contiguous():
+            raise ValueError(f"parents: {self.cfg.batch} contiguous int32 values on {self.arena.device} are wanted")
+        if stream is not None:
+            parents.record_stream(stream)
+        _check(less_reorder(self.ctx, self.cfg.batch if beams is None else beams, _ptr(parents), _stream_ptr(stream)),
+               "less_reorder")
+
+    def state_tensors(self) -> Dict[str, torch.Tensor]:
+        """The state where it lies (less_state_view), as tensors [batch, layers, heads, ...]: K, V, pos, acc, psi, H, z,
+        count."""
+        rc, v = less_state_view(self.ctx)
+        _check(rc, "less_state_view")
+        c, N, P = self.cfg, v.slots, v.slot_pitch
+        out = {}
+        for name, dtype, tail in (("K", torch.float16, (N, c.head_dim)), ("V", torch.float16, (N, c.head_dim)),
+                                  ("pos", torch.int32, (P,)), ("acc", torch.float32, (P,)),
+                                  ("psi", torch.float32, (N, c.rank)), ("H", torch.float32, (c.rank, c.head_dim)),
+                                  ("z", torch.float32, (c.rank,)), ("count", torch.int32, ())):
+            shape = (c.batch, c.layers, c.heads) + tail
+            nbytes = int(np.prod(shape)) * dtype.itemsize
+            at = getattr(v, name) - self.arena.data_ptr()
+            out[name] = self.arena[at:at + nbytes].view(dtype).view(shape)
+        out["pos"], out["acc"] = out["pos"][..., :N], out["acc"][..., :N]
+        return out
+
     def read_feature_maps(self, stream=None):
         R = self.cfg.rank
         phi = np.zeros((self.instances * self.group, R), dtype=np.float32)
@@ -614,6 +668,13 @@ class PagedCache:
         n = src.shape[0]
         self._call(self._lib.less_pages_fork, "less_pages_fork", n, self._list(src, "src"), self._list(dst, "dst", n),
                    stream=stream, keep=(src, dst))
+
+    def reorder(self, seqs, parents, stream=None):
+        """A step of beam search: sequence seqs[i] becomes what sequence seqs[parents[i]] was (whole pages shared, copies
+        of the last page's blocks for all children but one)."""
+        n = seqs.shape[0]
+        self._call(self._lib.less_pages_reorder, "less_pages_reorder", n, self._list(seqs, "seqs"),
+                   self._list(parents, "parents", n), stream=stream, keep=(seqs, parents))
 
     def trim(self, seqs, sinks, window, stream=None):
         """Releases the pages between the first `sinks` tokens and the last `window`."""
