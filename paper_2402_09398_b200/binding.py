@@ -36,7 +36,7 @@ EXPORTED = [
     "less_pages_trim", "less_pages_compact", "less_pages_write", "less_pages_attention",
     "less_pages_poll_status",
     "less_beams_workspace_bytes", "less_beam_select", "less_reorder", "less_state_view",
-    "less_pages_reorder",
+    "less_pages_reorder", "less_pages_shared_attention",
 ]
 LESS_NOALLOC_MAX_ROWS = 65536
 LESS_ERR_NOALLOC_TOO_LARGE = -12
@@ -156,6 +156,8 @@ def lib() -> C.CDLL:
                        ("trim", [i32, vp, i32, i32, vp]), ("compact", [vp]),
                        ("write", [i32, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp]),
                        ("attention", [i32, i32, i32, vp, vp, i32, i32, vp, i64, i32, i32, C.c_float, vp, vp]),
+                       ("shared_attention", [i32, i32, i32, vp, vp, i32, i32, i32, vp, i32, vp, i64, i32, i32, C.c_float,
+                                             vp, vp]),
                        ("poll_status", [vp])):
         fn = getattr(L, "less_pages_" + name)
         fn.restype = C.c_int
@@ -314,6 +316,12 @@ def less_pages_attention(cache: less_pages, layer_begin, layer_count, n, seqs, s
                          window, sinks, scale, out, stream) -> int:
     return lib().less_pages_attention(cache, layer_begin, layer_count, n, seqs, starts, rows, max_new, q, q_stride,
                                       window, sinks, scale, out, stream)
+
+
+def less_pages_shared_attention(cache: less_pages, layer_begin, layer_count, n, seqs, starts, rows, max_new, ngroups,
+                                groups, max_group, q, q_stride, window, sinks, scale, out, stream) -> int:
+    return lib().less_pages_shared_attention(cache, layer_begin, layer_count, n, seqs, starts, rows, max_new, ngroups,
+                                             groups, max_group, q, q_stride, window, sinks, scale, out, stream)
 
 
 def less_pages_poll_status(cache: less_pages, stream) -> int:
@@ -698,21 +706,41 @@ class PagedCache:
                    None if starts is None else self._list(starts, "starts", n + 1), rows, k.data_ptr(), ks,
                    v.data_ptr(), vs, stream=stream, keep=(k, v, seqs, starts))
 
+    def _out(self, q, out, stream):
+        if out is None:                                  # memory of the stream that writes it
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                return torch.empty_like(q, memory_format=torch.contiguous_format)
+        if out.shape != q.shape or out.dtype != self.dtype or out.device != self.device or not out.is_contiguous():
+            raise ValueError("out: a contiguous tensor of q's shape and type is wanted")
+        return out
+
     def attention(self, q, seqs, starts=None, max_new=None, layer_begin=0, window=0, sinks=0, scale=None, out=None,
                   stream=None):
         """q [rows, layers, heads * group, D]: attention of the last tokens of the listed sequences over the cache.
         max_new: the most new tokens of a sequence, as far as the host knows (default: all rows)."""
         n = seqs.shape[0]
         rows, layers, qs = self._rows(q, "q", self.heads * self.group)
-        if out is None:                                  # memory of the stream that writes it
-            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-                out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        elif out.shape != q.shape or out.dtype != self.dtype or out.device != self.device or not out.is_contiguous():
-            raise ValueError("out: a contiguous tensor of q's shape and type is wanted")
+        out = self._out(q, out, stream)
         self._call(self._lib.less_pages_attention, "less_pages_attention", layer_begin, layers, n,
                    self._list(seqs, "seqs"), None if starts is None else self._list(starts, "starts", n + 1), rows,
                    max(1, rows if max_new is None else max_new), q.data_ptr(), qs, window, sinks,
                    self.scale if scale is None else scale, out.data_ptr(), stream=stream, keep=(q, seqs, starts, out))
+        return out
+
+    def shared_attention(self, q, seqs, groups, starts=None, max_new=None, max_group=None, layer_begin=0, window=0,
+                         sinks=0, scale=None, out=None, stream=None):
+        """`attention` with the pages that the sequences of a group have in common read once for the group: the listed
+        sequences groups[g] .. groups[g + 1] (int32 [groups + 1], from 0 to all of them) are group g.
+        max_group: the most new tokens of a group, as far as the host knows (default: all rows)."""
+        n, ngroups = seqs.shape[0], groups.shape[0] - 1
+        rows, layers, qs = self._rows(q, "q", self.heads * self.group)
+        out = self._out(q, out, stream)
+        self._call(self._lib.less_pages_shared_attention, "less_pages_shared_attention", layer_begin, layers, n,
+                   self._list(seqs, "seqs"), None if starts is None else self._list(starts, "starts", n + 1), rows,
+                   max(1, rows if max_new is None else max_new), ngroups, self._list(groups, "groups"),
+                   max(1, rows if max_group is None else max_group), q.data_ptr(), qs, window, sinks,
+                   self.scale if scale is None else scale, out.data_ptr(), stream=stream,
+                   keep=(q, seqs, starts, groups, out))
         return out
 
     def poll_status(self, stream=None) -> int:

@@ -1,5 +1,5 @@
 // The paged 8-bit cache: parameters, index arithmetic, the stored tile order and the code formats, shared by
-// pages_ops.cu (maps and page moves), pages_write.cu and pages_attn.cu.
+// pages_ops.cu (maps and page moves), pages_write.cu, pages_attn.cu, pages_chunk.cu and pages_shared.cu.
 //
 // Order of a tile (16 tokens x D dimensions of one head, 16 * D bytes).  A tile lies in memory as a warp consumes
 // it: 16-byte pieces, piece = 32 * c + 4 * g + t of lane (g = lane / 4, t = lane % 4), so that a warp-wide 16-byte
@@ -39,6 +39,7 @@ struct PgParams {
   int32_t* fresh;          // [max(seqs, pages)]
   int32_t* counters;       // [kPgCounters] zero between calls
   float* partial;          // partial results of the step kernel
+  int4* shared;            // [seqs] of entries, [2 seqs] of groups: what attention over shared pages has found (pages_attn.cuh)
 };
 
 constexpr int kPgCounters = 1024;

@@ -1,4 +1,4 @@
-// What the two attention kernels over the paged 8-bit cache share (pages_attn.cu, pages_chunk.cu).
+// What the two attention kernels over the paged 8-bit cache share (pages_step.cuh, pages_chunk.cuh).
 #pragma once
 
 #include "pages.cuh"
@@ -15,7 +15,18 @@ struct PaArgs {
   int max_rows;                  // entries with more rows (tokens x query heads of a group) are not this kernel's
   int window, sinks;             // window 0 = all
   float scale;
+  // attention of sequences that share their first pages (pages_shared.cu); not read otherwise
+  const int4* groups;            // two of each group: {sequence, first row, rows, 0}, {sb, wb, eb, 0} of what it shares
+  const int4* entries;           // of each entry: {sb, wb, eb, 0} of its group
+  float* parts;                  // [splits][rows * nl * heads * group][D]: results over the shared blocks
+  float2* weights;               // [splits][rows * nl * heads * group]: (reference, sum); not written for entries that share nothing
+  int splits;
+  int out_layers;                // layers between the rows of `out`
 };
+
+// What a launch is for: all that an entry sees; the blocks that all entries of a group see (then the group is the entry,
+// and results are parts); what of an entry's blocks is not among those (then the parts are joined).
+enum PaMode { kAll, kShared, kRest };
 
 // the 16-token blocks that the tokens of an entry see: [0, sb) and [wb, eb)
 struct Blocks {
@@ -33,6 +44,54 @@ __device__ __forceinline__ Blocks visible_blocks(const PaArgs& a, int len, int c
   }
   return b;
 }
+
+// Shared blocks, all of them visible to every token of a group: [0, sb) and [wb, eb).  An entry's rest is what remains of
+// its own [0, sb) and [wb, eb): three stretches (sb and wb of a group are at most, at least those of its entries).
+struct RestBlocks {
+  int a, na, b, nb, c, nc;
+  __device__ __forceinline__ int count() const { return na + nb + nc; }
+  __device__ __forceinline__ int at(int u) const { return u < na ? a + u : u < na + nb ? b + u - na : c + u - na - nb; }
+};
+__device__ __forceinline__ RestBlocks rest_blocks(const Blocks& all, const int4& shared) {
+  RestBlocks r;
+  r.a = shared.x;
+  r.na = max(0, all.sb - shared.x);
+  r.b = all.wb;
+  r.nb = max(0, shared.y - all.wb);
+  r.c = max(shared.z, all.wb);
+  r.nc = max(0, all.eb - r.c);
+  return r;
+}
+
+// entry i and the blocks that it is about
+template <PaMode MODE>
+struct PaWork;
+template <>
+struct PaWork<kAll> {
+  typedef Blocks B;
+  static __device__ __forceinline__ PgEntry entry(const PgParams& p, const PaArgs& a, int i) { return pg_entry(p, a.seqs, a.starts, a.rows, i); }
+  static __device__ __forceinline__ B blocks(const PaArgs& a, int, const PgEntry& e) { return visible_blocks(a, e.len, e.count); }
+};
+template <>
+struct PaWork<kShared> {
+  typedef Blocks B;
+  static __device__ __forceinline__ PgEntry entry(const PgParams&, const PaArgs& a, int i) {
+    const int4 g = __ldcg(a.groups + 2 * i), b = __ldcg(a.groups + 2 * i + 1);
+    return {g.x, g.y, g.z, b.z * kPageBlock + g.z};       // every token lies behind the shared ones
+  }
+  static __device__ __forceinline__ B blocks(const PaArgs& a, int i, const PgEntry&) {
+    const int4 b = __ldcg(a.groups + 2 * i + 1);
+    return {b.x, b.y, b.z};
+  }
+};
+template <>
+struct PaWork<kRest> {
+  typedef RestBlocks B;
+  static __device__ __forceinline__ PgEntry entry(const PgParams& p, const PaArgs& a, int i) { return pg_entry(p, a.seqs, a.starts, a.rows, i); }
+  static __device__ __forceinline__ B blocks(const PaArgs& a, int i, const PgEntry& e) {
+    return rest_blocks(visible_blocks(a, e.len, e.count), __ldcg(a.entries + i));
+  }
+};
 
 __device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
   uint64_t r;
@@ -124,5 +183,14 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 f) {
 constexpr int kStepRows = 32, kStepRowsFew = 16;
 
 int launch_pages_chunk(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);
+
+// host: checks the arguments of an attention call and fills `p` and `a`; LESS_OK with a->n == 0: there is nothing to do
+int pa_args(const less_pages* d, int32_t layer_begin, int32_t layer_count, int32_t n, const int32_t* seqs, const int32_t* starts,
+            int32_t rows, int32_t max_new, const void* q, int64_t q_stride, int32_t window, int32_t sinks, float scale, void* out,
+            PgParams* p, PaArgs* a);
+int launch_pages_attention(const PgParams& p, PaArgs a, int dim, uint32_t flags, int32_t max_new, cudaStream_t s);
+// results of the groups' tokens over the blocks that they share, into a.parts (pages_prefix.cu)
+int launch_pages_prefix(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, int rows, bool many, size_t room, int counters,
+                        cudaStream_t s);
 
 }  // namespace less

@@ -589,10 +589,10 @@ __global__ void __launch_bounds__(128) pages_trim_kernel(PgParams p, int n, cons
 // host
 // ---------------------------------------------------------------------------
 struct PgLayout {
-  size_t moves, mark, off, fresh, counters, partial, total;
+  size_t moves, mark, off, fresh, counters, partial, shared, total;
 };
 
-// the workspace: status | counters | plan | partial results of the step kernel
+// the workspace: status | counters | plan | partial results of attention | what its entries share
 static PgLayout pg_layout(const less_pages* d) {
   PgLayout l;
   size_t at = 256;
@@ -608,6 +608,7 @@ static PgLayout pg_layout(const less_pages* d) {
   l.off = take((size_t)d->seqs * 4);
   l.fresh = take(most * 4);
   l.partial = take(LESS_PAGES_PARTIAL_BYTES);
+  l.shared = take((size_t)d->seqs * 48);
   l.total = at;
   return l;
 }
@@ -657,6 +658,7 @@ int pg_view(const less_pages* d, PgParams* p) {
   p->off = (int32_t*)(w + l.off);
   p->fresh = (int32_t*)(w + l.fresh);
   p->partial = (float*)(w + l.partial);
+  p->shared = (int4*)(w + l.shared);
   return LESS_OK;
 }
 

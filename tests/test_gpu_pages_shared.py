@@ -1,0 +1,239 @@
+"""Attention for groups of sequences that share their first pages, against the 64-bit model of pages_ref.py (which knows
+nothing of groups) within its bound, and beside ordinary attention."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_pages import DEV, HALF_STEP, ints, make
+import pages_ref
+
+pytestmark = pytest.mark.gpu
+
+
+def family(groups, seed=0, spare=2, **kw):
+    """groups: of each (tokens in common, [tokens of their own ...]).  Sequences in random rows of the table; the pages in
+    common are forks'.  Returns cache, model, the listed sequences, the group bounds."""
+    pt = kw.get("pt", 64)
+    rng = np.random.default_rng(seed)
+    n = sum(len(t) for _, t in groups)
+    room = max(-(-(pre + max(t)) // pt) for pre, t in groups)
+    pages = sum(-(-(pre + x) // pt) for pre, t in groups for x in t) + 3
+    c, m = make(pages=pages, seqs=n + spare, seq_pages=room, **kw)
+    rows = rng.permutation(n + spare)[:n].tolist()
+    bounds, at = [0], 0
+    for pre, tails in groups:
+        first, others = rows[at], rows[at + 1:at + len(tails)]
+        c.resize(ints([first]), ints([pre]))
+        assert m.resize([first], [pre])
+        if others:
+            c.fork(ints([first] * len(others)), ints(others))
+            m.fork([first] * len(others), others)
+        at += len(tails)
+        bounds.append(at)
+    lens = [pre + x for pre, tails in groups for x in tails]
+    c.resize(ints(rows), ints(lens))
+    assert m.resize(rows, lens)
+    codes = np.clip(np.rint(rng.normal(size=m.codes.shape) * 36), -127, 127)
+    m.codes[:] = codes.astype(np.int64) % 256 if m.fmt == "int8" else pages_ref.encode(codes * 3.0, "e4m3")
+    m.amax[:] = np.float32(rng.uniform(2.5, 4.0, m.amax.shape) * np.where(rng.random(m.amax.shape) < 0.02, 4, 1))
+    if m.fmt == "e4m3":                                    # what no token owns holds NaN
+        own = np.zeros((len(m.refs), pt), bool)
+        for s, n_tok in zip(rows, lens):
+            for j in range(n_tok):
+                own[m.table[s, j // pt], j % pt] = True
+        for page, tok in zip(*np.nonzero(~own)):
+            for which in (0, 1):
+                m.codes[:, page, :, which, tok // 16 * 16 * m.D + m.at[which][tok % 16]] = 0x7f
+    c.codes.copy_(torch.from_numpy(m.codes))
+    c.amax.copy_(torch.from_numpy(m.amax))
+    return c, m, rows, bounds
+
+
+def attend(c, m, seqs, bounds, new=None, tail=3, seed=1, max_new=None, max_group=None, window=0, sinks=0, layers=None,
+           layer_begin=0, q=None, slack=0.0, status=0):
+    """One call against the model; `tail` rows behind the last entry stay as they were.  The joining of parts rounds twice
+    more: 2^-22 of the largest |v|, which the model's 2^-19 covers."""
+    rng = np.random.default_rng(seed)
+    new = [1] * len(seqs) if new is None else new
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(int).tolist()
+    layers = m.L - layer_begin if layers is None else layers
+    shape = (starts[-1] + tail, layers, m.H * m.G, m.D)
+    q = torch.from_numpy(rng.normal(size=shape)).to(c.dtype) if q is None else q
+    out = torch.full(shape, 7.0, dtype=c.dtype, device=DEV)
+    one = all(x == 1 for x in new) and not tail
+    c.shared_attention(q.to(DEV), ints(seqs), ints(bounds), None if one else ints(starts), max_new=max_new or max(new),
+                       max_group=max_group, layer_begin=layer_begin, window=window, sinks=sinks, out=out)
+    got = out.double().cpu().numpy()
+    rows = starts[-1]
+    assert (got[rows:] == 7.0).all()
+    want, bound = m.attention(q[:rows].double().numpy(), seqs, starts, layer_begin, window, sinks)
+    if not m.bf16 and (shape[0] if max_group is None else max_group) * m.G > 16:
+        # by the caller's hint the groups are the many-token kernel's, which rounds probabilities to fp16 once: as for any
+        # entry of more than 16 rows in the model, |p' - p| <= 2^-11 p + 2^-25 moves the sum of p' v by at most
+        # (2^-11 + n 2^-25) max |v| times the sum of p
+        most = np.abs(m.val[np.isfinite(m.val)]).max() * np.nanmax(m.amax) / pages_ref.TOP[m.fmt]
+        bound = bound + (2.0 ** -11 + int(m.lens[seqs].max()) * 2.0 ** -25) * most
+    tol = HALF_STEP[c.dtype] * np.abs(want) + bound * (1 + slack) + 2.0 ** -24
+    err = np.abs(got[:rows] - want)
+    assert np.isfinite(got).all()
+    worst = np.unravel_index(np.argmax(err - tol), err.shape) if err.size else None
+    assert (err <= tol).all(), (worst, got[:rows][worst], want[worst], tol[worst])
+    assert c.poll_status() == status
+    return got
+
+
+KINDS = [("int8", torch.float16), ("e4m3", torch.float16), ("int8", torch.bfloat16), ("e4m3", torch.bfloat16)]
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("dim,pt,heads,group", [(128, 64, 2, 1), (64, 16, 1, 4), (128, 128, 1, 8), (64, 32, 3, 5)])
+def test_shapes(fmt, dtype, dim, pt, heads, group):
+    c, m, seqs, b = family([(300, [1, 5, 40, 130]), (20, [1, 1]), (129, [3]), (10, [20, 30, 9]), (64, [1, 64, 65])],
+                           dim=dim, pt=pt, heads=heads, group=group, fmt=fmt, dtype=dtype)
+    attend(c, m, seqs, b)
+    attend(c, m, seqs, b, tail=0)
+    attend(c, m, seqs, b, new=[1, 3, 2, 5, 1, 1, 3, 2, 4, 1, 1, 6, 1])
+
+
+@pytest.mark.parametrize("group", [1, 4])
+@pytest.mark.parametrize("each", [2, 9, 33, 70, 150])
+def test_rows_of_a_group(each, group):
+    """From a few rows to several tiles of the many-token kernel, with and without its keys split."""
+    tails = [1 + 7 * i % 60 for i in range(each)]
+    c, m, seqs, b = family([(500, tails), (1100, tails[:each // 2 + 1])], dim=64, pt=32, heads=2, group=group)
+    attend(c, m, seqs, b)
+    c, m, seqs, b = family([(1500, tails)], heads=1, group=group, dtype=torch.bfloat16, fmt="e4m3")
+    attend(c, m, seqs, b, max_group=each)
+
+
+def test_hints_that_are_wrong():
+    c, m, seqs, b = family([(400, [5, 9, 30, 70]), (90, [6, 6])], heads=2, group=4)
+    new = [3, 5, 1, 4, 6, 2]
+    for max_new, max_group in ((1, 1), (1, 1000), (6, 1), (200, 5), (32, 40)):
+        attend(c, m, seqs, b, new=new, max_new=max_new, max_group=max_group)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (100, 0), (100, 4), (37, 33), (64, 16), (1000, 20), (5000, 0), (300, 200)])
+@pytest.mark.parametrize("group", [2, 8])
+def test_windows(window, sinks, group):
+    c, m, seqs, b = family([(700, [1, 50, 90, 200]), (40, [1, 30]), (333, [20] * 5), (64, [600, 5])], heads=1, group=group,
+                           dim=64, pt=32)
+    attend(c, m, seqs, b, window=window, sinks=sinks)
+    attend(c, m, seqs, b, new=[1, 4, 2, 1, 1, 3, 1, 2, 3, 4, 5, 7, 1], window=window, sinks=sinks)
+
+
+def test_tokens_that_are_themselves_in_shared_pages():
+    """Forks that have not parted: the new tokens' own keys lie in pages in common, or right at their end."""
+    for pre in (16, 63, 64, 65, 127, 128, 129, 192):
+        c, m = make(heads=2, pages=30, seqs=5, seq_pages=5, pt=64)
+        c.resize(ints([1]), ints([pre]))
+        m.resize([1], [pre])
+        rng = np.random.default_rng(pre)
+        m.codes[:] = rng.integers(0, 255, m.codes.shape)
+        m.amax[:] = np.float32(rng.uniform(1, 2, m.amax.shape))
+        c.codes.copy_(torch.from_numpy(m.codes))
+        c.amax.copy_(torch.from_numpy(m.amax))
+        c.fork(ints([1, 1]), ints([3, 0]))
+        m.fork([1, 1], [3, 0])
+        for new in ([1, 1, 1], [2, 1, 5], [16, 16, 16]):
+            attend(c, m, [3, 1, 0], [0, 3], new=new)
+        attend(c, m, [3, 3, 1, 1], [0, 2, 4])              # a sequence listed twice shares all with itself
+        attend(c, m, [0, 1], [0, 1, 2])
+
+
+def test_groups_that_share_nothing():
+    c, m, seqs, b = family([(5, [9, 60]), (80, [4]), (0, [30, 31, 0]), (33, [1, 1])], heads=2, pt=64)
+    attend(c, m, seqs, [0, len(seqs)], new=[1, 2, 1, 4, 1, 0, 1, 1])    # one group of strangers, one without tokens
+    attend(c, m, seqs, b, new=[0, 2, 1, 0, 0, 0, 1, 0])
+    attend(c, m, seqs, [0, 0, 2, 2, 3, 8], new=[1, 2, 1, 4, 1, 0, 1, 1])   # groups without entries
+
+
+def test_more_new_tokens_than_a_sequence_has():
+    c, m, seqs, b = family([(3, [2, 4]), (100, [5, 6])], heads=1, pt=16, dim=64)
+    starts = [0, 9, 10, 11, 12]
+    q = torch.randn(12, 1, 1, 64).half()
+    got = c.shared_attention(q.to(DEV), ints(seqs), ints(b), ints(starts)).double().cpu().numpy()
+    want = c.attention(q.to(DEV), ints(seqs), ints(starts)).double().cpu().numpy()
+    assert np.abs(got - want).max() < 2e-3 and (got[:4] == 0).all() and c.poll_status() == 0
+
+
+def test_trimmed_and_reordered_beams():
+    c, m, seqs, b = family([(700, [3, 40, 41]), (300, [7, 9])], heads=2, pt=32)
+    c.trim(ints(seqs), 32, 150)
+    m.trim(seqs, 32, 150)
+    attend(c, m, seqs, b, window=150, sinks=20)
+    attend(c, m, seqs, b)                                  # what is not there any more is not seen
+
+
+def test_many_layers_pass_in_turns():
+    """More rows than there is room for the parts of: layers in several turns, and a layer that does not fit."""
+    c, m, seqs, b = family([(40, [1] * 60), (30, [2] * 60)], heads=16, group=1, dim=128, pt=16, layers=40)
+    q = torch.randn(120, 40, 16, 128, dtype=torch.float16, device=DEV)
+    got = c.shared_attention(q, ints(seqs), ints(b))
+    want = c.attention(q, ints(seqs))
+    assert (got - want).abs().max() < 4e-3 and c.poll_status() == 0
+    assert torch.equal(c.shared_attention(q[:, 3:7].contiguous(), ints(seqs), ints(b), layer_begin=3),
+                       c.shared_attention(q[:, 3:7], ints(seqs), ints(b), layer_begin=3))
+    c, m, seqs, b = family([(40, [30] * 60)], heads=32, group=4, dim=64, pt=16)
+    new = [20] * 60
+    q = torch.randn(1200, 1, 128, 64, dtype=torch.float16, device=DEV)
+    starts = ints(np.arange(61) * 20)
+    got = c.shared_attention(q, ints(seqs), ints(b), starts, max_new=20)
+    assert (got - c.attention(q, ints(seqs), starts, max_new=20)).abs().max() < 4e-3 and c.poll_status() == 0
+
+
+def test_lists_that_are_wrong():
+    c, m, seqs, b = family([(200, [3, 4, 5]), (90, [2, 2])], heads=2, group=2)
+    for bounds in ([0, 3, 4], [1, 3, 5], [0, 4, 3, 5], [0, -1, 5], [0, 6, 5], [0, 3, 1 << 30]):
+        attend(c, m, seqs, bounds, status=-8)              # nothing is shared, the result is right
+    bad = list(seqs)
+    bad[1] = 99
+    q = torch.randn(5, 1, 4, 128, dtype=torch.float16, device=DEV)
+    out = torch.full_like(q, 7.0)
+    c.shared_attention(q, ints(bad), ints(b), out=out)
+    assert c.poll_status() == -8 and (out[1] == 7).all()
+    want = c.attention(q, ints(seqs))
+    keep = [0, 2, 3, 4]
+    assert (out - want)[keep].abs().max() < 2e-3
+    for starts in ([0, 2, 1, 3, 4, 5], [0, 1, 2, 3, 4, 9]):
+        c.shared_attention(q, ints(seqs), ints(b), ints(starts), out=out)
+        assert c.poll_status() == -8
+
+
+@pytest.mark.parametrize("many", [False, True])
+def test_values_and_scores_far_apart(many):
+    """A first token that holds nearly all probability in the shared half, or in the rest; magnitudes 2^60 apart."""
+    each = 40 if many else 3
+    for where in ("shared", "rest", "zero"):
+        c, m, seqs, b = family([(256, [20] * each)], heads=1, group=1, dim=64, pt=64, seed=4, dtype=torch.bfloat16)
+        q = torch.randn(each, 1, 1, 64)
+        if where == "zero":
+            m.amax[:, m.table[seqs[0], 0]] = 0.0
+        else:
+            page = m.table[seqs[0], 0 if where == "shared" else 4]
+            m.amax[:, page, :, 1] *= 2.0 ** 60
+            m.amax[:, page, :, 0] *= 3.0
+        c.amax.copy_(torch.from_numpy(m.amax))
+        attend(c, m, seqs, b, tail=0, q=q.to(torch.bfloat16))
+
+
+def test_captured_beside_other_calls_and_on_a_stream():
+    c, m, seqs, b = family([(300, [4, 40, 80]), (65, [9, 2])], heads=2, group=2, pt=32)
+    q = torch.randn(5, 1, 4, 128, dtype=torch.float16, device=DEV)
+    s, g = ints(seqs), ints(b)
+    want = c.shared_attention(q, s, g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [c.shared_attention(q, s, g, stream=side) for _ in range(20)]
+    side.synchronize()
+    assert all(torch.equal(x, want) for x in got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one = c.shared_attention(q, s, g)
+        two = c.attention(q, s)
+        three = c.shared_attention(q, s, g)
+    for _ in range(3):
+        one.zero_(), three.zero_()
+        graph.replay()
+        assert torch.equal(one, want) and torch.equal(three, want) and (two - want).abs().max() < 2e-3
+    assert c.poll_status() == 0
