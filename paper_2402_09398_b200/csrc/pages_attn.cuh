@@ -16,17 +16,21 @@ struct PaArgs {
   int window, sinks;             // window 0 = all
   float scale;
   // attention of sequences that share their first pages (pages_shared.cu); not read otherwise
-  const int4* groups;            // two of each group: {sequence, first row, rows, 0}, {sb, wb, eb, 0} of what it shares
-  const int4* entries;           // of each entry: {sb, wb, eb, 0} of its group
+  const int4* groups;            // two of each group: {sequence, first row, tokens, first entry}, {sb, wb, eb, end of its entries}
+                                 // with the blocks that it shares; tokens -1: starts that descend
+  const int4* entries;           // of each entry: {sb, wb, eb, the most blocks that rows of a tile have beside the shared ones
+                                 // (of its group's tiles of 8 rows)}
   float* parts;                  // [splits][rows * nl * heads * group][D]: results over the shared blocks
   float2* weights;               // [splits][rows * nl * heads * group]: (reference, sum); not written for entries that share nothing
   int splits;
+  int twins;                     // the many-token kernel leaves two parts for each of its splits
   int out_layers;                // layers between the rows of `out`
 };
 
-// What a launch is for: all that an entry sees; the blocks that all entries of a group see (then the group is the entry,
-// and results are parts); what of an entry's blocks is not among those (then the parts are joined).
-enum PaMode { kAll, kShared, kRest };
+// What a launch is for: all that an entry sees; all that the entries of a group see (the group is then the entry; of a tile's
+// rows all see the shared blocks, and those of an entry the rest of its blocks); the shared blocks alone (again the group is
+// the entry, and results are parts); the rest of an entry's blocks (the parts are joined).
+enum PaMode { kAll, kTree, kShared, kRest };
 
 // the 16-token blocks that the tokens of an entry see: [0, sb) and [wb, eb)
 struct Blocks {
@@ -73,11 +77,24 @@ struct PaWork<kAll> {
   static __device__ __forceinline__ B blocks(const PaArgs& a, int, const PgEntry& e) { return visible_blocks(a, e.len, e.count); }
 };
 template <>
+struct PaWork<kTree> {
+  typedef Blocks B;
+  static __device__ __forceinline__ PgEntry entry(const PgParams&, const PaArgs& a, int i) {
+    const int4 g = __ldcg(a.groups + 2 * i);
+    return {g.x, g.y, g.z, 0};
+  }
+  static __device__ __forceinline__ B blocks(const PaArgs& a, int i, const PgEntry&) {
+    const int4 b = __ldcg(a.groups + 2 * i + 1);
+    return {b.x, b.y, b.z};
+  }
+};
+template <>
 struct PaWork<kShared> {
   typedef Blocks B;
   static __device__ __forceinline__ PgEntry entry(const PgParams&, const PaArgs& a, int i) {
     const int4 g = __ldcg(a.groups + 2 * i), b = __ldcg(a.groups + 2 * i + 1);
-    return {g.x, g.y, g.z, b.z * kPageBlock + g.z};       // every token lies behind the shared ones
+    const int tokens = b.x + b.z - b.y > 0 ? g.z : 0;
+    return {g.x, g.y, tokens, b.z * kPageBlock + tokens};  // every token lies behind the shared ones
   }
   static __device__ __forceinline__ B blocks(const PaArgs& a, int i, const PgEntry&) {
     const int4 b = __ldcg(a.groups + 2 * i + 1);
@@ -190,7 +207,8 @@ int pa_args(const less_pages* d, int32_t layer_begin, int32_t layer_count, int32
             PgParams* p, PaArgs* a);
 int launch_pages_attention(const PgParams& p, PaArgs a, int dim, uint32_t flags, int32_t max_new, cudaStream_t s);
 // results of the groups' tokens over the blocks that they share, into a.parts (pages_prefix.cu)
-int launch_pages_prefix(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, int rows, bool many, size_t room, int counters,
-                        cudaStream_t s);
+int launch_pages_prefix(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);
+// groups of few rows, in one launch (pages_tree.cu)
+int launch_pages_tree(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);
 
 }  // namespace less

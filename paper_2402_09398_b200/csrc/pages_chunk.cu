@@ -27,7 +27,7 @@ static int launch_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
   splits = splits > room ? room : splits;
   splits = splits < 1 ? 1 : splits;
   const int rc = pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3, kAll>, dim3((unsigned)(slots * heads + 1), (unsigned)splits),
-                           PC_THREADS, smem, s, p, a, (int)splits);
+                           pc_threads(kAll), smem, s, p, a, (int)splits);
   if (rc != LESS_OK || splits == 1) return rc;
   const int64_t warps = (int64_t)a.rows * heads * p.group;
   return pg_launch("pages_chunk_join_kernel", pages_chunk_join_kernel<T, D>, dim3((unsigned)((warps + 7) / 8)), 256, 0, s, p, a,

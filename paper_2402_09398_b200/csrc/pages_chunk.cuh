@@ -43,8 +43,11 @@ namespace less {
 
 constexpr int PC_ROWS = 128, PC_KEYS = 64;
 constexpr int PC_TILES = PC_KEYS / kPageBlock;            // stored tiles of a key tile
-constexpr int PC_SOFT_WARPS = 8, PC_DEQ_WARPS = 4;
-constexpr int PC_THREADS = (PC_SOFT_WARPS + PC_DEQ_WARPS + 2) * 32;
+constexpr int PC_SOFT_WARPS = 8;
+// Warps that convert codes.  Four keep up with 256 rows from L2; over the shared blocks of a group the codes come from memory
+// and are used by 128 rows or fewer: eight.
+__host__ __device__ constexpr int pc_deq_warps(PaMode mode) { return mode == kShared ? 6 : 4; }
+__host__ __device__ constexpr int pc_threads(PaMode mode) { return (PC_SOFT_WARPS + pc_deq_warps(mode) + 2) * 32; }
 constexpr int PC_STAGES = 4, PC_META = 8;
 constexpr float PC_WIDE = 64.f;                           // log2 of magnitudes that far apart need care (see the softmax)
 constexpr int PC_POLY = 1;                                // of eight pairs of exponentials, those on the FMA pipe (see ex2_poly)
@@ -161,7 +164,8 @@ __device__ __forceinline__ uint32_t pc_mask16(int j0, int pos, int window, int s
 }
 
 template <typename T, int D, bool E4M3, PaMode MODE>
-__global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, PaArgs a, int splits) {
+__global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgParams p, PaArgs a, int splits) {
+  constexpr int PC_DEQ_WARPS = pc_deq_warps(MODE), PC_THREADS = pc_threads(MODE), S_WARP = PC_SOFT_WARPS + PC_DEQ_WARPS;
   constexpr int QT = PC_ROWS * D * 2;                     // bytes of a Q tile
   constexpr int KT = PC_KEYS * D * 2;                     // of a K or V tile
   extern __shared__ __align__(1024) unsigned char pc_smem[];
@@ -190,7 +194,14 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   const int64_t row0 = (slot - pc_slot<MODE>(p, a, lo)) * (2 * PC_ROWS);
   // the step kernel's, or a slot before the first entry's (its rows need not start at 0), or no rows left
   if (rows <= a.max_rows || row0 < 0 || row0 >= rows) return;
-  const int valid = (int)min(rows - row0, (int64_t)2 * PC_ROWS), nx = valid > PC_ROWS ? 2 : 1;
+  const int valid = (int)min(rows - row0, (int64_t)2 * PC_ROWS);
+  // kShared, rows for one tile only: both row tiles hold them, and each takes every other key tile - two softmax chains
+  // instead of one (16 sequences over 100 003 tokens, 8 x 8 heads, with six warps that convert: 114 -> 98 us); a part of the
+  // results each
+  const bool twin = MODE == kShared && a.twins && valid <= PC_ROWS;
+  const int nx = valid > PC_ROWS || twin ? 2 : 1;
+  // key tile kt is the turn(kt)-th of a row tile that takes it
+  auto turn = [&](int kt) { return MODE == kShared && twin ? kt >> 1 : kt; };
   const int lj = lh / p.heads, h = lh - lj * p.heads, layer = a.layer0 + lj;
   const int base = e.len - e.count;                       // position of the entry's first token
   const int tok0 = (int)(row0 / p.group), tok1 = (int)((row0 + valid - 1) / p.group);
@@ -207,11 +218,14 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   const int64_t part_rows = (int64_t)a.rows * heads * p.group;
   auto part_row = [&](int64_t rr) {
     const int64_t tok = rr / p.group;
-    return blockIdx.y * part_rows + (e.row0 + tok) * heads * p.group + (int64_t)lh * p.group + (rr - tok * p.group);
+    return (int64_t)blockIdx.y * (a.twins ? 2 : 1) * part_rows + (e.row0 + tok) * heads * p.group + (int64_t)lh * p.group + (rr - tok * p.group);
   };
   if (nk == 0) {                                          // nothing to see
     if (MODE == kShared) {
-      for (int i = tid; i < valid; i += PC_THREADS) a.weights[part_row(row0 + i)] = make_float2(-INFINITY, 0.f);
+      for (int i = tid; i < valid; i += PC_THREADS) {
+        a.weights[part_row(row0 + i)] = make_float2(-INFINITY, 0.f);
+        if (a.twins) a.weights[part_rows + part_row(row0 + i)] = make_float2(-INFINITY, 0.f);
+      }
       return;
     }
     if (splits > 1) {
@@ -231,9 +245,9 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   if (tid == 0) {
     mbar_init(&sh->q_full, 4 * nx);
     for (int s = 0; s < PC_STAGES; ++s) {
-      mbar_init(&sh->k_full[s], PC_DEQ_WARPS / 2);
+      mbar_init(&sh->k_full[s], 2);
       mbar_init(&sh->k_empty[s], 1);
-      mbar_init(&sh->v_full[s], PC_DEQ_WARPS / 2);
+      mbar_init(&sh->v_full[s], 2);
       mbar_init(&sh->v_empty[s], 1);
     }
     for (int x = 0; x < 4; ++x) {
@@ -244,7 +258,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     sh->abort = 0;
     mbar_fence_init();
   }
-  if (warp == 12) tmem_alloc(&sh->tmem_base, 512);
+  if (warp == S_WARP) tmem_alloc(&sh->tmem_base, 512);
   fence_proxy_async_smem();
   tc_fence_before_sync();
   __syncthreads();
@@ -258,7 +272,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     // ---------------- softmax: thread = row ----------------
     const int x = warp >> 2, quad = warp & 3;
     if (x < nx) {
-      const int r = x * PC_ROWS + quad * 32 + lane;
+      const int r = (MODE == kShared && twin ? 0 : x * PC_ROWS) + quad * 32 + lane;
+      const int slot_r = x * PC_ROWS + quad * 32 + lane;
       const int64_t rr = row0 + min(r, valid - 1);
       const int tok = (int)(rr / p.group), hd = (int)(rr - (int64_t)tok * p.group);
       const int pos = base + tok;
@@ -307,10 +322,11 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       const uint32_t lane_addr = tmem + ((uint32_t)(quad * 32) << 16);
       const uint32_t ocol = lane_addr + OCOL + x * D;
       float M = -INFINITY, l = 0.f;
-      for (int kt = 0; kt < nk; ++kt) {
-        const int buf = kt & 1;
+      const int every = MODE == kShared && twin ? 2 : 1, kt_first = MODE == kShared && twin ? x : 0;
+      for (int kt = kt_first; kt < nk; kt += every) {
+        const int buf = turn(kt) & 1;
         const uint32_t scol = lane_addr + (2 * x + buf) * PC_KEYS;
-        wait_or_give_up(&sh->s_full[x][buf], (kt >> 1) & 1, abortp, status, 122);
+        wait_or_give_up(&sh->s_full[x][buf], (turn(kt) >> 1) & 1, abortp, status, 122);
         __syncwarp();                                     // after a give-up all waits return at once: no way out needed
         tc_fence_after_sync();
         const PcMeta& meta = sh->meta[kt % PC_META];
@@ -394,10 +410,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           const bool down = !none && most < kRefLeast && most > -INFINITY;
           if (again || !__any_sync(0xffffffffu, up || down)) break;
           float d = up || down ? most - (up && !none ? kRefUp : kRefNew) : 0.f;   // what the reference moves by
-          const float lowest = none ? -INFINITY : sh->lowest[r];
+          const float lowest = none ? -INFINITY : sh->lowest[slot_r];
           // down by 40 below the highest, so that O has room, and no further than l has
           if (down) d = fmaxf(d, fmaxf(lowest - M, (float)min(0, (int)(__float_as_uint(l) >> 23) - 127 - 90)));
-          if (up) sh->lowest[r] = fmaxf(lowest, ref + d - 40.f);
+          if (up) sh->lowest[slot_r] = fmaxf(lowest, ref + d - 40.f);
           if (up || down) {
             M = ref + d;
             d = M - ref;                                  // as it is rounded
@@ -405,8 +421,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           if (none) d = 0.f;
           l = pa_scaled(l, -d);
           const float f = pa_ex2(-d);
-          if (kt) {
-            wait_or_give_up(&sh->pv_done[x][(kt - 1) & 1], ((kt - 1) >> 1) & 1, abortp, status, 123);
+          if (turn(kt)) {
+            wait_or_give_up(&sh->pv_done[x][(turn(kt) - 1) & 1], ((turn(kt) - 1) >> 1) & 1, abortp, status, 123);
             tc_fence_after_sync();
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -426,13 +442,19 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         tc_fence_before_sync();
         mbar_arrive_warp(&sh->p_full[x][buf]);
       }
-      wait_or_give_up(&sh->pv_done[x][(nk - 1) & 1], ((nk - 1) >> 1) & 1, abortp, status, 124);
+      const int turns = MODE == kShared && twin ? (nk + 1 - x) >> 1 : nk;
+      if (MODE == kAll || turns) wait_or_give_up(&sh->pv_done[x][(turns - 1) & 1], ((turns - 1) >> 1) & 1, abortp, status, 124);
       tc_fence_after_sync();
-      if (!*abortp) {
+      if (MODE == kShared && a.twins && r < valid) {
+        if (!twin) a.weights[part_rows + part_row(rr)] = make_float2(-INFINITY, 0.f);
+        if (!turns) a.weights[x * part_rows + part_row(rr)] = make_float2(-INFINITY, 0.f);
+      }
+      if (!*abortp && (MODE == kAll || turns)) {
         // (one factor instead of two here makes the whole loop above 10 % slower)
         const float inv = l == 0.f ? 0.f : 1.f / l, unit = 0x1p-8f / pg_top<E4M3>();
         T* dst = out + (int64_t)(e.row0 + tok) * a.nl * p.heads * p.group * D + head_row + hd * D;
-        if (MODE == kShared && r < valid) a.weights[part_row(rr)] = pa_share(M, l);
+        const int64_t at = (MODE == kShared && twin ? x * part_rows : 0) + part_row(rr);
+        if (MODE == kShared && r < valid) a.weights[at] = pa_share(M, l);
         if (MODE == kAll && splits > 1 && r < valid) *reinterpret_cast<float2*>(part + (size_t)2 * PC_ROWS * D + 2 * r) = make_float2(M, l);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
@@ -444,7 +466,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
           for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(o[i]) * inv * unit;
           if (r < valid) {
             if (MODE == kShared) {
-              float* to = a.parts + part_row(rr) * D + 32 * c;
+              float* to = a.parts + at * D + 32 * c;
 #pragma unroll
               for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
             } else if (splits > 1) {
@@ -462,7 +484,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   } else if (warp < PC_SOFT_WARPS + PC_DEQ_WARPS) {
     // ---------------- codes -> operand tiles: two warps per key tile, a pair of stored tiles each ----------------
     constexpr int KP = D / 32;                            // 16-byte pieces of a lane in a stored tile
-    const int dw = warp & 1, odd = (warp - PC_SOFT_WARPS) >> 1, g = lane >> 2, t = lane & 3;
+    constexpr int PAIRS = PC_DEQ_WARPS / 2;
+    const int dw = warp & 1, first = (warp - PC_SOFT_WARPS) >> 1, g = lane >> 2, t = lane & 3;
     // positions of the rows of the two row tiles
     int first_pos[2], last_pos[2];
 #pragma unroll
@@ -470,11 +493,12 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       first_pos[x] = base + (int)((row0 + min(x * PC_ROWS, valid - 1)) / p.group);
       last_pos[x] = base + (int)((row0 + min((x + 1) * PC_ROWS, valid) - 1) / p.group);
     }
-    // lane 2 i + b knows tile b of this warp's pair in its i-th key tile of the batch, key tile batch + 2 i
+    // lane 2 i + b knows tile b of this warp's pair in its i-th key tile of the batch, key tile batch + PAIRS * i
+    auto nth = [&](int kt) { return kt / PAIRS * 2 & 30; };
     int page_l = -1, j_l = 0;
     float ak_l = 0.f, av_l = 0.f, vlast = 1.f;
     auto lookup = [&](int batch) {
-      const int u = (kt0 + batch + (lane & ~1)) * PC_TILES + 2 * dw + (lane & 1);
+      const int u = (kt0 + batch + (lane >> 1) * PAIRS) * PC_TILES + 2 * dw + (lane & 1);
       page_l = -1;
       j_l = 0;
       if (u < units) {
@@ -494,7 +518,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     auto load = [&](int kt, bool values) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int src = (kt & 30) + b;
+        const int src = nth(kt) + b;
         const int page = __shfl_sync(0xffffffffu, page_l, src), j = __shfl_sync(0xffffffffu, j_l, src);
         const float av = __shfl_sync(0xffffffffu, av_l, src);
         if (!values) {
@@ -531,10 +555,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
         }
       }
     };
-    lookup(odd);
-    load(odd, false);
-    load(odd, true);
-    for (int kt = odd; kt < nk; kt += 2) {
+    lookup(first);
+    load(first, false);
+    load(first, true);
+    for (int kt = first; kt < nk; kt += PAIRS) {
       const int st = kt % PC_STAGES, ph = (kt / PC_STAGES) & 1;
       wait_or_give_up(&sh->k_empty[st], ph ^ 1, abortp, status, 125);
       if (__any_sync(0xffffffffu, *abortp)) break;
@@ -580,9 +604,9 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       fence_proxy_async_smem();
       mbar_arrive_warp(&sh->k_full[st]);
       // V of this key tile is in its registers; pages of the next batch before the next K is asked for
-      if (kt + 2 < nk) {
-        if (((kt + 2) & 30) == 0) lookup(kt + 2);
-        load(kt + 2, false);
+      if (kt + PAIRS < nk) {
+        if (nth(kt + PAIRS) == 0) lookup(kt + PAIRS);
+        load(kt + PAIRS, false);
       }
       wait_or_give_up(&sh->v_empty[st], ph ^ 1, abortp, status, 126);
       if (__any_sync(0xffffffffu, *abortp)) break;
@@ -604,9 +628,9 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
       }
       fence_proxy_async_smem();
       mbar_arrive_warp(&sh->v_full[st]);
-      if (kt + 2 < nk) load(kt + 2, true);
+      if (kt + PAIRS < nk) load(kt + PAIRS, true);
     }
-  } else if (warp == 12) {
+  } else if (warp == S_WARP) {
     // ---------------- S = Q K^T ----------------
     constexpr uint32_t idesc = idesc_f16(PC_ROWS, PC_KEYS, 0, 0);
     const uint32_t on = elect_one();
@@ -617,25 +641,27 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     for (int kt = 0; kt < nk; ++kt) {
       const int st = kt % PC_STAGES;
       wait_or_give_up(&sh->k_full[st], (kt / PC_STAGES) & 1, abortp, status, 128);
-      for (int x = 0; x < nx; ++x) {
-        // the buffer held S and then P of key tile kt - 2
-        if (kt >= 2) wait_or_give_up(&sh->pv_done[x][kt & 1], ((kt >> 1) - 1) & 1, abortp, status, 129);
+      const int tn = turn(kt);
+      for (int x = MODE == kShared && twin ? kt & 1 : 0; x < nx; ++x) {
+        // the buffer held S and then P of the row tile's key tile before the last
+        if (tn >= 2) wait_or_give_up(&sh->pv_done[x][tn & 1], ((tn >> 1) - 1) & 1, abortp, status, 129);
         tc_fence_after_sync();
         const uint64_t a0 = desc_at(ad, x * (QT >> 4)), b0 = desc_at(bd, st * (KT >> 4));
-        const uint32_t s0 = tmem + (2 * x + (kt & 1)) * PC_KEYS;
+        const uint32_t s0 = tmem + (2 * x + (tn & 1)) * PC_KEYS;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
           mma_ss_if(on, s0, desc_at(a0, (ks >> 2) * (PC_ROWS * 128 >> 4) + (ks & 3) * 2),
                     desc_at(b0, (ks >> 2) * (PC_KEYS * 128 >> 4) + (ks & 3) * 2), idesc, ks ? 1u : 0u);
-        if (x == 0) {                                     // this warp meets the key tiles in order: it compares magnitudes
+        if (x == 0 || (MODE == kShared && twin)) {        // this warp meets the key tiles in order: it compares magnitudes
           const float4 lav = *reinterpret_cast<const float4*>(sh->meta[kt % PC_META].lav);
           lav_most = fmaxf(lav_most, fmaxf(fmaxf(lav.x, lav.y), fmaxf(lav.z, lav.w)));
           if (on && fminf(fminf(lav.x, lav.y), fminf(lav.z, lav.w)) < lav_most - PC_WIDE) sh->meta[kt % PC_META].part[0] = 7;
           __syncwarp();
         }
-        mma_commit_if(on, &sh->s_full[x][kt & 1]);
-        if (on) mbar_arrive(&sh->s_full[x][kt & 1]);      // passes on what came with k_full (the magnitudes)
+        mma_commit_if(on, &sh->s_full[x][tn & 1]);
+        if (on) mbar_arrive(&sh->s_full[x][tn & 1]);      // passes on what came with k_full (the magnitudes)
         __syncwarp();
+        if (MODE == kShared && twin) break;
       }
       if (__any_sync(0xffffffffu, *abortp)) break;
       mma_commit_if(on, &sh->k_empty[st]);
@@ -648,15 +674,17 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
     for (int kt = 0; kt < nk; ++kt) {
       const int st = kt % PC_STAGES;
       wait_or_give_up(&sh->v_full[st], (kt / PC_STAGES) & 1, abortp, status, 130);
-      for (int x = 0; x < nx; ++x) {
-        wait_or_give_up(&sh->p_full[x][kt & 1], (kt >> 1) & 1, abortp, status, 131);
+      const int tn = turn(kt);
+      for (int x = MODE == kShared && twin ? kt & 1 : 0; x < nx; ++x) {
+        wait_or_give_up(&sh->p_full[x][tn & 1], (tn >> 1) & 1, abortp, status, 131);
         tc_fence_after_sync();
         const uint64_t b0 = desc_at(bd, st * (KT >> 4));
-        const uint32_t p0 = tmem + (2 * x + (kt & 1)) * PC_KEYS;
+        const uint32_t p0 = tmem + (2 * x + (tn & 1)) * PC_KEYS;
 #pragma unroll
         for (int ks = 0; ks < PC_KEYS / 16; ++ks)
-          mma_ts_if(on, tmem + OCOL + x * D, p0 + 8 * ks, desc_at(b0, ks * 2), idesc, (kt | ks) ? 1u : 0u);
-        mma_commit_if(on, &sh->pv_done[x][kt & 1]);
+          mma_ts_if(on, tmem + OCOL + x * D, p0 + 8 * ks, desc_at(b0, ks * 2), idesc, (tn | ks) ? 1u : 0u);
+        mma_commit_if(on, &sh->pv_done[x][tn & 1]);
+        if (MODE == kShared && twin) break;
       }
       if (__any_sync(0xffffffffu, *abortp)) break;
       mma_commit_if(on, &sh->v_empty[st]);
@@ -665,7 +693,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) pages_chunk_kernel(PgParams p, 
   drain_after_abort(abortp);
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == 12) tmem_dealloc(tmem, 512);
+  if (warp == S_WARP) tmem_dealloc(tmem, 512);
 }
 
 // Joins the parts of split items: a warp per row of the output and head.  Part weights are l 2^(M - m), kept in fp32, the

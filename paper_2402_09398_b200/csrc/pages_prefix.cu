@@ -1,7 +1,6 @@
 // The first half of attention over shared pages (pages_shared.cu): the tokens of a group over the blocks that all of them
-// see, with the kernels of ordinary attention, for which the group is one entry.
+// see, with the many-token kernel, for which the group is one entry.
 #include "pages_chunk.cuh"
-#include "pages_step.cuh"
 
 namespace less {
 
@@ -20,12 +19,10 @@ static int launch_prefix_chunk(const PgParams& p, const PaArgs& a, cudaStream_t 
   const int64_t slots = (int64_t)a.rows * p.group / (2 * PC_ROWS) + a.n, heads = (int64_t)p.heads * a.nl;
   if (slots * heads >= 0x7fffffff) return LESS_ERR_INVALID_CONFIG;
   return pg_launch("pages_chunk_kernel", pages_chunk_kernel<T, D, E4M3, kShared>, dim3((unsigned)(slots * heads + 1), (unsigned)a.splits),
-                   PC_THREADS, smem, s, p, a, a.splits);
+                   pc_threads(kShared), smem, s, p, a, a.splits);
 }
 
-int launch_pages_prefix(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, int rows, bool many, size_t room, int counters,
-                        cudaStream_t s) {
-  if (!many) return launch_pages_step<kShared>(p, a, dim, flags, rows, room, counters, s);
+int launch_pages_prefix(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s) {
   const bool e4m3 = flags & LESS_PAGES_E4M3;
   if (flags & LESS_PAGES_BF16) {
     if (dim == 128) return e4m3 ? launch_prefix_chunk<__nv_bfloat16, 128, true>(p, a, s) : launch_prefix_chunk<__nv_bfloat16, 128, false>(p, a, s);

@@ -43,6 +43,10 @@ namespace less {
 constexpr int PS_WARPS = 6, PS_THREADS = PS_WARPS * 32;
 // CTAs per SM: two (168 registers a thread, 96 KB of tiles per CTA) unless the rows' sums need more registers
 __host__ __device__ constexpr int ps_ctas(int NT, int D) { return NT * D <= 128 ? 2 : 1; }
+// Blocks that an item is counted as more than it has: its beginning and end take a warp as long as some blocks, and with
+// sequences that end a few tokens behind what they share, an even cut of the blocks alone hands one warp dozens of items (64
+// sequences of 1 to 1000 tokens of their own, 32 heads: 234 us, of which SMs are busy for 66 on average).
+__host__ __device__ constexpr int ps_more(PaMode mode) { return mode == kAll ? 0 : 6; }
 constexpr int PS_RING = 4;                     // tiles of a warp: two being worked on, two on their way
 constexpr int PS_MIN_BLOCKS = 4;               // blocks a warp takes at least (one token of 250: 2 the same, 8: 9.7 -> 13.3 us)
 
@@ -77,7 +81,7 @@ struct Item {
   int blocks;
   int valid;                    // rows of this item
   int h, row0, tok_row, lj;
-  bool joined;                  // kRest: there are parts of its rows over shared blocks
+  int extra;                    // kRest: there are parts of its rows over shared blocks; kTree: rows that nobody writes, a bit each
 };
 
 struct PsShared {
@@ -90,6 +94,15 @@ struct PsShared {
   Item part[PS_WARPS][2];         // the item that a warp holds a part of: begun before its stretch (0), or going on behind it
   float* where[PS_WARPS][2];      // the part: rows x D values, then (maximum, sum) of the rows; null = none
   int last[2];                    // whether this CTA merges the part-0 / part-1 item over all CTAs
+};
+
+// kTree: the rows of a warp's item, each of an entry of its own perhaps
+struct PsTreeRow {
+  int first;                    // the first row of the same entry
+  int pos;                      // position of its token, -1 = sees nothing
+  int start, count;             // the entry's blocks beside the shared ones, where they begin behind these (first rows; else none)
+  int seq, len;
+  RestBlocks rest;
 };
 
 // a part lies in shared or in global memory; there it may come from another CTA of this launch: past L1
@@ -111,36 +124,36 @@ __device__ __forceinline__ int64_t row_offset(const PgParams& p, int layers, int
          ((int64_t)it.h * p.group + hd) * D;
 }
 
-// kRest: a row's N values from f (relative to 2^m, sum l) and the parts over shared blocks; row: its number among the parts
+// kRest: a row's N values from f (relative to 2^m, sum l) and the one or two parts over shared blocks; row: its number among
+// the parts
 template <int D, int N>
-__device__ __forceinline__ void join_shared(const PgParams& p, const PaArgs& a, int64_t row, int d0, float* f, float& m, float& l) {
+__device__ __forceinline__ void join_shared(const PgParams& p, const PaArgs& a, int64_t row, int d0, float* f, float m, float l) {
   const int64_t rows = (int64_t)a.rows * a.nl * p.heads * p.group;
-  float top = m;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, __ldcg(a.weights + s * rows + row).x);
-  float sum = l == 0.f ? 0.f : l * pa_ex2(m - top);
+  const float2 w0 = __ldcg(a.weights + row), w1 = a.splits > 1 ? __ldcg(a.weights + rows + row) : make_float2(-INFINITY, 0.f);
+  const float top = fmaxf(m, fmaxf(w0.x, w1.x));
+  float x = l == 0.f ? 0.f : l * pa_ex2(m - top), x0 = w0.y == 0.f ? 0.f : w0.y * pa_ex2(w0.x - top),
+        x1 = w1.y == 0.f ? 0.f : w1.y * pa_ex2(w1.x - top);
+  const float sum = x + x0 + x1, inv = sum == 0.f ? 0.f : 1.f / sum;
+  x *= inv;
+  x0 *= inv;
+  x1 *= inv;
+  const float* v = a.parts + row * D + d0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) f[i] *= sum;
-#pragma unroll 4
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 w = __ldcg(a.weights + s * rows + row);
-    if (w.y == 0.f) continue;                              // its values were not written
-    const float x = w.y * pa_ex2(w.x - top);
-    sum += x;
-    const float* v = a.parts + (s * rows + row) * D + d0;
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(v + i));
-      f[i] = fmaf(x, y.x, f[i]);
-      f[i + 1] = fmaf(x, y.y, f[i + 1]);
-      f[i + 2] = fmaf(x, y.z, f[i + 2]);
-      f[i + 3] = fmaf(x, y.w, f[i + 3]);
+  for (int i = 0; i < N; i += 4) {
+    float4 y = make_float4(f[i] * x, f[i + 1] * x, f[i + 2] * x, f[i + 3] * x);
+    if (x0 != 0.f) {                                       // else its values may not have been written
+      const float4 z = __ldcg(reinterpret_cast<const float4*>(v + i));
+      y = make_float4(fmaf(x0, z.x, y.x), fmaf(x0, z.y, y.y), fmaf(x0, z.z, y.z), fmaf(x0, z.w, y.w));
     }
+    if (x1 != 0.f) {
+      const float4 z = __ldcg(reinterpret_cast<const float4*>(v + rows * D + i));
+      y = make_float4(fmaf(x1, z.x, y.x), fmaf(x1, z.y, y.y), fmaf(x1, z.z, y.z), fmaf(x1, z.w, y.w));
+    }
+    f[i] = y.x;
+    f[i + 1] = y.y;
+    f[i + 2] = y.z;
+    f[i + 3] = y.w;
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int i = 0; i < N; ++i) f[i] *= inv;
-  m = top;
-  l = sum;
 }
 
 template <typename T, int D, int NT, bool E4M3, PaMode MODE>
@@ -153,6 +166,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   constexpr bool LO = std::is_same<T, __half>::value;
   extern __shared__ __align__(16) unsigned char ps_ring[];
   __shared__ PsShared sh;
+  __shared__ PsTreeRow tree[MODE == kTree ? PS_WARPS : 1][MODE == kTree ? R : 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   pg_wait();
 
@@ -160,10 +174,13 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   const int per_thread = pg_ceil(a.n, PS_THREADS);
   auto entry_items = [&](int i, const PgEntry& e, typename Work::B& b, int& tiles) -> int {
     const int64_t nr = (int64_t)e.count * p.group;
-    if (nr == 0 || nr > a.max_rows) return 0;
+    if (nr == 0 || nr > a.max_rows || (MODE == kTree && nr < 0)) return 0;
     b = Work::blocks(a, i, e);
     tiles = (int)((nr + R - 1) / R);
     return tiles * a.nl * p.heads;
+  };
+  auto tree_rest = [&](int i, const PgEntry& e) -> int {  // the most blocks beside the shared ones that an item of it has
+    return MODE == kTree && e.count > 0 ? __ldcg(a.entries + __ldcg(a.groups + 2 * i).w).w : 0;
   };
   int per_warp;
   int64_t pad = 0;
@@ -176,11 +193,11 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       const PgEntry e = Work::entry(p, a, i);
       if (per_thread == 1) sh.entry[tid] = e;
       // entries overlap then, and the items of all might not be counted in 32 bits (else the host has made sure of that)
-      if (MODE != kShared && pg_descends(a.starts, i)) most = 0x7fffffff;
+      if (MODE == kTree ? e.count < 0 : pg_descends(a.starts, i)) most = 0x7fffffff;
       const int items = entry_items(i, e, b, tiles);
       if (items) {
-        const int blocks = max(1, b.count());
-        mu += (int64_t)items * blocks;
+        const int blocks = max(1, b.count() + tree_rest(i, e));
+        mu += (int64_t)items * (blocks + ps_more(MODE));
         mi += items;
         most = max(most, blocks);
       }
@@ -265,8 +282,8 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       e = per_thread == 1 ? sh.entry[ei] : Work::entry(p, a, ei);
       items = entry_items(ei, e, vb, tiles);
       if (items == 0) continue;
-      real = max(1, vb.count());
-      blocks = pad ? (int)pad : real;
+      real = max(1, vb.count() + tree_rest(ei, e));
+      blocks = pad ? (int)pad : real + ps_more(MODE);
       return true;
     }
     return false;
@@ -300,10 +317,48 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     it.valid = min(R, e.count * p.group - it.row0);
     if (MODE == kRest) {
       const int4 of = __ldcg(a.entries + ei);
-      it.joined = of.x + of.z - of.y > 0;
+      it.extra = of.x + of.z - of.y > 0;
     }
     const int first = bo, end = (int)min((int64_t)blocks, bo + (ue - u));
-    const int last = vb.count() > 0 ? min(end, real) : first;       // what of it has tokens
+    int last = vb.count() > 0 ? min(end, real) : first;             // what of it has tokens
+    if (MODE == kTree) {
+      // whose the rows are; the blocks that their entries see beside the shared ones follow those
+      const int4 ge = __ldcg(a.groups + 2 * ei), gb = __ldcg(a.groups + 2 * ei + 1);
+      const int trow = e.row0 + (it.row0 + min(lane, it.valid - 1)) / p.group;
+      int who = ge.w + trow - e.row0;
+      if (a.starts) {
+        who = ge.w;
+        for (int c = ge.w; c < gb.w; c += 32) {
+          const int stop = c + lane < gb.w ? __ldg(a.starts + c + lane + 1) : 0x7fffffff;
+#pragma unroll
+          for (int k = 0; k < R; ++k) {
+            const int n = __popc(__ballot_sync(0xffffffffu, stop <= __shfl_sync(0xffffffffu, trow, k)));
+            if (lane == k) who += n;
+          }
+        }
+      }
+      const bool mine = lane < it.valid && who < gb.w;
+      PgEntry en = {0, 0, 0, 0};
+      if (mine) en = pg_entry(p, a.seqs, a.starts, a.rows, who);
+      const int before = __shfl_up_sync(0xffffffffu, who, 1);
+      const bool head = mine && (lane == 0 || before != who);
+      const uint32_t heads = __ballot_sync(0xffffffffu, head);
+      it.extra = (int)__ballot_sync(0xffffffffu, lane < it.valid && en.count == 0);
+      const RestBlocks rest = rest_blocks(visible_blocks(a, en.len, en.count), gb);
+      const int n = head && en.count ? rest.count() : 0;
+      int upto = n;
+#pragma unroll
+      for (int d = 1; d < R; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      __syncwarp();                                        // the item before has been read
+      if (lane < R)
+        tree[warp][lane] = {31 - __clz((int)(heads & (2u << lane) - 1u)), mine && en.count ? en.len - en.count + trow - en.row0 : -1,
+                            upto - n, n, en.seq, en.len, rest};
+      last = min(end, vb.count() + __shfl_sync(0xffffffffu, upto, R - 1));
+      __syncwarp();
+    }
     const int layer = a.layer0 + it.lj;
 
     // ---- pages and magnitudes: lane i knows the tile of block `batch + i` and, one batch ahead, `batch + 32 + i` ----
@@ -312,12 +367,32 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     struct Tile {
       const uint8_t* codes;       // null = none
       float ak, lav;              // magnitude of the keys, log2 of the values'
+      // kTree: position of the first token, the entry's length, the first row that sees it (-1: all do)
+      int j0, len, who;
     };
     auto lookup = [&](int b) {
-      Tile tl = {nullptr, 0.f, kNoValues};
+      Tile tl = {nullptr, 0.f, kNoValues, 0, 0, -1};
       if (b + lane < last) {
-        const int tok = vb.at(b + lane) * kPageBlock, inner = (tok & (p.pt - 1)) / kPageBlock;
-        const int page = pg_page(p, e.seq, tok >> p.pt_shift);
+        int seq = e.seq, block;
+        if (MODE == kTree) {
+          const int u = b + lane, behind = u - vb.count();
+          if (behind < 0) {
+            block = vb.at(u);
+            tl.len = 0x7fffffff;
+          } else {
+            for (int k = 0; k < it.valid; ++k)
+              if (tree[warp][k].count && behind >= tree[warp][k].start) tl.who = k;
+            const PsTreeRow& row = tree[warp][tl.who];
+            block = row.rest.at(behind - row.start);
+            seq = row.seq;
+            tl.len = row.len;
+          }
+          tl.j0 = block * kPageBlock;
+        } else {
+          block = vb.at(b + lane);
+        }
+        const int tok = block * kPageBlock, inner = (tok & (p.pt - 1)) / kPageBlock;
+        const int page = pg_page(p, seq, tok >> p.pt_shift);
         if (page >= 0) {
           const size_t slab = (size_t)page * p.heads * 2;
           tl.codes = head_codes + slab * ((size_t)p.pt * D) + (size_t)inner * TILE;
@@ -329,7 +404,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       }
       return tl;
     };
-    Tile cur = lookup(first), nxt = {nullptr, 0.f, kNoValues};
+    Tile cur = lookup(first), nxt = {nullptr, 0.f, kNoValues, 0, 0, -1};
     const size_t to_values = (size_t)p.pt * D;
     // the tiles of blocks b and b + 1 on their way to ring slots `slot` and `slot + 1`
     auto fetch = [&](const Tile& tl, int at, int slot) {
@@ -353,7 +428,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     // ---- its queries: operand fragments, the score factor and the position of the rows of this lane ----
     uint32_t qf[NT][D / 8];
     float crow[NT][2];
-    int pos[NT][2];
+    int pos[NT][2], owner[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = nt * 8 + g;
@@ -395,11 +470,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       for (int c = 0; c < 2; ++c) {
         const int rc = nt * 8 + 2 * t + c;
         crow[nt][c] = a.scale * 1.4426950408889634f / pg_top<E4M3>() * __shfl_sync(0xffffffffu, up, (2 * t + c) * 4);
-        pos[nt][c] = rc < it.valid ? e.len - e.count + (it.row0 + rc) / p.group : -1;
+        pos[nt][c] = MODE == kTree ? tree[warp][rc].pos : rc < it.valid ? e.len - e.count + (it.row0 + rc) / p.group : -1;
+        if (MODE == kTree) owner[nt][c] = tree[warp][rc].first;
       }
     }
     const int first_pos = e.len - e.count + it.row0 / p.group, last_pos = e.len - e.count + (it.row0 + it.valid - 1) / p.group;
-    const bool all_rows = it.valid == R;
+    const bool all_rows = it.valid == R && (MODE != kTree || it.extra == 0);
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -418,19 +494,27 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       const int at = (b - first) & 31;                     // lane of block b
       if (at == 0) {
         if (b != first) cur = nxt;
-        nxt = b + 32 < last ? lookup(b + 32) : Tile{nullptr, 0.f, kNoValues};
+        nxt = b + 32 < last ? lookup(b + 32) : Tile{nullptr, 0.f, kNoValues, 0, 0, -1};
       }
       fetch(at + 2 < 32 ? cur : nxt, (at + 2) & 31, slot ^ 2);
       cp_async_wait<1>();
       float ak[2], lav[2];
       bool here[2];
-      int j0[2];
+      int j0[2], len[2], who[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         ak[k] = __shfl_sync(0xffffffffu, cur.ak, at + k);
         lav[k] = __shfl_sync(0xffffffffu, cur.lav, at + k);
         here[k] = __shfl_sync(0xffffffffu, (int)(cur.codes != nullptr), at + k);
-        j0[k] = vb.at(b + k) * kPageBlock;
+        if (MODE == kTree) {
+          j0[k] = __shfl_sync(0xffffffffu, cur.j0, at + k);
+          len[k] = __shfl_sync(0xffffffffu, cur.len, at + k);
+          who[k] = __shfl_sync(0xffffffffu, cur.who, at + k);
+        } else {
+          j0[k] = vb.at(b + k) * kPageBlock;
+          len[k] = e.len;
+          who[k] = -1;
+        }
       }
       const unsigned char* tile = ring_g + slot * (2 * TILE);
       slot ^= 2;
@@ -465,7 +549,8 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const bool whole = all_rows && here[k] && j0[k] + kPageBlock - 1 <= first_pos &&
+        const bool whole = MODE == kTree ? all_rows && here[k] && who[k] < 0 :
+                           all_rows && here[k] && j0[k] + kPageBlock - 1 <= first_pos &&
                            (!a.window || j0[k] > last_pos - a.window || j0[k] + kPageBlock <= a.sinks);
         // this lane's tokens: accumulator rows g and g + 8
         const int ja = j0[k] + 4 * (g >> 1) + (g & 1), jb = ja + 2;
@@ -481,6 +566,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
             for (int i = 0; i < 4; ++i) {
               const int j = i < 2 ? ja : jb, at_row = pos[nt][i & 1];
               if (!here[k] || j > at_row || (a.window && j <= at_row - a.window && j >= a.sinks)) s[k][nt][i] = -INFINITY;
+              if (MODE == kTree && who[k] >= 0 && who[k] != owner[nt][i & 1]) s[k][nt][i] = -INFINITY;
             }
           }
         }
@@ -564,8 +650,8 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
         // tokens behind the end may hold any byte, a slot without a tile or values of magnitude 0 too; a NaN code would
         // survive its zero probability
         uint32_t keep = 0xffffffffu;
-        if (E4M3 && (!here[k] || lav[k] == kNoValues || j0[k] + kPageBlock > e.len)) {
-          const int left = here[k] && lav[k] != kNoValues ? e.len - (j0[k] + 4 * t) : 0;
+        if (E4M3 && (!here[k] || lav[k] == kNoValues || j0[k] > len[k] - kPageBlock)) {
+          const int left = here[k] && lav[k] != kNoValues ? len[k] - (j0[k] + 4 * t) : 0;
           keep = left <= 0 ? 0u : (left >= 4 ? keep : keep >> (8 * (4 - left)));
         }
 #pragma unroll
@@ -608,7 +694,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int rc = nt * 8 + 2 * t + c;
-        if (rc >= it.valid) continue;
+        if (rc >= it.valid || (MODE == kTree && it.extra >> rc & 1)) continue;
         const float unit = (sum > 0.f ? 1.f / sum : 0.f) * (0x1p-8f / pg_top<E4M3>());
         float f[D / 8];
 #pragma unroll
@@ -620,18 +706,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
 #pragma unroll
           for (int i = 0; i < D / 8; ++i) f[i] = sum;
         }
-        if (complete && MODE == kShared) {
-          const int64_t at = row_offset(p, a.nl, D, it, rc);
-#pragma unroll
-          for (int i = 0; i < D / 8; i += 4)
-            *reinterpret_cast<float4*>(a.parts + at + g * (D / 8) + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
-          if (g == 0) a.weights[at / D] = pa_share(m[nt][c], sum);
-        } else if (complete) {
-          if (MODE == kRest && it.joined) {
-            float2 ml = pa_share(m[nt][c], sum);
+        if (complete) {
+          if (MODE == kRest && it.extra) {
+            const float2 ml = pa_share(m[nt][c], sum);
             join_shared<D, D / 8>(p, a, row_offset(p, a.nl, D, it, rc) / D, g * (D / 8), f, ml.x, ml.y);
           }
-          T* dst = reinterpret_cast<T*>(a.out) + row_offset(p, MODE == kAll ? a.nl : a.out_layers, D, it, rc) + g * (D / 8);
+          T* dst = reinterpret_cast<T*>(a.out) + row_offset(p, MODE == kRest ? a.out_layers : a.nl, D, it, rc) + g * (D / 8);
 #pragma unroll
           for (int i = 0; i < D / 8; i += 8) store8<T>(dst + i, f + i);
         } else {
@@ -704,18 +784,12 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     f = make_float4(f.x * inv, f.y * inv, f.z * inv, f.w * inv);
   };
   auto row_done = [&](const Item& it, int r, float4 f, float mm, float ll) {
-    if (MODE == kShared) {
-      const int64_t at = row_offset(p, a.nl, D, it, r);
-      *reinterpret_cast<float4*>(a.parts + at + lane * 4) = f;
-      if (lane == 0) a.weights[at / D] = make_float2(mm, ll);
-      return;
-    }
-    if (MODE == kRest && it.joined) {
+    if (MODE == kRest && it.extra) {
       float v[4] = {f.x, f.y, f.z, f.w};
       join_shared<D, 4>(p, a, row_offset(p, a.nl, D, it, r) / D, lane * 4, v, mm, ll);
       f = make_float4(v[0], v[1], v[2], v[3]);
     }
-    store4(reinterpret_cast<T*>(a.out) + row_offset(p, MODE == kAll ? a.nl : a.out_layers, D, it, r) + lane * 4, f);
+    store4(reinterpret_cast<T*>(a.out) + row_offset(p, MODE == kRest ? a.out_layers : a.nl, D, it, r) + lane * 4, f);
   };
   // Inside the CTA: the items that go on behind one of its warps (part 1), or begin before the first (part 0 of warp 0),
   // all rows dealt out to the warps in turn
@@ -732,7 +806,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     float* mine = cta_slots + (size_t)(2 * blockIdx.x + wh) * SLOT;
     auto part_of = [&](int i) { return (const float*)sh.where[w0 + i][i == 0 ? wh : 0]; };
     for (int r = 0; r < it.valid; ++r, ++turn) {
-      if (turn % PS_WARPS != warp) continue;
+      if (turn % PS_WARPS != warp || (MODE == kTree && it.extra >> r & 1)) continue;
       float4 f;
       float mm, ll;
       merge_row(part_of, wl - w0 + 1, r, f, mm, ll);
@@ -775,6 +849,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     const int c0 = (int)div64(it.begin, per_cta), c1 = (int)div64(it.begin + it.blocks - 1, per_cta);
     auto part_of = [&](int i) { return cta_slots + (size_t)(2 * (c0 + i) + (i == 0 ? 1 : 0)) * SLOT; };
     for (int r = warp; r < it.valid; r += PS_WARPS) {
+      if (MODE == kTree && it.extra >> r & 1) continue;
       float4 f;
       float mm, ll;
       merge_row(part_of, c1 - c0 + 1, r, f, mm, ll);
@@ -807,9 +882,12 @@ inline int launch_step(const PgParams& p, const PaArgs& a, size_t room, int coun
 
 template <typename T, bool E4M3, PaMode MODE>
 inline int launch_step_dim(const PgParams& p, const PaArgs& a, int dim, int rows, size_t room, int counters, cudaStream_t s) {
-  if (dim == 128)
+  if constexpr (MODE == kTree)                             // tiles of 8 rows: what the host has counted is for these
+    return dim == 128 ? launch_step<T, 128, 1, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 64, 1, E4M3, MODE>(p, a, room, counters, s);
+  else if (dim == 128)
     return rows > 8 ? launch_step<T, 128, 2, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 128, 1, E4M3, MODE>(p, a, room, counters, s);
-  return rows > 8 ? launch_step<T, 64, 2, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 64, 1, E4M3, MODE>(p, a, room, counters, s);
+  else
+    return rows > 8 ? launch_step<T, 64, 2, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 64, 1, E4M3, MODE>(p, a, room, counters, s);
 }
 
 // rows: the most of an entry, as far as the host knows
