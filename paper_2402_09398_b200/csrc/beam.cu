@@ -26,6 +26,7 @@ constexpr int BM_TILE = BM_THREADS * BM_UNROLL;           // 16-byte pieces of a
 constexpr int BM_LIST = 2048;                             // candidates that a list holds
 constexpr int BM_MOST_BEAMS = 64, BM_MOST_KEEP = 128;
 constexpr int BM_JOINED = 8192;                           // candidates of a group that are joined, about
+constexpr int BM_DIRECT = 512;                            // as many are compared with one another at once
 constexpr float kRefFar = 40.f;                           // a logit that far above the reference moves it
 constexpr double kClose = 0x1p-17;                        // more than the errors of two sums
 
@@ -110,11 +111,17 @@ __device__ __forceinline__ int bm_token(unsigned long long key) { return (int)(0
 // a beam that takes part: its score is finite
 __device__ __forceinline__ bool bm_live(float score) { return fabsf(score) <= FLT_MAX; }
 
-// (value, beam, token) of a candidate of the group
+// (value, beam, token) of a candidate of the group; the value as an integer of the same order
 struct BmCand {
-  double v;
-  unsigned long long at;                                  // beam << 32 | token
+  long long v;
+  unsigned long long at;                                  // beam << 32 | token, ~0 = none
 };
+constexpr long long kNoCand = (long long)0x8000000000000000ull;
+__device__ __forceinline__ long long bm_order(double v) {
+  const long long b = __double_as_longlong(v + 0.0);      // the two zeros are equal
+  return b ^ (b >> 63 & 0x7fffffffffffffffll);
+}
+__device__ __forceinline__ double bm_value(long long o) { return __longlong_as_double(o ^ (o >> 63 & 0x7fffffffffffffffll)); }
 __device__ __forceinline__ bool bm_before(const BmCand& a, const BmCand& b) { return a.v > b.v || (a.v == b.v && a.at < b.at); }
 
 struct BmShared {
@@ -131,13 +138,13 @@ struct BmShared {
     unsigned long long high[BM_THREADS];
     double dsum[BM_THREADS / 32];
   };
-  BmCand top[BM_MOST_KEEP + 1];
+  BmCand top[BM_MOST_KEEP];
   float wmax[BM_THREADS / 32];
   float ref[BM_THREADS / 32], sum[BM_THREADS / 32];
   float bar;
   unsigned long long bar_key;
   BmCand bar_cand;
-  unsigned long long again;                               // beams whose sums are computed in 64 bits
+  unsigned long long again, done;                         // beams whose sums are computed in 64 bits; that have ended
   int count, last;
 };
 
@@ -264,21 +271,23 @@ __device__ __forceinline__ double bm_exp2(double x) {
   p = fma(p, z, 1.0);
   return p * __hiloint2double(((int)n + 1023) << 20, 0);
 }
+// Which thread adds which tokens, and the reference, do not depend on where a row lies: equal rows give equal sums.
 template <typename T>
-__device__ __noinline__ double bm_exact_sum(BmShared& sh, const BmArgs& a, int r, float ref) {
-  constexpr int N = BmType<T>::N;
-  const BmRow<T> row(a, r);
+__device__ __noinline__ double bm_exact_sum(BmShared& sh, const BmArgs& a, int r) {
+  const T* row = reinterpret_cast<const T*>(a.logits) + (int64_t)r * a.stride;
   const int tid = threadIdx.x;
-  const double m = ref, log2e = 1.44269504088896340735992;
+  unsigned long long top = 0;                              // the largest logit: a stretch's first
+  for (int s = 0; s < a.splits; ++s) top = max(top, __ldcg(a.keys + ((size_t)r * a.splits + s) * a.keep));
+  const double m = bm_logit(top), log2e = 1.44269504088896340735992;
   double s = 0.0;
-  for (int at = tid; at < row.pieces; at += BM_THREADS) {
+  constexpr int N = 8;
+  for (int at = tid; at < a.vocab; at += N * BM_THREADS) {
     float f[N];
-    BmType<T>::unpack(row.piece(at), f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = at + i * BM_THREADS < a.vocab ? BmType<T>::load(row + at + i * BM_THREADS) : -INFINITY;
 #pragma unroll
     for (int i = 0; i < N; ++i) s += bm_exp2(((double)fminf(f[i], BmType<T>::most) - m) * log2e);
   }
-  const int token = row.single(tid, true, true);
-  if (token >= 0) s += bm_exp2(((double)fminf(BmType<T>::load(row.base + token), BmType<T>::most) - m) * log2e);
 #pragma unroll
   for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
   __syncthreads();
@@ -298,11 +307,16 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
   const float2* sums = a.sums + (size_t)group * B * a.splits;
   const float* scores = a.scores + (size_t)group * B;
   const uint8_t* ended = a.ended ? a.ended + (size_t)group * B : nullptr;
+  // asked for early
+  const unsigned long long first_key = tid < total ? __ldcg(keys + tid) : 0;
+  if (tid == 0) sh.done = 0;
   __syncthreads();
   for (int b = warp; b < B; b += BM_THREADS / 32) {
     const float score = __ldcg(scores + b);
+    const bool done = ended && __ldcg(ended + b);
     double c = bm_live(score) ? (double)score : -INFINITY, lse = 0.0;
-    if (bm_live(score) && !(ended && __ldcg(ended + b))) {
+    if (done && lane == 0) atomicOr(&sh.done, 1ull << b);
+    if (bm_live(score) && !done) {
       float m = -INFINITY;
       for (int s = lane; s < a.splits; s += 32) {
         const float2 x = __ldcg(sums + b * a.splits + s);
@@ -326,45 +340,51 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     }
   }
   if (tid == 0) sh.again = 0;
-  // candidate i of the group's lists; at = ~0: none
-  auto cand = [&](int i) {
-    BmCand x = {-INFINITY, ~0ull};
-    const int b = i / per_beam, k = i - b * per_beam;
+  __syncthreads();
+  // candidate i of the group's lists, whose key is at hand; at = ~0: none
+  auto cand = [&](int i, unsigned long long key) {
+    BmCand x = {kNoCand, ~0ull};
+    const int b = i / per_beam;
     const double c = sh.j.score[b];
     if (c == -INFINITY) return x;
-    if (ended && __ldcg(ended + b)) {
-      if (k == 0 && a.end_token >= 0) x = {c, (unsigned long long)b << 32 | (uint32_t)a.end_token};
+    if (sh.done >> b & 1) {
+      if (i == b * per_beam && a.end_token >= 0) x = {bm_order(c), (unsigned long long)b << 32 | (uint32_t)a.end_token};
       return x;
     }
-    const unsigned long long key = __ldcg(keys + i);
-    if (key) x = {c + ((double)bm_logit(key) - sh.j.lse[b]), (unsigned long long)b << 32 | (uint32_t)bm_token(key)};
+    if (key) x = {bm_order(c + ((double)bm_logit(key) - sh.j.lse[b])), (unsigned long long)b << 32 | (uint32_t)bm_token(key)};
     return x;
   };
-  auto exact = [&](const BmCand& x) { return ended && __ldcg(ended + (x.at >> 32)); };   // its value has no sum in it
+  auto both_done = [&](const BmCand& x, const BmCand& y) { return sh.done >> (x.at >> 32) & sh.done >> (y.at >> 32) & 1; };   // no sums in them
+  auto differ = [&](const BmCand& x, const BmCand& y) {   // two neighbours whose order the errors of the sums could change
+    if (bm_value(x.v) - bm_value(y.v) <= kClose && x.at >> 32 != y.at >> 32 && !both_done(x, y))
+      atomicOr(&sh.again, 1ull << (x.at >> 32) | 1ull << (y.at >> 32));
+  };
 
   for (bool refined = false;; refined = true) {
+    if (tid == 0) sh.count = 0;
     __syncthreads();
-    // the bar: the keep-th of the threads' best ones
-    BmCand best = {-INFINITY, ~0ull};
+    long long bar = kNoCand + 1;
+    const bool direct = total <= BM_DIRECT;               // every candidate is compared with every other
+    if (!direct) {
+      // the bar: the keep-th of the threads' best ones, less what the errors of the sums could change
+      BmCand best = {kNoCand, ~0ull};
+      for (int i = tid; i < total; i += BM_THREADS) {
+        const BmCand x = cand(i, __ldcg(keys + i));
+        if (bm_before(x, best)) best = x;
+      }
+      sh.most[tid] = best;
+      if (tid == 0) sh.bar_cand.v = bar;
+      __syncthreads();
+      if (best.at != ~0ull) {
+        int larger = 0;
+        for (int i = 0; i < BM_THREADS; ++i) larger += bm_before(sh.most[i], best);
+        if (larger == K - 1) sh.bar_cand.v = bm_order(bm_value(best.v) - kClose);
+      }
+      __syncthreads();
+      bar = sh.bar_cand.v;
+    }
     for (int i = tid; i < total; i += BM_THREADS) {
-      const BmCand x = cand(i);
-      if (bm_before(x, best)) best = x;
-    }
-    sh.most[tid] = best;
-    if (tid == 0) {
-      sh.count = 0;
-      sh.bar_cand.v = -INFINITY;
-    }
-    __syncthreads();
-    if (best.at != ~0ull) {
-      int larger = 0;
-      for (int i = 0; i < BM_THREADS; ++i) larger += bm_before(sh.most[i], best);
-      if (larger == K - 1) sh.bar_cand = best;
-    }
-    __syncthreads();
-    const double bar = sh.bar_cand.v - kClose;
-    for (int i = tid; i < total; i += BM_THREADS) {
-      const BmCand x = cand(i);
+      const BmCand x = cand(i, direct && i == tid ? first_key : __ldcg(keys + i));
       if (x.at != ~0ull && x.v >= bar) {
         const int n = atomicAdd(&sh.count, 1);
         if (n < BM_LIST / 2) sh.j.cand[n] = x;
@@ -374,38 +394,31 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     const int count = sh.count;
     int found;
     if (count <= BM_LIST / 2) {
-      found = min(count, K + 1);
+      found = min(count, K);
       for (int i = tid; i < count; i += BM_THREADS) {
         const BmCand x = sh.j.cand[i];
         int rank = 0;
         for (int k = 0; k < count; ++k) rank += bm_before(sh.j.cand[k], x);
-        if (rank <= K) sh.top[rank] = x;
+        if (rank < K) sh.top[rank] = x;
       }
       __syncthreads();
-      if (!refined) {                                     // neighbours that the sums' errors could exchange
-        for (int i = tid; i + 1 < min(count, K); i += BM_THREADS) {
-          const BmCand x = sh.top[i], y = sh.top[i + 1];
-          if (x.v - y.v <= kClose && x.at >> 32 != y.at >> 32 && !(exact(x) && exact(y)))
-            atomicOr(&sh.again, 1ull << (x.at >> 32) | 1ull << (y.at >> 32));
-        }
+      if (!refined) {
+        for (int i = tid; i + 1 < found; i += BM_THREADS) differ(sh.top[i], sh.top[i + 1]);
         if (count > K) {                                  // and those that could come in
           const BmCand x = sh.top[K - 1];
-          for (int i = tid; i < count; i += BM_THREADS) {
-            const BmCand y = sh.j.cand[i];
-            if (bm_before(x, y) && x.v - y.v <= kClose && x.at >> 32 != y.at >> 32 && !(exact(x) && exact(y)))
-              atomicOr(&sh.again, 1ull << (x.at >> 32) | 1ull << (y.at >> 32));
-          }
+          for (int i = tid; i < count; i += BM_THREADS)
+            if (bm_before(x, sh.j.cand[i])) differ(x, sh.j.cand[i]);
         }
       }
     } else {
       // too many near the bar: one after the other, and all sums in 64 bits
       found = 0;
-      BmCand last = {INFINITY, 0};
+      BmCand last = {0x7fffffffffffffffll, 0};
       if (!refined && tid == 0) sh.again = ~0ull;
       for (; refined && found < K; ++found) {
-        BmCand x = {-INFINITY, ~0ull};
+        BmCand x = {kNoCand, ~0ull};
         for (int i = tid; i < total; i += BM_THREADS) {
-          const BmCand y = cand(i);
+          const BmCand y = cand(i, __ldcg(keys + i));
           if (y.at != ~0ull && bm_before(last, y) && bm_before(y, x)) x = y;
         }
         __syncthreads();
@@ -425,26 +438,22 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     if (refined || again == 0) {
       for (int i = tid; i < K; i += BM_THREADS) {
         const bool some = i < found;
-        const BmCand x = some ? sh.top[i] : BmCand{-INFINITY, 0};
+        const unsigned long long at = some ? sh.top[i].at : 0;
         const size_t o = (size_t)group * K + i;
-        const int token = some ? (int)(uint32_t)x.at : -1;
-        a.out_scores[o] = (float)x.v;
+        const int token = some ? (int)(uint32_t)at : -1;
+        a.out_scores[o] = some ? (float)bm_value(sh.top[i].v) : -INFINITY;
         a.out_tokens[o] = token;
-        a.out_parents[o] = group * B + (some ? (int)(x.at >> 32) : min(i, B - 1));
+        a.out_parents[o] = group * B + (some ? (int)(at >> 32) : min(i, B - 1));
         if (a.out_ended) a.out_ended[o] = some && token == a.end_token;
       }
       return;
     }
     for (int b = 0; b < B; ++b) {
-      if (!(again >> b & 1) || sh.j.score[b] == -INFINITY || (ended && __ldcg(ended + b))) continue;   // uniform over the block
-      float m = -INFINITY;
-      for (int s = 0; s < a.splits; ++s) {
-        const float2 x = __ldcg(sums + b * a.splits + s);
-        if (x.y > 0.f) m = fmaxf(m, x.x);
-      }
-      const double lse = bm_exact_sum<T>(sh, a, group * B + b, m);
+      if (!(again >> b & 1) || sh.j.score[b] == -INFINITY || (sh.done >> b & 1)) continue;   // uniform over the block
+      const double lse = bm_exact_sum<T>(sh, a, group * B + b);
       if (tid == 0) sh.j.lse[b] = lse;
     }
+    __syncthreads();
   }
 }
 
@@ -454,26 +463,26 @@ __global__ void __launch_bounds__(BM_THREADS, 4) beam_select_kernel(BmArgs a) {
   __shared__ BmShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / a.splits, split = blockIdx.x - r * a.splits, group = r / a.beams;
+  const BmRow<T> row(a, r);
+  const int p0 = min(row.pieces, split * a.per), p1 = min(row.pieces, p0 + a.per);
+  const bool front = split == 0, back = split == a.splits - 1;
+  uint4 w[BM_UNROLL];
+  auto load = [&](int at) {
+#pragma unroll
+    for (int u = 0; u < BM_UNROLL; ++u) {
+      const int i = at + u * BM_THREADS + tid;
+      if (i < p1) w[u] = row.piece(i);
+    }
+  };
   pg_wait();
+  // the first tile is asked for before it is known whether the beam takes part
   const float score = __ldcg(a.scores + r);
   const bool done = a.ended && __ldcg(a.ended + r);
+  load(p0);
+  const int single = row.single(tid, front, back);
+  const float lone = single >= 0 ? fminf(BmType<T>::load(row.base + single), BmType<T>::most) : -INFINITY;
   if (bm_live(score) && !done) {
-    const BmRow<T> row(a, r);
-    const int p0 = min(row.pieces, split * a.per), p1 = min(row.pieces, p0 + a.per);
-    const bool front = split == 0, back = split == a.splits - 1;
     unsigned long long* out = a.keys + ((size_t)r * a.splits + split) * a.keep;
-
-    uint4 w[BM_UNROLL];
-    auto load = [&](int at) {
-#pragma unroll
-      for (int u = 0; u < BM_UNROLL; ++u) {
-        const int i = at + u * BM_THREADS + tid;
-        if (i < p1) w[u] = row.piece(i);
-      }
-    };
-    load(p0);
-    const int single = row.single(tid, front, back);
-    const float lone = single >= 0 ? fminf(BmType<T>::load(row.base + single), BmType<T>::most) : -INFINITY;
 
     // ---- the first tile: reference and bar ----
     float best = lone;
@@ -623,13 +632,13 @@ static bool valid_beams(const less_beams* d) {
   return d->groups <= (1 << 20) / d->beams;               // rows
 }
 
-// A row is cut so that a call has some 2400 CTAs, four on a multiprocessor, but for no less than 4096 elements each, nor
-// into so many lists that joining them shows.
+// A row is cut so that all CTAs of a call, four on a multiprocessor, run at once, but for no less than 4096 elements each, nor
+// into so many lists that joining them shows (64 groups of 8 beams of 128 256: cut in five, 4.3 times as many, 77 us).
 static BmLayout bm_layout(const less_beams* d) {
   BmLayout l;
   const int64_t rows = (int64_t)d->groups * d->beams;
   int64_t s = pg_ceil(d->vocab, 4096);
-  if (s > (2400 + rows - 1) / rows) s = (2400 + rows - 1) / rows;
+  if (s > 4 * 148 / rows) s = 4 * 148 / rows;
   if (s > BM_JOINED / (d->beams * d->keep)) s = BM_JOINED / (d->beams * d->keep);
   l.splits = (int)(s < 1 ? 1 : s);
   size_t at = ((size_t)d->groups * 4 + 255) / 256 * 256;

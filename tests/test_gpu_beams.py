@@ -99,7 +99,7 @@ def test_ties_and_crowds(dtype):
     logits[1] = up.to(TYPES[dtype])
     logits[2] = up.flip(0).to(TYPES[dtype])
     logits[3, :, ::2] = -0.0
-    logits[4] = torch.randn(vocab, device=DEV).to(TYPES[dtype])
+    logits[4] = torch.randn(vocab, generator=torch.Generator().manual_seed(5)).to(TYPES[dtype])
     logits[5, 0, 12345], logits[5, 1, 12345], logits[5, 2, 9] = 1.0, 1.0, 1.0
     logits[6, :, :9000] = -float("inf")                   # first tiles without candidates
     scores = torch.full((groups, beams), -0.5, device=DEV)
@@ -146,6 +146,17 @@ def test_beams_closer_than_fp32_tells_apart(seed):
     steps = torch.randint(-2, 3, (4, beams), generator=g)
     scores = (-1.0 + steps * 2.0 ** -23).to(DEV)
     check(sel, logits, scores)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("seed", range(6))
+def test_equal_beams_at_different_addresses(dtype, seed):
+    """Rows of the same logits, each at another alignment: exact ties, the lowest beam first."""
+    beams, vocab = 7, [501, 8191, 20001][seed % 3]
+    sel = make(2, beams, vocab, 30, TYPES[dtype])
+    g = torch.Generator().manual_seed(seed)
+    logits = (torch.randn(2, 1, vocab, generator=g) * 2.5).to(TYPES[dtype]).expand(2, beams, vocab).contiguous().to(DEV)
+    check(sel, logits, torch.full((2, beams), -1.0, device=DEV))
 
 
 def test_in_place_captured_and_on_a_stream():
