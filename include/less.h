@@ -477,7 +477,8 @@ int less_pages_poll_status(const less_pages* cache, void* cuda_stream);
  * The selection.  The candidates of a group are (beam, token) with
  *     value = score[beam] + logit[beam, token] - log sum exp logit[beam]
  * and, for a beam that has ended, (beam, end_token) alone with value = score[beam].  The `keep` largest are the result,
- * largest first, ties to the lowest (beam, token); order and ties are those of 64-bit arithmetic.  A logit that is NaN
+ * largest first, ties to the lowest (beam, token); order and ties are those of 64-bit arithmetic (in a beam, those of the
+ * logits, also where a very large one makes equal values of them).  A logit that is NaN
  * counts as -inf, +inf as the largest finite value of its type; no candidate: a logit of -inf, a beam whose score is not
  * finite (a beam that does not exist has -inf).  Where there are fewer than `keep` candidates: score -inf, token -1, the
  * parent in the same place (the last one from beam `beams` on), not ended. */
@@ -491,7 +492,7 @@ enum {
 typedef struct less_beams {
   int32_t groups;
   int32_t beams;            /* 1 .. LESS_BEAMS_MOST_BEAMS; groups * beams <= 2^20 */
-  int32_t vocab;
+  int32_t vocab;            /* 1 .. 2^26 */
   int32_t keep;             /* 1 .. LESS_BEAMS_MOST_KEEP */
   int32_t end_token;        /* -1 = none */
   uint32_t flags;
@@ -504,8 +505,7 @@ size_t less_beams_workspace_bytes(const less_beams* beams);   /* 0 if the descri
 /* logits: device [groups, beams, vocab], `row_stride` elements from beam to beam (>= vocab, any alignment of the type);
  * scores: device fp32 [groups, beams]; ended: device bytes [groups, beams], not 0 = has ended, or NULL (with end_token -1 it
  * has to be NULL).  Results, device [groups, keep]: out_scores fp32 (values, rounded once), out_tokens, out_parents int32
- * (group * beams + beam), out_ended bytes (token == end_token) or NULL.  With keep == beams out_scores may be scores and
- * out_ended may be ended; no other buffers may overlap.  Asynchronous, allocates nothing, can be captured; one call at a
+ * (group * beams + beam), out_ended bytes (token == end_token) or NULL; none may overlap an input.  Asynchronous, allocates nothing, can be captured; one call at a
  * time per workspace, replays of captured ones included.  Runs on the current device. */
 int less_beam_select(const less_beams* beams, const void* logits, int64_t row_stride, const float* scores,
                      const uint8_t* ended, float* out_scores, int32_t* out_tokens, int32_t* out_parents,

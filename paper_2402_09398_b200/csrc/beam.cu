@@ -3,74 +3,97 @@
 //   v(b, t) = score_b + l(b, t) - log sum_u exp l(b, u),     ties to the lowest (b, t)
 //
 // Bound by memory: every logit of a live beam is read once (2 or 4 bytes; an exponential, a sum and two comparisons each).
-//   - A row of logits is cut over several CTAs.  Each takes its stretch in one pass: sum of exponentials relative to a
-//     reference (the largest logit of its first tile; moved only where a later one lies more than 2^57 above), and its
-//     `keep` largest logits.  Those pass a bar: the keep-th largest of the maxima of 64 (256) groups of threads over the
-//     first tile, which at least `keep` elements reach and, of n elements like those of the tile, about keep n / tile.
-//     They go to a list in shared memory, from which the largest are taken by counting for each how many are larger.
-//   - The CTA of a group that arrives last joins: the rows' sums, then the candidates of all beams the same way.
-// Within a beam the order is that of the logits, which is exact.  Between beams it hangs on the sums.  Their fp32
-// arithmetic is off by at most 2 * 2^-22 (exponentials) + 17 * 2^-23.2 (their arguments, whose mean distance from the largest
-// is at most log2 of the number of tokens) + 8 * 2^-24 (a thread's sum over a tile; the rest is in 64 bits), 2.8e-6 in all;
-// so where two neighbours in the order are of different beams and closer than kClose, the sums of these beams are computed
-// again in 64 bits and the candidates joined once more.  (Chances are some 1e-4 per kept candidate.)
+//   - A row of logits is cut into stretches, a CTA each, where there are too few rows to fill the GPU.  A CTA takes, in one
+//     pass, the sum of exponentials relative to a reference (the largest logit of its first tile; moved only
+//     where a later one lies more than 2^57 above) and its `keep` largest logits.  Those pass a bar: the keep-th largest of
+//     the maxima of 64 (256) groups of threads over the first tile, which at least `keep` elements reach and, of n elements
+//     like those of the tile, about keep n / tile.  They go to a list in shared memory, which is cut down to the largest
+//     `keep`, and the bar raised, whenever twice as many elements have been seen.
+//   - The CTA of a group that arrives last joins: the rows' sums, then the candidates of all beams, by counting for each how
+//     many come before it.
+// Within a beam the order is that of the logits, which is exact.  Between beams it hangs on the sums.  A term exp2(x) of
+// one is off, relative, by 2^-22 (the exponential), |x| 2^-23.4 (x: a product with a rounded factor, for fp32 logits of a
+// rounded difference) and 4 * 2^-24 (added to seven others of its piece; the rest is in 64 bits, rounded once at the end), so
+// a sum by at most 6e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it.
+// Where two neighbours in the order are of different beams and closer than that, the sums of these beams are computed again
+// in 64 bits and the candidates joined once more (a chance of some 1e-4 per kept candidate; WORST us for a row of 128 256).
 #include <float.h>
+
+#include <atomic>
 
 #include "less_internal.cuh"
 #include "pages_attn.cuh"
 
 namespace less {
 
-constexpr int BM_THREADS = 256, BM_UNROLL = 4;            // 16-byte pieces of a thread on their way
-constexpr int BM_TILE = BM_THREADS * BM_UNROLL;           // 16-byte pieces of a tile
-constexpr int BM_LIST = 2048;                             // candidates that a list holds
+constexpr int BM_THREADS = 256;
+constexpr int BM_RING = 8;                                // 16-byte pieces of a thread on their way (a thread's own, so no barriers)
+constexpr int BM_FIRST = 4;                               // of them those of the first tile
+constexpr int BM_LIST = 1280;                             // candidates that a list holds: more than 9 BM_MOST_KEEP
+constexpr int BM_CTAS = 4;                                // on a multiprocessor
 constexpr int BM_MOST_BEAMS = 64, BM_MOST_KEEP = 128;
 constexpr int BM_JOINED = 8192;                           // candidates of a group that are joined, about
-constexpr int BM_DIRECT = 512;                            // as many are compared with one another at once
+constexpr int BM_DIRECT = 320;                            // as many are compared with one another at once
 constexpr float kRefFar = 40.f;                           // a logit that far above the reference moves it
-constexpr double kClose = 0x1p-17;                        // more than the errors of two sums
+// error of a sum: kSumError + kTermError times the mean of |x|
+constexpr double kSumError = 6.0e-7, kTermError = 1.0e-7;
 
 struct BmArgs {
   const void* logits;
   int64_t stride;                                         // elements from row to row
   const float* scores;
   const uint8_t* ended;                                   // or null
-  int groups, beams, vocab, keep, end_token, splits, per; // per: 16-byte pieces of a CTA
+  int groups, beams, vocab, keep, end_token;
+  int splits, per;                                        // stretches of a row, 16-byte pieces of each
   float* out_scores;
   int32_t* out_tokens;
   int32_t* out_parents;
   uint8_t* out_ended;
   int32_t* counters;                                      // [groups] zero between calls
-  float2* sums;                                           // [rows][splits] (reference, sum)
+  float4* sums;                                           // [rows][splits] (reference, sum, sum of the terms times -x, 0)
   unsigned long long* keys;                               // [rows][splits][keep]
 };
 
+// Elements of 16 bytes and what is done with them packed.  NaN counts as -inf throughout: a maximum ignores it.
 template <typename T>
 struct BmType;
 template <>
 struct BmType<float> {
-  static constexpr int N = 4;                             // elements of 16 bytes
+  static constexpr int N = 4;
   static constexpr float most = FLT_MAX;
-  static __device__ __forceinline__ void unpack(uint4 w, float* f) {    // NaN counts as -inf
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = fmaxf(__uint_as_float(u[i]), -INFINITY);
-  }
+  static __device__ __forceinline__ float below(float x) { return __fsub_rd(x, 87.f); }
+  static __device__ __forceinline__ uint32_t pack(float x) { return __float_as_uint(x); }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+  static __device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) { return __float_as_uint(fminf(__uint_as_float(a), __uint_as_float(b))); }
+  static __device__ __forceinline__ float top(uint32_t m) { return __uint_as_float(m); }
+  static __device__ __forceinline__ void unpack(uint32_t u, float* f) { f[0] = __uint_as_float(u); }
   static __device__ __forceinline__ float load(const void* p) { return fmaxf(__ldcg((const float*)p), -INFINITY); }
 };
 template <>
 struct BmType<__half> {
   static constexpr int N = 8;
   static constexpr float most = 65504.f;
-  static __device__ __forceinline__ void unpack(uint4 w, float* f) {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-    const __half2 low = __half2half2(__ushort_as_half(0xfc00));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 x = __half22float2(__hmax2(*reinterpret_cast<const __half2*>(&u[i]), low));
-      f[2 * i] = x.x;
-      f[2 * i + 1] = x.y;
-    }
+  static __device__ __forceinline__ float below(float x) { return __half2float(__float2half_rd(x - 87.f)); }
+  static __device__ __forceinline__ uint32_t pack(float x) {
+    const __half2 h = __float2half2_rn(x);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    const __half2 h = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) {
+    const __half2 h = __hmin2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float top(uint32_t m) {
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&m));
+    return fmaxf(x.x, x.y);
+  }
+  static __device__ __forceinline__ void unpack(uint32_t u, float* f) {
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u));
+    f[0] = x.x;
+    f[1] = x.y;
   }
   static __device__ __forceinline__ float load(const void* p) {
     return fmaxf(__half2float(__ushort_as_half(__ldcg((const unsigned short*)p))), -INFINITY);
@@ -80,21 +103,43 @@ template <>
 struct BmType<__nv_bfloat16> {
   static constexpr int N = 8;
   static constexpr float most = 3.38953138925153547590470800371487866880e+38f;
-  static __device__ __forceinline__ void unpack(uint4 w, float* f) {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-    const __nv_bfloat162 low = __bfloat162bfloat162(__ushort_as_bfloat16(0xff80));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 c = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&u[i]), low);
-      const uint32_t x = *reinterpret_cast<const uint32_t*>(&c);
-      f[2 * i] = __uint_as_float(x << 16);
-      f[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
-    }
+  static __device__ __forceinline__ float below(float x) { return __bfloat162float(__float2bfloat16_rd(__fsub_rd(x, 87.f))); }
+  static __device__ __forceinline__ uint32_t pack(float x) {
+    const __nv_bfloat162 h = __float2bfloat162_rn(x);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 h = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 h = __hmin2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float top(uint32_t m) { return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u)); }
+  static __device__ __forceinline__ void unpack(uint32_t u, float* f) {
+    f[0] = __uint_as_float(u << 16);
+    f[1] = __uint_as_float(u & 0xffff0000u);
   }
   static __device__ __forceinline__ float load(const void* p) {
     return fmaxf(__uint_as_float((uint32_t)__ldcg((const unsigned short*)p) << 16), -INFINITY);
   }
 };
+
+template <typename T>
+__device__ __forceinline__ float bm_top(const uint4& w) {               // the largest; NaN: all are
+  typedef BmType<T> B;
+  return B::top(B::larger(B::larger(w.x, w.y), B::larger(w.z, w.w)));
+}
+template <typename T>
+__device__ __forceinline__ void bm_unpack(const uint4& w, uint32_t floor, float* f) {    // at least the floor
+  typedef BmType<T> B;
+  constexpr int N = B::N / 4;
+  B::unpack(B::larger(w.x, floor), f);
+  B::unpack(B::larger(w.y, floor), f + N);
+  B::unpack(B::larger(w.z, floor), f + 2 * N);
+  B::unpack(B::larger(w.w, floor), f + 3 * N);
+}
 
 // order of a beam's candidates: the logit, then the lower token; 0 = none
 __device__ __forceinline__ unsigned long long bm_key(float l, int token) {
@@ -114,8 +159,13 @@ __device__ __forceinline__ bool bm_live(float score) { return fabsf(score) <= FL
 // (value, beam, token) of a candidate of the group; the value as an integer of the same order
 struct BmCand {
   long long v;
-  unsigned long long at;                                  // beam << 32 | token, ~0 = none
+  unsigned long long at;                                  // what decides between equal values: the beam (6 bits), the larger
+                                                          // logit (32), the token (26); ~0 = none
 };
+__device__ __forceinline__ unsigned long long bm_at(int beam, unsigned long long key, int token) {
+  return (unsigned long long)beam << 58 | (unsigned long long)~(uint32_t)(key >> 32) << 26 | (uint32_t)token;
+}
+__device__ __forceinline__ int bm_beam(const BmCand& x) { return (int)(x.at >> 58); }
 constexpr long long kNoCand = (long long)0x8000000000000000ull;
 __device__ __forceinline__ long long bm_order(double v) {
   const long long b = __double_as_longlong(v + 0.0);      // the two zeros are equal
@@ -125,11 +175,12 @@ __device__ __forceinline__ double bm_value(long long o) { return __longlong_as_d
 __device__ __forceinline__ bool bm_before(const BmCand& a, const BmCand& b) { return a.v > b.v || (a.v == b.v && a.at < b.at); }
 
 struct BmShared {
+  uint4 ring[BM_RING][BM_THREADS];
   union {
     unsigned long long list[BM_LIST];
     struct {
       BmCand cand[BM_LIST / 2];
-      double score[BM_MOST_BEAMS], lse[BM_MOST_BEAMS];    // -inf = no candidates
+      double score[BM_MOST_BEAMS], lse[BM_MOST_BEAMS], err[BM_MOST_BEAMS];   // -inf = no candidates; error of the second
     } j;
   };
   union {
@@ -138,9 +189,13 @@ struct BmShared {
     unsigned long long high[BM_THREADS];
     double dsum[BM_THREADS / 32];
   };
-  BmCand top[BM_MOST_KEEP];
+  union {
+    BmCand top[BM_MOST_KEEP];
+    unsigned long long kept[BM_MOST_KEEP];
+  };
   float wmax[BM_THREADS / 32];
-  float ref[BM_THREADS / 32], sum[BM_THREADS / 32];
+  float ref[BM_THREADS / 32];
+  double pow2[32];                                        // 2^(k / 32)
   float bar;
   unsigned long long bar_key;
   BmCand bar_cand;
@@ -158,6 +213,22 @@ __device__ __forceinline__ float bm_block_max(BmShared& sh, float x) {
 #pragma unroll
   for (int w = 1; w < BM_THREADS / 32; ++w) x = fmaxf(x, sh.wmax[w]);
   return x;
+}
+
+// For each of `count` things how many come before it, before(k, i): eight lanes per thing.  Whole block; `put(i, rank)` is one
+// lane's.
+template <typename Before, typename Put>
+__device__ __forceinline__ void bm_rank(int count, Before before, Put put) {
+  for (int base = 0; base < count; base += BM_THREADS / 8) {
+    const int i = base + (int)threadIdx.x / 8;
+    int rank = 0;
+    if (i < count)
+#pragma unroll 4
+      for (int k = threadIdx.x & 7; k < count; k += 8) rank += before(k, i);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, d);
+    if (i < count && (threadIdx.x & 7) == 0) put(i, rank);
+  }
 }
 
 // The elements of a row by 16-byte pieces: `head` before the first whole one, `tail` behind the last
@@ -202,7 +273,7 @@ __device__ __noinline__ void bm_crowded(BmShared& sh, const BmArgs& a, const BmR
         n = 1;
       }
     } else if (at + tid < p1) {
-      BmType<T>::unpack(row.piece(at + tid), f);
+      bm_unpack<T>(row.piece(at + tid), BmType<T>::pack(-INFINITY), f);
       token = row.token(at + tid);
       n = N;
     }
@@ -278,15 +349,34 @@ __device__ __noinline__ double bm_exact_sum(BmShared& sh, const BmArgs& a, int r
   const int tid = threadIdx.x;
   unsigned long long top = 0;                              // the largest logit: a stretch's first
   for (int s = 0; s < a.splits; ++s) top = max(top, __ldcg(a.keys + ((size_t)r * a.splits + s) * a.keep));
-  const double m = bm_logit(top), log2e = 1.44269504088896340735992;
+  const float m = bm_logit(top);
+  if (tid < 32) sh.pow2[tid] = bm_exp2(tid / 32.0);
+  __syncthreads();
   double s = 0.0;
-  constexpr int N = 8;
-  for (int at = tid; at < a.vocab; at += N * BM_THREADS) {
-    float f[N];
+  constexpr int N = 4;
+  float f[N];
+  auto load = [&](int at) {
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = at + i * BM_THREADS < a.vocab ? BmType<T>::load(row + at + i * BM_THREADS) : -INFINITY;
+  };
+  load(tid);
+  for (int at = tid; at < a.vocab; at += N * BM_THREADS) {
+    float x[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += bm_exp2(((double)fminf(f[i], BmType<T>::most) - m) * log2e);
+    for (int i = 0; i < N; ++i) x[i] = fmaxf(fminf(f[i], BmType<T>::most), m - 680.f);   // smaller ones: below 2^-980 each
+    load(at + N * BM_THREADS);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      // l - m = k ln 2 / 32 + z, |z| <= 0.011; e^z by its Taylor polynomial of degree 5 (error below 3e-15)
+      const float k = rintf((x[i] - m) * 46.16624130844683f);
+      const double z = fma((double)k, -0.0216608493924982909192, (double)x[i] - (double)m);
+      double p = fma(1.0 / 120.0, z, 1.0 / 24.0);
+      p = fma(p, z, 1.0 / 6.0);
+      p = fma(p, z, 0.5);
+      p = fma(p, z, 1.0);
+      p = fma(p, z, 1.0) * sh.pow2[(int)k & 31];
+      s += __hiloint2double(__double2hiint(p) + (((int)k >> 5) << 20), __double2loint(p));
+    }
   }
 #pragma unroll
   for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
@@ -295,48 +385,60 @@ __device__ __noinline__ double bm_exact_sum(BmShared& sh, const BmArgs& a, int r
   __syncthreads();
   s = 0.0;
   for (int w = 0; w < BM_THREADS / 32; ++w) s += sh.dsum[w];
-  return m + log(s);
+  return (double)m + log(s);
 }
 
 // The candidates of a group: its beams' lists, an ended beam's one.  Whole block of the CTA that arrived last.
 template <typename T>
 __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.beams, K = a.keep;
-  const int per_beam = a.splits * K, total = B * per_beam;
-  const unsigned long long* keys = a.keys + (size_t)group * B * per_beam;
-  const float2* sums = a.sums + (size_t)group * B * a.splits;
+  const unsigned long long* keys = a.keys + (size_t)group * B * a.splits * K;
+  const float4* sums = a.sums + (size_t)group * B * a.splits;
   const float* scores = a.scores + (size_t)group * B;
   const uint8_t* ended = a.ended ? a.ended + (size_t)group * B : nullptr;
-  // asked for early
-  const unsigned long long first_key = tid < total ? __ldcg(keys + tid) : 0;
+  const int per_beam = a.splits * K, total = B * per_beam;
+  // (of a beam that is not live: what lies there, which nobody looks at)
+  auto key_of = [&](int i) { return __ldcg(keys + i); };
+  const unsigned long long first_key = tid < total ? key_of(tid) : 0;   // asked for early
   if (tid == 0) sh.done = 0;
   __syncthreads();
   for (int b = warp; b < B; b += BM_THREADS / 32) {
     const float score = __ldcg(scores + b);
     const bool done = ended && __ldcg(ended + b);
-    double c = bm_live(score) ? (double)score : -INFINITY, lse = 0.0;
+    double c = bm_live(score) ? (double)score : -INFINITY, lse = 0.0, err = 0.0;
     if (done && lane == 0) atomicOr(&sh.done, 1ull << b);
     if (bm_live(score) && !done) {
       float m = -INFINITY;
       for (int s = lane; s < a.splits; s += 32) {
-        const float2 x = __ldcg(sums + b * a.splits + s);
+        const float4 x = __ldcg(sums + b * a.splits + s);
         if (x.y > 0.f) m = fmaxf(m, x.x);
       }
 #pragma unroll
       for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-      double sum = 0.0;
+      double sum = 0.0, far = 0.0;
       for (int s = lane; s < a.splits; s += 32) {
-        const float2 x = __ldcg(sums + b * a.splits + s);
-        if (x.y > 0.f) sum += (double)x.y * bm_exp2(((double)x.x - (double)m) * 1.44269504088896340735992);
+        const float4 x = __ldcg(sums + b * a.splits + s);
+        if (!(x.y > 0.f)) continue;
+        const double back = ((double)x.x - (double)m) * 1.44269504088896340735992, scale = bm_exp2(back);
+        sum += (double)x.y * scale;
+        if (scale > 0.0) far += ((double)x.z - back * (double)x.y) * scale;
       }
 #pragma unroll
-      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (sum > 0.0) lse = (double)m + log(sum);
-      else c = -INFINITY;
+      for (int d = 16; d; d >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        far += __shfl_xor_sync(0xffffffffu, far, d);
+      }
+      if (sum > 0.0) {
+        lse = (double)m + log(sum);
+        err = kSumError + kTermError * far / sum;
+      } else {
+        c = -INFINITY;
+      }
     }
     if (lane == 0) {
       sh.j.score[b] = c;
       sh.j.lse[b] = lse;
+      sh.j.err[b] = err;
     }
   }
   if (tid == 0) sh.again = 0;
@@ -348,43 +450,55 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     const double c = sh.j.score[b];
     if (c == -INFINITY) return x;
     if (sh.done >> b & 1) {
-      if (i == b * per_beam && a.end_token >= 0) x = {bm_order(c), (unsigned long long)b << 32 | (uint32_t)a.end_token};
+      if (i == b * per_beam && a.end_token >= 0) x = {bm_order(c), bm_at(b, 0, a.end_token)};
       return x;
     }
-    if (key) x = {bm_order(c + ((double)bm_logit(key) - sh.j.lse[b])), (unsigned long long)b << 32 | (uint32_t)bm_token(key)};
+    if (key) x = {bm_order(c + ((double)bm_logit(key) - sh.j.lse[b])), bm_at(b, key, bm_token(key))};
     return x;
   };
-  auto both_done = [&](const BmCand& x, const BmCand& y) { return sh.done >> (x.at >> 32) & sh.done >> (y.at >> 32) & 1; };   // no sums in them
   auto differ = [&](const BmCand& x, const BmCand& y) {   // two neighbours whose order the errors of the sums could change
-    if (bm_value(x.v) - bm_value(y.v) <= kClose && x.at >> 32 != y.at >> 32 && !both_done(x, y))
-      atomicOr(&sh.again, 1ull << (x.at >> 32) | 1ull << (y.at >> 32));
+    const int i = bm_beam(x), j = bm_beam(y);
+    const double err = sh.j.err[i] + sh.j.err[j];         // an ended beam has none
+    if (i != j && err > 0.0 && bm_value(x.v) - bm_value(y.v) <= err) atomicOr(&sh.again, 1ull << i | 1ull << j);
   };
+  double most_err = 0.0;
+  for (int b = 0; b < B; ++b) most_err = fmax(most_err, sh.j.err[b]);
 
   for (bool refined = false;; refined = true) {
     if (tid == 0) sh.count = 0;
     __syncthreads();
     long long bar = kNoCand + 1;
-    const bool direct = total <= BM_DIRECT;               // every candidate is compared with every other
-    if (!direct) {
-      // the bar: the keep-th of the threads' best ones, less what the errors of the sums could change
+    if (total > BM_DIRECT) {
+      // the bar: the keep-th of the best ones of 64 (256) groups of threads, less what the errors of the sums could change
       BmCand best = {kNoCand, ~0ull};
       for (int i = tid; i < total; i += BM_THREADS) {
-        const BmCand x = cand(i, __ldcg(keys + i));
+        const BmCand x = cand(i, i == tid ? first_key : key_of(i));
         if (bm_before(x, best)) best = x;
       }
-      sh.most[tid] = best;
+      const bool wide = K > 32;
+      if (!wide) {
+#pragma unroll
+        for (int d = 1; d < 4; d <<= 1) {
+          const BmCand y = {__shfl_xor_sync(0xffffffffu, best.v, d), __shfl_xor_sync(0xffffffffu, best.at, d)};
+          if (bm_before(y, best)) best = y;
+        }
+      }
+      const int of = wide ? BM_THREADS : BM_THREADS / 4;
+      if (wide || (tid & 3) == 0) sh.most[wide ? tid : tid >> 2] = best;
       if (tid == 0) sh.bar_cand.v = bar;
       __syncthreads();
-      if (best.at != ~0ull) {
+      if (tid < of) {
+        const BmCand mine = sh.most[tid];
         int larger = 0;
-        for (int i = 0; i < BM_THREADS; ++i) larger += bm_before(sh.most[i], best);
-        if (larger == K - 1) sh.bar_cand.v = bm_order(bm_value(best.v) - kClose);
+#pragma unroll 8
+        for (int i = 0; i < of; ++i) larger += bm_before(sh.most[i], mine);
+        if (mine.at != ~0ull && larger == K - 1) sh.bar_cand.v = bm_order(bm_value(mine.v) - 2.0 * most_err);
       }
       __syncthreads();
       bar = sh.bar_cand.v;
     }
     for (int i = tid; i < total; i += BM_THREADS) {
-      const BmCand x = cand(i, direct && i == tid ? first_key : __ldcg(keys + i));
+      const BmCand x = cand(i, i == tid ? first_key : key_of(i));
       if (x.at != ~0ull && x.v >= bar) {
         const int n = atomicAdd(&sh.count, 1);
         if (n < BM_LIST / 2) sh.j.cand[n] = x;
@@ -395,12 +509,8 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     int found;
     if (count <= BM_LIST / 2) {
       found = min(count, K);
-      for (int i = tid; i < count; i += BM_THREADS) {
-        const BmCand x = sh.j.cand[i];
-        int rank = 0;
-        for (int k = 0; k < count; ++k) rank += bm_before(sh.j.cand[k], x);
-        if (rank < K) sh.top[rank] = x;
-      }
+      bm_rank(count, [&](int k, int i) { return bm_before(sh.j.cand[k], sh.j.cand[i]); },
+              [&](int i, int rank) { if (rank < K) sh.top[rank] = sh.j.cand[i]; });
       __syncthreads();
       if (!refined) {
         for (int i = tid; i + 1 < found; i += BM_THREADS) differ(sh.top[i], sh.top[i + 1]);
@@ -418,7 +528,7 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
       for (; refined && found < K; ++found) {
         BmCand x = {kNoCand, ~0ull};
         for (int i = tid; i < total; i += BM_THREADS) {
-          const BmCand y = cand(i, __ldcg(keys + i));
+          const BmCand y = cand(i, key_of(i));
           if (y.at != ~0ull && bm_before(last, y) && bm_before(y, x)) x = y;
         }
         __syncthreads();
@@ -438,12 +548,12 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     if (refined || again == 0) {
       for (int i = tid; i < K; i += BM_THREADS) {
         const bool some = i < found;
-        const unsigned long long at = some ? sh.top[i].at : 0;
+        const BmCand x = some ? sh.top[i] : BmCand{kNoCand, 0};
         const size_t o = (size_t)group * K + i;
-        const int token = some ? (int)(uint32_t)at : -1;
-        a.out_scores[o] = some ? (float)bm_value(sh.top[i].v) : -INFINITY;
+        const int token = some ? (int)(x.at & ((1u << 26) - 1)) : -1;
+        a.out_scores[o] = some ? (float)bm_value(x.v) : -INFINITY;
         a.out_tokens[o] = token;
-        a.out_parents[o] = group * B + (some ? (int)(at >> 32) : min(i, B - 1));
+        a.out_parents[o] = group * B + (some ? bm_beam(x) : min(i, B - 1));
         if (a.out_ended) a.out_ended[o] = some && token == a.end_token;
       }
       return;
@@ -458,45 +568,45 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(BM_THREADS, 4) beam_select_kernel(BmArgs a) {
+__global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs a) {
   constexpr int N = BmType<T>::N;
-  __shared__ BmShared sh;
+  extern __shared__ __align__(16) unsigned char bm_smem[];
+  BmShared& sh = *reinterpret_cast<BmShared*>(bm_smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring) + tid * 16;
+  pg_wait();
+
   const int r = blockIdx.x / a.splits, split = blockIdx.x - r * a.splits, group = r / a.beams;
   const BmRow<T> row(a, r);
   const int p0 = min(row.pieces, split * a.per), p1 = min(row.pieces, p0 + a.per);
   const bool front = split == 0, back = split == a.splits - 1;
-  uint4 w[BM_UNROLL];
-  auto load = [&](int at) {
-#pragma unroll
-    for (int u = 0; u < BM_UNROLL; ++u) {
-      const int i = at + u * BM_THREADS + tid;
-      if (i < p1) w[u] = row.piece(i);
-    }
-  };
-  pg_wait();
-  // the first tile is asked for before it is known whether the beam takes part
   const float score = __ldcg(a.scores + r);
   const bool done = a.ended && __ldcg(a.ended + r);
-  load(p0);
-  const int single = row.single(tid, front, back);
-  const float lone = single >= 0 ? fminf(BmType<T>::load(row.base + single), BmType<T>::most) : -INFINITY;
+  const unsigned char* source = reinterpret_cast<const unsigned char*>(row.base + row.token(p0 + tid));
+  auto fetch = [&](int i, int slot) {                     // piece i on its way
+    if (i < p1)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * (BM_THREADS * 16)),
+                   "l"(source + (int64_t)(i - p0 - tid) * 16) : "memory");
+  };
+  auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
   if (bm_live(score) && !done) {
     unsigned long long* out = a.keys + ((size_t)r * a.splits + split) * a.keep;
-
-    // ---- the first tile: reference and bar ----
-    float best = lone;
 #pragma unroll
-    for (int u = 0; u < BM_UNROLL; ++u) {
-      if (p0 + u * BM_THREADS + tid < p1) {
-        float f[N];
-        BmType<T>::unpack(w[u], f);
-#pragma unroll
-        for (int i = 0; i < N; ++i) best = fmaxf(best, f[i]);
-      }
+    for (int u = 0; u < BM_RING; u += 2) {                  // two pieces at a time
+      fetch(p0 + u * BM_THREADS + tid, u);
+      fetch(p0 + (u + 1) * BM_THREADS + tid, u + 1);
+      commit();
     }
+    const int single = row.single(tid, front, back);
+    const float lone = single >= 0 ? fminf(BmType<T>::load(row.base + single), BmType<T>::most) : -INFINITY;
+    // ---- its first tile: reference and bar ----
+    float best = lone;
+    asm volatile("cp.async.wait_group %0;" ::"n"((BM_RING - BM_FIRST) / 2) : "memory");
+#pragma unroll
+    for (int u = 0; u < BM_FIRST; ++u)
+      if (p0 + u * BM_THREADS + tid < p1) best = fmaxf(best, bm_top<T>(sh.ring[u][tid]));
     best = fminf(best, BmType<T>::most);
-    float ref = fmaxf(bm_block_max(sh, best), -FLT_MAX);
+    float ref = bm_block_max(sh, best);
     const bool wide = a.keep > 32;                        // 64 groups of four threads are enough for 32
     if (!wide) {
       best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
@@ -520,97 +630,201 @@ __global__ void __launch_bounds__(BM_THREADS, 4) beam_select_kernel(BmArgs a) {
       if (larger == a.keep - 1) sh.bar = mine;
     }
     __syncthreads();
-    const float bar = fmaxf(sh.bar, -FLT_MAX);            // -inf is no candidate
+    float bar = fmaxf(sh.bar, -FLT_MAX);                  // -inf is no candidate
 
-    // ---- the stretch ----
-    float limit = ref + kRefFar;
-    uint64_t sum2 = 0;                                    // of a tile
+    // ---- the pass ----
+    // `floor`: what is less counts as that, 2^-125 of the reference's term or nothing; -inf where the type has no such number
+    float limit, floor, care;                             // care: pieces above it need more than adding up (NaN: all)
     double sum = 0.0;
+    uint64_t far2 = 0;                                    // terms times x
+    auto refer = [&](float to) {                          // nothing seen so far: any reference will do, the next element moves it
+      ref = to == -INFINITY ? 0.f : to;
+      limit = to == -INFINITY ? -INFINITY : ref + kRefFar;
+      floor = fabsf(ref) < 0x1p100f ? BmType<T>::below(ref) : -INFINITY;
+      care = floor == -INFINITY ? NAN : limit;
+    };
+    refer(ref);
     auto push = [&](float l, int token) {
       const int n = atomicAdd(&sh.count, 1);
       if (n < BM_LIST) sh.list[n] = bm_key(l, token);
     };
     if (lone >= bar) push(lone, single);
-    if (lone > -INFINITY) sum = pa_ex2((lone - ref) * 1.4426950408889634f);
-    for (int at = p0; at < p1; at += BM_TILE) {
-      uint4 v[BM_UNROLL];
+    if (lone > -INFINITY) {
+      const float x = (lone - ref) * 1.4426950408889634f, y = pa_ex2(x);
+      sum = y;
+      if (y > 0.f) far2 = f32x2_pack(x * y, 0.f);
+    }
+    const uint64_t scale2 = f32x2_pack(1.4426950408889634f, 1.4426950408889634f);
+    // the terms of a piece: l log2(e) less the rounded ref log2(e), whose error is taken out of the sum at the end
+    auto add = [&](const float* f, uint64_t& part) {
+      const float c = -ref * 1.4426950408889634f;
+      const uint64_t back2 = f32x2_pack(c, c);
 #pragma unroll
-      for (int u = 0; u < BM_UNROLL; ++u) v[u] = w[u];
-      load(at + BM_TILE);
+      for (int e = 0; e < N; e += 2) {
+        const uint64_t x = f32x2_fma(f32x2_pack(f[e], f[e + 1]), scale2, back2);
+        float x0, x1;
+        f32x2_unpack(x, x0, x1);
+        const uint64_t y = f32x2_pack(pa_ex2(x0), pa_ex2(x1));
+        far2 = f32x2_fma(y, x, far2);
+        part = f32x2_add(part, y);
+      }
+    };
+    auto add_up = [&](uint64_t part) {
+      float s0, s1;
+      f32x2_unpack(part, s0, s1);
+      sum += (double)(s0 + s1);
+    };
+    int seen = 0, next_cut = 2 * BM_FIRST;                // pieces of a thread so far, and when the list is cut down next
+    for (int at = p0; at < p1; at += 2 * BM_THREADS) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(BM_RING / 2 - 1) : "memory");
+      const int slot = seen & (BM_RING - 1);
+      uint4 v[2] = {sh.ring[slot][tid], sh.ring[slot + 1][tid]};
+      const float tops[2] = {bm_top<T>(v[0]), bm_top<T>(v[1])}, higher = fmaxf(tops[0], tops[1]);
+      if (at + 2 * BM_THREADS <= p1 && higher <= care && bar > floor) {
+        float f[2][N];
+        uint64_t part[2] = {0, 0};
+        const uint32_t low = BmType<T>::pack(floor);
+        bm_unpack<T>(v[0], low, f[0]);
+        bm_unpack<T>(v[1], low, f[1]);
+        add(f[0], part[0]);
+        add(f[1], part[1]);
+        add_up(f32x2_add(part[0], part[1]));
+        if (higher >= bar) {
+          const int token = row.token(at + tid);
 #pragma unroll
-      for (int u = 0; u < BM_UNROLL; ++u) {
-        const int i = at + u * BM_THREADS + tid;
-        if (i >= p1) break;
-        float f[N];
-        BmType<T>::unpack(v[u], f);
-        float most = f[0];
+          for (int k = 0; k < 2; ++k)
+            if (tops[k] >= bar) {
 #pragma unroll
-        for (int e = 1; e < N; ++e) most = fmaxf(most, f[e]);
-        if (most > limit) {
+              for (int e = 0; e < N; ++e)
+                if (f[k][e] >= bar) push(f[k][e], token + k * (BM_THREADS * N) + e);
+            }
+        }
+      } else {
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+          const int i = at + k * BM_THREADS + tid;
+          if (i >= p1) break;
+          uint4 w = k ? v[1] : v[0];
+          float top = fmaxf(bm_top<T>(w), -INFINITY);
+          if (top > limit) {
+            top = fminf(top, BmType<T>::most);
+            if (limit == -INFINITY) {
+              sum = 0.0;
+              far2 = 0;
+              refer(top);
+            } else if (top > ref) {
+              const float back = (ref - top) * 1.4426950408889634f, scale = pa_ex2(back);
+              float s0, s1;
+              f32x2_unpack(far2, s0, s1);
+              far2 = scale > 0.f ? f32x2_pack((s0 + s1 + back * (float)sum) * scale, 0.f) : 0;
+              sum *= (double)scale;
+              refer(top);
+            }
+            const uint32_t most = BmType<T>::pack(BmType<T>::most);
+            w = make_uint4(BmType<T>::smaller(w.x, most), BmType<T>::smaller(w.y, most), BmType<T>::smaller(w.z, most),
+                           BmType<T>::smaller(w.w, most));
+          }
+          float f[N];
+          bm_unpack<T>(w, BmType<T>::pack(floor), f);
+          uint64_t part = 0;
+          if (floor == -INFINITY) {
+            for (int e = 0; e < N; ++e)
+              if (f[e] > -INFINITY) {
+                const float x = (f[e] - ref) * 1.4426950408889634f, y = pa_ex2(x);
+                part = f32x2_add(part, f32x2_pack(y, 0.f));
+                if (y > 0.f) far2 = f32x2_add(far2, f32x2_pack(x * y, 0.f));
+              }
+          } else {
+            add(f, part);
+          }
+          add_up(part);
+          if (top >= bar) {
+            const int token = row.token(i);
+            if (bar > floor) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) f[e] = fminf(f[e], BmType<T>::most);
-          most = fminf(most, BmType<T>::most);
-          if (most > ref) {
-            float s0, s1;
-            f32x2_unpack(sum2, s0, s1);
-            sum = (sum + (double)(s0 + s1)) * (double)pa_ex2((ref - most) * 1.4426950408889634f);
-            sum2 = 0;
-            ref = most;
-            limit = ref + kRefFar;
+              for (int e = 0; e < N; ++e)
+                if (f[e] >= bar) push(f[e], token + e);
+            } else {
+#pragma unroll 1
+              for (int e = 0; e < N; ++e) {               // as they are in memory
+                const float l = fminf(BmType<T>::load(row.base + token + e), BmType<T>::most);
+                if (l >= bar) push(l, token + e);
+              }
+            }
           }
         }
-        const uint64_t back2 = f32x2_pack(-ref, -ref), scale2 = f32x2_pack(1.4426950408889634f, 1.4426950408889634f);
-        uint64_t part = 0;
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          float x0, x1;
-          f32x2_unpack(f32x2_mul(f32x2_add(f32x2_pack(f[e], f[e + 1]), back2), scale2), x0, x1);
-          part = f32x2_add(part, f32x2_pack(pa_ex2(x0), pa_ex2(x1)));
-        }
-        sum2 = f32x2_add(sum2, part);
-        if (most >= bar) {
-          const int token = row.token(i);
-#pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (f[e] >= bar) push(f[e], token + e);
-        }
       }
-      float s0, s1;
-      f32x2_unpack(sum2, s0, s1);
-      sum += (double)(s0 + s1);
-      sum2 = 0;
+      fetch(at + BM_RING * BM_THREADS + tid, slot);       // (the pieces there have been read)
+      fetch(at + (BM_RING + 1) * BM_THREADS + tid, slot + 1);
+      commit();
+      seen += 2;
+      if (seen == next_cut) {
+        next_cut *= 2;
+        __syncthreads();
+        const int count = sh.count;
+        if (count > 2 * a.keep && count <= BM_THREADS) {
+          bm_rank(count, [&](int k, int i) { return sh.list[k] > sh.list[i]; },
+                  [&](int i, int rank) { if (rank < a.keep) sh.kept[rank] = sh.list[i]; });
+          __syncthreads();
+          for (int i = tid; i < a.keep; i += BM_THREADS) sh.list[i] = sh.kept[i];
+          if (tid == 0) {
+            sh.bar = bm_logit(sh.kept[a.keep - 1]);
+            sh.count = a.keep;
+          }
+        }
+        __syncthreads();
+        bar = fmaxf(bar, sh.bar);
+      }
+    }
+    if (limit == -INFINITY) {                             // nothing seen
+      sum = 0.0;
+      far2 = 0;
+      ref = -FLT_MAX;
+      floor = -INFINITY;
     }
     // ---- its sum and its largest ----
     const float high = bm_block_max(sh, ref);
-    double all = sum * (ref == high ? 1.0 : (double)pa_ex2((ref - high) * 1.4426950408889634f));
+    const float behind = (ref - high) * 1.4426950408889634f;
+    double scale = ref == high ? 1.0 : bm_exp2(behind);
+    if (floor != -INFINITY) scale *= 1.0 - 0.69314718055994531 * (double)fmaf(ref, 1.4426950408889634f, -(ref * 1.4426950408889634f));
+    float f0, f1;
+    f32x2_unpack(far2, f0, f1);
+    double all = sum * scale;
+    float far = scale > 0.0 ? (f0 + f1 + behind * (float)sum) * (float)scale : 0.f;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
-    if (lane == 0) sh.dsum[warp] = all;
+    for (int d = 16; d; d >>= 1) {
+      all += __shfl_xor_sync(0xffffffffu, all, d);
+      far += __shfl_xor_sync(0xffffffffu, far, d);
+    }
+    if (lane == 0) {
+      sh.dsum[warp] = all;
+      sh.ref[warp] = far;
+    }
     __syncthreads();
     if (tid == 0) {
       all = 0.0;
-      for (int i = 0; i < BM_THREADS / 32; ++i) all += sh.dsum[i];
-      a.sums[(size_t)r * a.splits + split] = make_float2(high, (float)all);
+      far = 0.f;
+      for (int i = 0; i < BM_THREADS / 32; ++i) {
+        all += sh.dsum[i];
+        far += sh.ref[i];
+      }
+      a.sums[(size_t)r * a.splits + split] = make_float4(high, (float)all, -far, 0.f);
     }
     const int count = sh.count;
     if (count > BM_LIST) {
       bm_crowded<T>(sh, a, row, p0, p1, front, back, out);
     } else {
-      for (int i = tid; i < count; i += BM_THREADS) {
-        const unsigned long long mine = sh.list[i];
-        int rank = 0;
-        for (int k = 0; k < count; ++k) rank += sh.list[k] > mine;
-        if (rank < a.keep) out[rank] = mine;
-      }
+      bm_rank(count, [&](int k, int i) { return sh.list[k] > sh.list[i]; },
+              [&](int i, int rank) { if (rank < a.keep) out[rank] = sh.list[i]; });
       for (int i = count + tid; i < a.keep; i += BM_THREADS) out[i] = 0;
     }
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
   // ---- the last CTA of the group joins ----
-  __threadfence();
   __syncthreads();
   if (tid == 0) {
-    const int n = a.beams * a.splits;
-    sh.last = atomicAdd(a.counters + group, 1) == n - 1;
+    __threadfence();                                      // what the block has written
+    sh.last = atomicAdd(a.counters + group, 1) == a.beams * a.splits - 1;
     if (sh.last) {
       a.counters[group] = 0;
       __threadfence();
@@ -622,31 +836,47 @@ __global__ void __launch_bounds__(BM_THREADS, 4) beam_select_kernel(BmArgs a) {
 
 struct BmLayout {
   size_t sums, keys, total;
-  int splits;
+  int splits, per;
 };
 
 static bool valid_beams(const less_beams* d) {
-  if (d->groups < 1 || d->beams < 1 || d->beams > BM_MOST_BEAMS || d->vocab < 1 || d->keep < 1 || d->keep > BM_MOST_KEEP) return false;
+  if (d->groups < 1 || d->beams < 1 || d->beams > BM_MOST_BEAMS || d->vocab < 1 || d->vocab > (1 << 26) || d->keep < 1 || d->keep > BM_MOST_KEEP) return false;
   if (d->flags & ~(uint32_t)(LESS_BEAMS_BF16 | LESS_BEAMS_F32) || d->flags == (LESS_BEAMS_BF16 | LESS_BEAMS_F32)) return false;
   if (d->end_token < -1 || d->end_token >= d->vocab) return false;
   return d->groups <= (1 << 20) / d->beams;               // rows
 }
 
 // A row is cut so that all CTAs of a call, four on a multiprocessor, run at once, but for no less than 4096 elements each, nor
-// into so many lists that joining them shows (64 groups of 8 beams of 128 256: cut in five, 4.3 times as many, 77 us).
+// into so many lists that joining them shows (64 groups of 8 beams of 128 256: one stretch a row; three 15 us more).
 static BmLayout bm_layout(const less_beams* d) {
   BmLayout l;
   const int64_t rows = (int64_t)d->groups * d->beams;
+  const int pieces = (int)(((int64_t)d->vocab * (d->flags & LESS_BEAMS_F32 ? 4 : 2) + 15) / 16);
   int64_t s = pg_ceil(d->vocab, 4096);
-  if (s > 4 * 148 / rows) s = 4 * 148 / rows;
+  if (s > BM_CTAS * 148 / rows) s = BM_CTAS * 148 / rows;
   if (s > BM_JOINED / (d->beams * d->keep)) s = BM_JOINED / (d->beams * d->keep);
   l.splits = (int)(s < 1 ? 1 : s);
+  l.per = pg_ceil(pieces, l.splits);
   size_t at = ((size_t)d->groups * 4 + 255) / 256 * 256;
   l.sums = at;
-  at = (at + (size_t)rows * l.splits * 8 + 255) / 256 * 256;
+  at = (at + (size_t)rows * l.splits * 16 + 255) / 256 * 256;
   l.keys = at;
   l.total = (at + (size_t)rows * l.splits * d->keep * 8 + 255) / 256 * 256;
   return l;
+}
+
+template <typename T>
+static int launch_select(const BmArgs& a, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return fail_cuda("cudaGetDevice");
+  if (dev >= 64 || !(done.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(BmShared)) != cudaSuccess)
+      return fail_cuda("shared memory opt-in of beam_select_kernel");
+    if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return pg_launch("beam_select_kernel", beam_select_kernel<T>, dim3((unsigned)(a.groups * a.beams * a.splits)), BM_THREADS,
+                   sizeof(BmShared), s, a);
 }
 
 }  // namespace less
@@ -669,13 +899,10 @@ extern "C" int less_beam_select(const less_beams* d, const void* logits, int64_t
   const BmLayout l = bm_layout(d);
   if (d->workspace_bytes < l.total) return LESS_ERR_ARENA_TOO_SMALL;
   char* w = (char*)d->workspace;
-  const int pieces = (int)(((int64_t)d->vocab * size + 15) / 16);
-  BmArgs a = {logits, row_stride, scores, ended, d->groups, d->beams, d->vocab, d->keep, d->end_token, l.splits,
-              (pieces + l.splits - 1) / l.splits, out_scores, out_tokens, out_parents, out_ended, (int32_t*)w, (float2*)(w + l.sums),
-              (unsigned long long*)(w + l.keys)};
-  const dim3 grid((unsigned)(d->groups * d->beams * l.splits));
+  BmArgs a = {logits, row_stride, scores, ended, d->groups, d->beams, d->vocab, d->keep, d->end_token, l.splits, l.per,
+              out_scores, out_tokens, out_parents, out_ended, (int32_t*)w, (float4*)(w + l.sums), (unsigned long long*)(w + l.keys)};
   cudaStream_t s = (cudaStream_t)stream;
-  if (d->flags & LESS_BEAMS_F32) return pg_launch("beam_select_kernel", beam_select_kernel<float>, grid, BM_THREADS, 0, s, a);
-  if (d->flags & LESS_BEAMS_BF16) return pg_launch("beam_select_kernel", beam_select_kernel<__nv_bfloat16>, grid, BM_THREADS, 0, s, a);
-  return pg_launch("beam_select_kernel", beam_select_kernel<__half>, grid, BM_THREADS, 0, s, a);
+  if (d->flags & LESS_BEAMS_F32) return launch_select<float>(a, s);
+  if (d->flags & LESS_BEAMS_BF16) return launch_select<__nv_bfloat16>(a, s);
+  return launch_select<__half>(a, s);
 }

@@ -20,7 +20,9 @@ def select(logits, scores, ended, end_token, keep, most):
                 top = x[g, b].max()
                 v[b] = scores[g, b] + (x[g, b] - (top + np.log(np.exp(x[g, b] - top).sum())))
         v = v.ravel()
-        order = np.argsort(-v, kind="stable")[:keep]
+        # equal values: the lowest beam, of one beam the larger logit (beside a very large one values lose it), the lowest token
+        beam = np.repeat(np.arange(beams), vocab)
+        order = np.lexsort((np.where(np.isnan(x[g]), -np.inf, -x[g]).ravel(), beam, -v))[:keep]
         for k in range(keep):
             some = k < len(order) and v[order[k]] > -np.inf
             out[2][g, k] = g * beams + (order[k] // vocab if some else min(k, beams - 1))

@@ -46,11 +46,11 @@ def test_descriptions(B):
     assert good > 0 and good % 256 == 0
     assert B.less_beams_workspace_bytes(desc(B, groups=50)) > good
     p = 4096
-    for bad in (dict(groups=0), dict(beams=0), dict(beams=65), dict(vocab=0), dict(keep=0), dict(keep=129), dict(flags=3),
+    for bad in (dict(groups=0), dict(beams=0), dict(beams=65), dict(vocab=0), dict(vocab=2 ** 26 + 1), dict(keep=0), dict(keep=129), dict(flags=3),
                 dict(flags=4), dict(end_token=-2), dict(end_token=1000), dict(groups=1 << 20)):
         assert B.less_beams_workspace_bytes(desc(B, **bad)) == 0, bad
         assert B.less_beam_select(desc(B, **bad), p, 1000, p, None, p, p, p, p, None) == BAD, bad
-    assert B.less_beams_workspace_bytes(desc(B, beams=64, keep=128, vocab=2 ** 31 - 1, end_token=5)) > good
+    assert B.less_beams_workspace_bytes(desc(B, beams=64, keep=128, vocab=2 ** 26, end_token=5)) > good
 
 
 def test_arguments(B):

@@ -50,6 +50,18 @@ def test_selection(dtype, groups, beams, vocab, keep):
     check(sel, *random_inputs(groups, beams, vocab, TYPES[dtype], seed=vocab))
 
 
+@pytest.mark.parametrize("groups,beams,vocab", [(700, 3, 700), (5000, 1, 90), (130, 16, 3), (2, 2, 400000), (33, 62, 40)])
+def test_many_rows_and_long_ones(groups, beams, vocab):
+    """More rows than are counted, rows of which a CTA takes several, rows of which many CTAs take a stretch."""
+    sel = make(groups, beams, vocab, dtype=torch.float16, end_token=vocab - 1)
+    logits, scores = random_inputs(groups, beams, vocab, torch.float16, seed=groups)
+    g = torch.Generator().manual_seed(1)
+    ended = (torch.rand((groups, beams), generator=g) < 0.2).to(DEV)
+    scores[torch.rand((groups, beams), generator=g).to(DEV) < 0.3] = -float("inf")
+    check(sel, logits, scores, ended)
+    check(sel, logits, scores)
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (3, 5), (8, 7), (13, 2)])
 def test_rows_at_any_address(dtype, pad, shift):
@@ -135,6 +147,33 @@ def test_infinities_and_extremes(dtype):
     check(sel, logits, scores)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_masked_beginnings_and_references_that_move(dtype):
+    """Stretches that begin with masked or NaN logits, references far below what follows, the type's lowest values beside
+    masked ones."""
+    most = torch.finfo(TYPES[dtype]).max
+    vocab = 70001                                         # several tiles of 16-byte pieces
+    sel = make(9, 2, vocab, 12, TYPES[dtype], end_token=0)
+    logits, scores = random_inputs(9, 2, vocab, TYPES[dtype], seed=2)
+    scores = scores[:1].repeat(9, 1).contiguous()
+    logits[0, 0, :40000] = -float("inf")
+    logits[0, 1, :69990] = float("nan")
+    logits[1, :, :50000] -= 3000.0                        # rises by more than the reference reaches
+    logits[2, :, ::3] = -float("inf")
+    logits[2, :, 1::3] = -most
+    logits[3] = -float("inf")
+    logits[3, 0, 69999] = -most
+    logits[3, 1, 5] = -most
+    logits[4] = -most
+    logits[4, 0, 60000:] = -float("inf")
+    logits[5] = logits[5] * 1e-3 + 40000.0                # all rounded to few values
+    logits[6, :, 30000] = float("inf")
+    logits[6, 1, 60000] = most
+    logits[7] = torch.linspace(-20, 20, vocab).to(TYPES[dtype])
+    logits[8] = torch.linspace(0, -90, vocab).to(TYPES[dtype])
+    check(sel, logits, scores)
+
+
 @pytest.mark.parametrize("seed", range(4))
 def test_beams_closer_than_fp32_tells_apart(seed):
     """The same logits in every beam, scores a few steps of 64-bit arithmetic's visible distance apart: the order is that of
@@ -159,7 +198,7 @@ def test_equal_beams_at_different_addresses(dtype, seed):
     check(sel, logits, torch.full((2, beams), -1.0, device=DEV))
 
 
-def test_in_place_captured_and_on_a_stream():
+def test_captured_and_on_a_stream():
     groups, beams, vocab = 5, 4, 3000
     sel = make(groups, beams, vocab, dtype=torch.bfloat16, end_token=3)
     logits, scores = random_inputs(groups, beams, vocab, torch.bfloat16)
@@ -171,13 +210,6 @@ def test_in_place_captured_and_on_a_stream():
         got = sel.select(logits, scores, ended, stream=side)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
-    # scores and ended updated in place: the C call
-    from paper_2402_09398_b200 import binding as B
-    s2, e2 = scores.clone(), ended.clone()
-    rc = B.less_beam_select(sel.desc, logits.data_ptr(), vocab, s2.data_ptr(), e2.data_ptr(), s2.data_ptr(),
-                            want.tokens.data_ptr(), want.parents.data_ptr(), e2.data_ptr(),
-                            torch.cuda.current_stream().cuda_stream)
-    assert rc == 0 and torch.equal(s2, want.scores) and torch.equal(e2, want.ended)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         out = sel.select(logits, scores, ended)
