@@ -498,6 +498,15 @@ class LessContext:
         _check(less_reorder(self.ctx, self.cfg.batch if beams is None else beams, _ptr(parents), _stream_ptr(stream)),
                "less_reorder")
 
+    def beam_step(self, select, logits, scores, ended=None, stream=None):
+        """A step of beam search: selects (`select`: a BeamSelect of this batch, keep == beams) and reorders the batch
+        accordingly.  Returns the choice."""
+        if select.keep != select.beams or select.groups * select.beams != self.cfg.batch:
+            raise ValueError(f"a selection of as many candidates as beams, {self.cfg.batch} in all, is wanted")
+        choice = select.select(logits, scores, ended, stream=stream)
+        self.reorder(choice.parents, beams=select.beams, stream=stream)
+        return choice
+
     def state_tensors(self) -> Dict[str, torch.Tensor]:
         """The state where it lies (less_state_view), as tensors [batch, layers, heads, ...]: K, V, pos, acc, psi, H, z,
         count."""
@@ -683,6 +692,15 @@ class PagedCache:
         n = seqs.shape[0]
         self._call(self._lib.less_pages_reorder, "less_pages_reorder", n, self._list(seqs, "seqs"),
                    self._list(parents, "parents", n), stream=stream, keep=(seqs, parents))
+
+    def beam_step(self, select, logits, scores, seqs, ended=None, stream=None):
+        """A step of beam search: selects (`select`: a BeamSelect, keep == beams) and makes the listed sequences, those of
+        group 0 first, follow their parents.  Returns the choice."""
+        if select.keep != select.beams or select.groups * select.beams != seqs.shape[0]:
+            raise ValueError(f"a selection of as many candidates as beams, {seqs.shape[0]} in all, is wanted")
+        choice = select.select(logits, scores, ended, stream=stream)
+        self.reorder(seqs, choice.parents.view(-1), stream=stream)
+        return choice
 
     def trim(self, seqs, sinks, window, stream=None):
         """Releases the pages between the first `sinks` tokens and the last `window`."""

@@ -13,10 +13,11 @@
 //     many come before it.
 // Within a beam the order is that of the logits, which is exact.  Between beams it hangs on the sums.  A term exp2(x) of
 // one is off, relative, by 2^-22 (the exponential), |x| 2^-23.4 (x: a product with a rounded factor, for fp32 logits of a
-// rounded difference) and 4 * 2^-24 (added to seven others of its piece; the rest is in 64 bits, rounded once at the end), so
-// a sum by at most 6e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it.
+// rounded difference) and 5 * 2^-24 (added to fifteen others; the rest is in 64 bits, rounded once at the end), so a sum
+// by at most 6e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it.
 // Where two neighbours in the order are of different beams and closer than that, the sums of these beams are computed again
-// in 64 bits and the candidates joined once more (a chance of some 1e-4 per kept candidate; WORST us for a row of 128 256).
+// to 1e-10 and the candidates joined once more (a chance of some 1e-4 per kept candidate; 65 us for a row of 128 256,
+// one CTA's work that waits for memory).
 #include <float.h>
 
 #include <atomic>
@@ -195,11 +196,10 @@ struct BmShared {
   };
   float wmax[BM_THREADS / 32];
   float ref[BM_THREADS / 32];
-  double pow2[32];                                        // 2^(k / 32)
   float bar;
   unsigned long long bar_key;
   BmCand bar_cand;
-  unsigned long long again, done;                         // beams whose sums are computed in 64 bits; that have ended
+  unsigned long long again, done;                         // beams whose sums are computed again; that have ended
   int count, last;
 };
 
@@ -324,7 +324,7 @@ __device__ __noinline__ void bm_crowded(BmShared& sh, const BmArgs& a, const BmR
   for (int i = tid; i < a.keep; i += BM_THREADS) out[i] = i < sh.count ? sh.list[i] : 0;
 }
 
-// log sum exp of a row in 64 bits.  2^f, |f| <= 1/2, by its Taylor polynomial of degree 11 (error below 1e-14)
+// 2^f, |f| <= 1/2, by its Taylor polynomial of degree 11 (error below 1e-14)
 __device__ __forceinline__ double bm_exp2(double x) {
   if (x < -1020.0) return 0.0;
   const double n = rint(x), z = (x - n) * 0.693147180559945309417232;
@@ -350,7 +350,10 @@ __device__ __noinline__ double bm_exact_sum(BmShared& sh, const BmArgs& a, int r
   unsigned long long top = 0;                              // the largest logit: a stretch's first
   for (int s = 0; s < a.splits; ++s) top = max(top, __ldcg(a.keys + ((size_t)r * a.splits + s) * a.keep));
   const float m = bm_logit(top);
-  if (tid < 32) sh.pow2[tid] = bm_exp2(tid / 32.0);
+  // l - m = k ln 2 / 1024 + z, |z| <= 3.4e-4: 2^(k / 1024) from a table in 64 bits, e^z - 1 as z + z^2 / 2 + z^3 / 6 in 32 (5e-11
+  // of e^z; with the roundings of z).  The unit for 64-bit arithmetic is the bound otherwise.
+  double* pow2 = reinterpret_cast<double*>(sh.ring);
+  for (int k = tid; k < 1024; k += BM_THREADS) pow2[k] = bm_exp2(k / 1024.0);
   __syncthreads();
   double s = 0.0;
   constexpr int N = 4;
@@ -367,15 +370,13 @@ __device__ __noinline__ double bm_exact_sum(BmShared& sh, const BmArgs& a, int r
     load(at + N * BM_THREADS);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      // l - m = k ln 2 / 32 + z, |z| <= 0.011; e^z by its Taylor polynomial of degree 5 (error below 3e-15)
-      const float k = rintf((x[i] - m) * 46.16624130844683f);
-      const double z = fma((double)k, -0.0216608493924982909192, (double)x[i] - (double)m);
-      double p = fma(1.0 / 120.0, z, 1.0 / 24.0);
-      p = fma(p, z, 1.0 / 6.0);
-      p = fma(p, z, 0.5);
-      p = fma(p, z, 1.0);
-      p = fma(p, z, 1.0) * sh.pow2[(int)k & 31];
-      s += __hiloint2double(__double2hiint(p) + (((int)k >> 5) << 20), __double2loint(p));
+      const float d = x[i] - m, back = d - x[i], rest = (x[i] - (d - back)) - (m + back);   // d + rest is the difference
+      const float k = rintf(d * 1477.3197218702985f);
+      const float z = fmaf(-k, -0x1.05c61p-39f, fmaf(-k, 0x1.62e43p-11f, d)) + rest;
+      const float q = fmaf(z * z, fmaf(z, 0.16666667f, 0.5f), z);
+      const double t = pow2[(int)k & 1023];
+      const double y = __hiloint2double(__double2hiint(t) + (((int)k >> 10) << 20), __double2loint(t));
+      s = fma(y, (double)q, s + y);
     }
   }
 #pragma unroll
