@@ -413,7 +413,7 @@ int less_pages_fork(const less_pages* cache, int32_t n, const int32_t* src, cons
  * pages are shared.  Of the children of a sequence one takes over the page that is still being filled (the sequence itself
  * if it is its own child, else the first of the list), the others get copies of its 16-token blocks in use, in the lowest
  * free pages, in the order of the list; pages that nobody holds any longer are released first.  A sequence is listed
- * once; n <= seqs and 16384.  All or nothing: LESS_ERR_PAGES_EXHAUSTED, LESS_ERR_BAD_STATE (a sequence listed twice),
+ * once; n <= seqs and 8192.  All or nothing: LESS_ERR_PAGES_EXHAUSTED, LESS_ERR_BAD_STATE (a sequence listed twice),
  * LESS_ERR_DEVICE_BOUNDS. */
 int less_pages_reorder(const less_pages* cache, int32_t n, const int32_t* seqs, const int32_t* parents, void* cuda_stream);
 

@@ -420,37 +420,46 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
 // Reorder, the plan: entry i becomes what entry parents[i] was.  Whole pages are shared: their counts change by the number
 // of an entry's children less one.  Of its children one inherits the page that is still being filled (the entry itself if
 // it is its own child, else the first of the list), the others get copies in the lowest free pages, among them those that
-// this call releases.  p.off[i] = number of the copy that entry i gets, p.fresh[i] = its new length, both for the second
+// this call releases.  p.off[i] = number of the copy that entry i gets, p.mark[i] = its new length, both for the second
 // kernel; a copy's source carries the number of its 16-token blocks in use, less one, in its top four bits.
-constexpr int PO_REORDER = 16384;                      // entries of a call: their columns of the table pass through 64 KB
+// The entries lie in shared memory, so that what is left is a chain of some loads and scans (512 entries of up to 16 pages,
+// with the entries in global memory: 25 us; PLAN now).
+constexpr int PO_REORDER = 8192;                       // entries of a call
+constexpr int PO_ENTRY = 20;                           // bytes of each: sequence, length, parent, children, the first of them
 __global__ void __launch_bounds__(PO_THREADS) pages_reorder_plan_kernel(PgParams p, int n, const int32_t* seqs,
                                                                         const int32_t* parents) {
+  extern __shared__ int32_t po_entries[];
   __shared__ int sums[PO_THREADS / 32];
   __shared__ Listed listed;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int32_t *seq = po_entries, *length = seq + n, *parent = length + n, *children = parent + n, *heir = children + n;
   pg_wait();
   for (int i = tid; i < min(PO_BITS, p.seqs + 31) / 32; i += PO_THREADS) listed.seen[i] = 0;
   bool bad = pg_stopped(p), again = false;
   __syncthreads();
   for (int i = tid; i < n; i += PO_THREADS) {
     const int s = __ldg(seqs + i), a = __ldg(parents + i);
-    if (s < 0 || s >= p.seqs || a < 0 || a >= n || !pg_len_ok(p, __ldcg(p.lens + s))) {
+    const int len = s >= 0 && s < p.seqs ? __ldcg(p.lens + s) : -1;
+    if (a < 0 || a >= n || !pg_len_ok(p, len)) {
       pg_status(p.status, kPagesBounds, 40);
       bad = true;
     } else {
       again |= listed_again(listed, p, s);
     }
-    p.fresh[i] = 0;                                    // children of entry i
-    p.off[i] = 0x7fffffff;                             // its heir
+    seq[i] = s;
+    length[i] = len;
+    parent[i] = a;
+    children[i] = 0;
+    heir[i] = 0x7fffffff;                              // -1: the entry itself
   }
   bad = __syncthreads_or(bad);
   if (!bad && p.seqs > PO_BITS) {                      // too many sequences for the bitmap
-    for (int i = tid; i < n; i += PO_THREADS) p.mark[__ldg(seqs + i)] = n;
+    for (int i = tid; i < n; i += PO_THREADS) p.mark[seq[i]] = n;
     __syncthreads();
-    for (int i = tid; i < n; i += PO_THREADS) atomicMin(p.mark + __ldg(seqs + i), i);
+    for (int i = tid; i < n; i += PO_THREADS) atomicMin(p.mark + seq[i], i);
     __syncthreads();
     again = false;
-    for (int i = tid; i < n; i += PO_THREADS) again |= __ldcg(p.mark + __ldg(seqs + i)) != i;
+    for (int i = tid; i < n; i += PO_THREADS) again |= __ldcg(p.mark + seq[i]) != i;
   }
   if (!bad && again) pg_status(p.status, kPagesState, 41);
   if (__syncthreads_or(bad || again)) {
@@ -458,59 +467,69 @@ __global__ void __launch_bounds__(PO_THREADS) pages_reorder_plan_kernel(PgParams
     return;
   }
   for (int i = tid; i < n; i += PO_THREADS) {
-    const int a = __ldg(parents + i);
-    atomicAdd(p.fresh + a, 1);
-    atomicMin(p.off + a, a == i ? -1 : i);
+    const int a = parent[i];
+    atomicAdd(children + a, 1);
+    atomicMin(heir + a, a == i ? -1 : i);
   }
   __syncthreads();
-  // counts of the pages that lose or gain holders; `sign` -1 takes it back
+  // counts of the pages that lose or gain holders, four entries of a warp at a time; `sign` -1 takes it back
   auto count = [&](int sign) {
-    for (int i = warp; i < n; i += PO_THREADS / 32) {
-      const int s = __ldg(seqs + i), more = __ldcg(p.fresh + i) - 1, len = __ldcg(p.lens + s), whole = len >> p.pt_shift;
-      if (more == 0) continue;
-      const int32_t* row = p.table + (size_t)s * p.seq_pages;
-      for (int o = lane; o < pg_ceil(len, p.pt); o += 32) {
-        const int page = __ldcg(row + o), d = o < whole ? more : min(more, 0);
-        if (page >= 0 && page < p.pages && d) atomicAdd(p.refs + page, sign * d);
+    constexpr int N = 4;
+    for (int i0 = warp * N; i0 < n; i0 += PO_THREADS / 32 * N) {
+      int most = 0;
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (i0 + k < n && children[i0 + k] != 1) most = max(most, pg_ceil(length[i0 + k], p.pt));
+      for (int o = lane; o < most; o += 32) {
+        int page[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const int i = i0 + k;
+          page[k] = -1;
+          if (i < n && children[i] != 1 && o < pg_ceil(length[i], p.pt)) page[k] = __ldcg(p.table + (size_t)seq[i] * p.seq_pages + o);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          if (page[k] < 0 || page[k] >= p.pages) continue;
+          const int more = children[i0 + k] - 1, d = o < length[i0 + k] >> p.pt_shift ? more : min(more, 0);
+          if (d) atomicAdd(p.refs + page[k], sign * d);
+        }
       }
     }
     __syncthreads();
   };
   count(1);
+  // the copies: behind the counts, so that their pages are asked for while those are on their way
   int total = 0;
   for (int base = 0; base < n; base += PO_THREADS) {
     const int i = base + tid;
     int held = -1, used = 0;
     if (i < n) {
-      const int a = __ldg(parents + i), s = __ldg(seqs + a), len = __ldcg(p.lens + s), heir = __ldcg(p.off + a);
-      if ((len & (p.pt - 1)) && (heir < 0 ? a : heir) != i) {
-        held = __ldcg(p.table + (size_t)s * p.seq_pages + (len >> p.pt_shift));
+      const int a = parent[i], len = length[a], h = heir[a];
+      if ((len & (p.pt - 1)) && (h < 0 ? a : h) != i) {
+        held = __ldcg(p.table + (size_t)seq[a] * p.seq_pages + (len >> p.pt_shift));
         used = pg_ceil(len & (p.pt - 1), kPageBlock);
       }
       if (held >= p.pages) held = -1;
     }
     int sum;
     const int at = total + block_scan(held >= 0, sums, &sum) - 1;
-    if (i < n) p.mark[i] = held >= 0 ? at : -1;        // (all of p.off is read before it is written)
+    if (i < n) {
+      p.off[i] = held >= 0 ? at : -1;
+      p.mark[i] = length[parent[i]];
+    }
     if (held >= 0) p.moves[1 + 2 * at] = (int)((uint32_t)held | (uint32_t)(used - 1) << 28);
     total += sum;
   }
-  __syncthreads();
-  bad = total && take_free(p, first_group(p), 0, nullptr, sums) < total;
+  bad = total && take_free(p, first_group(p), total, p.fresh, sums) < total;
   if (bad) {
-    count(-1);                                         // (the numbers of children are still there)
+    count(-1);
     if (tid == 0) pg_status(p.status, kPagesExhausted, 42);
   } else {
-    if (total) take_free(p, first_group(p), total, p.fresh, sums);
     for (int k = tid; k < total; k += PO_THREADS) {
       const int page = __ldcg(p.fresh + k);
       p.moves[2 + 2 * k] = page;
       p.refs[page] = 1;
-    }
-    __syncthreads();
-    for (int i = tid; i < n; i += PO_THREADS) {
-      p.off[i] = __ldcg(p.mark + i);
-      p.fresh[i] = __ldcg(p.lens + __ldg(seqs + __ldg(parents + i)));
     }
   }
   if (tid == 0) p.moves[0] = bad ? -1 : total;
@@ -526,23 +545,23 @@ __global__ void __launch_bounds__(PM_THREADS) pages_reorder_move_kernel(PgParams
   const int moves = __ldcg(p.moves);
   if (moves < 0) return;
   for (int c0 = blockIdx.x * columns; c0 < p.seq_pages; c0 += gridDim.x * columns) {
-    const int cols = min(columns, p.seq_pages - c0);
     __syncthreads();
-    for (int u = tid; u < n * cols; u += PM_THREADS) {
-      const int i = u / cols, o = u - i * cols;
-      po_rows[u] = __ldcg(p.table + (size_t)__ldg(seqs + i) * p.seq_pages + c0 + o);
+#pragma unroll 4
+    for (int u = tid; u < n * columns; u += PM_THREADS) {
+      const int i = u / columns, o = c0 + u - i * columns;
+      if (o < p.seq_pages) po_rows[u] = __ldcg(p.table + (size_t)__ldg(seqs + i) * p.seq_pages + o);
     }
     __syncthreads();
-    for (int u = tid; u < n * cols; u += PM_THREADS) {
-      const int i = u / cols, o = u - i * cols, a = __ldg(parents + i);
-      if (a == i) continue;
-      const int copy = __ldcg(p.off + i);
-      int page = po_rows[a * cols + o];
-      if (copy >= 0 && c0 + o == __ldcg(p.fresh + i) >> p.pt_shift) page = __ldcg(p.moves + 2 + 2 * copy);
-      p.table[(size_t)__ldg(seqs + i) * p.seq_pages + c0 + o] = page;
+#pragma unroll 4
+    for (int u = tid; u < n * columns; u += PM_THREADS) {
+      const int i = u / columns, o = c0 + u - i * columns, a = __ldg(parents + i), copy = __ldcg(p.off + i), len = __ldcg(p.mark + i);
+      if (a == i || o >= p.seq_pages) continue;
+      int page = po_rows[a * columns + o - c0];
+      if (copy >= 0 && o == len >> p.pt_shift) page = __ldcg(p.moves + 2 + 2 * copy);
+      p.table[(size_t)__ldg(seqs + i) * p.seq_pages + o] = page;
     }
   }
-  for (int i = blockIdx.x * PM_THREADS + tid; i < n; i += gridDim.x * PM_THREADS) p.lens[__ldg(seqs + i)] = __ldcg(p.fresh + i);
+  for (int i = blockIdx.x * PM_THREADS + tid; i < n; i += gridDim.x * PM_THREADS) p.lens[__ldg(seqs + i)] = __ldcg(p.mark + i);
   const int lane = tid & 31, runs = p.heads * 2, per_move = p.layers * runs, blocks = p.pt / kPageBlock;
   const int64_t work = (int64_t)moves * per_move;
   for (int64_t w = (int64_t)blockIdx.x * (PM_THREADS / 32) + (tid >> 5); w < work; w += (int64_t)gridDim.x * (PM_THREADS / 32)) {
@@ -731,22 +750,26 @@ int less_pages_reorder(const less_pages* d, int32_t n, const int32_t* seqs, cons
   if (!seqs || !parents) return LESS_ERR_NULL_POINTER;
   if (((uintptr_t)seqs | (uintptr_t)parents) & 3) return LESS_ERR_MISALIGNED;
   cudaStream_t s = (cudaStream_t)stream;
-  rc = pg_launch("pages_reorder_plan_kernel", pages_reorder_plan_kernel, dim3(1), PO_THREADS, 0, s, p, n, seqs, parents);
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return fail_cuda("cudaGetDevice");
+  if (dev >= 64 || !(done.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (cudaFuncSetAttribute(pages_reorder_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PO_REORDER * PO_ENTRY) != cudaSuccess)
+      return fail_cuda("shared memory opt-in of pages_reorder_plan_kernel");
+    if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  rc = pg_launch("pages_reorder_plan_kernel", pages_reorder_plan_kernel, dim3(1), PO_THREADS, (size_t)n * PO_ENTRY, s, p, n, seqs, parents);
   if (rc != LESS_OK) return rc;
-  // columns of the table that a CTA takes at a time: as many as 48 KB hold (64 KB with more than 12 288 entries)
-  const int room = n > 12288 ? 16384 : 12288;
-  int columns = room / n;
+  // columns of the table that a CTA takes at a time: about a thousand cells
+  int columns = 1024 / n;
   if (columns > d->seq_pages) columns = d->seq_pages;
-  if (columns > 64) columns = 64;
-  const size_t smem = (size_t)n * columns * 4;
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(pages_reorder_move_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024) != cudaSuccess)
-    return fail_cuda("shared memory opt-in of pages_reorder_move_kernel");
+  if (columns < 1) columns = 1;
   // at most every entry but one of a family has a page copied
   const int64_t ctas = (int64_t)n * d->layers * pg_ceil(d->heads * 2, PM_THREADS / 32), cuts = pg_ceil(d->seq_pages, columns);
   const int64_t most = ctas > cuts ? ctas : cuts;
   const int grid = (int)(most < 8 * pg_sms() ? most : 8 * pg_sms());
-  return pg_launch("pages_reorder_move_kernel", pages_reorder_move_kernel, dim3(grid), PM_THREADS, smem, s, p, d->head_dim, n, seqs, parents,
-                   columns);
+  return pg_launch("pages_reorder_move_kernel", pages_reorder_move_kernel, dim3(grid), PM_THREADS, (size_t)n * columns * 4, s, p, d->head_dim,
+                   n, seqs, parents, columns);
 }
 
 int less_pages_trim(const less_pages* d, int32_t n, const int32_t* seqs, int32_t sinks, int32_t window, void* stream) {

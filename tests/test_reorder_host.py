@@ -42,7 +42,7 @@ def test_without_a_context(B):
 
 def test_paged(B):
     d, p = desc(B, seqs=20000), 4096
-    assert B.less_pages_reorder(d, -1, p, p, None) == BAD and B.less_pages_reorder(d, 16385, p, p, None) == BAD
+    assert B.less_pages_reorder(d, -1, p, p, None) == BAD and B.less_pages_reorder(d, 8193, p, p, None) == BAD
     assert B.less_pages_reorder(desc(B), 4, p, p, None) == BAD
     assert B.less_pages_reorder(d, 1, None, p, None) == NULL and B.less_pages_reorder(d, 1, p, None, None) == NULL
     assert B.less_pages_reorder(d, 1, 4098, p, None) == MISALIGNED and B.less_pages_reorder(d, 1, p, 4097, None) == MISALIGNED
