@@ -34,6 +34,7 @@ __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, Pa
     sum_rest = 0;
     lead = -1;
   }
+  const int g0 = __ldg(groups + g), g1 = __ldg(groups + g + 1);
   bool bad = false;
   for (int i = tid; i < ngroups; i += PX_THREADS) {
     const int b = __ldg(groups + i), e = __ldg(groups + i + 1);
@@ -41,9 +42,11 @@ __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, Pa
   }
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) pg_status(p.status, kPagesBounds, 50);
-  const int e0 = !bad ? __ldg(groups + g) : g ? a.n : 0, e1 = bad ? a.n : __ldg(groups + g + 1);
+  const int e0 = !bad ? g0 : g ? a.n : 0, e1 = bad ? a.n : g1;
+  PgEntry mine = {0, 0, 0, 0};                            // the first of the thread's entries: looked up once
   for (int i = e0 + tid; i < e1; i += PX_THREADS) {
     const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, i);
+    if (i == e0 + tid) mine = e;
     const int rows = a.starts ? __ldg(a.starts + i + 1) - __ldg(a.starts + i) : 1;
     if (rows < 0) descends = 1;
     if (rows != e.count || e.len < e.count) refused = 1;   // not to be trusted: nobody of the group shares
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, Pa
   const int end = a.starts ? min(max(__ldg(a.starts + e1), row0), a.rows) : max(e1, row0);
   const int64_t tiles = ((int64_t)(end - row0) * p.group + 7) / 8;
   for (int i = e0 + tid; i < e1; i += PX_THREADS) {
-    const PgEntry e = pg_entry(p, a.seqs, a.starts, a.rows, i);
+    const PgEntry e = i == e0 + tid ? mine : pg_entry(p, a.seqs, a.starts, a.rows, i);
     if (e.count == 0) continue;
     const int rest = rest_blocks(visible_blocks(a, e.len, e.count), blocks).count();
     atomicMax(&most_rest, rest);

@@ -95,10 +95,10 @@ __global__ void __launch_bounds__(RO_THREADS, RO_CTAS) state_reorder_kernel(RoAr
     __syncthreads();
   };
   auto fetch = [&](const Tile& x, int buf) {
-    const int all = sources * x.n;
-    for (int i = tid; i < all; i += RO_THREADS) {
-      const int s = i / x.n, u = i - s * x.n;
-      ro_copy16(smem + (uint32_t)(buf * RO_UNITS + s * x.n + u) * 16, x.row0 + source[s] * x.pitch + (int64_t)u * 16);
+    for (int s = tid >> 5; s < sources; s += RO_THREADS / 32) {
+      const unsigned char* from_row = x.row0 + source[s] * x.pitch;
+      const uint32_t to = smem + (uint32_t)(buf * RO_UNITS + s * x.n) * 16;
+      for (int u = tid & 31; u < x.n; u += 32) ro_copy16(to + u * 16, from_row + (int64_t)u * 16);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -134,11 +134,11 @@ __global__ void __launch_bounds__(RO_THREADS, RO_CTAS) state_reorder_kernel(RoAr
     }
     __syncthreads();
     const uint4* in = reinterpret_cast<const uint4*>(ro_smem) + buf * RO_UNITS;
-    const int all = moves * cur.n;
-    for (int i = tid; i < all; i += RO_THREADS) {
-      const int m = i / cur.n, u = i - m * cur.n;
-      unsigned char* dst = const_cast<unsigned char*>(cur.row0) + moved[m] * cur.pitch + (int64_t)u * 16;
-      *reinterpret_cast<uint4*>(dst) = in[from[m] * cur.n + u];
+    for (int m = tid >> 5; m < moves; m += RO_THREADS / 32) {
+      uint4* dst = reinterpret_cast<uint4*>(const_cast<unsigned char*>(cur.row0) + moved[m] * cur.pitch);
+      const uint4* src = in + from[m] * cur.n;
+#pragma unroll 4
+      for (int u = tid & 31; u < cur.n; u += 32) dst[u] = src[u];
     }
     __syncthreads();
     cur = nxt;
