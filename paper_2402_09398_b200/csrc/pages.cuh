@@ -39,7 +39,6 @@ struct PgParams {
   int32_t* fresh;          // [max(seqs, pages)]
   int32_t* counters;       // [kPgCounters] zero between calls
   float* partial;          // partial results of the step kernel
-  int4* shared;            // [seqs] of entries, [2 seqs] of groups: what attention over shared pages has found (pages_attn.cuh)
 };
 
 constexpr int kPgCounters = 1024;
@@ -169,6 +168,8 @@ inline int pg_launch(const char* name, void (*kernel)(P...), dim3 grid, int thre
 
 // host: checks a description; on success fills the device view
 int pg_view(const less_pages* d, PgParams* p);
+// the part of the workspace for what entries share: int4 [seqs] of entries, then [2 seqs] of groups (pages_attn.cuh)
+void* pg_shared(const less_pages* d);
 int pg_sms();
 
 }  // namespace less

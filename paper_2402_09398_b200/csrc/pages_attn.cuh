@@ -15,7 +15,10 @@ struct PaArgs {
   int max_rows;                  // entries with more rows (tokens x query heads of a group) are not this kernel's
   int window, sinks;             // window 0 = all
   float scale;
-  // attention of sequences that share their first pages (pages_shared.cu); not read otherwise
+};
+
+// attention of sequences that share their first pages (pages_shared.cu)
+struct PaSharedArgs : PaArgs {
   const int4* groups;            // two of each group: {sequence, first row, tokens, first entry}, {sb, wb, eb, end of its entries}
                                  // with the blocks that it shares; tokens -1: starts that descend
   const int4* entries;           // of each entry: {sb, wb, eb, the most blocks that rows of a tile have beside the shared ones
@@ -72,40 +75,44 @@ template <PaMode MODE>
 struct PaWork;
 template <>
 struct PaWork<kAll> {
+  typedef PaArgs Args;
   typedef Blocks B;
   static __device__ __forceinline__ PgEntry entry(const PgParams& p, const PaArgs& a, int i) { return pg_entry(p, a.seqs, a.starts, a.rows, i); }
   static __device__ __forceinline__ B blocks(const PaArgs& a, int, const PgEntry& e) { return visible_blocks(a, e.len, e.count); }
 };
 template <>
 struct PaWork<kTree> {
+  typedef PaSharedArgs Args;
   typedef Blocks B;
-  static __device__ __forceinline__ PgEntry entry(const PgParams&, const PaArgs& a, int i) {
+  static __device__ __forceinline__ PgEntry entry(const PgParams&, const PaSharedArgs& a, int i) {
     const int4 g = __ldcg(a.groups + 2 * i);
     return {g.x, g.y, g.z, 0};
   }
-  static __device__ __forceinline__ B blocks(const PaArgs& a, int i, const PgEntry&) {
+  static __device__ __forceinline__ B blocks(const PaSharedArgs& a, int i, const PgEntry&) {
     const int4 b = __ldcg(a.groups + 2 * i + 1);
     return {b.x, b.y, b.z};
   }
 };
 template <>
 struct PaWork<kShared> {
+  typedef PaSharedArgs Args;
   typedef Blocks B;
-  static __device__ __forceinline__ PgEntry entry(const PgParams&, const PaArgs& a, int i) {
+  static __device__ __forceinline__ PgEntry entry(const PgParams&, const PaSharedArgs& a, int i) {
     const int4 g = __ldcg(a.groups + 2 * i), b = __ldcg(a.groups + 2 * i + 1);
     const int tokens = b.x + b.z - b.y > 0 ? g.z : 0;
     return {g.x, g.y, tokens, b.z * kPageBlock + tokens};  // every token lies behind the shared ones
   }
-  static __device__ __forceinline__ B blocks(const PaArgs& a, int i, const PgEntry&) {
+  static __device__ __forceinline__ B blocks(const PaSharedArgs& a, int i, const PgEntry&) {
     const int4 b = __ldcg(a.groups + 2 * i + 1);
     return {b.x, b.y, b.z};
   }
 };
 template <>
 struct PaWork<kRest> {
+  typedef PaSharedArgs Args;
   typedef RestBlocks B;
-  static __device__ __forceinline__ PgEntry entry(const PgParams& p, const PaArgs& a, int i) { return pg_entry(p, a.seqs, a.starts, a.rows, i); }
-  static __device__ __forceinline__ B blocks(const PaArgs& a, int i, const PgEntry& e) {
+  static __device__ __forceinline__ PgEntry entry(const PgParams& p, const PaSharedArgs& a, int i) { return pg_entry(p, a.seqs, a.starts, a.rows, i); }
+  static __device__ __forceinline__ B blocks(const PaSharedArgs& a, int i, const PgEntry& e) {
     return rest_blocks(visible_blocks(a, e.len, e.count), __ldcg(a.entries + i));
   }
 };
@@ -207,8 +214,8 @@ int pa_args(const less_pages* d, int32_t layer_begin, int32_t layer_count, int32
             PgParams* p, PaArgs* a);
 int launch_pages_attention(const PgParams& p, PaArgs a, int dim, uint32_t flags, int32_t max_new, cudaStream_t s);
 // results of the groups' tokens over the blocks that they share, into a.parts (pages_prefix.cu)
-int launch_pages_prefix(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);
+int launch_pages_prefix(const PgParams& p, const PaSharedArgs& a, int dim, uint32_t flags, cudaStream_t s);
 // groups of few rows, in one launch (pages_tree.cu)
-int launch_pages_tree(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s);
+int launch_pages_tree(const PgParams& p, const PaSharedArgs& a, int dim, uint32_t flags, cudaStream_t s);
 
 }  // namespace less

@@ -139,8 +139,8 @@ __device__ __forceinline__ void mma_commit_if(uint32_t on, uint64_t* bar) {
 // Slots of the grid: entry i owns slots [starts[i] G / 256 + i, starts[i + 1] G / 256 + i + 1) - at least as many as it
 // has pairs of row tiles
 template <PaMode MODE>
-__device__ __forceinline__ int64_t pc_slot(const PgParams& p, const PaArgs& a, int i) {
-  if (MODE == kShared) return (int64_t)__ldcg(a.groups + 2 * i).y * p.group / (2 * PC_ROWS) + i;
+__device__ __forceinline__ int64_t pc_slot(const PgParams& p, const typename PaWork<MODE>::Args& a, int i) {
+  if constexpr (MODE == kShared) return (int64_t)__ldcg(a.groups + 2 * i).y * p.group / (2 * PC_ROWS) + i;
   const int row = a.starts ? min(max(__ldg(a.starts + i), 0), a.rows) : i;
   return (int64_t)row * p.group / (2 * PC_ROWS) + i;
 }
@@ -164,7 +164,7 @@ __device__ __forceinline__ uint32_t pc_mask16(int j0, int pos, int window, int s
 }
 
 template <typename T, int D, bool E4M3, PaMode MODE>
-__global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgParams p, PaArgs a, int splits) {
+__global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgParams p, typename PaWork<MODE>::Args a, int splits) {
   constexpr int PC_DEQ_WARPS = pc_deq_warps(MODE), PC_THREADS = pc_threads(MODE), S_WARP = PC_SOFT_WARPS + PC_DEQ_WARPS;
   constexpr int QT = PC_ROWS * D * 2;                     // bytes of a Q tile
   constexpr int KT = PC_KEYS * D * 2;                     // of a K or V tile
@@ -198,14 +198,18 @@ __global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgPara
   // kShared, rows for one tile only: both row tiles hold them, and each takes every other key tile - two softmax chains
   // instead of one (16 sequences over 100 003 tokens, 8 x 8 heads, with six warps that convert: 114 -> 98 us); a part of the
   // results each
-  const bool twin = MODE == kShared && a.twins && valid <= PC_ROWS;
+  bool twins = false;                                      // the host has counted on two parts a split
+  if constexpr (MODE == kShared) twins = a.twins;
+  const bool twin = twins && valid <= PC_ROWS;
   const int nx = valid > PC_ROWS || twin ? 2 : 1;
   // key tile kt is the turn(kt)-th of a row tile that takes it
   auto turn = [&](int kt) { return MODE == kShared && twin ? kt >> 1 : kt; };
   const int lj = lh / p.heads, h = lh - lj * p.heads, layer = a.layer0 + lj;
   const int base = e.len - e.count;                       // position of the entry's first token
   const int tok0 = (int)(row0 / p.group), tok1 = (int)((row0 + valid - 1) / p.group);
-  const Blocks vb = MODE == kShared ? PaWork<kShared>::blocks(a, lo, e) : visible_blocks(a, base + tok1 + 1, tok1 - tok0 + 1);
+  Blocks vb;
+  if constexpr (MODE == kShared) vb = PaWork<kShared>::blocks(a, lo, e);
+  else vb = visible_blocks(a, base + tok1 + 1, tok1 - tok0 + 1);
   const int units = base + tok1 < 0 ? 0 : vb.count();
   // with few items the key tiles are dealt out to `splits` CTAs (blockIdx.y), whose results are joined by a second kernel
   const int nk_all = pg_ceil(units, PC_TILES), share = max(pg_ceil(nk_all, splits), splits > 1 ? PC_SPLIT_TILES : 1);
@@ -218,13 +222,13 @@ __global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgPara
   const int64_t part_rows = (int64_t)a.rows * heads * p.group;
   auto part_row = [&](int64_t rr) {
     const int64_t tok = rr / p.group;
-    return (int64_t)blockIdx.y * (a.twins ? 2 : 1) * part_rows + (e.row0 + tok) * heads * p.group + (int64_t)lh * p.group + (rr - tok * p.group);
+    return (int64_t)blockIdx.y * (twins ? 2 : 1) * part_rows + (e.row0 + tok) * heads * p.group + (int64_t)lh * p.group + (rr - tok * p.group);
   };
   if (nk == 0) {                                          // nothing to see
-    if (MODE == kShared) {
+    if constexpr (MODE == kShared) {
       for (int i = tid; i < valid; i += PC_THREADS) {
         a.weights[part_row(row0 + i)] = make_float2(-INFINITY, 0.f);
-        if (a.twins) a.weights[part_rows + part_row(row0 + i)] = make_float2(-INFINITY, 0.f);
+        if (twins) a.weights[part_rows + part_row(row0 + i)] = make_float2(-INFINITY, 0.f);
       }
       return;
     }
@@ -445,7 +449,7 @@ __global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgPara
       const int turns = MODE == kShared && twin ? (nk + 1 - x) >> 1 : nk;
       if (MODE == kAll || turns) wait_or_give_up(&sh->pv_done[x][(turns - 1) & 1], ((turns - 1) >> 1) & 1, abortp, status, 124);
       tc_fence_after_sync();
-      if (MODE == kShared && a.twins && r < valid) {
+      if constexpr (MODE == kShared) if (twins && r < valid) {
         if (!twin) a.weights[part_rows + part_row(rr)] = make_float2(-INFINITY, 0.f);
         if (!turns) a.weights[x * part_rows + part_row(rr)] = make_float2(-INFINITY, 0.f);
       }
@@ -454,7 +458,7 @@ __global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgPara
         const float inv = l == 0.f ? 0.f : 1.f / l, unit = 0x1p-8f / pg_top<E4M3>();
         T* dst = out + (int64_t)(e.row0 + tok) * a.nl * p.heads * p.group * D + head_row + hd * D;
         const int64_t at = (MODE == kShared && twin ? x * part_rows : 0) + part_row(rr);
-        if (MODE == kShared && r < valid) a.weights[at] = pa_share(M, l);
+        if constexpr (MODE == kShared) if (r < valid) a.weights[at] = pa_share(M, l);
         if (MODE == kAll && splits > 1 && r < valid) *reinterpret_cast<float2*>(part + (size_t)2 * PC_ROWS * D + 2 * r) = make_float2(M, l);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
@@ -465,7 +469,7 @@ __global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgPara
 #pragma unroll
           for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(o[i]) * inv * unit;
           if (r < valid) {
-            if (MODE == kShared) {
+            if constexpr (MODE == kShared) {
               float* to = a.parts + at * D + 32 * c;
 #pragma unroll
               for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
@@ -494,11 +498,11 @@ __global__ void __launch_bounds__(pc_threads(MODE), 1) pages_chunk_kernel(PgPara
       last_pos[x] = base + (int)((row0 + min((x + 1) * PC_ROWS, valid) - 1) / p.group);
     }
     // lane 2 i + b knows tile b of this warp's pair in its i-th key tile of the batch, key tile batch + PAIRS * i
-    auto nth = [&](int kt) { return kt / PAIRS * 2 & 30; };
+    auto nth = [&](int kt) { return PAIRS == 2 ? kt & 30 : kt / PAIRS * 2 & 30; };
     int page_l = -1, j_l = 0;
     float ak_l = 0.f, av_l = 0.f, vlast = 1.f;
     auto lookup = [&](int batch) {
-      const int u = (kt0 + batch + (lane >> 1) * PAIRS) * PC_TILES + 2 * dw + (lane & 1);
+      const int u = (kt0 + batch + (PAIRS == 2 ? lane & ~1 : (lane >> 1) * PAIRS)) * PC_TILES + 2 * dw + (lane & 1);
       page_l = -1;
       j_l = 0;
       if (u < units) {

@@ -677,9 +677,10 @@ int pg_view(const less_pages* d, PgParams* p) {
   p->off = (int32_t*)(w + l.off);
   p->fresh = (int32_t*)(w + l.fresh);
   p->partial = (float*)(w + l.partial);
-  p->shared = (int4*)(w + l.shared);
   return LESS_OK;
 }
+
+void* pg_shared(const less_pages* d) { return (char*)d->workspace + pg_layout(d).shared; }
 
 int pg_sms() {
   static std::atomic<int> sms[64];

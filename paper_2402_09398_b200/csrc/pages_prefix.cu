@@ -5,7 +5,7 @@
 namespace less {
 
 template <typename T, int D, bool E4M3>
-static int launch_prefix_chunk(const PgParams& p, const PaArgs& a, cudaStream_t s) {
+static int launch_prefix_chunk(const PgParams& p, const PaSharedArgs& a, cudaStream_t s) {
   constexpr size_t smem = (size_t)(2 * PC_ROWS + 2 * PC_STAGES * PC_KEYS) * D * 2 + sizeof(PcShared);
   static std::atomic<unsigned long long> done{0};
   int dev = 0;
@@ -22,7 +22,7 @@ static int launch_prefix_chunk(const PgParams& p, const PaArgs& a, cudaStream_t 
                    pc_threads(kShared), smem, s, p, a, a.splits);
 }
 
-int launch_pages_prefix(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, cudaStream_t s) {
+int launch_pages_prefix(const PgParams& p, const PaSharedArgs& a, int dim, uint32_t flags, cudaStream_t s) {
   const bool e4m3 = flags & LESS_PAGES_E4M3;
   if (flags & LESS_PAGES_BF16) {
     if (dim == 128) return e4m3 ? launch_prefix_chunk<__nv_bfloat16, 128, true>(p, a, s) : launch_prefix_chunk<__nv_bfloat16, 128, false>(p, a, s);

@@ -19,7 +19,7 @@ constexpr int PX_THREADS = 1024, PX_PER = 8;              // table entries of a 
 // One CTA per group.  A list of groups that is not [0 .. n] ascending is reported; then all entries are one group that shares
 // nothing.
 constexpr int PX_TILES = 1024;                            // tiles of 8 rows whose blocks are counted one by one
-__global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, PaArgs a, const int32_t* groups, int ngroups) {
+__global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, PaSharedArgs a, const int32_t* groups, int ngroups) {
   __shared__ int common, least_seen, most_len, least_wb, some, lead, refused, descends, most_rest;
   __shared__ unsigned long long sum_rest;
   __shared__ int tile_rest[PX_TILES];
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, Pa
 // Joins the parts of a row into the first: a warp per row, all loads of eight parts on their way at once.  (Rows that share
 // nothing have no parts; what becomes of what lies there nobody reads.)
 template <int D>
-__global__ void __launch_bounds__(256) pages_parts_kernel(PgParams p, PaArgs a, int parts) {
+__global__ void __launch_bounds__(256) pages_parts_kernel(PgParams p, PaSharedArgs a, int parts) {
   constexpr int LANES = D / 4, N = 8;
   pg_wait();
   const int lane = threadIdx.x % LANES;
@@ -189,7 +189,7 @@ extern "C" int less_pages_shared_attention(const less_pages* d, int32_t layer_be
                                            int64_t q_stride, int32_t window, int32_t sinks, float scale, void* out,
                                            void* stream) {
   PgParams p;
-  PaArgs a;
+  PaSharedArgs a = {};
   int rc = pa_args(d, layer_begin, layer_count, n, seqs, starts, rows, max_new, q, q_stride, window, sinks, scale, out, &p, &a);
   if (rc != LESS_OK) return rc;
   if (n > d->seqs || ngroups < (n ? 1 : 0) || ngroups > n || max_group < 1) return LESS_ERR_INVALID_CONFIG;
@@ -203,8 +203,9 @@ extern "C" int less_pages_shared_attention(const less_pages* d, int32_t layer_be
   const int64_t layer_rows = (int64_t)rows * d->heads * d->group, fit = (int64_t)(room / row_bytes) / layer_rows;
   if (own > kSharedRows || save < kSharedLeast || (fit == 0 && all > kTreeRows))
     return launch_pages_attention(p, a, d->head_dim, d->flags, max_new, s);
-  a.entries = p.shared;
-  a.groups = p.shared + d->seqs;
+  int4* found = (int4*)pg_shared(d);
+  a.entries = found;
+  a.groups = found + d->seqs;
   rc = pg_launch("pages_common_kernel", pages_common_kernel, dim3(ngroups), PX_THREADS, 0, s, p, a, groups, ngroups);
   if (rc != LESS_OK) return rc;
   if (all <= kTreeRows) {
@@ -220,7 +221,7 @@ extern "C" int less_pages_shared_attention(const less_pages* d, int32_t layer_be
     a.layer0 = layer_begin + l0;
     a.q = (const char*)q + l0 * layer;
     a.out = (char*)out + l0 * layer;
-    PaArgs b = a;
+    PaSharedArgs b = a;
     b.n = ngroups;
     b.window = b.sinks = 0;
     b.max_rows = 0;

@@ -127,7 +127,7 @@ __device__ __forceinline__ int64_t row_offset(const PgParams& p, int layers, int
 // kRest: a row's N values from f (relative to 2^m, sum l) and the one or two parts over shared blocks; row: its number among
 // the parts
 template <int D, int N>
-__device__ __forceinline__ void join_shared(const PgParams& p, const PaArgs& a, int64_t row, int d0, float* f, float m, float l) {
+__device__ __forceinline__ void join_shared(const PgParams& p, const PaSharedArgs& a, int64_t row, int d0, float* f, float m, float l) {
   const int64_t rows = (int64_t)a.rows * a.nl * p.heads * p.group;
   const float2 w0 = __ldcg(a.weights + row), w1 = a.splits > 1 ? __ldcg(a.weights + rows + row) : make_float2(-INFINITY, 0.f);
   const float top = fmaxf(m, fmaxf(w0.x, w1.x));
@@ -157,7 +157,7 @@ __device__ __forceinline__ void join_shared(const PgParams& p, const PaArgs& a, 
 }
 
 template <typename T, int D, int NT, bool E4M3, PaMode MODE>
-__global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(PgParams p, PaArgs a) {
+__global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(PgParams p, typename PaWork<MODE>::Args a) {
   typedef PaWork<MODE> Work;
   constexpr int R = 8 * NT, MT = D / 16;
   constexpr int TILE = 16 * D, CH = TILE / 512;           // bytes of a tile; 16-byte pieces per lane
@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     return tiles * a.nl * p.heads;
   };
   auto tree_rest = [&](int i, const PgEntry& e) -> int {  // the most blocks beside the shared ones that an item of it has
-    return MODE == kTree && e.count > 0 ? __ldcg(a.entries + __ldcg(a.groups + 2 * i).w).w : 0;
+    if constexpr (MODE == kTree) return e.count > 0 ? __ldcg(a.entries + __ldcg(a.groups + 2 * i).w).w : 0;
+    return 0;
   };
   int per_warp;
   int64_t pad = 0;
@@ -315,13 +316,13 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     it.lj = index / tiles / p.heads;
     it.tok_row = e.row0;
     it.valid = min(R, e.count * p.group - it.row0);
-    if (MODE == kRest) {
+    if constexpr (MODE == kRest) {
       const int4 of = __ldcg(a.entries + ei);
       it.extra = of.x + of.z - of.y > 0;
     }
     const int first = bo, end = (int)min((int64_t)blocks, bo + (ue - u));
     int last = vb.count() > 0 ? min(end, real) : first;             // what of it has tokens
-    if (MODE == kTree) {
+    if constexpr (MODE == kTree) {
       // whose the rows are; the blocks that their entries see beside the shared ones follow those
       const int4 ge = __ldcg(a.groups + 2 * ei), gb = __ldcg(a.groups + 2 * ei + 1);
       const int trow = e.row0 + (it.row0 + min(lane, it.valid - 1)) / p.group;
@@ -707,11 +708,15 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
           for (int i = 0; i < D / 8; ++i) f[i] = sum;
         }
         if (complete) {
-          if (MODE == kRest && it.extra) {
-            const float2 ml = pa_share(m[nt][c], sum);
-            join_shared<D, D / 8>(p, a, row_offset(p, a.nl, D, it, rc) / D, g * (D / 8), f, ml.x, ml.y);
+          int layers = a.nl;
+          if constexpr (MODE == kRest) {
+            layers = a.out_layers;
+            if (it.extra) {
+              const float2 ml = pa_share(m[nt][c], sum);
+              join_shared<D, D / 8>(p, a, row_offset(p, a.nl, D, it, rc) / D, g * (D / 8), f, ml.x, ml.y);
+            }
           }
-          T* dst = reinterpret_cast<T*>(a.out) + row_offset(p, MODE == kRest ? a.out_layers : a.nl, D, it, rc) + g * (D / 8);
+          T* dst = reinterpret_cast<T*>(a.out) + row_offset(p, layers, D, it, rc) + g * (D / 8);
 #pragma unroll
           for (int i = 0; i < D / 8; i += 8) store8<T>(dst + i, f + i);
         } else {
@@ -784,12 +789,16 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     f = make_float4(f.x * inv, f.y * inv, f.z * inv, f.w * inv);
   };
   auto row_done = [&](const Item& it, int r, float4 f, float mm, float ll) {
-    if (MODE == kRest && it.extra) {
-      float v[4] = {f.x, f.y, f.z, f.w};
-      join_shared<D, 4>(p, a, row_offset(p, a.nl, D, it, r) / D, lane * 4, v, mm, ll);
-      f = make_float4(v[0], v[1], v[2], v[3]);
+    int layers = a.nl;
+    if constexpr (MODE == kRest) {
+      layers = a.out_layers;
+      if (it.extra) {
+        float v[4] = {f.x, f.y, f.z, f.w};
+        join_shared<D, 4>(p, a, row_offset(p, a.nl, D, it, r) / D, lane * 4, v, mm, ll);
+        f = make_float4(v[0], v[1], v[2], v[3]);
+      }
     }
-    store4(reinterpret_cast<T*>(a.out) + row_offset(p, MODE == kRest ? a.out_layers : a.nl, D, it, r) + lane * 4, f);
+    store4(reinterpret_cast<T*>(a.out) + row_offset(p, layers, D, it, r) + lane * 4, f);
   };
   // Inside the CTA: the items that go on behind one of its warps (part 1), or begin before the first (part 0 of warp 0),
   // all rows dealt out to the warps in turn
@@ -860,7 +869,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
 
 // room: bytes at p.partial
 template <typename T, int D, int NT, bool E4M3, PaMode MODE>
-inline int launch_step(const PgParams& p, const PaArgs& a, size_t room, int counters, cudaStream_t s) {
+inline int launch_step(const PgParams& p, const typename PaWork<MODE>::Args& a, size_t room, int counters, cudaStream_t s) {
   constexpr size_t smem = (size_t)PS_WARPS * PS_RING * 2 * 16 * D;
   static std::atomic<unsigned long long> done{0};
   int dev = 0;
@@ -881,7 +890,7 @@ inline int launch_step(const PgParams& p, const PaArgs& a, size_t room, int coun
 }
 
 template <typename T, bool E4M3, PaMode MODE>
-inline int launch_step_dim(const PgParams& p, const PaArgs& a, int dim, int rows, size_t room, int counters, cudaStream_t s) {
+inline int launch_step_dim(const PgParams& p, const typename PaWork<MODE>::Args& a, int dim, int rows, size_t room, int counters, cudaStream_t s) {
   if constexpr (MODE == kTree)                             // tiles of 8 rows: what the host has counted is for these
     return dim == 128 ? launch_step<T, 128, 1, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 64, 1, E4M3, MODE>(p, a, room, counters, s);
   else if (dim == 128)
@@ -892,7 +901,7 @@ inline int launch_step_dim(const PgParams& p, const PaArgs& a, int dim, int rows
 
 // rows: the most of an entry, as far as the host knows
 template <PaMode MODE>
-inline int launch_pages_step(const PgParams& p, const PaArgs& a, int dim, uint32_t flags, int rows, size_t room, int counters, cudaStream_t s) {
+inline int launch_pages_step(const PgParams& p, const typename PaWork<MODE>::Args& a, int dim, uint32_t flags, int rows, size_t room, int counters, cudaStream_t s) {
   const bool e4m3 = flags & LESS_PAGES_E4M3;
   if (flags & LESS_PAGES_BF16)
     return e4m3 ? launch_step_dim<__nv_bfloat16, true, MODE>(p, a, dim, rows, room, counters, s)
