@@ -242,8 +242,7 @@ enum {
   LESS_KERNEL_GATHER = 9,
   LESS_KERNEL_MASKED_PACK = 10,
   LESS_KERNEL_MASKED_OUT = 11,
-  LESS_KERNEL_REORDER = 12,
-  LESS_KERNEL_COUNT = 13
+  LESS_KERNEL_COUNT = 12
 };
 int less_profile(less_ctx* ctx, int enable);
 int less_profile_read(less_ctx* ctx, float* ms_total_host, int64_t* launches_host);

@@ -50,7 +50,7 @@ LESS_BEAMS_MOST_BEAMS = 64
 LESS_BEAMS_MOST_KEEP = 128
 
 KERNEL_NAMES = ["feature_map", "decode", "rowstat", "colsum", "attn_out", "select", "build", "finalize",
-                "psi", "gather", "masked_pack", "masked_out", "reorder"]
+                "psi", "gather", "masked_pack", "masked_out"]
 
 
 class less_config(C.Structure):

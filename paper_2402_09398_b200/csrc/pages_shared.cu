@@ -174,7 +174,7 @@ constexpr int kSharedRows = 128;
 constexpr int kTreeRows = 32;
 // Bytes that sharing could save at most, as far as the host knows, below which it is not tried: finding out what is shared
 // takes 4 us.
-constexpr int64_t kSharedLeast = (int64_t)16 << 20;
+constexpr double kSharedLeast = 16 << 20;
 // Parts of a row that the second half joins itself (join_shared); more are joined by a kernel of their own first.
 constexpr int kJoinParts = 2;
 constexpr size_t kStepBytes = (size_t)10 << 20;           // of the partial results: those of the second half's step kernel
@@ -198,7 +198,7 @@ extern "C" int less_pages_shared_attention(const less_pages* d, int32_t layer_be
   if ((uintptr_t)groups & 3) return LESS_ERR_MISALIGNED;
   cudaStream_t s = (cudaStream_t)stream;
   const int64_t own = (int64_t)(starts ? max_new : 1) * d->group, all = (int64_t)max_group * d->group;
-  const int64_t save = (int64_t)(n - ngroups) * layer_count * d->heads * d->seq_pages * d->page_tokens * 2 * d->head_dim;
+  const double save = (double)(n - ngroups) * layer_count * d->heads * d->seq_pages * d->page_tokens * 2 * d->head_dim;
   const size_t row_bytes = (size_t)d->head_dim * 4 + 8, room = LESS_PAGES_PARTIAL_BYTES - kStepBytes;
   const int64_t layer_rows = (int64_t)rows * d->heads * d->group, fit = (int64_t)(room / row_bytes) / layer_rows;
   if (own > kSharedRows || save < kSharedLeast || (fit == 0 && all > kTreeRows))

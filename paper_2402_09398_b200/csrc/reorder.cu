@@ -5,6 +5,8 @@
 // batch-major, so a group's rows are `beams` byte strings, and what a CTA takes of them (a piece of the same bytes of every
 // row) can be permuted without regard to any other CTA: it brings the pieces of all sources into shared memory, waits, and
 // writes.  Two such tiles per CTA, so that one is on its way while the other is written; two CTAs per multiprocessor.
+#include <atomic>
+
 #include "less_internal.cuh"
 #include "pipeline.cuh"
 
@@ -110,6 +112,10 @@ __global__ void __launch_bounds__(RO_THREADS, RO_CTAS) state_reorder_kernel(RoAr
     if (g != group) {                                       // a new group: nothing is on its way
       enter(g);
       group = g;
+      if (moves == 0) {                                     // a group in which all beams live on
+        t = min(end, (g + 1) * per_group) - 1;
+        continue;
+      }
       cur = tile(t);
       fetch(cur, buf);
       if (t == g * per_group) {                             // live slots: 4 bytes per instance, rows need not be 16-byte aligned
@@ -172,13 +178,17 @@ extern "C" int less_reorder(less_ctx* c, int32_t beams, const int32_t* parents, 
   a.batch = d.B;
   a.beams = beams;
   const size_t smem = (size_t)2 * RO_UNITS * 16 + (size_t)4 * beams * 2;
-  if (cudaFuncSetAttribute(state_reorder_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * RO_UNITS * 16 + 8 * RO_UNITS) !=
-      cudaSuccess)
-    return fail_cuda("shared memory opt-in of state_reorder_kernel");
+  static std::atomic<unsigned long long> done{0};
+  if (c->device >= 64 || !(done.load(std::memory_order_relaxed) >> c->device & 1)) {
+    if (cudaFuncSetAttribute(state_reorder_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * RO_UNITS * 16 + 8 * RO_UNITS) !=
+        cudaSuccess)
+      return fail_cuda("shared memory opt-in of state_reorder_kernel");
+    if (c->device < 64) done.fetch_or(1ull << c->device, std::memory_order_relaxed);
+  }
   const int64_t tiles = a.tiles[RO_ARRAYS] * (d.B / beams);
   const int grid = (int)(tiles < (int64_t)RO_CTAS * c->sms ? tiles : (int64_t)RO_CTAS * c->sms);
   cudaStream_t s = (cudaStream_t)stream;
-  LaunchScope scope(c, LESS_KERNEL_REORDER, s, "state_reorder_kernel");
+  c->launches += 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(RO_THREADS);

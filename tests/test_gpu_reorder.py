@@ -98,12 +98,15 @@ def test_record_views_are_the_exported_records():
 
 
 @pytest.mark.parametrize("kw", [dict(layers=1, heads=4), dict(layers=2, heads=16, hidden=512), dict(group=4, hidden=128),
-                                dict(flags=2)])
+                                dict(flags=2), dict(layers=1, heads=8, hidden=512, small="1")])
 @pytest.mark.parametrize("captured", [False, True])
-def test_steps_and_reorderings_back_to_back(kw, captured):
-    """Decode steps with reorderings between them, launched without a pause, against the same calls with a wait behind
-    each: bit for bit."""
-    batch, beams, steps = 8, 4, 24
+def test_steps_and_reorderings_back_to_back(monkeypatch, kw, captured):
+    """Decode steps (of a few heads: as one launch) with reorderings between them, launched without a pause, against the
+    same calls with a wait behind each: bit for bit."""
+    kw = dict(kw)
+    small = kw.pop("small", "0")
+    monkeypatch.setenv("LESS_SMALL_STEP", small)
+    batch, beams, steps = 4 if small == "1" else 8, 4, 24
     rng = np.random.default_rng(1)
     parents = [ints(np.arange(batch) // beams * beams + rng.integers(0, beams, batch)) for _ in range(steps)]
     results = []
@@ -189,6 +192,24 @@ def everything(cache, model):
     same_maps(cache, model)
     assert np.array_equal(cache.codes.cpu().numpy(), model.codes)
     assert np.array_equal(cache.amax.double().cpu().numpy(), model.amax, equal_nan=True)
+
+
+def test_groups_that_live_on_are_left_alone():
+    ctx = context(40, slots=(50, 51))
+    st = scramble(ctx)
+    before = snapshot(st)
+    parents = list(range(40))
+    for turn in range(3):
+        if turn == 1:
+            parents[8:16] = [9, 9, 10, 15, 12, 13, 8, 8]
+        if turn == 2:
+            parents[39] = 32
+        st = scramble(ctx, turn)
+        before = snapshot(st)
+        ctx.reorder(ints(parents), beams=8)
+        assert all(torch.equal(st[k], before[k][torch.tensor(parents, device=DEV)]) for k in st)
+    assert ctx.poll_status() == 0
+    ctx.close()
 
 
 @pytest.mark.parametrize("seed", range(8))
