@@ -14,7 +14,8 @@
 // Within a beam the order is that of the logits, which is exact.  Between beams it hangs on the sums.  A term exp2(x) of
 // one is off, relative, by 2^-22 (the exponential), |x| 2^-23.4 (x: a product with a rounded factor, for fp32 logits of a
 // rounded difference) and 5 * 2^-24 (added to fifteen others; the rest is in 64 bits, rounded once at the end), so a sum
-// by at most 6e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it.
+// by at most 6e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it (a thread's -x, and twice
+// its largest x where it has logits above its reference).
 // Where two neighbours in the order are of different beams and closer than that, the sums of these beams are computed again
 // to 1e-10 and the candidates joined once more (a chance of some 1e-4 per kept candidate; 65 us for a row of 128 256,
 // one CTA's work that waits for memory).
@@ -51,7 +52,7 @@ struct BmArgs {
   int32_t* out_parents;
   uint8_t* out_ended;
   int32_t* counters;                                      // [groups] zero between calls
-  float4* sums;                                           // [rows][splits] (reference, sum, sum of the terms times -x, 0)
+  float4* sums;                                           // [rows][splits] (reference, sum, sum of the terms times |x| or a little more, 0)
   unsigned long long* keys;                               // [rows][splits][keep]
 };
 
@@ -638,6 +639,7 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
     float limit, floor, care;                             // care: pieces above it need more than adding up (NaN: all)
     double sum = 0.0;
     uint64_t far2 = 0;                                    // terms times x
+    float highest = -INFINITY;                            // of the logits added
     auto refer = [&](float to) {                          // nothing seen so far: any reference will do, the next element moves it
       ref = to == -INFINITY ? 0.f : to;
       limit = to == -INFINITY ? -INFINITY : ref + kRefFar;
@@ -690,6 +692,7 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
         add(f[0], part[0]);
         add(f[1], part[1]);
         add_up(f32x2_add(part[0], part[1]));
+        highest = fmaxf(highest, higher);
         if (higher >= bar) {
           const int token = row.token(at + tid);
 #pragma unroll
@@ -719,12 +722,14 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
               f32x2_unpack(far2, s0, s1);
               far2 = scale > 0.f ? f32x2_pack((s0 + s1 + back * (float)sum) * scale, 0.f) : 0;
               sum *= (double)scale;
+              highest = -INFINITY;                        // all so far lie below the new one
               refer(top);
             }
             const uint32_t most = BmType<T>::pack(BmType<T>::most);
             w = make_uint4(BmType<T>::smaller(w.x, most), BmType<T>::smaller(w.y, most), BmType<T>::smaller(w.z, most),
                            BmType<T>::smaller(w.w, most));
           }
+          highest = fmaxf(highest, top);
           float f[N];
           bm_unpack<T>(w, BmType<T>::pack(floor), f);
           uint64_t part = 0;
@@ -791,7 +796,8 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
     float f0, f1;
     f32x2_unpack(far2, f0, f1);
     double all = sum * scale;
-    float far = scale > 0.0 ? (f0 + f1 + behind * (float)sum) * (float)scale : 0.f;
+    const float up = fmaxf(0.f, (highest - ref) * 1.4426950408889634f);   // terms with x > 0 count with 2 up - x >= x
+    float far = scale > 0.0 ? (f0 + f1 + (behind - 2.f * up) * (float)sum) * (float)scale : 0.f;
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
       all += __shfl_xor_sync(0xffffffffu, all, d);

@@ -122,6 +122,24 @@ def test_ties_and_crowds(dtype):
     check(sel, logits, scores)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("peak", [3.0, 9.0, 20.0, 36.0])
+def test_order_of_beams_whose_peaks_come_late(dtype, peak):
+    """The same logits in two orders, the largest among the first ones or far behind them (where it is added relative to a
+    reference up to 2^52 smaller), and scores that differ by some 1e-7: the order is that of the 64-bit values."""
+    groups, vocab = 320, 20000                            # a stretch a row
+    g = torch.Generator().manual_seed(int(peak))
+    logits = torch.randn(groups, 1, vocab, generator=g).repeat(1, 2, 1)
+    logits[:, 0, 15000] = peak + 3 * torch.rand(groups, generator=g)
+    logits[:, 1, 15000] = logits[:, 0, 5]
+    logits[:, 1, 5] = logits[:, 0, 15000]
+    first = torch.randint(24, 60, (groups,), generator=g)
+    apart = torch.randint(1, 24, (groups,), generator=g) * (2 * torch.randint(0, 2, (groups,), generator=g) - 1)
+    scores = -0.5 - torch.stack([first, first + apart], 1) * 2.0 ** -24
+    sel = make(groups, 2, vocab, 2, TYPES[dtype])
+    check(sel, logits.to(TYPES[dtype]).to(DEV), scores.to(DEV))
+
+
 def test_crowds_with_many_kept():
     sel = make(2, 2, 40000, 128, torch.float32)
     logits = torch.zeros(2, 2, 40000, device=DEV)
