@@ -270,7 +270,7 @@ int less_import_state(less_ctx* ctx, const int32_t* inst_host, int32_t n, const 
 
 /* Beam search: row b of the batch becomes what row parents[b] was - slots, scores, psi, H and z of all layers and heads -
  * in place.  parents: device int32 [batch] (what less_beam_select gives); the batch consists of groups of `beams` rows
- * (beams <= 3072, batch a multiple), and a row's parent is of its own group: where one is not, no row changes and the
+ * (beams <= 2048, batch a multiple), and a row's parent is of its own group: where one is not, no row changes and the
  * status word reads LESS_ERR_DEVICE_BOUNDS.  The position is the context's and stays.  Asynchronous; can be captured. */
 int less_reorder(less_ctx* ctx, int32_t beams, const int32_t* parents, void* cuda_stream);
 

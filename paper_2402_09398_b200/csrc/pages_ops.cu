@@ -422,8 +422,9 @@ __global__ void __launch_bounds__(PM_THREADS) pages_move_kernel(PgParams p, int 
 // it is its own child, else the first of the list), the others get copies in the lowest free pages, among them those that
 // this call releases.  p.off[i] = number of the copy that entry i gets, p.mark[i] = its new length, both for the second
 // kernel; a copy's source carries the number of its 16-token blocks in use, less one, in its top four bits.
-// The entries lie in shared memory, so that what is left is a chain of some loads and scans (512 entries of up to 16 pages,
-// with the entries in global memory: 25 us; PLAN now).
+// Bound by latency: a chain of some dependent loads and scans in one CTA, which all need all entries.  These lie in shared
+// memory and four entries' pages are counted at a time (512 entries of up to 16 pages: 25 us with the entries in global
+// memory, 18 us now).
 constexpr int PO_REORDER = 8192;                       // entries of a call
 constexpr int PO_ENTRY = 20;                           // bytes of each: sequence, length, parent, children, the first of them
 __global__ void __launch_bounds__(PO_THREADS) pages_reorder_plan_kernel(PgParams p, int n, const int32_t* seqs,
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(PO_THREADS) pages_reorder_plan_kernel(PgParams
   bool bad = pg_stopped(p), again = false;
   __syncthreads();
   for (int i = tid; i < n; i += PO_THREADS) {
-    const int s = __ldg(seqs + i), a = __ldg(parents + i);
+    const int s = __ldg(seqs + i), a = __ldcg(parents + i);   // (a selection has written the latter: past L1)
     const int len = s >= 0 && s < p.seqs ? __ldcg(p.lens + s) : -1;
     if (a < 0 || a >= n || !pg_len_ok(p, len)) {
       pg_status(p.status, kPagesBounds, 40);
@@ -536,7 +537,9 @@ __global__ void __launch_bounds__(PO_THREADS) pages_reorder_plan_kernel(PgParams
 }
 
 // Carries it out: the entries' rows of the table, a CTA per stretch of columns (in place, through shared memory), and the
-// blocks in use of the pages that are copied, a warp per head's keys or values of one in one layer.
+// blocks in use of the pages that are copied, a warp per head's keys or values of one in one layer.  Bound by memory: a
+// copied page's blocks in use are read and written once (512 sequences in eight layers, 176 MB: 36 us; both kernels 56 us.
+// With the tables' rows in global memory and all columns in one CTA: 76 us).
 __global__ void __launch_bounds__(PM_THREADS) pages_reorder_move_kernel(PgParams p, int D, int n, const int32_t* seqs,
                                                                         const int32_t* parents, int columns) {
   extern __shared__ int32_t po_rows[];                 // [n][columns]
@@ -554,7 +557,7 @@ __global__ void __launch_bounds__(PM_THREADS) pages_reorder_move_kernel(PgParams
     __syncthreads();
 #pragma unroll 4
     for (int u = tid; u < n * columns; u += PM_THREADS) {
-      const int i = u / columns, o = c0 + u - i * columns, a = __ldg(parents + i), copy = __ldcg(p.off + i), len = __ldcg(p.mark + i);
+      const int i = u / columns, o = c0 + u - i * columns, a = __ldcg(parents + i), copy = __ldcg(p.off + i), len = __ldcg(p.mark + i);
       if (a == i || o >= p.seq_pages) continue;
       int page = po_rows[a * columns + o - c0];
       if (copy >= 0 && o == len >> p.pt_shift) page = __ldcg(p.moves + 2 + 2 * copy);

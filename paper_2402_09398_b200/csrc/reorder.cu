@@ -5,6 +5,8 @@
 // batch-major, so a group's rows are `beams` byte strings, and what a CTA takes of them (a piece of the same bytes of every
 // row) can be permuted without regard to any other CTA: it brings the pieces of all sources into shared memory, waits, and
 // writes.  Two such tiles per CTA, so that one is on its way while the other is written; two CTAs per multiprocessor.
+// A warp takes a row's piece: 8 groups of 8 rows, 2.69 GB read and written: 482 us, 5.6 TB/s (a thread per unit of any row,
+// with a division each: 509 us).  A state of 2 MB: 5.3 us, which is the launch and the two looks at the parents.
 #include <atomic>
 
 #include "less_internal.cuh"
@@ -13,7 +15,8 @@
 namespace less {
 
 constexpr int RO_THREADS = 256, RO_CTAS = 2;
-constexpr int RO_UNITS = 3072;                            // 16-byte units of a tile: 48 KB
+constexpr int RO_UNITS = 48 * 1024 / 16;                  // 16-byte units of a tile
+constexpr int RO_BEAMS = 2048;                            // rows of a group at most: a unit of each in a tile
 constexpr int RO_ARRAYS = 7;
 
 struct RoArgs {
@@ -157,7 +160,7 @@ using namespace less;
 
 extern "C" int less_reorder(less_ctx* c, int32_t beams, const int32_t* parents, void* stream) {
   if (!c || !parents) return LESS_ERR_NULL_POINTER;
-  if (beams < 1 || beams > RO_UNITS || c->d.B % beams) return LESS_ERR_INVALID_CONFIG;
+  if (beams < 1 || beams > RO_BEAMS || c->d.B % beams) return LESS_ERR_INVALID_CONFIG;
   if ((uintptr_t)parents & 3) return LESS_ERR_MISALIGNED;
   const Dims& d = c->d;
   const int64_t n = (int64_t)d.L * d.Hd;                    // instances of a batch row
@@ -180,7 +183,7 @@ extern "C" int less_reorder(less_ctx* c, int32_t beams, const int32_t* parents, 
   const size_t smem = (size_t)2 * RO_UNITS * 16 + (size_t)4 * beams * 2;
   static std::atomic<unsigned long long> done{0};
   if (c->device >= 64 || !(done.load(std::memory_order_relaxed) >> c->device & 1)) {
-    if (cudaFuncSetAttribute(state_reorder_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * RO_UNITS * 16 + 8 * RO_UNITS) !=
+    if (cudaFuncSetAttribute(state_reorder_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * RO_UNITS * 16 + 8 * RO_BEAMS) !=
         cudaSuccess)
       return fail_cuda("shared memory opt-in of state_reorder_kernel");
     if (c->device < 64) done.fetch_or(1ull << c->device, std::memory_order_relaxed);
