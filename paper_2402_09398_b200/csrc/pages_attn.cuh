@@ -21,11 +21,12 @@ struct PaArgs {
 struct PaSharedArgs : PaArgs {
   const int4* groups;            // two of each group: {sequence, first row, tokens, first entry}, {sb, wb, eb, end of its entries}
                                  // with the blocks that it shares; tokens -1: starts that descend
-  const int4* entries;           // of each entry: {sb, wb, eb, the most blocks that rows of a tile have beside the shared ones
-                                 // (of its group's tiles of 8 rows)}
+  const int4* entries;           // of each entry: {sb, wb, eb, the most blocks that rows of a tile of its group have beside
+                                 // the shared ones}
   float* parts;                  // [splits][rows * nl * heads * group][D]: results over the shared blocks
   float2* weights;               // [splits][rows * nl * heads * group]: (reference, sum); not written for entries that share nothing
   int splits;
+  int tile;                      // rows of a tile of groups in one pass
   int twins;                     // the many-token kernel leaves two parts for each of its splits
   int out_layers;                // layers between the rows of `out`
 };

@@ -6,7 +6,7 @@
 // with (m, l, o) reference, sum and quotient of a softmax over the shared blocks (s) and over the rest (r): the two halves
 // are the kernels of ordinary attention, once with a group as one entry, whose rows are the tokens of all its sequences, once
 // with the sequences as entries and the other blocks.  The second joins them where it would have written its result.
-// Groups of few rows (tokens x query heads of a KV head) take one pass instead: a tile of 8 rows goes over the shared blocks
+// Groups of few rows (tokens x query heads of a KV head) take one pass instead: a tile of 8 or 16 rows goes over the shared blocks
 // and then over the rest of the entries that its rows are of, each masked for the other rows (pages_tree.cu).
 // What a group shares is found on the device: the leading pages that the tables of all its sequences have in common, of
 // these the blocks that all its tokens see (a window moves with a sequence's end).  So a group is only a hint.
@@ -18,7 +18,7 @@ constexpr int PX_THREADS = 1024, PX_PER = 8;              // table entries of a 
 
 // One CTA per group.  A list of groups that is not [0 .. n] ascending is reported; then all entries are one group that shares
 // nothing.
-constexpr int PX_TILES = 1024;                            // tiles of 8 rows whose blocks are counted one by one
+constexpr int PX_TILES = 1024;                            // tiles whose blocks are counted one by one
 __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, PaSharedArgs a, const int32_t* groups, int ngroups) {
   __shared__ int common, least_seen, most_len, least_wb, some, lead, refused, descends, most_rest;
   __shared__ unsigned long long sum_rest;
@@ -94,10 +94,10 @@ __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, Pa
     }
     if (blocks.x + blocks.z - blocks.y <= 0) blocks = make_int4(0, 0, 0, 0);
   }
-  // the most blocks beside the shared ones that the rows of a tile of 8 have
+  // the most blocks beside the shared ones that the rows of a tile have
   const int row0 = e0 < a.n ? (a.starts ? min(max(__ldg(a.starts + e0), 0), a.rows) : e0) : a.rows;
   const int end = a.starts ? min(max(__ldg(a.starts + e1), row0), a.rows) : max(e1, row0);
-  const int64_t tiles = ((int64_t)(end - row0) * p.group + 7) / 8;
+  const int64_t tiles = ((int64_t)(end - row0) * p.group + a.tile - 1) / a.tile;
   for (int i = e0 + tid; i < e1; i += PX_THREADS) {
     const PgEntry e = i == e0 + tid ? mine : pg_entry(p, a.seqs, a.starts, a.rows, i);
     if (e.count == 0) continue;
@@ -105,13 +105,13 @@ __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, Pa
     atomicMax(&most_rest, rest);
     atomicAdd(&sum_rest, (unsigned long long)rest);
     if (tiles <= PX_TILES && !descends) {
-      const int from = (e.row0 - row0) * p.group;          // below 8 * PX_TILES
-      for (int k = from / 8; k <= (from + e.count * p.group - 1) / 8; ++k) atomicAdd(&tile_rest[k], rest);
+      const int from = (e.row0 - row0) * p.group;          // below PX_TILES * a.tile
+      for (int k = from / a.tile; k <= (from + e.count * p.group - 1) / a.tile; ++k) atomicAdd(&tile_rest[k], rest);
     }
   }
   __syncthreads();
   int most = tid < tiles ? tile_rest[tid] : 0;
-  if (tiles > PX_TILES || descends) most = (int)min((unsigned long long)8 * most_rest, sum_rest);
+  if (tiles > PX_TILES || descends) most = (int)min((unsigned long long)a.tile * most_rest, sum_rest);
   most = __reduce_max_sync(0xffffffffu, most);
   __syncthreads();                                         // most_rest has been read
   if (tid == 0) most_rest = 0;
@@ -170,8 +170,13 @@ __global__ void __launch_bounds__(256) pages_parts_kernel(PgParams p, PaSharedAr
 // Rows of an entry (tokens x query heads of a group) up to which sharing is worth it: an entry with more fills a tile of the
 // many-token kernel on its own, which reads codes once per 256 rows.
 constexpr int kSharedRows = 128;
-// Rows of a group up to which it takes one pass, reading the shared blocks once per 8 rows.
+// Rows of a group up to which it takes one pass, reading the shared blocks once per tile of rows: two launches instead of
+// three or four (a group of 16 rows, 8 heads, 4000 shared: 31 us, in two halves 41; of 64 rows over 16 000: 62 and 52).
 constexpr int kTreeRows = 32;
+// Tiles of 8 rows let two CTAs run on a multiprocessor, tiles of 16 read the shared blocks half as often.  They are taken
+// where the former could read that many bytes again (16 groups of 16 rows, 8 heads, 4000 shared, 131 MB: 56 us with 8 rows, 64
+// with 16; of 32 rows, 262 MB: 114 and 99; of 16 rows over 16 000, 524 MB: 185 and 151).
+constexpr double kTreeAgain = 192 << 20;
 // Bytes that sharing could save at most, as far as the host knows, below which it is not tried: finding out what is shared
 // takes 4 us.
 constexpr double kSharedLeast = 16 << 20;
@@ -198,7 +203,8 @@ extern "C" int less_pages_shared_attention(const less_pages* d, int32_t layer_be
   if ((uintptr_t)groups & 3) return LESS_ERR_MISALIGNED;
   cudaStream_t s = (cudaStream_t)stream;
   const int64_t own = (int64_t)(starts ? max_new : 1) * d->group, all = (int64_t)max_group * d->group;
-  const double save = (double)(n - ngroups) * layer_count * d->heads * d->seq_pages * d->page_tokens * 2 * d->head_dim;
+  const double most = (double)layer_count * d->heads * d->seq_pages * d->page_tokens * 2 * d->head_dim;   // bytes of a sequence
+  const double save = (n - ngroups) * most;
   const size_t row_bytes = (size_t)d->head_dim * 4 + 8, room = LESS_PAGES_PARTIAL_BYTES - kStepBytes;
   const int64_t layer_rows = (int64_t)rows * d->heads * d->group, fit = (int64_t)(room / row_bytes) / layer_rows;
   if (own > kSharedRows || save < kSharedLeast || (fit == 0 && all > kTreeRows))
@@ -206,6 +212,7 @@ extern "C" int less_pages_shared_attention(const less_pages* d, int32_t layer_be
   int4* found = (int4*)pg_shared(d);
   a.entries = found;
   a.groups = found + d->seqs;
+  a.tile = all <= kTreeRows && (double)((all + 7) / 8 - (all + 15) / 16) * ngroups * most >= kTreeAgain ? 16 : 8;
   rc = pg_launch("pages_common_kernel", pages_common_kernel, dim3(ngroups), PX_THREADS, 0, s, p, a, groups, ngroups);
   if (rc != LESS_OK) return rc;
   if (all <= kTreeRows) {

@@ -891,12 +891,9 @@ inline int launch_step(const PgParams& p, const typename PaWork<MODE>::Args& a, 
 
 template <typename T, bool E4M3, PaMode MODE>
 inline int launch_step_dim(const PgParams& p, const typename PaWork<MODE>::Args& a, int dim, int rows, size_t room, int counters, cudaStream_t s) {
-  if constexpr (MODE == kTree)                             // tiles of 8 rows: what the host has counted is for these
-    return dim == 128 ? launch_step<T, 128, 1, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 64, 1, E4M3, MODE>(p, a, room, counters, s);
-  else if (dim == 128)
+  if (dim == 128)
     return rows > 8 ? launch_step<T, 128, 2, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 128, 1, E4M3, MODE>(p, a, room, counters, s);
-  else
-    return rows > 8 ? launch_step<T, 64, 2, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 64, 1, E4M3, MODE>(p, a, room, counters, s);
+  return rows > 8 ? launch_step<T, 64, 2, E4M3, MODE>(p, a, room, counters, s) : launch_step<T, 64, 1, E4M3, MODE>(p, a, room, counters, s);
 }
 
 // rows: the most of an entry, as far as the host knows

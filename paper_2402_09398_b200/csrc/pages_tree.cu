@@ -4,7 +4,7 @@
 namespace less {
 
 int launch_pages_tree(const PgParams& p, const PaSharedArgs& a, int dim, uint32_t flags, cudaStream_t s) {
-  return launch_pages_step<kTree>(p, a, dim, flags, 8, LESS_PAGES_PARTIAL_BYTES, kPgCounters, s);
+  return launch_pages_step<kTree>(p, a, dim, flags, a.tile, LESS_PAGES_PARTIAL_BYTES, kPgCounters, s);
 }
 
 }  // namespace less

@@ -15,13 +15,13 @@ def reach(saved, layers=1, heads=2, dim=128, pt=64, **_):
     return -(-(16 << 20) // (saved * layers * heads * pt * 2 * dim))
 
 
-def family(groups, seed=0, spare=2, **kw):
+def family(groups, seed=0, spare=2, wide=False, **kw):
     """groups: of each (tokens in common, [tokens of their own ...]).  Sequences in random rows of the table; the pages in
-    common are forks'.  Returns cache, model, the listed sequences, the group bounds."""
+    common are forks'.  wide: tables so long that groups of few rows take tiles of 16.  Returns cache, model, the listed sequences, the group bounds."""
     pt = kw.get("pt", 64)
     rng = np.random.default_rng(seed)
     n = sum(len(t) for _, t in groups)
-    room = max(reach(1, **kw), max(-(-(pre + max(t)) // pt) for pre, t in groups))
+    room = max(reach(1, **kw) * (12 if wide else 1), max(-(-(pre + max(t)) // pt) for pre, t in groups))
     pages = sum(-(-(pre + x) // pt) for pre, t in groups for x in t) + 3
     c, m = make(pages=pages, seqs=n + spare, seq_pages=room, **kw)
     rows = rng.permutation(n + spare)[:n].tolist()
@@ -107,6 +107,26 @@ def test_shapes(fmt, dtype, dim, pt, heads, group, hint):
     attend(c, m, seqs, b, max_group=hint)
     attend(c, m, seqs, b, tail=0, max_group=hint)
     attend(c, m, seqs, b, new=[1, 3, 2, 5, 1, 1, 3, 2, 4, 1, 1, 6, 1], max_group=hint)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("dim,pt,heads,group", [(128, 64, 2, 1), (64, 16, 1, 4), (128, 128, 1, 8), (64, 32, 3, 5)])
+def test_tiles_of_sixteen_rows(fmt, dtype, dim, pt, heads, group):
+    c, m, seqs, b = family([(300, [1, 5, 40, 130]), (20, [1, 1]), (129, [3]), (10, [20, 30, 9]), (64, [1, 64, 65])],
+                           dim=dim, pt=pt, heads=heads, group=group, fmt=fmt, dtype=dtype, wide=True)
+    for window, sinks in ((0, 0), (100, 20)):
+        attend(c, m, seqs, b, window=window, sinks=sinks, max_group=32 // group)
+        attend(c, m, seqs, b, window=window, sinks=sinks, tail=0, max_group=32 // group)
+        attend(c, m, seqs, b, window=window, sinks=sinks, new=[1, 3, 2, 5, 1, 1, 3, 2, 0, 1, 1, 6, 1], max_group=32 // group)
+    attend(c, m, seqs, [0, 13], max_group=32 // group)     # one group of strangers
+
+
+@pytest.mark.parametrize("each", [2, 17, 70])
+def test_tiles_of_sixteen_rows_of_long_groups(each):
+    tails = [1 + 7 * i % 60 for i in range(each)]
+    c, m, seqs, b = family([(900, tails), (1100, tails[:each // 2 + 1])], heads=2, group=4, pt=32, wide=True)
+    attend(c, m, seqs, b, max_group=8)
+    attend(c, m, seqs, b, new=[1 + i % 5 for i in range(len(seqs))], max_group=8)
 
 
 @pytest.mark.parametrize("group", [1, 4])
