@@ -1,5 +1,6 @@
 // The paged 8-bit cache: parameters, index arithmetic, the stored tile order and the code formats, shared by
-// pages_ops.cu (maps and page moves), pages_write.cu, pages_attn.cu, pages_chunk.cu and pages_shared.cu.
+// pages_ops.cu (maps and page moves), pages_write.cu and the files of attention (pages_attn.cu, pages_step.cuh,
+// pages_chunk.cuh, pages_chunk.cu, pages_shared.cu, pages_prefix.cu, pages_tree.cu).
 //
 // Order of a tile (16 tokens x D dimensions of one head, 16 * D bytes).  A tile lies in memory as a warp consumes
 // it: 16-byte pieces, piece = 32 * c + 4 * g + t of lane (g = lane / 4, t = lane % 4), so that a warp-wide 16-byte

@@ -45,7 +45,9 @@ constexpr int PC_ROWS = 128, PC_KEYS = 64;
 constexpr int PC_TILES = PC_KEYS / kPageBlock;            // stored tiles of a key tile
 constexpr int PC_SOFT_WARPS = 8;
 // Warps that convert codes.  Four keep up with 256 rows from L2; over the shared blocks of a group the codes come from memory
-// and are used by 128 rows or fewer: eight.
+// and are used by 128 rows or fewer, in two chains: six (then warps 8 - 13 convert, and 14 and 15 issue).  16 sequences over
+// 100 003 tokens, 8 x 8 heads: 98 us; eight, with fewer registers each, took longer, as did codes asked for into L2 ahead of
+// time and six stages for values.
 __host__ __device__ constexpr int pc_deq_warps(PaMode mode) { return mode == kShared ? 6 : 4; }
 __host__ __device__ constexpr int pc_threads(PaMode mode) { return (PC_SOFT_WARPS + pc_deq_warps(mode) + 2) * 32; }
 constexpr int PC_STAGES = 4, PC_META = 8;

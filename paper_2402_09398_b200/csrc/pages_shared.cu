@@ -8,6 +8,9 @@
 // with the sequences as entries and the other blocks.  The second joins them where it would have written its result.
 // Groups of few rows (tokens x query heads of a KV head) take one pass instead: a tile of 8 or 16 rows goes over the shared blocks
 // and then over the rest of the entries that its rows are of, each masked for the other rows (pages_tree.cu).
+// Bound: the halves are ordinary attention's kernels, see there; of the 124 us of 16 sequences over one text of 100 003 tokens
+// (8 KV heads x 8, 238 MB at least) the first half takes 98, the second 18, the look at the tables 8.  Ordinary attention: 385 to
+// 457.  64 sequences behind 4096 tokens in common, 32 heads: 33, 68 and 7 us (ordinary 344 to 364).
 // What a group shares is found on the device: the leading pages that the tables of all its sequences have in common, of
 // these the blocks that all its tokens see (a window moves with a sequence's end).  So a group is only a hint.
 #include "pages_step.cuh"
@@ -168,7 +171,7 @@ __global__ void __launch_bounds__(256) pages_parts_kernel(PgParams p, PaSharedAr
 }
 
 // Rows of an entry (tokens x query heads of a group) up to which sharing is worth it: an entry with more fills a tile of the
-// many-token kernel on its own, which reads codes once per 256 rows.
+// many-token kernel on its own, which reads codes once per 256 rows (more than 128: half a tile at least).
 constexpr int kSharedRows = 128;
 // Rows of a group up to which it takes one pass, reading the shared blocks once per tile of rows: two launches instead of
 // three or four (a group of 16 rows, 8 heads, 4000 shared: 31 us, in two halves 41; of 64 rows over 16 000: 62 and 52).
@@ -178,9 +181,10 @@ constexpr int kTreeRows = 32;
 // with 16; of 32 rows, 262 MB: 114 and 99; of 16 rows over 16 000, 524 MB: 185 and 151).
 constexpr double kTreeAgain = 192 << 20;
 // Bytes that sharing could save at most, as far as the host knows, below which it is not tried: finding out what is shared
-// takes 4 us.
+// takes 4 to 8 us, which is what ordinary attention takes to read that often (10 us for four short sequences).
 constexpr double kSharedLeast = 16 << 20;
-// Parts of a row that the second half joins itself (join_shared); more are joined by a kernel of their own first.
+// Parts of a row that the second half joins itself (join_shared); more are joined by a kernel of their own first (36 parts:
+// 8 us of its own).
 constexpr int kJoinParts = 2;
 constexpr size_t kStepBytes = (size_t)10 << 20;           // of the partial results: those of the second half's step kernel
 

@@ -45,7 +45,8 @@ constexpr int PS_WARPS = 6, PS_THREADS = PS_WARPS * 32;
 __host__ __device__ constexpr int ps_ctas(int NT, int D) { return NT * D <= 128 ? 2 : 1; }
 // Blocks that an item is counted as more than it has: its beginning and end take a warp as long as some blocks, and with
 // sequences that end a few tokens behind what they share, an even cut of the blocks alone hands one warp dozens of items (64
-// sequences of 1 to 1000 tokens of their own, 32 heads: 234 us, of which SMs are busy for 66 on average).
+// sequences of 1 to 1000 tokens of their own, 32 heads: 234 us, of which SMs are busy for 66 on average; with 6 blocks more
+// each 68 us, with 3, 10 or 16 longer).
 __host__ __device__ constexpr int ps_more(PaMode mode) { return mode == kAll ? 0 : 6; }
 constexpr int PS_RING = 4;                     // tiles of a warp: two being worked on, two on their way
 constexpr int PS_MIN_BLOCKS = 4;               // blocks a warp takes at least (one token of 250: 2 the same, 8: 9.7 -> 13.3 us)
