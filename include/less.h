@@ -455,10 +455,11 @@ int less_pages_attention(const less_pages* cache, int32_t layer_begin, int32_t l
 /* less_pages_attention for sequences that share their first pages (forks of one sequence: beams, samples, conversations
  * behind one instruction): the same result up to rounding, with the shared pages read once for a group of entries.
  * groups: device int32 [ngroups + 1], ascending from 0 to n: entries [groups[g], groups[g + 1]) are a group (a list that is
- * not so is LESS_ERR_DEVICE_BOUNDS, and then nothing is shared).  What its sequences share - leading pages that their
+ * not so is LESS_ERR_DEVICE_BOUNDS where it is looked at, and then nothing is shared).  What its sequences share - leading pages that their
  * tables have in common, as far as every token of the group sees them - is found on the device, so a group is a hint only.
  * max_group: the most new tokens of a group, as far as the host knows; like max_new it chooses among kernels.
- * n <= seqs; 1 <= ngroups <= n (n > 0).  Entries of many new tokens (max_new * group > 128) share nothing. */
+ * n <= seqs; 1 <= ngroups <= n (n > 0).  Entries of many new tokens (max_new * group > 128)
+ * share nothing, nor does what could save less than 16 MB by the sizes of the tables: that is ordinary attention. */
 int less_pages_shared_attention(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n,
                                 const int32_t* seqs, const int32_t* starts, int32_t rows, int32_t max_new,
                                 int32_t ngroups, const int32_t* groups, int32_t max_group, const void* q,
