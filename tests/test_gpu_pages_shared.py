@@ -141,6 +141,16 @@ def test_rows_of_a_group(each, group):
     attend(c, m, seqs, b, max_group=each)
 
 
+@pytest.mark.parametrize("each", [9, 40, 150])
+def test_more_rows_than_the_hint(each):
+    """Two chains of key tiles for 128 rows each, however many there are."""
+    tails = [1 + 7 * i % 60 for i in range(each)]
+    c, m, seqs, b = family([(1500, tails), (10, [1, 2]), (700, tails[:each // 2 + 1])], dim=64, pt=32, heads=2, group=4)
+    for hint in (9, 20, 32):
+        attend(c, m, seqs, b, max_group=hint)
+    attend(c, m, seqs, b, new=[1 + i % 4 for i in range(len(seqs))], max_group=20)
+
+
 def test_hints_that_are_wrong():
     c, m, seqs, b = family([(400, [5, 9, 30, 70]), (90, [6, 6])], heads=2, group=4)
     new = [3, 5, 1, 4, 6, 2]
