@@ -19,6 +19,9 @@
 // Where two neighbours in the order are of different beams and closer than that, the sums of these beams are computed again
 // to 1e-10 and the candidates joined once more (a chance of some 1e-4 per kept candidate; 65 us for a row of 128 256,
 // one CTA's work that waits for memory).
+// Measured: 64 x 8 beams of 128 256 bf16 logits (119 MB of live ones): 55 us, 2.2 TB/s, issue slots half used - some 88
+// instructions per warp and 512 bytes - and 465 live rows on 148 multiprocessors of four CTAs; 4 beams of 32 000: 14 us, a chain
+// of waits.  With the rows loaded to registers instead of through a ring of copies 72 us.
 #include <float.h>
 
 #include <atomic>

@@ -26,7 +26,7 @@ struct PaSharedArgs : PaArgs {
   float* parts;                  // [splits][rows * nl * heads * group][D]: results over the shared blocks
   float2* weights;               // [splits][rows * nl * heads * group]: (reference, sum); not written for entries that share nothing
   int splits;
-  int tile;                      // rows of a tile of groups in one pass
+  int tile;                      // rows of a tile of groups in one pass; 0: they are not
   int twins;                     // the many-token kernel leaves two parts for each of its splits
   int out_layers;                // layers between the rows of `out`
 };

@@ -10,7 +10,7 @@
 // and then over the rest of the entries that its rows are of, each masked for the other rows (pages_tree.cu).
 // Bound: the halves are ordinary attention's kernels, see there; of the 124 us of 16 sequences over one text of 100 003 tokens
 // (8 KV heads x 8, 238 MB at least) the first half takes 98, the second 18, the look at the tables 8.  Ordinary attention: 385 to
-// 457.  64 sequences behind 4096 tokens in common, 32 heads: 33, 68 and 7 us (ordinary 344 to 364).
+// 457.  64 sequences behind 4096 tokens in common, 32 heads: 99 us (ordinary 344 to 364).
 // What a group shares is found on the device: the leading pages that the tables of all its sequences have in common, of
 // these the blocks that all its tokens see (a window moves with a sequence's end).  So a group is only a hint.
 #include "pages_step.cuh"
@@ -97,31 +97,32 @@ __global__ void __launch_bounds__(PX_THREADS) pages_common_kernel(PgParams p, Pa
     }
     if (blocks.x + blocks.z - blocks.y <= 0) blocks = make_int4(0, 0, 0, 0);
   }
-  // the most blocks beside the shared ones that the rows of a tile have
   const int row0 = e0 < a.n ? (a.starts ? min(max(__ldg(a.starts + e0), 0), a.rows) : e0) : a.rows;
   const int end = a.starts ? min(max(__ldg(a.starts + e1), row0), a.rows) : max(e1, row0);
-  const int64_t tiles = ((int64_t)(end - row0) * p.group + a.tile - 1) / a.tile;
-  for (int i = e0 + tid; i < e1; i += PX_THREADS) {
-    const PgEntry e = i == e0 + tid ? mine : pg_entry(p, a.seqs, a.starts, a.rows, i);
-    if (e.count == 0) continue;
-    const int rest = rest_blocks(visible_blocks(a, e.len, e.count), blocks).count();
-    atomicMax(&most_rest, rest);
-    atomicAdd(&sum_rest, (unsigned long long)rest);
-    if (tiles <= PX_TILES && !descends) {
-      const int from = (e.row0 - row0) * p.group;          // below PX_TILES * a.tile
-      for (int k = from / a.tile; k <= (from + e.count * p.group - 1) / a.tile; ++k) atomicAdd(&tile_rest[k], rest);
+  if (a.tile) {                                            // the most blocks beside the shared ones that the rows of a tile have
+    const int64_t tiles = ((int64_t)(end - row0) * p.group + a.tile - 1) / a.tile;
+    for (int i = e0 + tid; i < e1; i += PX_THREADS) {
+      const PgEntry e = i == e0 + tid ? mine : pg_entry(p, a.seqs, a.starts, a.rows, i);
+      if (e.count == 0) continue;
+      const int rest = rest_blocks(visible_blocks(a, e.len, e.count), blocks).count();
+      atomicMax(&most_rest, rest);
+      atomicAdd(&sum_rest, (unsigned long long)rest);
+      if (tiles <= PX_TILES && !descends) {
+        const int from = (e.row0 - row0) * p.group;          // below PX_TILES * a.tile
+        for (int k = from / a.tile; k <= (from + e.count * p.group - 1) / a.tile; ++k) atomicAdd(&tile_rest[k], rest);
+      }
     }
+    __syncthreads();
+    int most = tid < tiles ? tile_rest[tid] : 0;
+    if (tiles > PX_TILES || descends) most = (int)min((unsigned long long)a.tile * most_rest, sum_rest);
+    most = __reduce_max_sync(0xffffffffu, most);
+    __syncthreads();                                         // most_rest has been read
+    if (tid == 0) most_rest = 0;
+    __syncthreads();
+    if (lane == 0) atomicMax(&most_rest, most);
+    __syncthreads();
+    blocks.w = most_rest;
   }
-  __syncthreads();
-  int most = tid < tiles ? tile_rest[tid] : 0;
-  if (tiles > PX_TILES || descends) most = (int)min((unsigned long long)a.tile * most_rest, sum_rest);
-  most = __reduce_max_sync(0xffffffffu, most);
-  __syncthreads();                                         // most_rest has been read
-  if (tid == 0) most_rest = 0;
-  __syncthreads();
-  if (lane == 0) atomicMax(&most_rest, most);
-  __syncthreads();
-  blocks.w = most_rest;
   for (int i = e0 + tid; i < e1; i += PX_THREADS) entries[i] = blocks;
   if (tid == 0) {
     of[2 * g] = make_int4(seq, row0, descends ? -1 : end - row0, e0);
@@ -216,7 +217,7 @@ extern "C" int less_pages_shared_attention(const less_pages* d, int32_t layer_be
   int4* found = (int4*)pg_shared(d);
   a.entries = found;
   a.groups = found + d->seqs;
-  a.tile = all <= kTreeRows && (double)((all + 7) / 8 - (all + 15) / 16) * ngroups * most >= kTreeAgain ? 16 : 8;
+  if (all <= kTreeRows) a.tile = (double)((all + 7) / 8 - (all + 15) / 16) * ngroups * most >= kTreeAgain ? 16 : 8;
   rc = pg_launch("pages_common_kernel", pages_common_kernel, dim3(ngroups), PX_THREADS, 0, s, p, a, groups, ngroups);
   if (rc != LESS_OK) return rc;
   if (all <= kTreeRows) {
