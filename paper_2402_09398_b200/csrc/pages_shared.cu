@@ -8,9 +8,12 @@
 // with the sequences as entries and the other blocks.  The second joins them where it would have written its result.
 // Groups of few rows (tokens x query heads of a KV head) take one pass instead: a tile of 8 or 16 rows goes over the shared blocks
 // and then over the rest of the entries that its rows are of, each masked for the other rows (pages_tree.cu).
-// Bound: the halves are ordinary attention's kernels, see there; of the 124 us of 16 sequences over one text of 100 003 tokens
-// (8 KV heads x 8, 238 MB at least) the first half takes 98, the second 18, the look at the tables 8.  Ordinary attention: 385 to
-// 457.  64 sequences behind 4096 tokens in common, 32 heads: 99 us (ordinary 344 to 364).
+// The second half waits for the first only where it joins: it runs beside the kernel that joins parts (the 16 sequences below: 124 ->
+// 114 us).
+// Bound: the halves are ordinary attention's kernels, see there.  16 sequences over one text of 100 003 tokens (8 KV heads x 8,
+// 212 MB): 114 us; one after the other the look at the tables takes 12, the first half 96, the joining of its parts 10, the
+// second half 20.  Ordinary attention: 385 to 457.  64 sequences behind 4096 tokens in common, 32 heads: 97 us (ordinary 344 to
+// 364).
 // What a group shares is found on the device: the leading pages that the tables of all its sequences have in common, of
 // these the blocks that all its tokens see (a window moves with a sequence's end).  So a group is only a hint.
 #include "pages_step.cuh"

@@ -169,7 +169,10 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   __shared__ PsShared sh;
   __shared__ PsTreeRow tree[MODE == kTree ? PS_WARPS : 1][MODE == kTree ? R : 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  pg_wait();
+  // kRest: the kernel before it in the stream gives the parts that are joined, nothing else that is read here; what that one
+  // has waited for is complete.  So it is waited for only where parts are read, and before any CTA ends.
+  auto wait_parts = [] { if (MODE == kRest) pdl_wait_primary(); };
+  if (MODE == kRest) pdl_launch_dependents(); else pg_wait();
 
   // ---- the list of blocks: a thread counts the entries of a stretch of its own, one scan orders them ----
   const int per_thread = pg_ceil(a.n, PS_THREADS);
@@ -229,7 +232,10 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
         xi += sh.sum_i[w];
       }
     }
-    if (most == 0x7fffffff) return;                        // pg_entry has reported it
+    if (most == 0x7fffffff) {                              // pg_entry has reported it
+      wait_parts();
+      return;
+    }
     sh.units[tid + 1] = xu;
     sh.items[tid + 1] = xi;
     if (tid == 0) {
@@ -261,7 +267,10 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
   auto before = [&](int j) -> int64_t { return pad ? (int64_t)sh.items[j] * pad : sh.units[j]; };
   const int64_t total = before(PS_THREADS), per_cta = (int64_t)PS_WARPS * per_warp;
   const int64_t cta_begin = (int64_t)blockIdx.x * per_cta, cta_end = min(total, cta_begin + per_cta);
-  if (cta_begin >= total) return;
+  if (cta_begin >= total) {
+    wait_parts();
+    return;
+  }
   int64_t u = min(total, cta_begin + (int64_t)warp * per_warp);
   const int64_t ue = min(total, u + per_warp);
   if (lane < 2) sh.where[warp][lane] = nullptr;
@@ -688,6 +697,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
     float* slot_out = SLOT * 4 <= PS_RING * 2 * TILE && done ? reinterpret_cast<float*>(ps_ring + warp * (PS_RING * 2 * TILE))
                                                              : slots + (size_t)warp * SLOT;
     __syncwarp();
+    if (complete) wait_parts();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -744,6 +754,7 @@ __global__ void __launch_bounds__(PS_THREADS, ps_ctas(NT, D)) pages_step_kernel(
       if (!next_entry()) break;             // as above
     }
   }
+  wait_parts();
   __syncthreads();
 
   // ---- merge: a warp takes a row, lanes own four dimensions each (with D 64 the upper half repeats the lower) ----
