@@ -301,3 +301,34 @@ def test_captured_beside_other_calls_and_on_a_stream():
         assert torch.equal(one, want) and torch.equal(four, want)
         assert near(two, want, m) and near(three, want, m)
     assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("groups,heads", [([(3000, [4, 40, 80] * 4)], 2), ([(300, [30, 60] * 3)] * 40, 4)])
+def test_calls_right_behind_one_another(groups, heads):
+    """Writes and attention without a pause give what they give with one after each: in parts that are joined by a kernel of
+    their own (one long text), and in one or two (many groups)."""
+    c, m, seqs, b = family(groups, heads=heads, group=4, pt=32)
+    s, g = ints(seqs), ints(b)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    qs = [torch.randn(len(seqs), 1, heads * 4, 128, dtype=torch.float16, device=DEV, generator=gen) for _ in range(6)]
+    kv = [torch.randn(len(seqs), 1, heads, 128, dtype=torch.float16, device=DEV, generator=gen) for _ in range(6)]
+    codes, amax = c.codes.clone(), c.amax.clone()
+
+    def run(pause):
+        c.codes.copy_(codes), c.amax.copy_(amax)
+        out = []
+        for i in range(6):
+            c.write(kv[i], kv[-1 - i], s)
+            pause()
+            out.append(c.shared_attention(qs[i], s, g, max_group=100))
+            pause()
+            out.append(c.shared_attention(qs[-1 - i], s, g, max_group=100))
+            pause()
+        torch.cuda.synchronize()
+        return torch.stack(out)
+
+    want = run(torch.cuda.synchronize)
+    assert not torch.equal(want[0], want[2])
+    for _ in range(5):
+        assert torch.equal(run(lambda: None), want)
+    assert c.poll_status() == 0
