@@ -13,8 +13,8 @@
 //     many come before it.
 // Within a beam the order is that of the logits, which is exact.  Between beams it hangs on the sums.  A term exp2(x) of
 // one is off, relative, by 2^-22 (the exponential), |x| 2^-23.4 (x: a product with a rounded factor, for fp32 logits of a
-// rounded difference) and 5 * 2^-24 (added to fifteen others; the rest is in 64 bits, rounded once at the end), so a sum
-// by at most 6e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it (a thread's -x, and twice
+// rounded difference) and 6 * 2^-24 (added to fifteen others; the rest is in 64 bits, rounded once at the end), so a sum
+// by at most 6.1e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it (a thread's -x, and twice
 // its largest x where it has logits above its reference).
 // Where two neighbours in the order are of different beams and closer than that, the sums of these beams are computed again
 // to 1e-10 and the candidates joined once more (a chance of some 1e-4 per kept candidate; 65 us for a row of 128 256,
@@ -40,8 +40,9 @@ constexpr int BM_MOST_BEAMS = 64, BM_MOST_KEEP = 128;
 constexpr int BM_JOINED = 8192;                           // candidates of a group that are joined, about
 constexpr int BM_DIRECT = 320;                            // as many are compared with one another at once
 constexpr float kRefFar = 40.f;                           // a logit that far above the reference moves it
+constexpr float kRefPacked = 65536.f;                      // references beyond: differences are taken before they are scaled
 // error of a sum: kSumError + kTermError times the mean of |x|
-constexpr double kSumError = 6.0e-7, kTermError = 1.0e-7;
+constexpr double kSumError = 6.1e-7, kTermError = 1.0e-7;
 
 struct BmArgs {
   const void* logits;
@@ -646,7 +647,7 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
     auto refer = [&](float to) {                          // nothing seen so far: any reference will do, the next element moves it
       ref = to == -INFINITY ? 0.f : to;
       limit = to == -INFINITY ? -INFINITY : ref + kRefFar;
-      floor = fabsf(ref) < 0x1p100f ? BmType<T>::below(ref) : -INFINITY;
+      floor = fabsf(ref) <= kRefPacked ? BmType<T>::below(ref) : -INFINITY;
       care = floor == -INFINITY ? NAN : limit;
     };
     refer(ref);
@@ -661,7 +662,13 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
       if (y > 0.f) far2 = f32x2_pack(x * y, 0.f);
     }
     const uint64_t scale2 = f32x2_pack(1.4426950408889634f, 1.4426950408889634f);
-    // the terms of a piece: l log2(e) less the rounded ref log2(e), whose error is taken out of the sum at the end
+    // The terms of a piece: l log2(e) less the rounded ref log2(e).  That rounding, `off` (2^-8 at most, with references of
+    // 2^16 at most), is taken out of the sum at the end: 2^-off to the second order, the third below 4e-9.
+    auto off = [&] { return floor == -INFINITY ? 0.f : fmaf(ref, 1.4426950408889634f, -(ref * 1.4426950408889634f)); };
+    auto back_by = [](float d) {
+      const double u = 0.69314718055994531 * (double)d;
+      return fma(u, fma(u, 0.5, -1.0), 1.0);
+    };
     auto add = [&](const float* f, uint64_t& part) {
       const float c = -ref * 1.4426950408889634f;
       const uint64_t back2 = f32x2_pack(c, c);
@@ -737,12 +744,13 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
           bm_unpack<T>(w, BmType<T>::pack(floor), f);
           uint64_t part = 0;
           if (floor == -INFINITY) {
-            for (int e = 0; e < N; ++e)
-              if (f[e] > -INFINITY) {
-                const float x = (f[e] - ref) * 1.4426950408889634f, y = pa_ex2(x);
-                part = f32x2_add(part, f32x2_pack(y, 0.f));
-                if (y > 0.f) far2 = f32x2_add(far2, f32x2_pack(x * y, 0.f));
-              }
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+              const float x0 = (f[e] - ref) * 1.4426950408889634f, x1 = (f[e + 1] - ref) * 1.4426950408889634f;   // -inf: no term
+              const float y0 = pa_ex2(x0), y1 = pa_ex2(x1);
+              part = f32x2_add(part, f32x2_pack(y0, y1));
+              far2 = f32x2_add(far2, f32x2_pack(y0 > 0.f ? x0 * y0 : 0.f, y1 > 0.f ? x1 * y1 : 0.f));
+            }
           } else {
             add(f, part);
           }
@@ -795,7 +803,7 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
     const float high = bm_block_max(sh, ref);
     const float behind = (ref - high) * 1.4426950408889634f;
     double scale = ref == high ? 1.0 : bm_exp2(behind);
-    if (floor != -INFINITY) scale *= 1.0 - 0.69314718055994531 * (double)fmaf(ref, 1.4426950408889634f, -(ref * 1.4426950408889634f));
+    scale *= back_by(off());
     float f0, f1;
     f32x2_unpack(far2, f0, f1);
     double all = sum * scale;
