@@ -371,11 +371,12 @@ __device__ __noinline__ double bm_exact_sum(BmShared& sh, const BmArgs& a, int r
   for (int at = tid; at < a.vocab; at += N * BM_THREADS) {
     float x[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = fmaxf(fminf(f[i], BmType<T>::most), m - 680.f);   // smaller ones: below 2^-980 each
+    for (int i = 0; i < N; ++i) x[i] = fminf(f[i], BmType<T>::most);
     load(at + N * BM_THREADS);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float d = x[i] - m, back = d - x[i], rest = (x[i] - (d - back)) - (m + back);   // d + rest is the difference
+      float d = x[i] - m, back = d - x[i], rest = (x[i] - (d - back)) - (m + back);   // d + rest is the difference
+      if (d < -680.f) d = -680.f, rest = 0.f;              // below 2^-980 each (-inf among them, where rest is no number)
       const float k = rintf(d * 1477.3197218702985f);
       const float z = fmaf(-k, -0x1.05c61p-39f, fmaf(-k, 0x1.62e43p-11f, d)) + rest;
       const float q = fmaf(z * z, fmaf(z, 0.16666667f, 0.5f), z);

@@ -45,3 +45,19 @@ def test_masks_that_are_finite(dtype, copies):
         rows[4 * i + 2, ::3] = -far
         rows[4 * i + 3, 17000] = far
     one_beam(dtype, rows, copies)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_equal_beams_of_large_logits(dtype, sign):
+    """Beams whose order hangs on the second summation."""
+    far = FAR[dtype] + ([] if dtype == "fp16" else [2.0 ** 31, 2.0 ** 33, 1.5 * 2.0 ** 33, 2.0 ** 34, 1e11, 1e12, 1e15])
+    vocab = 20011
+    rows = body(3 * len(far), vocab, seed=2)
+    for i, x in enumerate(far):
+        rows[3 * i] += sign * x
+        rows[3 * i + 1] = sign * x
+        rows[3 * i + 2] = sign * x
+        rows[3 * i + 2, ::2] = sign * x * (1 - sign * 2.0 ** -7)    # two values, far apart from 1e5 on
+    logits = rows.to(TYPES[dtype])[:, None].expand(-1, 2, -1).contiguous().to(DEV)
+    check(make(len(rows), 2, vocab, 4, TYPES[dtype]), logits, torch.full((len(rows), 2), -0.5, device=DEV))
