@@ -658,7 +658,9 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
     };
     if (lone >= bar) push(lone, single);
     if (lone > -INFINITY) {
-      const float x = (lone - ref) * 1.4426950408889634f, y = pa_ex2(x);
+      // as the terms of pieces are (`add`), whose correction it shares
+      const float x = floor == -INFINITY ? (lone - ref) * 1.4426950408889634f :
+                                           fmaf(lone, 1.4426950408889634f, -(ref * 1.4426950408889634f)), y = pa_ex2(x);
       sum = y;
       if (y > 0.f) far2 = f32x2_pack(x * y, 0.f);
     }

@@ -1,6 +1,7 @@
 """The sums of beam search's selection over the whole range of logits, against beams_ref.py within the bounds of
 test_gpu_beams.py: a term is off by at most 2^-22 (exponential) + 6 * 2^-24 (additions) + |x| 2^-23.4 of itself, x the
 distance in bits from the reference, so a score by less than 2.8e-6 as long as the terms that count lie within 23 bits."""
+import numpy as np
 import pytest
 import torch
 
@@ -61,3 +62,43 @@ def test_equal_beams_of_large_logits(dtype, sign):
         rows[3 * i + 2, ::2] = sign * x * (1 - sign * 2.0 ** -7)    # two values, far apart from 1e5 on
     logits = rows.to(TYPES[dtype])[:, None].expand(-1, 2, -1).contiguous().to(DEV)
     check(make(len(rows), 2, vocab, 4, TYPES[dtype]), logits, torch.full((len(rows), 2), -0.5, device=DEV))
+
+
+def beside_ended(dtype, rows, keep=2, seed=0):
+    """Every row as a beam beside one that has ended, whose score is that of the row's first candidate up to three steps of
+    fp32: the order is that of the 64-bit values."""
+    rows = rows.to(TYPES[dtype])
+    n, vocab = rows.shape
+    logits = torch.zeros(n, 2, vocab, dtype=TYPES[dtype])
+    logits[:, 0] = rows
+    x = rows.double().numpy()
+    top = x.max(-1)
+    value = -0.0625 + (top - (top + np.log(np.exp(x - top[:, None]).sum(-1))))
+    step = np.random.default_rng(seed).integers(-3, 4, n)
+    score = value.astype(np.float32)
+    score = score + step.astype(np.float32) * np.spacing(np.abs(score))
+    near = np.abs(score.astype(np.float64) - value) < 1e-9          # than the second summation tells apart
+    score = np.where(near, score + np.spacing(np.abs(score)), score)
+    scores = torch.tensor([[-0.0625, float(s)] for s in score])
+    ended = torch.tensor([[False, True]]).repeat(n, 1)
+    check(make(n, 2, vocab, keep, TYPES[dtype], end_token=vocab - 1), logits.to(DEV), scores.to(DEV), ended.to(DEV))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("where", ["first", "last"])
+def test_a_peak_at_either_end(dtype, where):
+    """A row whose probability lies in its first or last element, before or behind the whole 16 bytes."""
+    groups, vocab = 64, 50257
+    g = torch.Generator().manual_seed(3)
+    peak = (30 + 150 * torch.rand(groups, generator=g)) * (2 * torch.randint(0, 2, (groups,), generator=g) - 1)
+    rows = peak[:, None] - 16 + torch.randn(groups, vocab, generator=g)
+    rows[:, 0 if where == "first" else -1] = peak
+    beside_ended(dtype, rows)
+    # the same logits, the peak in the midst of the second beam's
+    logits = rows.to(TYPES[dtype])[:, None].repeat(1, 2, 1)
+    at = 0 if where == "first" else vocab - 1
+    logits[:, 1, at], logits[:, 1, 30000] = logits[:, 0, 30000], logits[:, 0, at]
+    first = torch.randint(24, 60, (groups,), generator=g)
+    apart = torch.randint(1, 24, (groups,), generator=g) * (2 * torch.randint(0, 2, (groups,), generator=g) - 1)
+    scores = -0.5 - torch.stack([first, first + apart], 1) * 2.0 ** -24
+    check(make(groups, 2, vocab, 2, TYPES[dtype]), logits.to(DEV), scores.to(DEV))
