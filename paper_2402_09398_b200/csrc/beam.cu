@@ -651,6 +651,13 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
       floor = fabsf(ref) <= kRefPacked ? BmType<T>::below(ref) : -INFINITY;
       care = floor == -INFINITY ? NAN : limit;
     };
+    // Terms are l log2(e) less the rounded ref log2(e).  That rounding, `off` (2^-8 at most, with references of 2^16 at most),
+    // is taken out of the sum at the end: 2^-off to the second order, the third below 4e-9.
+    auto off = [&] { return floor == -INFINITY ? 0.f : fmaf(ref, 1.4426950408889634f, -(ref * 1.4426950408889634f)); };
+    auto back_by = [](float d) {
+      const double u = 0.69314718055994531 * (double)d;
+      return fma(u, fma(u, 0.5, -1.0), 1.0);
+    };
     refer(ref);
     auto push = [&](float l, int token) {
       const int n = atomicAdd(&sh.count, 1);
@@ -665,13 +672,6 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
       if (y > 0.f) far2 = f32x2_pack(x * y, 0.f);
     }
     const uint64_t scale2 = f32x2_pack(1.4426950408889634f, 1.4426950408889634f);
-    // The terms of a piece: l log2(e) less the rounded ref log2(e).  That rounding, `off` (2^-8 at most, with references of
-    // 2^16 at most), is taken out of the sum at the end: 2^-off to the second order, the third below 4e-9.
-    auto off = [&] { return floor == -INFINITY ? 0.f : fmaf(ref, 1.4426950408889634f, -(ref * 1.4426950408889634f)); };
-    auto back_by = [](float d) {
-      const double u = 0.69314718055994531 * (double)d;
-      return fma(u, fma(u, 0.5, -1.0), 1.0);
-    };
     auto add = [&](const float* f, uint64_t& part) {
       const float c = -ref * 1.4426950408889634f;
       const uint64_t back2 = f32x2_pack(c, c);
@@ -730,13 +730,16 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
               far2 = 0;
               refer(top);
             } else if (top > ref) {
-              const float back = (ref - top) * 1.4426950408889634f, scale = pa_ex2(back);
+              // In 64 bits, so that it adds nothing to the errors of the terms so far; their own `off` is taken out, and
+              // the new one, which the end takes out, put in.
+              const double back = ((double)ref - (double)top) * 1.44269504088896340735992, scale = bm_exp2(back);
               float s0, s1;
               f32x2_unpack(far2, s0, s1);
-              far2 = scale > 0.f ? f32x2_pack((s0 + s1 + back * (float)sum) * scale, 0.f) : 0;
-              sum *= (double)scale;
+              far2 = scale > 0.0 ? f32x2_pack((s0 + s1 + (float)back * (float)sum) * (float)scale, 0.f) : 0;
+              sum *= scale * back_by(off());
               highest = -INFINITY;                        // all so far lie below the new one
               refer(top);
+              sum *= back_by(-off());
             }
             const uint32_t most = BmType<T>::pack(BmType<T>::most);
             w = make_uint4(BmType<T>::smaller(w.x, most), BmType<T>::smaller(w.y, most), BmType<T>::smaller(w.z, most),

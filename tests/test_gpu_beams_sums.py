@@ -102,3 +102,27 @@ def test_a_peak_at_either_end(dtype, where):
     apart = torch.randint(1, 24, (groups,), generator=g) * (2 * torch.randint(0, 2, (groups,), generator=g) - 1)
     scores = -0.5 - torch.stack([first, first + apart], 1) * 2.0 ** -24
     check(make(groups, 2, vocab, 2, TYPES[dtype]), logits.to(DEV), scores.to(DEV))
+
+
+def climbing(dtype, groups, seed):
+    """Rows in which a thread meets logits far above its reference (39 of at most 40) before one that moves it: the former
+    have most of the probability.  `first` is the reference, `mid` the former, `last` the latter.  (x is 56.3 there: half a
+    step of it, 2^-19, times ln 2 1.3e-6, log2 e in fp32 39 * 1.93e-8, a term 6e-7: 2.7e-6 of four fifths of the sum.)"""
+    g = torch.Generator().manual_seed(seed)
+    per = 8 if dtype != "fp32" else 4                     # elements of 16 bytes; 256 threads, a first tile of four of each
+    stride, vocab = 256 * per, 24 * 256 * per
+    first = ((20 + 150 * torch.rand(groups, generator=g)) * (2 * torch.randint(0, 2, (groups,), generator=g) - 1)).to(TYPES[dtype]).float()
+    mid, last = (first + 39.0).to(TYPES[dtype]).float(), (first + 42.0).to(TYPES[dtype]).float()
+    rows = first[:, None] - 10 + torch.randn(groups, vocab, generator=g).clamp(max=4)
+    rows[:, 77] = first
+    for piece in range(6, 16):
+        at = piece * stride + 5 * per
+        rows[:, at:at + per] = mid[:, None]
+    rows[:, 20 * stride + 5 * per] = last
+    return rows
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("copies", [1, 10])
+def test_references_that_move_under_much_of_a_sum(dtype, copies):
+    one_beam(dtype, climbing(dtype, 64, 0), copies)
