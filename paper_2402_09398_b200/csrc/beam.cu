@@ -732,10 +732,12 @@ __global__ void __launch_bounds__(BM_THREADS, BM_CTAS) beam_select_kernel(BmArgs
             } else if (top > ref) {
               // In 64 bits, so that it adds nothing to the errors of the terms so far; their own `off` is taken out, and
               // the new one, which the end takes out, put in.
-              const double back = ((double)ref - (double)top) * 1.44269504088896340735992, scale = bm_exp2(back);
+              const double scale = bm_exp2(((double)ref - (double)top) * 1.44269504088896340735992);
               float s0, s1;
               f32x2_unpack(far2, s0, s1);
-              far2 = scale > 0.0 ? f32x2_pack((s0 + s1 + (float)back * (float)sum) * (float)scale, 0.f) : 0;
+              // errors so far are those of x as it was, of either sign (up: as at the end)
+              const float up = fmaxf(0.f, (highest - ref) * 1.4426950408889634f);
+              far2 = scale > 0.0 ? f32x2_pack((s0 + s1 - 2.f * up * (float)sum) * (float)scale, 0.f) : 0;
               sum *= scale * back_by(off());
               highest = -INFINITY;                        // all so far lie below the new one
               refer(top);

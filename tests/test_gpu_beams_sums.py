@@ -126,3 +126,9 @@ def climbing(dtype, groups, seed):
 @pytest.mark.parametrize("copies", [1, 10])
 def test_references_that_move_under_much_of_a_sum(dtype, copies):
     one_beam(dtype, climbing(dtype, 64, 0), copies)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("seed", range(3))
+def test_order_where_references_move_under_much_of_a_sum(dtype, seed):
+    beside_ended(dtype, climbing(dtype, 320, seed), seed=seed)      # a stretch a row
