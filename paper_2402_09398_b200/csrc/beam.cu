@@ -16,7 +16,7 @@
 // rounded difference) and 6 * 2^-24 (added to fifteen others; the rest is in 64 bits, rounded once at the end), so a sum
 // by at most 6.1e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it (a thread's -x, and twice
 // its largest x where it has logits above its reference).
-// Where two neighbours in the order are of different beams and closer than that, the sums of these beams are computed again
+// Where two candidates are of different beams and closer than that, the sums of these beams are computed again
 // to 1e-10 and the candidates joined once more (a chance of some 1e-4 per kept candidate; 65 us for a row of 128 256,
 // one CTA's work that waits for memory).
 // Measured: 64 x 8 beams of 128 256 bf16 logits (119 MB of live ones): 55 us, 2.2 TB/s, issue slots half used - some 88
@@ -463,7 +463,7 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     if (key) x = {bm_order(c + ((double)bm_logit(key) - sh.j.lse[b])), bm_at(b, key, bm_token(key))};
     return x;
   };
-  auto differ = [&](const BmCand& x, const BmCand& y) {   // two neighbours whose order the errors of the sums could change
+  auto differ = [&](const BmCand& x, const BmCand& y) {   // whether the errors of the sums could change the order of two
     const int i = bm_beam(x), j = bm_beam(y);
     const double err = sh.j.err[i] + sh.j.err[j];         // an ended beam has none
     if (i != j && err > 0.0 && bm_value(x.v) - bm_value(y.v) <= err) atomicOr(&sh.again, 1ull << i | 1ull << j);
@@ -520,12 +520,16 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
               [&](int i, int rank) { if (rank < K) sh.top[rank] = sh.j.cand[i]; });
       __syncthreads();
       if (!refined) {
-        for (int i = tid; i + 1 < found; i += BM_THREADS) differ(sh.top[i], sh.top[i + 1]);
-        if (count > K) {                                  // and those that could come in
-          const BmCand x = sh.top[K - 1];
-          for (int i = tid; i < count; i += BM_THREADS)
-            if (bm_before(x, sh.j.cand[i])) differ(x, sh.j.cand[i]);
-        }
+        // every two, not neighbours alone: one between them may be of a beam whose sum has a smaller error
+        const double reach = 2.0 * most_err;
+        for (int i = tid; i < found; i += BM_THREADS)
+          for (int k = i + 1; k < found && bm_value(sh.top[i].v) - bm_value(sh.top[k].v) <= reach; ++k) differ(sh.top[i], sh.top[k]);
+        if (count > K)                                    // and those that could come in
+          for (int i = tid; i < count; i += BM_THREADS) {
+            const BmCand x = sh.j.cand[i];
+            if (!bm_before(sh.top[K - 1], x)) continue;
+            for (int k = K - 1; k >= 0 && bm_value(sh.top[k].v) - bm_value(x.v) <= reach; --k) differ(sh.top[k], x);
+          }
       }
     } else {
       // too many near the bar: one after the other, and all sums in 64 bits

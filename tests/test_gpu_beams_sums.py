@@ -132,3 +132,26 @@ def test_references_that_move_under_much_of_a_sum(dtype, copies):
 @pytest.mark.parametrize("seed", range(3))
 def test_order_where_references_move_under_much_of_a_sum(dtype, seed):
     beside_ended(dtype, climbing(dtype, 320, seed), seed=seed)      # a stretch a row
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("keep", [2, 4, 6])
+def test_order_of_beams_with_others_between(dtype, keep):
+    """Beams of one value but for some 1e-6, whose sums have errors of different bounds: a peak that comes late, one that is
+    the first tile's, and ended ones, which have none, among them."""
+    groups, beams = 320, 6
+    rows = climbing(dtype, groups, 7).to(TYPES[dtype])
+    vocab = rows.shape[1]
+    logits = torch.zeros(groups, beams, vocab, dtype=TYPES[dtype])
+    logits[:, 0], logits[:, 2], logits[:, 4] = rows, rows.flip(1), rows.roll(1000, 1)
+    x = rows.double().numpy()
+    top = x.max(-1)
+    value = -0.0625 + (top - (top + np.log(np.exp(x - top[:, None]).sum(-1))))
+    rng = np.random.default_rng(keep)
+    live = np.float32(-0.0625) + rng.integers(-60, 61, (groups, 3)).astype(np.float32) * np.float32(2.0 ** -27)
+    near = (value[:, None] + rng.uniform(-1.5e-6, 1.5e-6, (groups, 3))).astype(np.float32)
+    scores = torch.zeros(groups, beams)
+    scores[:, ::2], scores[:, 1::2] = torch.from_numpy(live), torch.from_numpy(near)
+    ended = torch.zeros(groups, beams, dtype=torch.bool)
+    ended[:, 1::2] = True
+    check(make(groups, beams, vocab, keep, TYPES[dtype], end_token=vocab - 1), logits.to(DEV), scores.to(DEV), ended.to(DEV))
