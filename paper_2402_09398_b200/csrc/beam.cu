@@ -166,7 +166,7 @@ __device__ __forceinline__ bool bm_live(float score) { return fabsf(score) <= FL
 struct BmCand {
   long long v;
   unsigned long long at;                                  // what decides between equal values: the beam (6 bits), the larger
-                                                          // logit (32), the token (26); ~0 = none
+                                                          // logit (32; no key's high half is 0), the token (26); ~0 = none
 };
 __device__ __forceinline__ unsigned long long bm_at(int beam, unsigned long long key, int token) {
   return (unsigned long long)beam << 58 | (unsigned long long)~(uint32_t)(key >> 32) << 26 | (uint32_t)token;
@@ -457,7 +457,7 @@ __device__ __noinline__ void bm_join(BmShared& sh, const BmArgs& a, int group) {
     const double c = sh.j.score[b];
     if (c == -INFINITY) return x;
     if (sh.done >> b & 1) {
-      if (i == b * per_beam && a.end_token >= 0) x = {bm_order(c), bm_at(b, 0, a.end_token)};
+      if (i == b * per_beam && a.end_token >= 0) x = {bm_order(c), bm_at(b, ~0ull, a.end_token)};   // (its only one)
       return x;
     }
     if (key) x = {bm_order(c + ((double)bm_logit(key) - sh.j.lse[b])), bm_at(b, key, bm_token(key))};

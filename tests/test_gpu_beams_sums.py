@@ -155,3 +155,18 @@ def test_order_of_beams_with_others_between(dtype, keep):
     ended = torch.zeros(groups, beams, dtype=torch.bool)
     ended[:, 1::2] = True
     check(make(groups, beams, vocab, keep, TYPES[dtype], end_token=vocab - 1), logits.to(DEV), scores.to(DEV), ended.to(DEV))
+
+
+def test_the_last_token_of_the_last_beam():
+    """64 beams of 2^26 tokens, the last beam ended with the last token."""
+    vocab = 1 << 26
+    sel = make(1, 64, vocab, 4, torch.float16, end_token=vocab - 1)
+    logits = torch.empty(1, 64, vocab, dtype=torch.float16, device=DEV)   # of beams that are not looked at
+    scores = torch.full((1, 64), -float("inf"), device=DEV)
+    ended = torch.zeros(1, 64, dtype=torch.bool, device=DEV)
+    scores[0, 63], ended[0, 63] = -2.0, True
+    scores[0, 7], ended[0, 7] = -2.0, True
+    got = sel.select(logits, scores, ended)
+    assert got.tokens.tolist() == [[vocab - 1, vocab - 1, -1, -1]] and got.parents.tolist() == [[7, 63, 2, 3]]
+    assert got.scores.tolist() == [[-2.0, -2.0, -float("inf"), -float("inf")]]
+    assert got.ended.tolist() == [[True, True, False, False]]
