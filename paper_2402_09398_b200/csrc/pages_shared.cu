@@ -171,6 +171,8 @@ __global__ void __launch_bounds__(256) pages_parts_kernel(PgParams p, PaSharedAr
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   reinterpret_cast<float4*>(a.parts + row * D)[lane] = make_float4(f.x * inv, f.y * inv, f.z * inv, f.w * inv);
+  // the first part's weight, which all lanes of the row have read (with D 64 two rows of a warp go ways of their own)
+  __syncwarp(D == 128 ? 0xffffffffu : 0xffffu << (threadIdx.x & 16));
   if (lane == 0) a.weights[row] = make_float2(m, sum);
 }
 
