@@ -453,13 +453,17 @@ int less_pages_attention(const less_pages* cache, int32_t layer_begin, int32_t l
                          int64_t q_stride, int32_t window, int32_t sinks, float scale, void* out, void* cuda_stream);
 
 /* less_pages_attention for sequences that share their first pages (forks of one sequence: beams, samples, conversations
- * behind one instruction): the same result up to rounding, with the shared pages read once for a group of entries.
+ * behind one instruction): the same result up to rounding, with the shared pages read once for a group of entries.  (In
+ * groups of more than 32 rows, tokens x query heads of a KV head, probabilities over shared pages are rounded to fp16 once,
+ * as less_pages_attention does for entries of many new tokens; for few it keeps 22 bits of them with fp16 outputs.)
  * groups: device int32 [ngroups + 1], ascending from 0 to n: entries [groups[g], groups[g + 1]) are a group (a list that is
  * not so is LESS_ERR_DEVICE_BOUNDS where it is looked at, and then nothing is shared).  What its sequences share - leading pages that their
  * tables have in common, as far as every token of the group sees them - is found on the device, so a group is a hint only.
  * max_group: the most new tokens of a group, as far as the host knows; like max_new it chooses among kernels.
  * n <= seqs; 1 <= ngroups <= n (n > 0).  Entries of many new tokens (max_new * group > 128)
- * share nothing, nor does what could save less than 16 MB by the sizes of the tables: that is ordinary attention. */
+ * share nothing, nor does what could save less than 16 MB if all tables were full (seq_pages pages, lengths are not
+ * known to the host): that is ordinary attention.  Short sequences in wide tables are better off with less_pages_attention,
+ * which need not find out what is shared (4 - 8 us). */
 int less_pages_shared_attention(const less_pages* cache, int32_t layer_begin, int32_t layer_count, int32_t n,
                                 const int32_t* seqs, const int32_t* starts, int32_t rows, int32_t max_new,
                                 int32_t ngroups, const int32_t* groups, int32_t max_group, const void* q,
@@ -477,8 +481,10 @@ int less_pages_poll_status(const less_pages* cache, void* cuda_stream);
  * The selection.  The candidates of a group are (beam, token) with
  *     value = score[beam] + logit[beam, token] - log sum exp logit[beam]
  * and, for a beam that has ended, (beam, end_token) alone with value = score[beam].  The `keep` largest are the result,
- * largest first, ties to the lowest (beam, token); order and ties are those of 64-bit arithmetic (in a beam, those of the
- * logits, also where a very large one makes equal values of them).  A logit that is NaN
+ * largest first, ties to the lowest (beam, token).  The order is that of these values in 64-bit arithmetic, with sums good to
+ * 1e-10 wherever it hangs on them: beams of the same logits and scores tie, others may come in either order where their
+ * values are closer than that.  In a beam it is that of the logits, also where a very large one makes equal values of them.
+ * Any finite logit is fine.  A logit that is NaN
  * counts as -inf, +inf as the largest finite value of its type; no candidate: a logit of -inf, a beam whose score is not
  * finite (a beam that does not exist has -inf).  Where there are fewer than `keep` candidates: score -inf, token -1, the
  * parent in the same place (the last one from beam `beams` on), not ended. */
@@ -504,7 +510,8 @@ size_t less_beams_workspace_bytes(const less_beams* beams);   /* 0 if the descri
 
 /* logits: device [groups, beams, vocab], `row_stride` elements from beam to beam (>= vocab, any alignment of the type);
  * scores: device fp32 [groups, beams]; ended: device bytes [groups, beams], not 0 = has ended, or NULL (with end_token -1 it
- * has to be NULL).  Results, device [groups, keep]: out_scores fp32 (values, rounded once), out_tokens, out_parents int32
+ * has to be NULL).  Results, device [groups, keep]: out_scores fp32 (values; their log-sums are good to
+ * 1e-6 as a rule, 6e-6 at worst), out_tokens, out_parents int32
  * (group * beams + beam), out_ended bytes (token == end_token) or NULL; none may overlap an input.  Asynchronous, allocates nothing, can be captured; one call at a
  * time per workspace, replays of captured ones included.  Runs on the current device. */
 int less_beam_select(const less_beams* beams, const void* logits, int64_t row_stride, const float* scores,

@@ -17,11 +17,14 @@
 // by at most 6.1e-7 + 1e-7 times the mean of |x| weighted with the terms, which is summed up beside it (a thread's -x, and twice
 // its largest x where it has logits above its reference).
 // Where two candidates are of different beams and closer than that, the sums of these beams are computed again
-// to 1e-10 and the candidates joined once more (a chance of some 1e-4 per kept candidate; 65 us for a row of 128 256,
-// one CTA's work that waits for memory).
+// to 1e-10 and the candidates joined once more (a chance of some 1e-4 per kept candidate: of 60 inputs of the large case below
+// one; 58 us for a row of 128 256, one CTA's work that waits for memory, so two such rows make 176 us of its 61 us between events).
+// References beyond 2^16 take differences before they scale them (32 x 8 beams of 128 256 fp32 logits near 1e6: 78 us instead
+// of 61).  A stretch that has more equal logits at its bar than the list holds is gone through again in order: rows that
+// begin with thousands of tokens masked with one finite value take 600 us (with -inf 55: that is no candidate).
 // Measured: 64 x 8 beams of 128 256 bf16 logits (119 MB of live ones): 55 us, 2.2 TB/s, issue slots half used - some 88
-// instructions per warp and 512 bytes - and 465 live rows on 148 multiprocessors of four CTAs; 4 beams of 32 000: 14 us, a chain
-// of waits.  With the rows loaded to registers instead of through a ring of copies 72 us.
+// instructions per warp and 512 bytes - and 465 live rows on 148 multiprocessors of four CTAs; 4 beams of 32 000: 14 - 17 us, a
+// chain of waits.  With the rows loaded to registers instead of through a ring of copies 72 us.
 #include <float.h>
 
 #include <atomic>
@@ -877,7 +880,8 @@ static bool valid_beams(const less_beams* d) {
 }
 
 // A row is cut so that all CTAs of a call, four on a multiprocessor, run at once, but for no less than 4096 elements each, nor
-// into so many lists that joining them shows (64 groups of 8 beams of 128 256: one stretch a row; three 15 us more).
+// into so many lists that joining them shows (64 groups of 8 beams of 128 256: one stretch a row; three 15 us more).  The
+// workspace goes by this, and may be asked for without a device: B200's 148 multiprocessors, not the current device's.
 static BmLayout bm_layout(const less_beams* d) {
   BmLayout l;
   const int64_t rows = (int64_t)d->groups * d->beams;

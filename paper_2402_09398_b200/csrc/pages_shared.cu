@@ -14,6 +14,9 @@
 // 212 MB): 114 us; one after the other the look at the tables takes 12, the first half 96, the joining of its parts 10, the
 // second half 20.  Ordinary attention: 385 to 457.  64 sequences behind 4096 tokens in common, 32 heads: 97 us (ordinary 344 to
 // 364).
+// Of more than 32 rows a group, probabilities over the shared blocks are rounded to fp16 once (11 bits), as the many-token kernel
+// does; the rests, and groups in one pass, keep 22 bits next to an fp16 output, as ordinary attention of few tokens does.  (The
+// 64 sequences below: the mean error against 64 bits is 2.15e-4 instead of 2.07e-4.)
 // What a group shares is found on the device: the leading pages that the tables of all its sequences have in common, of
 // these the blocks that all its tokens see (a window moves with a sequence's end).  So a group is only a hint.
 #include "pages_step.cuh"
@@ -184,10 +187,13 @@ constexpr int kSharedRows = 128;
 constexpr int kTreeRows = 32;
 // Tiles of 8 rows let two CTAs run on a multiprocessor, tiles of 16 read the shared blocks half as often.  They are taken
 // where the former could read that many bytes again (16 groups of 16 rows, 8 heads, 4000 shared, 131 MB: 56 us with 8 rows, 64
-// with 16; of 32 rows, 262 MB: 114 and 99; of 16 rows over 16 000, 524 MB: 185 and 151).
+// with 16; of 32 rows, 262 MB: 114 and 99; of 16 rows over 16 000, 524 MB: 185 and 151).  The host knows what tables can hold,
+// not lengths: the figures are of tables as wide as the longest sequence.  With wider ones 16 x 4 beams of 100 - 3000 tokens
+// take tiles of 16 rows as well (512 pages of 64 tokens: 53 us instead of 47).
 constexpr double kTreeAgain = 192 << 20;
 // Bytes that sharing could save at most, as far as the host knows, below which it is not tried: finding out what is shared
-// takes 4 to 8 us, which is what ordinary attention takes to read that often (10 us for four short sequences).
+// takes 4 to 8 us, which is what ordinary attention takes to read that often (10 us for four short sequences).  Again by what
+// tables can hold: four sequences of 266 tokens take 11 us with a table as wide as they are, 15.5 with one of 512 pages.
 constexpr double kSharedLeast = 16 << 20;
 // Parts of a row that the second half joins itself (join_shared); more are joined by a kernel of their own first (36 parts:
 // 8 us of its own).

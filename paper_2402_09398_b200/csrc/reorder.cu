@@ -6,7 +6,7 @@
 // row) can be permuted without regard to any other CTA: it brings the pieces of all sources into shared memory, waits, and
 // writes.  Two such tiles per CTA, so that one is on its way while the other is written; two CTAs per multiprocessor.
 // A warp takes a row's piece: 8 groups of 8 rows, 2.69 GB read and written: 482 us, 5.6 TB/s (a thread per unit of any row,
-// with a division each: 509 us).  A state of 2 MB: 5.3 us, which is the launch and the two looks at the parents.
+// with a division each: 509 us).  A state of 2 MB: 5.3 - 8 us, which is the launch and the two looks at the parents.
 #include <atomic>
 
 #include "less_internal.cuh"
