@@ -797,6 +797,8 @@ class BeamSelect:
         desc.workspace, desc.workspace_bytes = self.workspace.data_ptr(), nbytes
         self.desc, self.dtype, self.device = desc, dtype, self.workspace.device
         self.groups, self.beams, self.vocab, self.keep = groups, beams, vocab, keep
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.device).synchronize()   # calls may be on any stream: it is cleared by then
         self._index = self.device.index
         self._streams = set()                            # those that the workspace is recorded on
         self._lib = lib()
